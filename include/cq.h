@@ -298,6 +298,100 @@ cq_status cq_prepack(const cq_codebook_weights* W, void* dst, size_t dst_bytes, 
  */
 cq_status cq_decode_dense(const cq_codebook_weights* W, int g, uint16_t* Wc_bf16, cq_stream stream);
 
+/*
+ * The operators that stand around the layer in a model.  Their rows may be fp32, f16 or bf16 (element kinds CQ_A_F32, CQ_A_F16,
+ * CQ_A_BF16 as above; stored values are rounded to nearest, ties to even, without saturation), of any width, and need only the
+ * alignment of their elements (rows that start on 16 bytes and are whole groups of eight values move 16 bytes at a time).
+ * Sums are held in fp32 and added in an order that depends on the sizes alone.  T = 0 is allowed.
+ */
+
+/* the gate of a block: none, one value per token [T], or one per value [T, H]; of the block's kind */
+enum { CQ_GATE_NONE = 0, CQ_GATE_ROW = 1, CQ_GATE_ELEM = 2 };
+
+/*
+ * The norms before and after a block, fused with its gate and the residual sum (N(v) = v / sqrt(mean(v^2) + eps)):
+ *     u  = N(y) * w_post            (w_post NULL: u = y)
+ *     h' = residual_scale * h + branch_scale * a * u,      a = 1, the gate, or sigmoid(gate)
+ *     x  = N(h') * w_pre            the next block's input, from h' before it is rounded
+ *   h, h' [T, H] of stream_kind: the residual stream.  y [T, H] (the block's output), x [T, H] and the gate of block_kind:
+ *   CQ_A_F32 (what cq_moe_forward takes and gives) or stream_kind.  w_pre, w_post [H] of weight_kind: CQ_A_F32 or stream_kind.
+ *   y NULL: x = N(h) * w_pre alone (in front of the first block); h_out is then not written.
+ *   x_out NULL: h' alone (behind the last block).  h_out may be h, and x_out may be y if their kinds agree.
+ *   1 <= H <= 32768; 0 < eps < inf.
+ */
+typedef struct {
+  int H;
+  int stream_kind, block_kind, weight_kind;
+  int gate_kind;    /* CQ_GATE_... */
+  int gate_sigmoid; /* non-zero: a = sigmoid(gate) */
+  float eps, residual_scale, branch_scale;
+  const void* w_pre;
+  const void* w_post;
+} cq_block_norm_spec;
+cq_status cq_block_norm(const cq_block_norm_spec* P, const void* h, const void* y, const void* gate, int T, void* h_out,
+                        void* x_out, cq_stream stream);
+
+/*
+ * Its gradients, from h' as the forward pass stored it (with y NULL: from its h), y, the gate, and the gradients d_h_out of h'
+ * and d_x of x (either may be NULL: zero).  d_h [T, H] of stream_kind; d_y [T, H] and d_gate (NULL: not wanted) of block_kind;
+ * d_w_pre (needs d_x), d_w_post [H] of weight_kind (NULL: not wanted).  d_h may be d_h_out.
+ *   workspace: cq_block_norm_grad_workspace_bytes(P, T) bytes, which never falls as T grows; not needed without d_w_pre and d_w_post.
+ */
+size_t cq_block_norm_grad_workspace_bytes(const cq_block_norm_spec* P, int T);
+cq_status cq_block_norm_grad(const cq_block_norm_spec* P, const void* h, const void* y, const void* gate, const void* d_h_out,
+                             const void* d_x, int T, void* d_h, void* d_y, void* d_gate, void* d_w_pre, void* d_w_post,
+                             void* workspace, size_t workspace_bytes, cq_stream stream);
+
+/*
+ * Load-balancing loss of a router, sequence by sequence, with the counts it rests on:
+ *     p_t = softmax(logits_t),  c[s,e] = assignments of sequence s to expert e,  n_s = its tokens that count
+ *     P[s,e] = mean of p_t[e] over those tokens,  loss = alpha / S' * sum_s E * sum_e c[s,e] / (top_k n_s) * P[s,e]
+ *   (S' = sequences with a token that counts; without any the loss is 0.)
+ *   logits [T, E] of logit_kind, topk_ids [T, top_k] (as cq_route_permute leaves them; ids outside [0, E) are not counted).
+ *   seq_offsets [n_seqs + 1] i32, non-decreasing: sequence s holds tokens seq_offsets[s] .. seq_offsets[s+1]-1, possibly none;
+ *   tokens outside all of them are left out.  NULL with n_seqs = 1: one sequence of all tokens.
+ *   token_mask [T] bytes or NULL: tokens whose byte is 0 (padding) are left out, whatever their logits hold.  A token all of whose
+ *   logits are -inf counts, with probabilities of 0.
+ *   Outputs: loss [1] f32, counts [n_seqs, E] i32, probs [n_seqs, E] f32 (P), tokens [n_seqs + 1] i32 (n_s, then S').
+ *   E <= 1024, top_k <= min(E, 64).  workspace: cq_balance_loss_workspace_bytes(T, E, n_seqs) bytes.
+ */
+size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs);
+cq_status cq_balance_loss(const void* logits, int logit_kind, const int32_t* topk_ids, const int32_t* seq_offsets, int n_seqs,
+                          const uint8_t* token_mask, int T, int E, int top_k, float alpha, float* loss, int32_t* counts,
+                          float* probs, int32_t* tokens, void* workspace, size_t workspace_bytes, cq_stream stream);
+
+/*
+ * Its gradient with respect to the logits (the counts are constants), from the counts and tokens above:
+ *     d_logits[t,e] = d_loss alpha E / (S' n_s) p_t[e] (f[s,e] - sum_j f[s,j] p_t[j]),  f = c / (top_k n_s);  0 for tokens left out.
+ *   d_loss [1] f32 on the device, or NULL: 1.  d_logits [T, E] of logit_kind.
+ */
+cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t* counts, const int32_t* tokens,
+                               const int32_t* seq_offsets, int n_seqs, const uint8_t* token_mask, int T, int E, int top_k,
+                               float alpha, const float* d_loss, void* d_logits, cq_stream stream);
+
+/*
+ * Low-rank adapters of many requests beside a projection that all of them share (clustered weights are never edited: what
+ * differs between tenants is added beside them):
+ *     out_t = base_t + scale[a] * B_a (A_a x_t),   a = adapter_ids[t];   a outside [0, n): out_t = base_t
+ *   A [n, rank, K] and B [n, N, rank] of `kind`; scale [n] f32 or NULL (1); ranks [n] i32 or NULL: adapter a has ranks[a] <= rank
+ *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256.
+ *   X [T, K] of x_kind with rows ldx values apart; base [T, N] (NULL: zero) and out [T, N] of out_kind, rows ld_base and ld_out
+ *   values apart; out may be base.  adapter_ids [T] on the device, in any order.
+ *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, T) bytes, which never falls as T grows.
+ */
+typedef struct {
+  int n, rank, K, N;
+  int kind;
+  const void* A;
+  const void* B;
+  const float* scale;
+  const int32_t* ranks;
+} cq_adapters;
+size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T);
+cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x_kind, long ldx, const int32_t* adapter_ids, int T,
+                           const void* base, long ld_base, void* out, int out_kind, long ld_out, void* workspace,
+                           size_t workspace_bytes, cq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ CQ_OK = 0
 CQ_A_INT8_CODES, CQ_A_F16, CQ_A_F32, CQ_A_BF16 = 0, 1, 2, 3
 CQ_EPI_NONE, CQ_EPI_SWIGLU = 0, 1
 CQ_OUT_F32, CQ_OUT_F16 = 0, 1
+CQ_GATE_NONE, CQ_GATE_ROW, CQ_GATE_ELEM = 0, 1, 2
 
 EXPORTS = [
     "cq_status_string", "cq_rotate_quant_workspace_bytes", "cq_rotate_quant",
@@ -27,6 +28,8 @@ EXPORTS = [
     "cq_stream_read", "cq_mfma_loop", "cq_rotation_split_bytes", "cq_rotation_split",
     "cq_rotate_quant_split_workspace_bytes", "cq_rotate_quant_split", "cq_hadamard_quant",
     "cq_codebook_grouped_gemm_lut", "cq_expand_centroid_budget",
+    "cq_block_norm", "cq_block_norm_grad_workspace_bytes", "cq_block_norm_grad", "cq_balance_loss_workspace_bytes",
+    "cq_balance_loss", "cq_balance_loss_grad", "cq_adapter_workspace_bytes", "cq_adapter_apply",
 ]
 
 
@@ -48,6 +51,18 @@ class MoeLayout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in
                 ("total", "XR", "Q", "Q16", "scale", "logits", "topk_ids", "topk_w", "offsets", "perm", "inv_perm",
                  "src_token", "Hbuf", "Obuf", "scratch", "HQ", "HQ16", "hscale")]
+
+
+class BlockNormSpec(ctypes.Structure):
+    _fields_ = [("H", ctypes.c_int), ("stream_kind", ctypes.c_int), ("block_kind", ctypes.c_int), ("weight_kind", ctypes.c_int),
+                ("gate_kind", ctypes.c_int), ("gate_sigmoid", ctypes.c_int), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float), ("w_pre", ctypes.c_void_p),
+                ("w_post", ctypes.c_void_p)]
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("rank", ctypes.c_int), ("K", ctypes.c_int), ("N", ctypes.c_int), ("kind", ctypes.c_int),
+                ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ranks", ctypes.c_void_p)]
 
 
 _lib = None
@@ -116,6 +131,23 @@ def load_library() -> ctypes.CDLL:
     lib.cq_decode_dense.argtypes = [ctypes.POINTER(CodebookWeights), ci, vp, vp]
     lib.cq_device_info.restype = ci
     lib.cq_device_info.argtypes = [ctypes.POINTER(ci)] * 5
+    ns, ad, cf, cl = ctypes.POINTER(BlockNormSpec), ctypes.POINTER(Adapters), ctypes.c_float, ctypes.c_long
+    lib.cq_block_norm.restype = ci
+    lib.cq_block_norm.argtypes = [ns, vp, vp, vp, ci, vp, vp, vp]
+    lib.cq_block_norm_grad_workspace_bytes.restype = sz
+    lib.cq_block_norm_grad_workspace_bytes.argtypes = [ns, ci]
+    lib.cq_block_norm_grad.restype = ci
+    lib.cq_block_norm_grad.argtypes = [ns, vp, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cq_balance_loss_workspace_bytes.restype = sz
+    lib.cq_balance_loss_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.cq_balance_loss.restype = ci
+    lib.cq_balance_loss.argtypes = [vp, ci, vp, vp, ci, vp, ci, ci, ci, cf, vp, vp, vp, vp, vp, sz, vp]
+    lib.cq_balance_loss_grad.restype = ci
+    lib.cq_balance_loss_grad.argtypes = [vp, ci, vp, vp, vp, ci, vp, ci, ci, ci, cf, vp, vp, vp]
+    lib.cq_adapter_workspace_bytes.restype = sz
+    lib.cq_adapter_workspace_bytes.argtypes = [ad, ci]
+    lib.cq_adapter_apply.restype = ci
+    lib.cq_adapter_apply.argtypes = [ad, vp, ci, cl, vp, ci, vp, cl, vp, ci, cl, vp, sz, vp]
     lib.cq_stream_read.restype = ci
     lib.cq_stream_read.argtypes = [vp, sz, vp, vp]
     lib.cq_mfma_loop.restype = ci
@@ -501,3 +533,225 @@ def cq_mfma_loop(workgroups: int, iters: int):
     sink = torch.empty(workgroups * 256, dtype=torch.float32, device="cuda")
     _check(lib.cq_mfma_loop(workgroups, iters, _ptr(sink), _stream()))
     return workgroups * 4 * iters * 16 * 32768.0
+
+
+# ------------------------------------------------------------------------------------------------
+# the operators around the layer
+# ------------------------------------------------------------------------------------------------
+def _kind(dtype, what: str) -> int:
+    import torch
+    kind = {torch.float32: CQ_A_F32, torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16}.get(dtype)
+    if kind is None:
+        raise ValueError(f"{what}: {dtype} is not one of float32, float16, bfloat16")
+    return kind
+
+
+def _tensor(t, what: str, shape, dtype=None):
+    """A contiguous GPU tensor of that shape (None in the shape: any size) and type; returns it."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: not on the GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype} where {dtype} is needed")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: not contiguous")
+    return t
+
+
+class BlockNorm:
+    """The norms around a block, its gate and its residual scales (cq_block_norm_spec).
+
+    w_pre [H]: weights of the norm in front of the next block (None: no such norm); w_post [H]: of the norm behind the block
+    (None: its output is taken as it is).  block_dtype: type of the block's input, output and gate, float32 (what
+    cq_moe_forward takes and gives) or the residual stream's."""
+
+    def __init__(self, w_pre=None, w_post=None, eps: float = 1e-6, residual_scale: float = 1.0, branch_scale: float = 1.0,
+                 gate_sigmoid: bool = False, block_dtype=None):
+        import torch
+        if w_pre is None and w_post is None:
+            self.H, self.weight_dtype = None, torch.float32
+        else:
+            some = w_pre if w_pre is not None else w_post
+            self.H, self.weight_dtype = int(some.shape[0]), some.dtype
+        for name, w in (("w_pre", w_pre), ("w_post", w_post)):
+            if w is not None:
+                _tensor(w, name, (self.H,), self.weight_dtype)
+        self.w_pre, self.w_post = w_pre, w_post
+        self.block_dtype = torch.float32 if block_dtype is None else block_dtype
+        self.weight_kind, self.block_kind = _kind(self.weight_dtype, "weights"), _kind(self.block_dtype, "block_dtype")
+        self.eps, self.residual_scale, self.branch_scale = float(eps), float(residual_scale), float(branch_scale)
+        self.gate_sigmoid = bool(gate_sigmoid)
+
+    def struct(self, h, gate=None) -> BlockNormSpec:
+        gate_kind = CQ_GATE_NONE if gate is None else CQ_GATE_ROW if gate.dim() == 1 else CQ_GATE_ELEM
+        return BlockNormSpec(h.shape[1], _kind(h.dtype, "h"), self.block_kind, self.weight_kind, gate_kind, self.gate_sigmoid,
+                             self.eps, self.residual_scale, self.branch_scale, _ptr(self.w_pre), _ptr(self.w_post))
+
+    def check(self, h, y, gate):
+        _tensor(h, "h", (None, self.H))
+        if y is None:
+            if gate is not None:
+                raise ValueError("gate: there is no block output that it could gate")
+            return
+        _tensor(y, "y", h.shape, self.block_dtype)
+        if gate is not None:
+            _tensor(gate, "gate", h.shape[:1] if gate.dim() == 1 else h.shape, self.block_dtype)
+
+
+def cq_block_norm(norm: BlockNorm, h, y=None, gate=None, h_out=None, x_out=None) -> Dict[str, object]:
+    """h' = residual_scale h + branch_scale gate N(y) w_post and x = N(h') w_pre: {"h": h', "x": x or None}.
+
+    y None: x = N(h) w_pre alone, and "h" is h itself."""
+    torch = _torch()
+    lib = load_library()
+    norm.check(h, y, gate)
+    if y is None:
+        h_new = h
+    else:
+        h_new = torch.empty_like(h) if h_out is None else _tensor(h_out, "h_out", h.shape, h.dtype)
+    x = None
+    if norm.w_pre is not None:
+        x = (torch.empty(h.shape, dtype=norm.block_dtype, device=h.device) if x_out is None
+             else _tensor(x_out, "x_out", h.shape, norm.block_dtype))
+    s = norm.struct(h, gate)
+    _check(lib.cq_block_norm(ctypes.byref(s), _ptr(h), _ptr(y), _ptr(gate), h.shape[0], None if y is None else _ptr(h_new),
+                             _ptr(x), _stream()))
+    return {"h": h_new, "x": x}
+
+
+def cq_block_norm_grad(norm: BlockNorm, h, y=None, gate=None, dh=None, dx=None, want_weights: bool = True) -> Dict[str, object]:
+    """Gradients of cq_block_norm from its h' (with y None: its h), y, gate and the gradients dh of h' and dx of x (None: zero):
+    {"dh", "dw_pre", "dgate", "dw_post", "dy"}, None where there is no such input."""
+    torch = _torch()
+    lib = load_library()
+    norm.check(h, y, gate)
+    if dh is not None:
+        _tensor(dh, "dh", h.shape, h.dtype)
+    if dx is not None:
+        if norm.w_pre is None:
+            raise ValueError("dx: there is no norm in front of a next block")
+        _tensor(dx, "dx", h.shape, norm.block_dtype)
+    T, H = h.shape
+    out = {"dh": torch.empty_like(h), "dw_pre": None, "dgate": None, "dw_post": None, "dy": None}
+    if y is not None:
+        out["dy"] = torch.empty_like(y)
+        if gate is not None:
+            out["dgate"] = torch.empty_like(gate)
+        if want_weights and norm.w_post is not None:
+            out["dw_post"] = torch.empty_like(norm.w_post)
+    if want_weights and dx is not None:
+        out["dw_pre"] = torch.empty_like(norm.w_pre)
+    s = norm.struct(h, gate)
+    ws = _ws(lib.cq_block_norm_grad_workspace_bytes(ctypes.byref(s), T))
+    _check(lib.cq_block_norm_grad(ctypes.byref(s), _ptr(h), _ptr(y), _ptr(gate), _ptr(dh), _ptr(dx), T, _ptr(out["dh"]),
+                                  _ptr(out["dy"]), _ptr(out["dgate"]), _ptr(out["dw_pre"]), _ptr(out["dw_post"]), _ptr(ws),
+                                  ws.numel(), _stream()))
+    return out
+
+
+def _balance_args(logits, seq_offsets, token_mask):
+    import torch
+    _tensor(logits, "logits", (None, None))
+    kind = _kind(logits.dtype, "logits")
+    S = 1
+    if seq_offsets is not None:
+        S = _tensor(seq_offsets, "seq_offsets", (None,), torch.int32).shape[0] - 1
+    if token_mask is not None:
+        _tensor(token_mask, "token_mask", logits.shape[:1])
+        if token_mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"token_mask: {token_mask.dtype} is not one of bool, uint8")
+    return kind, S
+
+
+def cq_balance_loss(logits, ids, alpha: float, seq_offsets=None, token_mask=None) -> Dict[str, object]:
+    """Load-balancing loss of router logits [T, E] and selected experts ids [T, k] (cq_route_permute's "logits" and "ids"):
+    {"loss" [1], "counts" [S, E], "probs" [S, E], "tokens" [S + 1]}; sequence by sequence with seq_offsets [S + 1]."""
+    torch = _torch()
+    lib = load_library()
+    kind, S = _balance_args(logits, seq_offsets, token_mask)
+    T, E = logits.shape
+    _tensor(ids, "ids", (T, None), torch.int32)
+    dev = logits.device
+    out = {"loss": torch.empty(1, dtype=torch.float32, device=dev), "counts": torch.empty((max(S, 0), E), dtype=torch.int32, device=dev),
+           "probs": torch.empty((max(S, 0), E), dtype=torch.float32, device=dev),
+           "tokens": torch.empty(S + 1, dtype=torch.int32, device=dev)}
+    ws = _ws(lib.cq_balance_loss_workspace_bytes(T, E, S))
+    _check(lib.cq_balance_loss(_ptr(logits), kind, _ptr(ids), _ptr(seq_offsets), S, _ptr(token_mask), T, E, ids.shape[1], alpha,
+                               _ptr(out["loss"]), _ptr(out["counts"]), _ptr(out["probs"]), _ptr(out["tokens"]), _ptr(ws),
+                               ws.numel(), _stream()))
+    return out
+
+
+def cq_balance_loss_grad(logits, counts, tokens, top_k: int, alpha: float, seq_offsets=None, token_mask=None, dloss=None):
+    """d loss / d logits from cq_balance_loss's counts and tokens, times dloss [1] (on the GPU; None: 1)."""
+    torch = _torch()
+    lib = load_library()
+    kind, S = _balance_args(logits, seq_offsets, token_mask)
+    T, E = logits.shape
+    _tensor(counts, "counts", (S, E), torch.int32)
+    _tensor(tokens, "tokens", (S + 1,), torch.int32)
+    if dloss is not None and (dloss.dtype != torch.float32 or dloss.numel() != 1 or not dloss.is_cuda):
+        raise ValueError("dloss: one float32 value on the GPU is needed")
+    out = torch.empty_like(logits)
+    _check(lib.cq_balance_loss_grad(_ptr(logits), kind, _ptr(counts), _ptr(tokens), _ptr(seq_offsets), S, _ptr(token_mask), T, E,
+                                    top_k, alpha, _ptr(dloss), _ptr(out), _stream()))
+    return out
+
+
+class DeviceAdapters:
+    """Low-rank adapters on the device: A [n, rank, K], B [n, N, rank], scale [n] f32 or None, ranks [n] i32 or None."""
+
+    def __init__(self, A, B, scale=None, ranks=None):
+        import torch
+        _tensor(A, "A", (None, None, None))
+        self.n, self.rank, self.K = A.shape
+        self.kind = _kind(A.dtype, "A")
+        _tensor(B, "B", (self.n, None, self.rank), A.dtype)
+        self.N = B.shape[1]
+        if scale is not None:
+            _tensor(scale, "scale", (self.n,), torch.float32)
+        if ranks is not None:
+            _tensor(ranks, "ranks", (self.n,), torch.int32)
+        self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
+        self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind, _ptr(A), _ptr(B), _ptr(scale), _ptr(ranks))
+
+    def struct(self) -> Adapters:
+        return self._struct
+
+
+def _rows(t, what: str, shape, dtype=None) -> int:
+    """Checks a GPU matrix whose rows are contiguous; returns how many values they are apart."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: not on the GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype} where {dtype} is needed")
+    if t.dim() != 2 or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    T, n = t.shape
+    if n > 1 and t.stride(1) != 1 or T > 1 and t.stride(0) < n:
+        raise ValueError(f"{what}: rows of stride {t.stride()} are not contiguous rows one after another")
+    return t.stride(0) if T > 1 else n
+
+
+def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_dtype=None):
+    """out[t] = base[t] + scale[a] B_a (A_a X[t]) with a = ids[t] (i32; outside [0, n): out[t] = base[t]).
+
+    base: the shared projection's output [T, N] (None: zero); out may be base.  Without either, out_dtype (float32) is the
+    output's type.  X, base and out may be slices of wider rows."""
+    torch = _torch()
+    lib = load_library()
+    T = X.shape[0]
+    ldx = _rows(X, "X", (None, adapters.K))
+    x_kind = _kind(X.dtype, "X")
+    _tensor(ids, "ids", (T,), torch.int32)
+    if out is None:
+        dtype = base.dtype if base is not None else (out_dtype or torch.float32)
+        out = torch.empty((T, adapters.N), dtype=dtype, device=X.device)
+    ldo = _rows(out, "out", (T, adapters.N))
+    ldb = _rows(base, "base", (T, adapters.N), out.dtype) if base is not None else 0
+    s = adapters.struct()
+    ws = _ws(lib.cq_adapter_workspace_bytes(ctypes.byref(s), T))
+    _check(lib.cq_adapter_apply(ctypes.byref(s), _ptr(X), x_kind, ldx, _ptr(ids), T, _ptr(base), ldb, _ptr(out),
+                                _kind(out.dtype, "out"), ldo, _ptr(ws), ws.numel(), _stream()))
+    return out

@@ -1,0 +1,91 @@
+// The norm behind a block, its gate, the residual sum and the norm before the next block, in one pass over the rows:
+//   u = N(y) w_post (or y),  h' = rho h + beta a u,  x = N(h') w_pre,  N(v) = v / sqrt(mean v^2 + eps).
+// Two row sums (y^2, then h'^2) stand between loads and stores; the row stays in registers in fp32 throughout, so that x comes
+// from the unrounded h'.  Bound by HBM: y and h are read once, h' and x written once, about ten operations per value.
+#include "block_norm.h"
+
+namespace {
+
+template <int SK, int BK, int NT, int C, bool VEC>
+__global__ __launch_bounds__(NT) void block_norm_kernel(norm_args P, void* h_out, void* x_out) {
+  __shared__ float lds[2][NT / 64];
+  const size_t row = (size_t)blockIdx.x * P.H;
+  const int c0 = threadIdx.x * 8;
+  float h[C][8];
+#pragma unroll
+  for (int j = 0; j < C; ++j) row_load8<SK, VEC>(P.h, row + c0 + j * NT * 8, P.H - c0 - j * NT * 8, h[j]);
+  if (P.y) {
+    float y[C][8];
+#pragma unroll
+    for (int j = 0; j < C; ++j) row_load8<BK, VEC>(P.y, row + c0 + j * NT * 8, P.H - c0 - j * NT * 8, y[j]);
+    float q = P.beta;
+    if (P.w_post) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0] = fmaf(y[j][i], y[j][i], s[0]);
+      group_sum<NT, 1>(s, lds[0]);
+      q *= 1.f / sqrtf(s[0] / (float)P.H + P.eps);
+    }
+    if (P.gate_kind == CQ_GATE_ROW) {
+      const float z = elem_load<BK>(P.gate, blockIdx.x);
+      q *= P.sigmoid ? sigmoid_of(z) : z;
+    }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int c = c0 + j * NT * 8;
+      if (P.w_post) {
+        float w[8];
+        weight_load8<SK, VEC>(P.w_post, P.wf32, c, P.H - c, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[j][i] *= w[i];
+      }
+      if (P.gate_kind == CQ_GATE_ELEM) {
+        float z[8];
+        row_load8<BK, VEC>(P.gate, row + c, P.H - c, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[j][i] *= P.sigmoid ? sigmoid_of(z[i]) : z[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[j][i] = fmaf(q, y[j][i], P.rho * h[j][i]);
+      row_store8<SK, VEC>(h_out, row + c, P.H - c, h[j]);
+    }
+  }
+  if (!x_out) return;
+  float s[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[0] = fmaf(h[j][i], h[j][i], s[0]);
+  group_sum<NT, 1>(s, lds[1]);
+  const float r = 1.f / sqrtf(s[0] / (float)P.H + P.eps);
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int c = c0 + j * NT * 8;
+    float w[8];
+    weight_load8<SK, VEC>(P.w_pre, P.wf32, c, P.H - c, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] *= h[j][i] * r;
+    row_store8<BK, VEC>(x_out, row + c, P.H - c, w);
+  }
+}
+
+}  // namespace
+
+extern "C" cq_status cq_block_norm(const cq_block_norm_spec* P, const void* h, const void* y, const void* gate, int T,
+                                   void* h_out, void* x_out, cq_stream stream) {
+  const cq_status st = check_norm_spec(P, T);
+  if (st != CQ_OK) return st;
+  if (T == 0) return CQ_OK;
+  if (!h || (!y && !x_out) || (y && !h_out) || (x_out && !P->w_pre)) return CQ_ERR_NULL;
+  if (y && P->gate_kind != CQ_GATE_NONE && !gate) return CQ_ERR_NULL;
+  const norm_args a = make_norm_args(P, T, h, y, gate);
+  const void* const rows[] = {h, y, a.gate_kind == CQ_GATE_ELEM ? gate : nullptr, y ? h_out : nullptr, x_out, P->w_pre, a.w_post};
+  const bool vec = rows_aligned(P->H, rows, 7);
+#define LAUNCH(SK, BK, NT, C, VEC)                                                                                  \
+  hipLaunchKernelGGL((block_norm_kernel<SK, BK, NT, C, VEC>), dim3(T), dim3(NT), 0, (hipStream_t)stream, a, h_out, x_out)
+  CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, vec, P->H);
+#undef LAUNCH
+  return cq_check_launch();
+}
