@@ -374,7 +374,7 @@ cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t
  * differs between tenants is added beside them):
  *     out_t = base_t + scale[a] * B_a (A_a x_t),   a = adapter_ids[t];   a outside [0, n): out_t = base_t
  *   A [n, rank, K] and B [n, N, rank] of `kind`; scale [n] f32 or NULL (1); ranks [n] i32 or NULL: adapter a has ranks[a] <= rank
- *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256.
+ *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256; K, N <= 2^23.
  *   X [T, K] of x_kind with rows ldx values apart; base [T, N] (NULL: zero) and out [T, N] of out_kind, rows ld_base and ld_out
  *   values apart; out may be base.  adapter_ids [T] on the device, in any order.
  *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, T) bytes, which never falls as T grows.
