@@ -183,6 +183,12 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _raw_stream(t) -> int:
+    """_stream() for a call on a tensor of the current device, without the Stream object (2.7 us less on the host)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
 def _ws(nbytes: int):
     torch = _torch()
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device="cuda")
@@ -538,16 +544,25 @@ def cq_mfma_loop(workgroups: int, iters: int):
 # ------------------------------------------------------------------------------------------------
 # the operators around the layer
 # ------------------------------------------------------------------------------------------------
+_KINDS: Dict[object, int] = {}      # filled once torch is known
+_BYTES: Dict[tuple, int] = {}       # workspace sizes by the sizes that they are functions of
+
+
 def _kind(dtype, what: str) -> int:
-    import torch
-    kind = {torch.float32: CQ_A_F32, torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16}.get(dtype)
+    kind = _KINDS.get(dtype)
     if kind is None:
-        raise ValueError(f"{what}: {dtype} is not one of float32, float16, bfloat16")
+        import torch
+        _KINDS.update({torch.float32: CQ_A_F32, torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16})
+        if dtype not in _KINDS:
+            raise ValueError(f"{what}: {dtype} is not one of float32, float16, bfloat16")
+        kind = _KINDS[dtype]
     return kind
 
 
 def _tensor(t, what: str, shape, dtype=None):
     """A contiguous GPU tensor of that shape (None in the shape: any size) and type; returns it."""
+    if t.is_cuda and t.shape == shape and (dtype is None or t.dtype == dtype) and t.is_contiguous():
+        return t
     if not t.is_cuda:
         raise ValueError(f"{what}: not on the GPU")
     if dtype is not None and t.dtype != dtype:
@@ -557,6 +572,12 @@ def _tensor(t, what: str, shape, dtype=None):
     if not t.is_contiguous():
         raise ValueError(f"{what}: not contiguous")
     return t
+
+
+def _scratch(like, nbytes: int):
+    """Device memory for one call; the caching allocator hands it on in the order of the stream."""
+    import torch
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=like.device)
 
 
 class BlockNorm:
@@ -583,13 +604,20 @@ class BlockNorm:
         self.eps, self.residual_scale, self.branch_scale = float(eps), float(residual_scale), float(branch_scale)
         self.gate_sigmoid = bool(gate_sigmoid)
 
+        self._specs: Dict[tuple, BlockNormSpec] = {}
+
     def struct(self, h, gate=None) -> BlockNormSpec:
         gate_kind = CQ_GATE_NONE if gate is None else CQ_GATE_ROW if gate.dim() == 1 else CQ_GATE_ELEM
-        return BlockNormSpec(h.shape[1], _kind(h.dtype, "h"), self.block_kind, self.weight_kind, gate_kind, self.gate_sigmoid,
-                             self.eps, self.residual_scale, self.branch_scale, _ptr(self.w_pre), _ptr(self.w_post))
+        key = (h.shape[1], h.dtype, gate_kind)
+        spec = self._specs.get(key)
+        if spec is None:
+            spec = self._specs[key] = BlockNormSpec(
+                h.shape[1], _kind(h.dtype, "h"), self.block_kind, self.weight_kind, gate_kind, self.gate_sigmoid, self.eps,
+                self.residual_scale, self.branch_scale, _ptr(self.w_pre), _ptr(self.w_post))
+        return spec
 
     def check(self, h, y, gate):
-        _tensor(h, "h", (None, self.H))
+        _tensor(h, "h", (h.shape[0], self.H or h.shape[-1]) if h.dim() == 2 else (None, self.H))
         if y is None:
             if gate is not None:
                 raise ValueError("gate: there is no block output that it could gate")
@@ -603,28 +631,29 @@ def cq_block_norm(norm: BlockNorm, h, y=None, gate=None, h_out=None, x_out=None)
     """h' = residual_scale h + branch_scale gate N(y) w_post and x = N(h') w_pre: {"h": h', "x": x or None}.
 
     y None: x = N(h) w_pre alone, and "h" is h itself."""
-    torch = _torch()
-    lib = load_library()
+    lib = _lib or load_library()
     norm.check(h, y, gate)
     if y is None:
         h_new = h
     else:
-        h_new = torch.empty_like(h) if h_out is None else _tensor(h_out, "h_out", h.shape, h.dtype)
+        h_new = h.new_empty(h.shape) if h_out is None else _tensor(h_out, "h_out", h.shape, h.dtype)
     x = None
     if norm.w_pre is not None:
-        x = (torch.empty(h.shape, dtype=norm.block_dtype, device=h.device) if x_out is None
-             else _tensor(x_out, "x_out", h.shape, norm.block_dtype))
-    s = norm.struct(h, gate)
-    _check(lib.cq_block_norm(ctypes.byref(s), _ptr(h), _ptr(y), _ptr(gate), h.shape[0], None if y is None else _ptr(h_new),
-                             _ptr(x), _stream()))
+        if x_out is not None:
+            x = _tensor(x_out, "x_out", h.shape, norm.block_dtype)
+        else:
+            x = h.new_empty(h.shape) if h.dtype == norm.block_dtype else h.new_empty(h.shape, dtype=norm.block_dtype)
+    st = lib.cq_block_norm(norm.struct(h, gate), h.data_ptr(), _ptr(y), _ptr(gate), h.shape[0],
+                           None if y is None else h_new.data_ptr(), _ptr(x), _raw_stream(h))
+    if st:
+        raise CqError(st)
     return {"h": h_new, "x": x}
 
 
 def cq_block_norm_grad(norm: BlockNorm, h, y=None, gate=None, dh=None, dx=None, want_weights: bool = True) -> Dict[str, object]:
     """Gradients of cq_block_norm from its h' (with y None: its h), y, gate and the gradients dh of h' and dx of x (None: zero):
     {"dh", "dw_pre", "dgate", "dw_post", "dy"}, None where there is no such input."""
-    torch = _torch()
-    lib = load_library()
+    lib = _lib or load_library()
     norm.check(h, y, gate)
     if dh is not None:
         _tensor(dh, "dh", h.shape, h.dtype)
@@ -633,30 +662,38 @@ def cq_block_norm_grad(norm: BlockNorm, h, y=None, gate=None, dh=None, dx=None, 
             raise ValueError("dx: there is no norm in front of a next block")
         _tensor(dx, "dx", h.shape, norm.block_dtype)
     T, H = h.shape
-    out = {"dh": torch.empty_like(h), "dw_pre": None, "dgate": None, "dw_post": None, "dy": None}
+    o_dh, dw_pre, dgate, dw_post, dy = h.new_empty(h.shape), None, None, None, None
     if y is not None:
-        out["dy"] = torch.empty_like(y)
+        dy = y.new_empty(y.shape)
         if gate is not None:
-            out["dgate"] = torch.empty_like(gate)
+            dgate = gate.new_empty(gate.shape)
         if want_weights and norm.w_post is not None:
-            out["dw_post"] = torch.empty_like(norm.w_post)
+            dw_post = norm.w_post.new_empty(H)
     if want_weights and dx is not None:
-        out["dw_pre"] = torch.empty_like(norm.w_pre)
+        dw_pre = norm.w_pre.new_empty(H)
     s = norm.struct(h, gate)
-    ws = _ws(lib.cq_block_norm_grad_workspace_bytes(ctypes.byref(s), T))
-    _check(lib.cq_block_norm_grad(ctypes.byref(s), _ptr(h), _ptr(y), _ptr(gate), _ptr(dh), _ptr(dx), T, _ptr(out["dh"]),
-                                  _ptr(out["dy"]), _ptr(out["dgate"]), _ptr(out["dw_pre"]), _ptr(out["dw_post"]), _ptr(ws),
-                                  ws.numel(), _stream()))
-    return out
+    ws, nbytes = None, 0
+    if dw_pre is not None or dw_post is not None:
+        nbytes = _BYTES.get(("norm", T, H))
+        if nbytes is None:
+            nbytes = _BYTES["norm", T, H] = lib.cq_block_norm_grad_workspace_bytes(s, T)
+        ws = _scratch(h, nbytes)
+    st = lib.cq_block_norm_grad(s, h.data_ptr(), _ptr(y), _ptr(gate), _ptr(dh), _ptr(dx), T, o_dh.data_ptr(), _ptr(dy), _ptr(dgate),
+                                _ptr(dw_pre), _ptr(dw_post), _ptr(ws), nbytes, _raw_stream(h))
+    if st:
+        raise CqError(st)
+    return {"dh": o_dh, "dw_pre": dw_pre, "dgate": dgate, "dw_post": dw_post, "dy": dy}
 
 
 def _balance_args(logits, seq_offsets, token_mask):
     import torch
-    _tensor(logits, "logits", (None, None))
+    _tensor(logits, "logits", logits.shape if logits.dim() == 2 else (None, None))
     kind = _kind(logits.dtype, "logits")
     S = 1
     if seq_offsets is not None:
-        S = _tensor(seq_offsets, "seq_offsets", (None,), torch.int32).shape[0] - 1
+        S = _tensor(seq_offsets, "seq_offsets", seq_offsets.shape[:1], torch.int32).shape[0] - 1
+        if S < 1:
+            raise ValueError("seq_offsets: the first and the last offset of every sequence are needed")
     if token_mask is not None:
         _tensor(token_mask, "token_mask", logits.shape[:1])
         if token_mask.dtype not in (torch.bool, torch.uint8):
@@ -667,35 +704,43 @@ def _balance_args(logits, seq_offsets, token_mask):
 def cq_balance_loss(logits, ids, alpha: float, seq_offsets=None, token_mask=None) -> Dict[str, object]:
     """Load-balancing loss of router logits [T, E] and selected experts ids [T, k] (cq_route_permute's "logits" and "ids"):
     {"loss" [1], "counts" [S, E], "probs" [S, E], "tokens" [S + 1]}; sequence by sequence with seq_offsets [S + 1]."""
-    torch = _torch()
-    lib = load_library()
+    import torch
+    lib = _lib or load_library()
     kind, S = _balance_args(logits, seq_offsets, token_mask)
     T, E = logits.shape
-    _tensor(ids, "ids", (T, None), torch.int32)
-    dev = logits.device
-    out = {"loss": torch.empty(1, dtype=torch.float32, device=dev), "counts": torch.empty((max(S, 0), E), dtype=torch.int32, device=dev),
-           "probs": torch.empty((max(S, 0), E), dtype=torch.float32, device=dev),
-           "tokens": torch.empty(S + 1, dtype=torch.int32, device=dev)}
-    ws = _ws(lib.cq_balance_loss_workspace_bytes(T, E, S))
-    _check(lib.cq_balance_loss(_ptr(logits), kind, _ptr(ids), _ptr(seq_offsets), S, _ptr(token_mask), T, E, ids.shape[1], alpha,
-                               _ptr(out["loss"]), _ptr(out["counts"]), _ptr(out["probs"]), _ptr(out["tokens"]), _ptr(ws),
-                               ws.numel(), _stream()))
-    return out
+    k = ids.shape[-1]
+    _tensor(ids, "ids", (T, k), torch.int32)
+    loss = torch.empty(1, dtype=torch.float32, device=logits.device)
+    counts = ids.new_empty((S, E))
+    probs = loss.new_empty((S, E))
+    tokens = ids.new_empty(S + 1)
+    nbytes = _BYTES.get(("balance", T, E, S))
+    if nbytes is None:
+        nbytes = _BYTES["balance", T, E, S] = lib.cq_balance_loss_workspace_bytes(T, E, S)
+    ws = _scratch(logits, nbytes)
+    st = lib.cq_balance_loss(logits.data_ptr(), kind, ids.data_ptr(), _ptr(seq_offsets), S, _ptr(token_mask), T, E, k, alpha,
+                             loss.data_ptr(), counts.data_ptr(), probs.data_ptr(), tokens.data_ptr(), ws.data_ptr(), nbytes,
+                             _raw_stream(logits))
+    if st:
+        raise CqError(st)
+    return {"loss": loss, "counts": counts, "probs": probs, "tokens": tokens}
 
 
 def cq_balance_loss_grad(logits, counts, tokens, top_k: int, alpha: float, seq_offsets=None, token_mask=None, dloss=None):
     """d loss / d logits from cq_balance_loss's counts and tokens, times dloss [1] (on the GPU; None: 1)."""
-    torch = _torch()
-    lib = load_library()
+    import torch
+    lib = _lib or load_library()
     kind, S = _balance_args(logits, seq_offsets, token_mask)
     T, E = logits.shape
     _tensor(counts, "counts", (S, E), torch.int32)
     _tensor(tokens, "tokens", (S + 1,), torch.int32)
     if dloss is not None and (dloss.dtype != torch.float32 or dloss.numel() != 1 or not dloss.is_cuda):
         raise ValueError("dloss: one float32 value on the GPU is needed")
-    out = torch.empty_like(logits)
-    _check(lib.cq_balance_loss_grad(_ptr(logits), kind, _ptr(counts), _ptr(tokens), _ptr(seq_offsets), S, _ptr(token_mask), T, E,
-                                    top_k, alpha, _ptr(dloss), _ptr(out), _stream()))
+    out = logits.new_empty(logits.shape)
+    st = lib.cq_balance_loss_grad(logits.data_ptr(), kind, counts.data_ptr(), tokens.data_ptr(), _ptr(seq_offsets), S,
+                                  _ptr(token_mask), T, E, top_k, alpha, _ptr(dloss), out.data_ptr(), _raw_stream(logits))
+    if st:
+        raise CqError(st)
     return out
 
 
@@ -715,6 +760,7 @@ class DeviceAdapters:
             _tensor(ranks, "ranks", (self.n,), torch.int32)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
         self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind, _ptr(A), _ptr(B), _ptr(scale), _ptr(ranks))
+        self._bytes: Dict[int, int] = {}
 
     def struct(self) -> Adapters:
         return self._struct
@@ -722,6 +768,8 @@ class DeviceAdapters:
 
 def _rows(t, what: str, shape, dtype=None) -> int:
     """Checks a GPU matrix whose rows are contiguous; returns how many values they are apart."""
+    if t.is_cuda and t.shape == shape and (dtype is None or t.dtype == dtype) and t.is_contiguous():
+        return shape[1]
     if not t.is_cuda:
         raise ValueError(f"{what}: not on the GPU")
     if dtype is not None and t.dtype != dtype:
@@ -739,19 +787,26 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
 
     base: the shared projection's output [T, N] (None: zero); out may be base.  Without either, out_dtype (float32) is the
     output's type.  X, base and out may be slices of wider rows."""
-    torch = _torch()
-    lib = load_library()
+    import torch
+    lib = _lib or load_library()
     T = X.shape[0]
-    ldx = _rows(X, "X", (None, adapters.K))
+    ldx = _rows(X, "X", (T, adapters.K))
     x_kind = _kind(X.dtype, "X")
     _tensor(ids, "ids", (T,), torch.int32)
     if out is None:
         dtype = base.dtype if base is not None else (out_dtype or torch.float32)
         out = torch.empty((T, adapters.N), dtype=dtype, device=X.device)
-    ldo = _rows(out, "out", (T, adapters.N))
+        ldo = adapters.N
+    else:
+        ldo = _rows(out, "out", (T, adapters.N))
     ldb = _rows(base, "base", (T, adapters.N), out.dtype) if base is not None else 0
     s = adapters.struct()
-    ws = _ws(lib.cq_adapter_workspace_bytes(ctypes.byref(s), T))
-    _check(lib.cq_adapter_apply(ctypes.byref(s), _ptr(X), x_kind, ldx, _ptr(ids), T, _ptr(base), ldb, _ptr(out),
-                                _kind(out.dtype, "out"), ldo, _ptr(ws), ws.numel(), _stream()))
+    nbytes = adapters._bytes.get(T)
+    if nbytes is None:
+        nbytes = adapters._bytes[T] = lib.cq_adapter_workspace_bytes(s, T)
+    ws = _scratch(X, nbytes)
+    st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),
+                              _kind(out.dtype, "out"), ldo, ws.data_ptr(), nbytes, _raw_stream(X))
+    if st:
+        raise CqError(st)
     return out

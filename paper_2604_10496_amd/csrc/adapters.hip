@@ -118,20 +118,8 @@ __device__ __forceinline__ split_frag split_pack(const float (&v)[8]) {
   return f;
 }
 
-// Eight consecutive 16-bit values as they are; the first `left` exist, the others are zero (VEC: all or none).
-template <bool VEC>
-__device__ __forceinline__ cq_v4u raw_load8(const void* p, size_t at, int left) {
-  cq_v4u w = {0u, 0u, 0u, 0u};
-  const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + at;
-  if constexpr (VEC) {
-    if (left > 0) w = *reinterpret_cast<const cq_v4u*>(q);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) w[i >> 1] |= (uint32_t)q[i] << (16 * (i & 1));
-  }
-  return w;
-}
+// Eight consecutive 16-bit values as they are; the first `left` exist, the others are zero.
+__device__ __forceinline__ cq_v4u raw_load8(const void* p, size_t at, int left) { return row_fetch<CQ_A_BF16>(p, at, left).w[0]; }
 
 // How a pair of types is multiplied
 enum { kSame16 = 0, kSplit = 1, kFloat = 2 };
@@ -142,7 +130,7 @@ constexpr int product_path() {
 
 // low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of
 // K, which its eight wavefronts share out in steps of 64 and add up in LDS.
-template <int XK, int WK, int RT, bool VEC>
+template <int XK, int WK, int RT>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_args P) {
   constexpr int RW = RT * 16, LD = RW + 4;
   __shared__ float lds[kDownWaves][16][LD];
@@ -170,11 +158,11 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
       for (int half = 0; half < 2; ++half) {
         const int k = k0 + g * 16 + half * 8, left = k_end - k;   // this lane's eight of the 32 values of a product
         if constexpr (product_path<XK, WK>() == kSame16) {
-          const cq_v4u x = raw_load8<VEC>(P.X, (size_t)t * P.ldx + k, left);
+          const cq_v4u x = raw_load8(P.X, (size_t)t * P.ldx + k, left);
 #pragma unroll
           for (int i = 0; i < RT; ++i) {
             const bool in = r0 + i * 16 + col < rank;
-            const cq_v4u w = raw_load8<VEC>(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0);
+            const cq_v4u w = raw_load8(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0);
             if constexpr (XK == CQ_A_BF16)
               acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w), __builtin_bit_cast(cq_v8bf16, x), acc[i], 0, 0, 0);
             else
@@ -182,13 +170,13 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
           }
         } else {
           float x[8];
-          row_load8<XK, VEC>(P.X, (size_t)t * P.ldx + k, left, x);
+          row_load8<XK>(P.X, (size_t)t * P.ldx + k, left, x);
           if constexpr (product_path<XK, WK>() == kSplit) {
             const split_frag xs = split_pack(x);
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
               const bool in = r0 + i * 16 + col < rank;
-              const cq_v8bf16 w = __builtin_bit_cast(cq_v8bf16, raw_load8<VEC>(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0));
+              const cq_v8bf16 w = __builtin_bit_cast(cq_v8bf16, raw_load8(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0));
 #pragma unroll
               for (int p = 0; p < 3; ++p) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xs.part[p], acc[i], 0, 0, 0);
             }
@@ -197,7 +185,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
             for (int i = 0; i < RT; ++i) {
               const bool in = r0 + i * 16 + col < rank;
               float w[8];
-              row_load8<WK, VEC>(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0, w);
+              row_load8<WK>(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0, w);
 #pragma unroll
               for (int q = 0; q < 8; ++q) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[q], x[q], acc[i], 0, 0, 0);
             }
@@ -228,7 +216,7 @@ __device__ __forceinline__ int out_row(int tile, int i) {
   return (tile >> 1) * 32 + (i >> 2) * 8 + (tile & 1) * 4 + (i & 3);
 }
 
-template <int WK, int OK, bool VECW, bool VECO>
+template <int WK, int OK>
 __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args P) {
   __shared__ int rows[kUpTile], adapters[kUpTile], found;
   if (!find_rows<kUpTile>(P, rows, adapters, &found)) return;
@@ -255,7 +243,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args 
         if (here && r < rank) {
           for (int p = 0; p < P.parts; ++p) {
             float u[8];
-            row_load8<CQ_A_F32, true>(P.low, ((size_t)p * P.T + t) * P.Rp + r, 8, u);
+            row_load8<CQ_A_F32>(P.low, ((size_t)p * P.T + t) * P.Rp + r, 8, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += u[i];
           }
@@ -267,12 +255,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args 
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int n = n0 + out_row<OK>(j, col);
-            cq_v4u b = raw_load8<VECW>(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0);
-            if (VECW && rank - r < 8) {   // columns beyond the adapter's rank may hold anything
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (r + i >= rank) b[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
-            }
+            const cq_v4u b = raw_load8(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0);
             const cq_v8bf16 w = __builtin_bit_cast(cq_v8bf16, b);
 #pragma unroll
             for (int p = 0; p < 3; ++p) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, vs.part[p], acc[j], 0, 0, 0);
@@ -282,11 +265,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args 
           for (int j = 0; j < 4; ++j) {
             const int n = n0 + out_row<OK>(j, col);
             float w[8];
-            row_load8<WK, VECW>(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0, w);
-            if (VECW && rank - r < 8) {   // columns beyond the adapter's rank may hold anything
-#pragma unroll
-              for (int i = 0; i < 8; ++i) w[i] = r + i < rank ? w[i] : 0.f;
-            }
+            row_load8<WK>(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0, w);
 #pragma unroll
             for (int q = 0; q < 8; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[q], v[q], acc[j], 0, 0, 0);
           }
@@ -299,15 +278,15 @@ __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int n = n0 + out_row<OK>(j, g * 4), left = P.N - n;
-          if (VECO) {
-            if (left <= 0) continue;
+          if (left >= 4) {
+            typedef cq_v4f cq_v4f_any __attribute__((aligned(4)));
             cq_v4f v = {0.f, 0.f, 0.f, 0.f};
-            if (P.base) v = *reinterpret_cast<const cq_v4f*>(reinterpret_cast<const float*>(P.base) + b + n);
+            if (P.base) v = *reinterpret_cast<const cq_v4f_any*>(reinterpret_cast<const float*>(P.base) + b + n);
             if (rank > 0) v += scale * acc[j];
-            *reinterpret_cast<cq_v4f*>(reinterpret_cast<float*>(P.out) + o + n) = v;
+            *reinterpret_cast<cq_v4f_any*>(reinterpret_cast<float*>(P.out) + o + n) = v;
           } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 3; ++q) {
               if (q >= left) continue;
               float v = P.base ? elem_load<OK>(P.base, b + n + q) : 0.f;
               if (rank > 0) v = fmaf(scale, acc[j][q], v);
@@ -322,12 +301,12 @@ __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args 
           float v[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = 0.f;
-          if (P.base) row_load8<OK, VECO>(P.base, b + n, left, v);
+          if (P.base) row_load8<OK>(P.base, b + n, left, v);
           if (rank > 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, acc[j + (i >> 2)][i & 3], v[i]);
           }
-          row_store8<OK, VECO>(P.out, o + n, left, v);
+          row_store8<OK>(P.out, o + n, left, v);
         }
       }
     }
@@ -404,39 +383,25 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   const bool leaders = T <= kLeaderTokens;
   const dim3 down(leaders ? T : (T + kDownTile - 1) / kDownTile, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
   const dim3 up(leaders ? T : (T + kUpTile - 1) / kUpTile, (W->N + 64 * kUpWaves - 1) / (64 * kUpWaves));
-  const bool vec_k = W->K % 8 == 0 && ldx % 8 == 0 && (((uintptr_t)X | (uintptr_t)W->A) % 16) == 0;
-  const bool vec_r = W->rank % 8 == 0 && ((uintptr_t)W->B % 16) == 0;
-  const bool vec_n = W->N % 8 == 0 && (ld_out | (long)P.ldb) % 8 == 0 && (((uintptr_t)out | (uintptr_t)base) % 16) == 0;
-#define DOWN3(XK, WK, RT, VEC) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, VEC>), down, dim3(64 * kDownWaves), 0, s, P)
-#define DOWN2(XK, WK, RT)              \
-  do {                                 \
-    if (vec_k) DOWN3(XK, WK, RT, true); \
-    else DOWN3(XK, WK, RT, false);     \
-  } while (0)
-#define DOWN1(XK, WK)                        \
-  do {                                       \
-    if (W->rank <= 16) DOWN2(XK, WK, 1);     \
+#define DOWN2(XK, WK, RT) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT>), down, dim3(64 * kDownWaves), 0, s, P)
+#define DOWN1(XK, WK)                         \
+  do {                                        \
+    if (W->rank <= 16) DOWN2(XK, WK, 1);      \
     else if (W->rank <= 32) DOWN2(XK, WK, 2); \
-    else DOWN2(XK, WK, 4);                   \
+    else DOWN2(XK, WK, 4);                    \
   } while (0)
-#define DOWN(WK)                                             \
-  do {                                                       \
-    if (x_kind == CQ_A_F32) DOWN1(CQ_A_F32, WK);             \
-    else if (x_kind == CQ_A_F16) DOWN1(CQ_A_F16, WK);        \
-    else DOWN1(CQ_A_BF16, WK);                               \
+#define DOWN(WK)                                      \
+  do {                                                \
+    if (x_kind == CQ_A_F32) DOWN1(CQ_A_F32, WK);      \
+    else if (x_kind == CQ_A_F16) DOWN1(CQ_A_F16, WK); \
+    else DOWN1(CQ_A_BF16, WK);                        \
   } while (0)
-#define UP2(WK, OK)                                                                                              \
-  do {                                                                                                           \
-    if (vec_r && vec_n) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, true, true>), up, dim3(64 * kUpWaves), 0, s, P);   \
-    else if (vec_r) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, true, false>), up, dim3(64 * kUpWaves), 0, s, P);      \
-    else if (vec_n) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, false, true>), up, dim3(64 * kUpWaves), 0, s, P);      \
-    else hipLaunchKernelGGL((adapter_up_kernel<WK, OK, false, false>), up, dim3(64 * kUpWaves), 0, s, P);                \
-  } while (0)
-#define UP(WK)                                             \
-  do {                                                     \
-    if (out_kind == CQ_A_F32) UP2(WK, CQ_A_F32);           \
-    else if (out_kind == CQ_A_F16) UP2(WK, CQ_A_F16);      \
-    else UP2(WK, CQ_A_BF16);                               \
+#define UP2(WK, OK) hipLaunchKernelGGL((adapter_up_kernel<WK, OK>), up, dim3(64 * kUpWaves), 0, s, P)
+#define UP(WK)                                    \
+  do {                                            \
+    if (out_kind == CQ_A_F32) UP2(WK, CQ_A_F32);  \
+    else if (out_kind == CQ_A_F16) UP2(WK, CQ_A_F16); \
+    else UP2(WK, CQ_A_BF16);                      \
   } while (0)
   if (W->kind == CQ_A_F32) { DOWN(CQ_A_F32); UP(CQ_A_F32); }
   else if (W->kind == CQ_A_F16) { DOWN(CQ_A_F16); UP(CQ_A_F16); }

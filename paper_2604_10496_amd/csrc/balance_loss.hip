@@ -1,24 +1,35 @@
 // Load-balancing loss of a router over sequences, with per-expert counts, and its gradient:
 //   p_t = softmax(z_t),  f_se = c_se / (k n_s),  P_se = mean of p_te over the n_s tokens of sequence s that count,
 //   L = alpha / S' sum_s E sum_e f_se P_se (S' sequences with a token),   dz_te = g alpha E / (S' n_s) p_te (f_se - sum_j f_sj p_tj).
-// Tokens are taken in tiles of kTile.  A tile's share of a sequence goes to slot  tile + sequence  of the workspace: from one
+// One pass over the logits in either direction, bound by HBM for long batches and by latency for the others.  L lanes share a
+// token (four neighbouring experts each), so that a wavefront reads 64 / L tokens in one contiguous load, and works on several
+// loads at a time.
+// Forward: tokens are taken in tiles.  A tile's share of a sequence goes to slot  tile + sequence  of the workspace: from one
 // pair to the next in order either the tile or the sequence grows by one at least, so the slots differ, and a second launch
-// adds every sequence's slots in order.  Counts are integers added in LDS; no atomics on floats, no global atomics.
+// adds every sequence's slots in a fixed order; its last workgroup adds the sequences' losses.  Counts are integers added in LDS;
+// no atomics on floats.  Few logits take one workgroup and one launch.
 #include <math.h>
 
 #include "cq_rows.h"
 
 namespace {
 
-constexpr int kTile = 64;
 constexpr int kMaxExperts = 1024;
 
 struct balance_args {
   const void* z;
   const int32_t *ids, *offsets;
   const uint8_t* mask;
-  int T, E, k, S;
+  int T, E, k, S, tile;
   float alpha;
+};
+
+// workspace: per slot probability sums [E] f32, counts [E] i32, tokens i32; per sequence and 32 experts a loss f32; a counter
+struct balance_ws {
+  float* probs;
+  int32_t *counts, *tokens;
+  float* loss;
+  uint32_t* done;
 };
 
 __device__ __forceinline__ int offset_at(const balance_args& P, int s) {
@@ -27,177 +38,356 @@ __device__ __forceinline__ int offset_at(const balance_args& P, int s) {
   return o < 0 ? 0 : (o > P.T ? P.T : o);
 }
 
-// the sequence that token t lies in: the last one that begins at or before it (-1: none does)
+// the last sequence that begins at or before token t (-1: none does); t is the same in the whole wavefront
 __device__ __forceinline__ int sequence_of(const balance_args& P, int t) {
-  int lo = 0, hi = P.S;   // offsets[lo - 1] <= t < offsets[hi] in a non-decreasing list
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (offset_at(P, mid) <= t) lo = mid + 1;
-    else hi = mid;
+  if (!P.offsets) return 0;
+  int n = 0;
+  for (int c = 0; c < P.S; c += 64) {
+    const int s = c + (threadIdx.x & 63);
+    const int here = __popcll(__ballot(s < P.S && offset_at(P, s) <= t));
+    n += here;
+    if (here < 64) break;
   }
-  return lo - 1;
+  return n - 1;
 }
 
-__device__ __forceinline__ float wave_max(float v) {
+// four consecutive values, the first `left` of which exist; the others read as -inf
+template <int KIND>
+__device__ __forceinline__ void load4(const void* p, size_t at, int left, float (&v)[4]) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  for (int i = 0; i < 4; ++i) v[i] = -INFINITY;
+  if (left >= 4) {
+    if constexpr (KIND == CQ_A_F32) {
+      const cq_v4u w = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const float*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    } else {
+      typedef __attribute__((__vector_size__(8))) uint16_t v4h;
+      typedef v4h v4h_any __attribute__((aligned(2)));
+      const v4h w = *reinterpret_cast<const v4h_any*>(reinterpret_cast<const uint16_t*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = KIND == CQ_A_BF16 ? __uint_as_float((uint32_t)w[i] << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) v[i] = elem_load<KIND>(p, at + i);
+  }
+}
+
+template <int KIND>
+__device__ __forceinline__ void store4(void* p, size_t at, int left, const float (&v)[4]) {
+  if (left >= 4) {
+    if constexpr (KIND == CQ_A_F32) {
+      *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<float*>(p) + at) =
+          cq_v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      typedef __attribute__((__vector_size__(8))) uint16_t v4h;
+      typedef v4h v4h_any __attribute__((aligned(2)));
+      v4h w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = KIND == CQ_A_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v[i]) : __builtin_bit_cast(uint16_t, (_Float16)v[i]);
+      *reinterpret_cast<v4h_any*>(reinterpret_cast<uint16_t*>(p) + at) = w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < left) elem_store<KIND>(p, at + i, v[i]);
+  }
+}
+
+// sum and maximum over the L lanes of a token
+template <int L>
+__device__ __forceinline__ float token_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float token_max(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
 
-// p_t of one token in a wavefront: lane l holds experts l, l + 64, ...  A row without a logit above -inf has p = 0.
-template <int KIND, int C>
-__device__ __forceinline__ void softmax_row(const balance_args& P, int t, int lane, float (&p)[C]) {
+// logits -> probabilities of a token; lane i of its L lanes holds experts 4 i + 4 L j ...  A token without a logit above -inf
+// has no probabilities: zeros.
+template <int L, int C>
+__device__ __forceinline__ void softmax_token(float (&p)[C][4]) {
   float m = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < C; ++j) {
-    const int e = lane + j * 64;
-    p[j] = e < P.E ? elem_load<KIND>(P.z, (size_t)t * P.E + e) : -INFINITY;
-    m = fmaxf(m, p[j]);
-  }
-  m = wave_max(m);
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, p[j][i]);
+  m = token_max<L>(m);
+  const float from = m == -INFINITY ? 0.f : m;   // (exp(-inf) = 0; a NaN stays one)
   float sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < C; ++j) {
-    p[j] = m == -INFINITY && !(p[j] != p[j]) ? 0.f : expf(p[j] - m);
-    sum += p[j];
-  }
-  sum = wave_sum(sum);
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[j][i] = expf(p[j][i] - from);
+      sum += p[j][i];
+    }
+  sum = token_sum<L>(sum);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int j = 0; j < C; ++j) p[j] *= inv;
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[j][i] *= inv;
 }
 
-// workspace: per slot probability sums [E] f32, counts [E] i32, tokens i32; per sequence its loss f32
-struct balance_ws {
-  float* probs;
-  int32_t *counts, *tokens;
-  float* loss;
+template <int NT, int L, int C>
+struct segment_lds {
+  float p[NT / 64][L * C * 4];   // per wavefront
+  int c[kMaxExperts < L * C * 4 ? kMaxExperts : L * C * 4];
+  int n;
 };
 
-template <int KIND, int C>
+// Tokens [a, b) of one sequence: probability sums per wavefront, counts and the tokens that count, into LDS.  Ends with a barrier.
+template <int KIND, int NT, int L, int C>
+__device__ __forceinline__ void segment(const balance_args& P, int a, int b, segment_lds<NT, L, C>& S) {
+  constexpr int U = C == 1 ? 4 : 1;   // loads in flight
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L) * 4;
+  for (int e = threadIdx.x; e < P.E; e += NT) S.c[e] = 0;
+  if (threadIdx.x == 0) S.n = P.mask ? 0 : b - a;
+  __syncthreads();
+  float acc[C][4];
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+  for (int t0 = a; t0 < b; t0 += U * (NT / L)) {
+    float p[U][C][4];
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * (NT / L) + threadIdx.x / L;
+      in[u] = t < b && (!P.mask || P.mask[t]);
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        const int e = e0 + j * L * 4;
+        load4<KIND>(P.z, (size_t)t * P.E + e, in[u] ? P.E - e : 0, p[u][j]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      softmax_token<L, C>(p[u]);
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] += p[u][j][i];
+    }
+    if (P.mask) {
+      int n = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) n += __popcll(__ballot(in[u] && lane % L == 0));
+      if (lane == 0 && n) atomicAdd(&S.n, n);
+    }
+  }
+  const int assignments = (b - a) * P.k;
+  for (int i = threadIdx.x; i < assignments; i += NT) {
+    if (P.mask && !P.mask[a + i / P.k]) continue;
+    const int id = P.ids[(size_t)a * P.k + i];
+    if (id >= 0 && id < P.E) atomicAdd(&S.c[id], 1);
+  }
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v = acc[j][i];
+#pragma unroll
+      for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+      if (lane < L) S.p[wave][e0 + j * L * 4 + i] = v;
+    }
+  __syncthreads();
+}
+
+template <int KIND, int L, int C>
 __global__ __launch_bounds__(256) void balance_tile_kernel(balance_args P, balance_ws W) {
-  __shared__ float lds_p[4][kMaxExperts];
-  __shared__ int lds_c[kMaxExperts];
-  __shared__ int lds_n;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t0 = blockIdx.x * kTile, t1 = min(P.T, t0 + kTile);
-  int s = sequence_of(P, t0);
-  if (s < 0) s = 0;
-  for (; s < P.S; ++s) {
+  __shared__ segment_lds<256, L, C> lds;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *W.done = 0;
+  const int t0 = blockIdx.x * P.tile, t1 = min(P.T, t0 + P.tile);
+  for (int s = max(sequence_of(P, t0), 0); s < P.S; ++s) {
     const int a0 = offset_at(P, s), b0 = offset_at(P, s + 1);
     if (a0 >= t1) break;
     const int a = max(a0, t0), b = min(b0, t1);
     if (a >= b) continue;
-    for (int e = threadIdx.x; e < P.E; e += 256) lds_c[e] = 0;
-    if (threadIdx.x == 0) lds_n = 0;
-    __syncthreads();
-    float acc[C];
-#pragma unroll
-    for (int j = 0; j < C; ++j) acc[j] = 0.f;
-    for (int t = a + wave; t < b; t += 4) {
-      if (P.mask && !P.mask[t]) continue;
-      if (lane == 0) atomicAdd(&lds_n, 1);
-      if (lane < P.k) {
-        const int id = P.ids[(size_t)t * P.k + lane];
-        if (id >= 0 && id < P.E) atomicAdd(&lds_c[id], 1);
-      }
-      float p[C];
-      softmax_row<KIND, C>(P, t, lane, p);
-#pragma unroll
-      for (int j = 0; j < C; ++j) acc[j] += p[j];
-    }
-#pragma unroll
-    for (int j = 0; j < C; ++j)
-      if (lane + j * 64 < P.E) lds_p[wave][lane + j * 64] = acc[j];
-    __syncthreads();
+    segment<KIND, 256, L, C>(P, a, b, lds);
     const size_t slot = (size_t)blockIdx.x + s;
     for (int e = threadIdx.x; e < P.E; e += 256) {
-      W.probs[slot * P.E + e] = (lds_p[0][e] + lds_p[1][e]) + (lds_p[2][e] + lds_p[3][e]);
-      W.counts[slot * P.E + e] = lds_c[e];
+      W.probs[slot * P.E + e] = (lds.p[0][e] + lds.p[1][e]) + (lds.p[2][e] + lds.p[3][e]);
+      W.counts[slot * P.E + e] = lds.c[e];
     }
-    if (threadIdx.x == 0) W.tokens[slot] = lds_n;
+    if (threadIdx.x == 0) W.tokens[slot] = lds.n;
     __syncthreads();
   }
 }
 
-__global__ __launch_bounds__(256) void balance_sequence_kernel(balance_args P, balance_ws W, int32_t* counts, float* probs,
-                                                               int32_t* tokens) {
-  __shared__ float lds[4];
-  const int s = blockIdx.x;
+// Few logits: everything in one workgroup, sequence after sequence.
+template <int KIND, int L, int C>
+__global__ __launch_bounds__(1024) void balance_one_kernel(balance_args P, int32_t* counts, float* probs, int32_t* tokens, float* loss) {
+  __shared__ segment_lds<1024, L, C> lds;
+  __shared__ float sums[16];
+  float total[1] = {0.f};
+  int used = 0;
+  for (int s = 0; s < P.S; ++s) {
+    const int a = offset_at(P, s), b = max(a, offset_at(P, s + 1));
+    segment<KIND, 1024, L, C>(P, a, b, lds);
+    const int n = lds.n;
+    used += n > 0;
+    if (threadIdx.x < P.E) {
+      const int e = threadIdx.x;
+      float p = 0.f;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) p += lds.p[w][e];
+      p = n > 0 ? p / (float)n : 0.f;
+      probs[(size_t)s * P.E + e] = p;
+      counts[(size_t)s * P.E + e] = lds.c[e];
+      if (n > 0) total[0] = fmaf((float)lds.c[e] / ((float)P.k * (float)n), p, total[0]);
+    }
+    if (threadIdx.x == 0) tokens[s] = n;
+    __syncthreads();
+  }
+  group_sum<1024, 1>(total, sums);
+  if (threadIdx.x == 0) {
+    tokens[P.S] = used;
+    loss[0] = used > 0 ? P.alpha * (float)P.E * total[0] / (float)used : 0.f;
+  }
+}
+
+// One workgroup per sequence and 32 experts: 32 threads take its slots in turn for every expert.  The workgroup that ends last
+// adds the losses.
+__global__ __launch_bounds__(1024) void balance_sequence_kernel(balance_args P, balance_ws W, int32_t* counts, float* probs,
+                                                                int32_t* tokens, float* loss) {
+  __shared__ float lds_p[32][33];
+  __shared__ int lds_c[32][33];
+  __shared__ int lds_n;
+  __shared__ bool last;
+  __shared__ float sums[16];
+  const int s = blockIdx.x, x = threadIdx.x & 31, y = threadIdx.x >> 5, e = blockIdx.y * 32 + x;
   const int a = offset_at(P, s), b = offset_at(P, s + 1);
-  const int i0 = a / kTile, i1 = b > a ? (b - 1) / kTile : i0 - 1;
+  const int i0 = a / P.tile, i1 = b > a ? (b - 1) / P.tile : i0 - 1;
+  if (threadIdx.x == 0) lds_n = 0;
+  __syncthreads();
   int n = 0;
-  for (int i = i0; i <= i1; ++i) n += W.tokens[(size_t)i + s];
-  float loss[1] = {0.f};
-  for (int e = threadIdx.x; e < P.E; e += 256) {
-    float p = 0.f;
-    int c = 0;
-    for (int i = i0; i <= i1; ++i) {
+  for (int i = i0 + threadIdx.x; i <= i1; i += 1024) n += W.tokens[(size_t)i + s];
+  if (n) atomicAdd(&lds_n, n);
+  float p = 0.f;
+  int c = 0;
+  if (e < P.E) {
+#pragma unroll 4
+    for (int i = i0 + y; i <= i1; i += 32) {
       p += W.probs[((size_t)i + s) * P.E + e];
       c += W.counts[((size_t)i + s) * P.E + e];
     }
-    p = n > 0 ? p / (float)n : 0.f;
-    probs[(size_t)s * P.E + e] = p;
-    counts[(size_t)s * P.E + e] = c;
-    if (n > 0) loss[0] = fmaf((float)c / ((float)P.k * (float)n), p, loss[0]);
   }
-  group_sum<256, 1>(loss, lds);
-  if (threadIdx.x == 0) {
-    tokens[s] = n;
-    W.loss[s] = loss[0];
-  }
-}
-
-__global__ __launch_bounds__(256) void balance_total_kernel(balance_args P, balance_ws W, int32_t* tokens, float* loss) {
-  __shared__ float lds[4];
-  __shared__ int lds_used;
-  if (threadIdx.x == 0) lds_used = 0;
+  lds_p[y][x] = p;
+  lds_c[y][x] = c;
   __syncthreads();
-  float sum[1] = {0.f};
-  int used = 0;
-  for (int s = threadIdx.x; s < P.S; s += 256) {
-    sum[0] += W.loss[s];
-    used += tokens[s] > 0;
+  n = lds_n;
+  if (threadIdx.x < 32) {
+    p = 0.f;
+    c = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      p += lds_p[i][x];
+      c += lds_c[i][x];
+    }
+    float part = 0.f;
+    if (e < P.E) {
+      p = n > 0 ? p / (float)n : 0.f;
+      probs[(size_t)s * P.E + e] = p;
+      counts[(size_t)s * P.E + e] = c;
+      if (n > 0) part = (float)c / ((float)P.k * (float)n) * p;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor(part, o, 32);
+    if (threadIdx.x == 0) {
+      // (what the last workgroup reads goes through the caches that all compute units share)
+      __hip_atomic_store(&W.loss[(size_t)s * gridDim.y + blockIdx.y], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (blockIdx.y == 0) __hip_atomic_store(&tokens[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const uint32_t before = __hip_atomic_fetch_add(W.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+      last = before == gridDim.x * gridDim.y - 1;
+    }
   }
-  if (used) atomicAdd(&lds_used, used);
-  group_sum<256, 1>(sum, lds);
+  __syncthreads();
+  if (!last) return;
+  if (threadIdx.x == 0) lds_n = 0;
+  __syncthreads();
+  float total[1] = {0.f};
+  for (size_t i = threadIdx.x; i < (size_t)P.S * gridDim.y; i += 1024)
+    total[0] += __hip_atomic_load(&W.loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  int used = 0;
+  for (int i = threadIdx.x; i < P.S; i += 1024) used += __hip_atomic_load(&tokens[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
+  if (used) atomicAdd(&lds_n, used);
+  group_sum<1024, 1>(total, sums);
   if (threadIdx.x == 0) {
-    tokens[P.S] = lds_used;
-    loss[0] = lds_used > 0 ? P.alpha * (float)P.E * sum[0] / (float)lds_used : 0.f;
+    tokens[P.S] = lds_n;
+    loss[0] = lds_n > 0 ? P.alpha * (float)P.E * total[0] / (float)lds_n : 0.f;
   }
 }
 
-template <int KIND, int C>
+template <int KIND, int L, int C>
 __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const int32_t* counts, const int32_t* tokens,
                                                            const float* d_loss, void* dz) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t = blockIdx.x * 4 + wave;
-  if (t >= P.T) return;
-  const int s = sequence_of(P, t);
-  const bool counted = s >= 0 && t < offset_at(P, s + 1) && !(P.mask && !P.mask[t]);
-  float p[C];
+  constexpr int U = C == 1 ? 4 : 1;
+  const int e0 = (threadIdx.x % L) * 4, t0 = blockIdx.x * (U * (256 / L));
+  const int s0 = sequence_of(P, t0);
+  float p[U][C][4];
+  bool in[U];
 #pragma unroll
-  for (int j = 0; j < C; ++j) p[j] = 0.f;
-  if (counted) {
-    softmax_row<KIND, C>(P, t, lane, p);
-    const int n = tokens[s];
-    const float per = n > 0 ? 1.f / ((float)P.k * (float)n) : 0.f;
-    float f[C], dot = 0.f;
+  for (int u = 0; u < U; ++u) {
+    const int t = t0 + u * (256 / L) + threadIdx.x / L;
+    in[u] = t < P.T && (!P.mask || P.mask[t]);
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const int e = lane + j * 64;
-      f[j] = e < P.E ? (float)counts[(size_t)s * P.E + e] * per : 0.f;
-      dot = fmaf(f[j], p[j], dot);
+      const int e = e0 + j * L * 4;
+      load4<KIND>(P.z, (size_t)t * P.E + e, in[u] ? P.E - e : 0, p[u][j]);
     }
-    dot = wave_sum(dot);
-    const int used = tokens[P.S];
-    const float w = (d_loss ? d_loss[0] : 1.f) * (n > 0 && used > 0 ? P.alpha * (float)P.E / ((float)used * (float)n) : 0.f);
-#pragma unroll
-    for (int j = 0; j < C; ++j) p[j] = w * p[j] * (f[j] - dot);
   }
+  const int used = tokens[P.S];
+  const float g = (d_loss ? d_loss[0] : 1.f) * P.alpha * (float)P.E;
+  float f[C][4];
+  float w = 0.f;
+  int s = s0, have = -2;
 #pragma unroll
-  for (int j = 0; j < C; ++j)
-    if (lane + j * 64 < P.E) elem_store<KIND>(dz, (size_t)t * P.E + lane + j * 64, p[j]);
+  for (int u = 0; u < U; ++u) {
+    const int t = t0 + u * (256 / L) + threadIdx.x / L;
+    softmax_token<L, C>(p[u]);
+    if (P.offsets) {
+      while (s + 1 < P.S && offset_at(P, s + 1) <= t) ++s;
+      in[u] = in[u] && s >= 0 && t < offset_at(P, s + 1);
+    }
+    if (s != have) {
+      have = s;
+      const int n = s >= 0 ? tokens[s] : 0;
+      const float per = n > 0 ? 1.f / ((float)P.k * (float)n) : 0.f;
+      w = n > 0 && used > 0 ? g / ((float)used * (float)n) : 0.f;
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = e0 + j * L * 4 + i;
+          f[j][i] = e < P.E && s >= 0 ? (float)counts[(size_t)s * P.E + e] * per : 0.f;
+        }
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dot = fmaf(f[j][i], p[u][j][i], dot);
+    dot = token_sum<L>(dot);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[u][j][i] = in[u] ? w * p[u][j][i] * (f[j][i] - dot) : 0.f;
+      const int e = e0 + j * L * 4;
+      store4<KIND>(dz, (size_t)t * P.E + e, t < P.T ? P.E - e : 0, p[u][j]);
+    }
+  }
 }
 
 cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, int E, int k) {
@@ -207,14 +397,24 @@ cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, in
   return CQ_OK;
 }
 
-size_t slots_of(int T, int S) { return (size_t)(T + kTile - 1) / kTile + S; }
+// Tokens per workgroup: one round of loads in flight for up to 64 experts; more where the second launch would have to add more
+// than 512 tiles.
+int tile_of(int T) { return T <= (64 << 9) ? 64 : T <= (128 << 9) ? 128 : 256; }
+
+size_t slots_of(int T, int S) { return (size_t)T / 64 + 1 + S; }   // (never falls as T grows)
+
+bool in_one(int T, int E, int S) { return (long)T * E <= 32768 && S <= 4 && E <= 256; }
 
 #define CQ_BALANCE_WIDTHS(LAUNCH, KIND, E)      \
   do {                                          \
-    if ((E) <= 64) LAUNCH(KIND, 1);             \
-    else if ((E) <= 128) LAUNCH(KIND, 2);       \
-    else if ((E) <= 256) LAUNCH(KIND, 4);       \
-    else LAUNCH(KIND, 16);                      \
+    if ((E) <= 4) LAUNCH(KIND, 1, 1);           \
+    else if ((E) <= 8) LAUNCH(KIND, 2, 1);      \
+    else if ((E) <= 16) LAUNCH(KIND, 4, 1);     \
+    else if ((E) <= 32) LAUNCH(KIND, 8, 1);     \
+    else if ((E) <= 64) LAUNCH(KIND, 16, 1);    \
+    else if ((E) <= 128) LAUNCH(KIND, 32, 1);   \
+    else if ((E) <= 256) LAUNCH(KIND, 64, 1);   \
+    else LAUNCH(KIND, 64, 4);                   \
   } while (0)
 #define CQ_BALANCE_DISPATCH(LAUNCH, kind, E)                               \
   do {                                                                     \
@@ -228,7 +428,7 @@ size_t slots_of(int T, int S) { return (size_t)(T + kTile - 1) / kTile + S; }
 extern "C" size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs) {
   if (T < 0 || E <= 0 || E > kMaxExperts || n_seqs <= 0) return 0;
   const size_t slots = slots_of(T, n_seqs);
-  return 2 * cq_align_up(slots * E * 4, 256) + cq_align_up(slots * 4, 256) + cq_align_up((size_t)n_seqs * 4, 256);
+  return 2 * cq_align_up(slots * E * 4, 256) + cq_align_up(slots * 4, 256) + cq_align_up((size_t)n_seqs * ((E + 31) / 32) * 4, 256) + 256;
 }
 
 extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const int32_t* topk_ids, const int32_t* seq_offsets,
@@ -240,7 +440,7 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   if ((T > 0 && (!logits || !topk_ids)) || !loss || !counts || !probs || !tokens) return CQ_ERR_NULL;
   if (!workspace || workspace_bytes < cq_balance_loss_workspace_bytes(T, E, n_seqs)) return CQ_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, alpha};
+  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T), alpha};
   const size_t slots = slots_of(T, n_seqs);
   balance_ws W;
   char* at = (char*)workspace;
@@ -251,14 +451,23 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   W.tokens = (int32_t*)at;
   at += cq_align_up(slots * 4, 256);
   W.loss = (float*)at;
-  if (T > 0) {
-#define LAUNCH(KIND, C) \
-  hipLaunchKernelGGL((balance_tile_kernel<KIND, C>), dim3((T + kTile - 1) / kTile), dim3(256), 0, s, P, W)
+  W.done = (uint32_t*)(at + cq_align_up((size_t)n_seqs * ((E + 31) / 32) * 4, 256));
+  if (in_one(T, E, n_seqs)) {
+    // (in_one has no more than 256 experts)
+#define LAUNCH(KIND, L, C)                                                                                                       \
+  do {                                                                                                                           \
+    if constexpr (C == 1)                                                                                                        \
+      hipLaunchKernelGGL((balance_one_kernel<KIND, L, C>), dim3(1), dim3(1024), 0, s, P, counts, probs, tokens, loss);            \
+  } while (0)
     CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
 #undef LAUNCH
+    return cq_check_launch();
   }
-  hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seqs), dim3(256), 0, s, P, W, counts, probs, tokens);
-  hipLaunchKernelGGL(balance_total_kernel, dim3(1), dim3(256), 0, s, P, W, tokens, loss);
+  const int tiles = T > 0 ? (T - 1) / P.tile + 1 : 1;
+#define LAUNCH(KIND, L, C) hipLaunchKernelGGL((balance_tile_kernel<KIND, L, C>), dim3(tiles), dim3(256), 0, s, P, W)
+  CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
+#undef LAUNCH
+  hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seqs, (E + 31) / 32), dim3(1024), 0, s, P, W, counts, probs, tokens, loss);
   return cq_check_launch();
 }
 
@@ -269,10 +478,13 @@ extern "C" cq_status cq_balance_loss_grad(const void* logits, int logit_kind, co
   if (st != CQ_OK) return st;
   if (T == 0) return CQ_OK;
   if (!logits || !counts || !tokens || !d_logits) return CQ_ERR_NULL;
-  const balance_args P = {logits, nullptr, seq_offsets, token_mask, T, E, top_k, n_seqs, alpha};
-#define LAUNCH(KIND, C)                                                                                                \
-  hipLaunchKernelGGL((balance_grad_kernel<KIND, C>), dim3((T - 1) / 4 + 1), dim3(256), 0, (hipStream_t)stream, P, counts, \
-                     tokens, d_loss, d_logits)
+  const balance_args P = {logits, nullptr, seq_offsets, token_mask, T, E, top_k, n_seqs, 0, alpha};
+#define LAUNCH(KIND, L, C)                                                                                                       \
+  do {                                                                                                                           \
+    constexpr int kTokens = (C == 1 ? 4 : 1) * (256 / L);                                                                        \
+    hipLaunchKernelGGL((balance_grad_kernel<KIND, L, C>), dim3((T - 1) / kTokens + 1), dim3(256), 0, (hipStream_t)stream, P, counts, \
+                       tokens, d_loss, d_logits);                                                                                \
+  } while (0)
   CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
 #undef LAUNCH
   return cq_check_launch();

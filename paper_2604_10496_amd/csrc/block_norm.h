@@ -44,48 +44,36 @@ inline norm_args make_norm_args(const cq_block_norm_spec* P, int T, const void* 
   return a;
 }
 
-// Whether rows of width H may be moved 16 bytes at a time: every row starts on 16 bytes and is whole groups of eight values.
-inline bool rows_aligned(int H, const void* const* p, int n) {
-  uintptr_t all = 0;
-  for (int i = 0; i < n; ++i) all |= reinterpret_cast<uintptr_t>(p[i]);
-  return H % 8 == 0 && all % 16 == 0;
-}
-
-template <int SK, bool VEC>
-__device__ __forceinline__ void weight_load8(const void* w, int wf32, int c, int left, float (&v)[8]) {
+template <int SK>
+__device__ __forceinline__ void slot_weights(const void* w, int wf32, const row_slot& s, int H, float (&v)[8]) {
   if (SK == CQ_A_F32 || wf32)
-    row_load8<CQ_A_F32, VEC>(w, c, left, v);
+    row_values<CQ_A_F32>(slot_fetch<CQ_A_F32>(w, 0, s, H, true), v);
   else
-    row_load8<SK, VEC>(w, c, left, v);
+    row_values<SK>(slot_fetch<SK>(w, 0, s, H, true), v);
 }
 
 __device__ __forceinline__ float sigmoid_of(float z) { return 1.f / (1.f + expf(-z)); }
 
 }  // namespace
 
-// Runs LAUNCH(SK, BK, NT, C, VEC) for the kinds, the width and the alignment of a call.  A row belongs to one workgroup of NT
-// threads, each of which holds C groups of eight values.
-#define CQ_NORM_WIDTHS(LAUNCH, SK, BK, VEC, H)            \
-  do {                                                    \
-    if ((H) <= 512) LAUNCH(SK, BK, 64, 1, VEC);           \
-    else if ((H) <= 2048) LAUNCH(SK, BK, 256, 1, VEC);    \
-    else if ((H) <= 4096) LAUNCH(SK, BK, 512, 1, VEC);    \
-    else if ((H) <= 8192) LAUNCH(SK, BK, 1024, 1, VEC);   \
-    else if ((H) <= 16384) LAUNCH(SK, BK, 1024, 2, VEC);  \
-    else LAUNCH(SK, BK, 1024, 4, VEC);                    \
+// Runs LAUNCH(SK, BK, NT, C) for the kinds and the width of a call.  A row belongs to NT threads, each of which holds C groups
+// of eight values.
+#define CQ_NORM_WIDTHS(LAUNCH, SK, BK, H)            \
+  do {                                               \
+    if ((H) <= 512) LAUNCH(SK, BK, 64, 1);           \
+    else if ((H) <= 2048) LAUNCH(SK, BK, 256, 1);    \
+    else if ((H) <= 4096) LAUNCH(SK, BK, 512, 1);    \
+    else if ((H) <= 8192) LAUNCH(SK, BK, 1024, 1);   \
+    else if ((H) <= 16384) LAUNCH(SK, BK, 1024, 2);  \
+    else LAUNCH(SK, BK, 1024, 4);                    \
   } while (0)
-#define CQ_NORM_KINDS(LAUNCH, sk, bk, VEC, H)                                                          \
-  do {                                                                                                 \
-    if ((sk) == CQ_A_F32) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F32, CQ_A_F32, VEC, H);                          \
-    else if ((sk) == CQ_A_F16 && (bk) == CQ_A_F16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F16, CQ_A_F16, VEC, H); \
-    else if ((sk) == CQ_A_F16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F16, CQ_A_F32, VEC, H);                     \
-    else if ((bk) == CQ_A_BF16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_BF16, CQ_A_BF16, VEC, H);                  \
-    else CQ_NORM_WIDTHS(LAUNCH, CQ_A_BF16, CQ_A_F32, VEC, H);                                          \
-  } while (0)
-#define CQ_NORM_DISPATCH(LAUNCH, sk, bk, vec, H)               \
-  do {                                                         \
-    if (vec) CQ_NORM_KINDS(LAUNCH, sk, bk, true, H);           \
-    else CQ_NORM_KINDS(LAUNCH, sk, bk, false, H);              \
+#define CQ_NORM_DISPATCH(LAUNCH, sk, bk, H)                                                       \
+  do {                                                                                            \
+    if ((sk) == CQ_A_F32) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F32, CQ_A_F32, H);                          \
+    else if ((sk) == CQ_A_F16 && (bk) == CQ_A_F16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F16, CQ_A_F16, H); \
+    else if ((sk) == CQ_A_F16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_F16, CQ_A_F32, H);                     \
+    else if ((bk) == CQ_A_BF16) CQ_NORM_WIDTHS(LAUNCH, CQ_A_BF16, CQ_A_BF16, H);                  \
+    else CQ_NORM_WIDTHS(LAUNCH, CQ_A_BF16, CQ_A_F32, H);                                          \
   } while (0)
 
 #endif  // CQ_BLOCK_NORM_H_

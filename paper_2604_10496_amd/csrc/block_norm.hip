@@ -6,19 +6,29 @@
 
 namespace {
 
-template <int SK, int BK, int NT, int C, bool VEC>
+template <int SK, int BK, int NT, int C>
 __global__ __launch_bounds__(NT) void block_norm_kernel(norm_args P, void* h_out, void* x_out) {
   __shared__ float lds[2][NT / 64];
   const size_t row = (size_t)blockIdx.x * P.H;
-  const int c0 = threadIdx.x * 8;
-  float h[C][8];
+  const int H = P.H;
+  auto slot = [&](int j) { return row_slot((threadIdx.x + j * NT) * 8, H); };
+  row8<SK> h_raw[C];
+  row8<BK> y_raw[C];
 #pragma unroll
-  for (int j = 0; j < C; ++j) row_load8<SK, VEC>(P.h, row + c0 + j * NT * 8, P.H - c0 - j * NT * 8, h[j]);
+  for (int j = 0; j < C; ++j) {
+    y_raw[j] = slot_fetch<BK>(P.y, row, slot(j), H, P.y != nullptr);
+    h_raw[j] = slot_fetch<SK>(P.h, row, slot(j), H, true);
+  }
+  float q = P.beta;
+  if (P.gate_kind == CQ_GATE_ROW) {
+    const float z = elem_load<BK>(P.gate, blockIdx.x);
+    q *= P.sigmoid ? sigmoid_of(z) : z;
+  }
+  float h[C][8];
   if (P.y) {
     float y[C][8];
 #pragma unroll
-    for (int j = 0; j < C; ++j) row_load8<BK, VEC>(P.y, row + c0 + j * NT * 8, P.H - c0 - j * NT * 8, y[j]);
-    float q = P.beta;
+    for (int j = 0; j < C; ++j) slot_values<BK>(y_raw[j], slot(j), H, y[j]);
     if (P.w_post) {
       float s[1] = {0.f};
 #pragma unroll
@@ -26,48 +36,48 @@ __global__ __launch_bounds__(NT) void block_norm_kernel(norm_args P, void* h_out
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] = fmaf(y[j][i], y[j][i], s[0]);
       group_sum<NT, 1>(s, lds[0]);
-      q *= 1.f / sqrtf(s[0] / (float)P.H + P.eps);
-    }
-    if (P.gate_kind == CQ_GATE_ROW) {
-      const float z = elem_load<BK>(P.gate, blockIdx.x);
-      q *= P.sigmoid ? sigmoid_of(z) : z;
+      q *= 1.f / sqrtf(s[0] / (float)H + P.eps);
     }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const int c = c0 + j * NT * 8;
       if (P.w_post) {
         float w[8];
-        weight_load8<SK, VEC>(P.w_post, P.wf32, c, P.H - c, w);
+        slot_weights<SK>(P.w_post, P.wf32, slot(j), H, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[j][i] *= w[i];
       }
       if (P.gate_kind == CQ_GATE_ELEM) {
         float z[8];
-        row_load8<BK, VEC>(P.gate, row + c, P.H - c, z);
+        row_values<BK>(slot_fetch<BK>(P.gate, row, slot(j), H, true), z);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[j][i] *= P.sigmoid ? sigmoid_of(z[i]) : z[i];
       }
+      slot_values<SK>(h_raw[j], slot(j), H, h[j]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[j][i] = fmaf(q, y[j][i], P.rho * h[j][i]);
-      row_store8<SK, VEC>(h_out, row + c, P.H - c, h[j]);
+      slot_store<SK>(h_out, row, slot(j), H, true, h[j]);
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < C; ++j) slot_values<SK>(h_raw[j], slot(j), H, h[j]);
   }
   if (!x_out) return;
   float s[1] = {0.f};
 #pragma unroll
-  for (int j = 0; j < C; ++j)
+  for (int j = 0; j < C; ++j) {
+    const int skip = slot(j).skip;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[0] = fmaf(h[j][i], h[j][i], s[0]);
+    for (int i = 0; i < 8; ++i) s[0] = H % 8 != 0 && i < skip ? s[0] : fmaf(h[j][i], h[j][i], s[0]);
+  }
   group_sum<NT, 1>(s, lds[1]);
-  const float r = 1.f / sqrtf(s[0] / (float)P.H + P.eps);
+  const float r = 1.f / sqrtf(s[0] / (float)H + P.eps);
 #pragma unroll
   for (int j = 0; j < C; ++j) {
-    const int c = c0 + j * NT * 8;
     float w[8];
-    weight_load8<SK, VEC>(P.w_pre, P.wf32, c, P.H - c, w);
+    slot_weights<SK>(P.w_pre, P.wf32, slot(j), H, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] *= h[j][i] * r;
-    row_store8<BK, VEC>(x_out, row + c, P.H - c, w);
+    slot_store<BK>(x_out, row, slot(j), H, true, w);
   }
 }
 
@@ -81,11 +91,9 @@ extern "C" cq_status cq_block_norm(const cq_block_norm_spec* P, const void* h, c
   if (!h || (!y && !x_out) || (y && !h_out) || (x_out && !P->w_pre)) return CQ_ERR_NULL;
   if (y && P->gate_kind != CQ_GATE_NONE && !gate) return CQ_ERR_NULL;
   const norm_args a = make_norm_args(P, T, h, y, gate);
-  const void* const rows[] = {h, y, a.gate_kind == CQ_GATE_ELEM ? gate : nullptr, y ? h_out : nullptr, x_out, P->w_pre, a.w_post};
-  const bool vec = rows_aligned(P->H, rows, 7);
-#define LAUNCH(SK, BK, NT, C, VEC)                                                                                  \
-  hipLaunchKernelGGL((block_norm_kernel<SK, BK, NT, C, VEC>), dim3(T), dim3(NT), 0, (hipStream_t)stream, a, h_out, x_out)
-  CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, vec, P->H);
+#define LAUNCH(SK, BK, NT, C)                                                                                  \
+  hipLaunchKernelGGL((block_norm_kernel<SK, BK, NT, C>), dim3(T), dim3(NT), 0, (hipStream_t)stream, a, h_out, x_out)
+  CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, P->H);
 #undef LAUNCH
   return cq_check_launch();
 }

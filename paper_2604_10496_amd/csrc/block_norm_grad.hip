@@ -4,13 +4,16 @@
 //                                                               dm = du w_post,  dy = q (dm - m mean(dm m)).
 // The sums of squares are taken again, together with mean(dn h') in the first of two row sums and with the sum behind a row's
 // gate in the second, so that the forward pass keeps no statistics.
-// A workgroup takes rows b, b + parts, ...; its share of the weights' gradients stays in registers and goes to the workspace
+// Bound by HBM (five or six rows in, two or three out).  One workgroup of 1024 threads per compute unit takes 1024 / NT rows at
+// a time and asks for the next ones before it works on these, so that loads are in flight across the two barriers of a row sum.
+// The shares of the weights' gradients stay in registers, are added over a workgroup's rows in LDS and go to the workspace
 // once, [parts][H] each; a second launch adds the parts in order.  No atomics: the results do not depend on timing.
 #include "block_norm.h"
 
 namespace {
 
-constexpr int kMostParts = 512;
+constexpr int kThreads = 1024;
+constexpr int kMostParts = 256;   // one workgroup per compute unit
 
 inline int grad_parts(int T) { return T < kMostParts ? T : kMostParts; }
 
@@ -22,170 +25,256 @@ struct norm_grad_args {
   float *part_pre, *part_post;
 };
 
-template <int SK, int BK, int NT, int C, bool VEC>
-__global__ __launch_bounds__(NT) void block_norm_grad_kernel(norm_grad_args G) {
+// what a thread reads of one row (ELEM: the gate has one value per value of the row)
+template <int SK, int BK, int C, bool ELEM>
+struct grad_row {
+  row8<SK> dh[C], h[C];
+  row8<BK> dx[C], y[C], gate[ELEM ? C : 1];
+  float z;   // the row's own gate
+};
+
+template <int SK, int BK, int NT, int C, bool ELEM>
+__device__ __forceinline__ void fetch_row(const norm_grad_args& G, int t, grad_row<SK, BK, C, ELEM>& R) {
   const norm_args& P = G.f;
+  const bool in = t < P.T;
+  const size_t row = (size_t)t * P.H;
+  R.z = 1.f;
+  if (P.gate_kind == CQ_GATE_ROW && in) R.z = elem_load<BK>(P.gate, t);
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const row_slot s((threadIdx.x % NT + j * NT) * 8, P.H);
+    R.h[j] = slot_fetch<SK>(P.h, row, s, P.H, in && G.dx);
+    R.dx[j] = slot_fetch<BK>(G.dx, row, s, P.H, in && G.dx);
+    R.dh[j] = slot_fetch<SK>(G.dh_out, row, s, P.H, in && G.dh_out);
+    R.y[j] = slot_fetch<BK>(P.y, row, s, P.H, in && P.y);
+    if constexpr (ELEM) R.gate[j] = slot_fetch<BK>(P.gate, row, s, P.H, in);
+  }
+}
+
+template <int SK, int BK, int NT, int C, bool ELEM>
+__global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_args G) {
+  constexpr int kGroups = kThreads / NT;
+  // rows of 32 bits and several groups of eight leave no registers for the next row
+  constexpr bool kAhead = C == 1 && SK != CQ_A_F32 && BK != CQ_A_F32;
+  const norm_args& P = G.f;
+  const int H = P.H;
   // (two sets, used by rows in turn: a row's sums are read while the next row's may be written already)
-  __shared__ float lds[2][2][3 * (NT / 64)];
-  const int c0 = threadIdx.x * 8;
-  const float inv_H = 1.f / (float)P.H;
+  __shared__ float sums[2][2][3 * (kThreads / 64)];
+  // Both weights, where each thread has its own eight in its own place: loads of them from memory would wait for the next
+  // rows', which were asked for before.  Later the rows' shares of the weights' gradients.
+  __shared__ __align__(16) float lds[C > 1 ? 4 : (NT * 16 > kThreads * 8 || kGroups == 1 ? NT * 16 : kThreads * 8)];
+  auto slot = [&](int j) { return row_slot((threadIdx.x % NT + j * NT) * 8, H); };
+  auto weights = [&](const void* w, int which, int j, float (&v)[8]) {
+    if constexpr (C == 1) {
+      const cq_v4f* q = reinterpret_cast<const cq_v4f*>(&lds[(which * NT + threadIdx.x % NT) * 8]);
+      const cq_v4f a = q[0], b = q[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+      slot_weights<SK>(w, P.wf32, slot(j), H, v);
+    }
+  };
+  if constexpr (C == 1) {
+    if (threadIdx.x < NT) {
+      float w[2][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[0][i] = w[1][i] = 1.f;
+      if (G.dx) slot_weights<SK>(P.w_pre, P.wf32, slot(0), H, w[0]);
+      if (P.w_post) slot_weights<SK>(P.w_post, P.wf32, slot(0), H, w[1]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[(n * NT + threadIdx.x) * 8 + i] = w[n][i];
+    }
+    __syncthreads();
+  }
+  // rows part, part + parts, ...: first one row for every workgroup, then the second of each, so that few rows spread out
+  int t = __builtin_amdgcn_readfirstlane((threadIdx.x / NT) * G.parts + blockIdx.x);   // (one row per wavefront)
+  const float inv_H = 1.f / (float)H;
   float acc_pre[C][8], acc_post[C][8];
 #pragma unroll
   for (int j = 0; j < C; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc_pre[j][i] = acc_post[j][i] = 0.f;
+  grad_row<SK, BK, C, ELEM> R, next;
+  if constexpr (kAhead) fetch_row<SK, BK, NT, C, ELEM>(G, t, next);
   int set = 0;
-  for (int t = blockIdx.x; t < P.T; t += G.parts, set ^= 1) {
-    const size_t row = (size_t)t * P.H;
+  for (int first = blockIdx.x; first < P.T; first += kGroups * G.parts, t += kGroups * G.parts, set ^= 1) {
+    if constexpr (kAhead) {
+      R = next;
+      if (first + kGroups * G.parts < P.T) fetch_row<SK, BK, NT, C, ELEM>(G, t + kGroups * G.parts, next);
+    } else {
+      fetch_row<SK, BK, NT, C, ELEM>(G, t, R);
+    }
+    const bool in = t < P.T;
+    const size_t row = (size_t)t * H;
     float d[C][8];   // gradient that reaches h'
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const int c = c0 + j * NT * 8;
-      if (G.dh_out) {
-        row_load8<SK, VEC>(G.dh_out, row + c, P.H - c, d[j]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[j][i] = 0.f;
-      }
-    }
+    for (int j = 0; j < C; ++j) slot_values<SK>(R.dh[j], slot(j), H, d[j]);
     if (G.dx) {
-      float h[C][8], dx[C][8];
       float s[2] = {0.f, 0.f};   // h'^2, dx w h'
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        const int c = c0 + j * NT * 8;
-        float w[8];
-        row_load8<SK, VEC>(P.h, row + c, P.H - c, h[j]);
-        row_load8<BK, VEC>(G.dx, row + c, P.H - c, dx[j]);
-        weight_load8<SK, VEC>(P.w_pre, P.wf32, c, P.H - c, w);
+        float w[8], h[8], dx[8];
+        weights(P.w_pre, 0, j, w);
+        slot_values<SK>(R.h[j], slot(j), H, h);
+        slot_values<BK>(R.dx[j], slot(j), H, dx);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          s[0] = fmaf(h[j][i], h[j][i], s[0]);
-          s[1] = fmaf(dx[j][i] * w[i], h[j][i], s[1]);
+          s[0] = fmaf(h[i], h[i], s[0]);
+          s[1] = fmaf(dx[i] * w[i], h[i], s[1]);
         }
       }
-      group_sum<NT, 2>(s, lds[set][0]);
+      group_sum<NT, 2>(s, sums[set][0]);
       const float r = 1.f / sqrtf(s[0] * inv_H + P.eps);
       const float back = r * r * s[1] * inv_H;   // D = dh' + r (dn - h' r^2 mean(dn h'))
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        const int c = c0 + j * NT * 8;
-        float w[8];
-        weight_load8<SK, VEC>(P.w_pre, P.wf32, c, P.H - c, w);
+        forget_values(R.h[j]);
+        forget_values(R.dx[j]);
+        float w[8], h[8], dx[8];
+        weights(P.w_pre, 0, j, w);
+        slot_values<SK>(R.h[j], slot(j), H, h);
+        slot_values<BK>(R.dx[j], slot(j), H, dx);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          d[j][i] = fmaf(r, fmaf(-back, h[j][i], dx[j][i] * w[i]), d[j][i]);
-          acc_pre[j][i] = fmaf(dx[j][i], h[j][i] * r, acc_pre[j][i]);
+          d[j][i] = fmaf(r, fmaf(-back, h[i], dx[i] * w[i]), d[j][i]);
+          acc_pre[j][i] = fmaf(dx[i], h[i] * r, acc_pre[j][i]);
         }
       }
     }
     const float rho = P.y ? P.rho : 1.f;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const int c = c0 + j * NT * 8;
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = rho * d[j][i];
-      row_store8<SK, VEC>(G.dh, row + c, P.H - c, v);
+      slot_store<SK>(G.dh, row, slot(j), H, in, v);
     }
-    if (P.y) {
-      float y[C][8];
-      float ga = 1.f;
-      if (P.gate_kind == CQ_GATE_ROW) {
-        const float z = elem_load<BK>(P.gate, t);
-        ga = P.sigmoid ? sigmoid_of(z) : z;
+    if (!P.y) continue;
+    const float ga = P.gate_kind == CQ_GATE_ROW && P.sigmoid ? sigmoid_of(R.z) : R.z;
+    // y, u's weight and the gate of eight values
+    auto factors = [&](int j, float (&y)[8], float (&w)[8], float (&a)[8]) {
+      slot_values<BK>(R.y[j], slot(j), H, y);
+      if (C == 1 || P.w_post) {
+        weights(P.w_post, 1, j, w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 1.f;
       }
-      // s: y^2, the sum behind mean(dm y) without beta, and behind the row's gate
+      if constexpr (ELEM) {
+        row_values<BK>(R.gate[j], a);
+        if (P.sigmoid) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) a[i] = sigmoid_of(a[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = ga;
+      }
+    };
+    // y^2, the sum behind mean(dm y) without beta, and behind the row's gate
+    float q = 1.f, back = 0.f;
+    if (P.w_post || P.gate_kind == CQ_GATE_ROW) {
       float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        const int c = c0 + j * NT * 8;
-        float w[8];
-        row_load8<BK, VEC>(P.y, row + c, P.H - c, y[j]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.f;
-        if (P.w_post) weight_load8<SK, VEC>(P.w_post, P.wf32, c, P.H - c, w);
-        float z[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = ga;
-        if (P.gate_kind == CQ_GATE_ELEM) {
-          row_load8<BK, VEC>(P.gate, row + c, P.H - c, z);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z[i] = P.sigmoid ? sigmoid_of(z[i]) : z[i];
-        }
+        float y[8], w[8], a[8];
+        factors(j, y, w, a);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float dw = d[j][i] * w[i];
-          s[0] = fmaf(y[j][i], y[j][i], s[0]);
-          s[1] = fmaf(dw * z[i], y[j][i], s[1]);
-          s[2] = fmaf(dw, y[j][i], s[2]);
+          s[0] = fmaf(y[i], y[i], s[0]);
+          s[1] = fmaf(dw * a[i], y[i], s[1]);
+          s[2] = fmaf(dw, y[i], s[2]);
         }
       }
-      float q = 1.f, back = 0.f;
-      if (P.w_post || P.gate_kind == CQ_GATE_ROW) group_sum<NT, 3>(s, lds[set][1]);
+      group_sum<NT, 3>(s, sums[set][1]);
       if (P.w_post) {
         q = 1.f / sqrtf(s[0] * inv_H + P.eps);
-        back = q * q * s[1] * inv_H;
+        back = P.beta * q * q * s[1] * inv_H;
       }
-      if (P.gate_kind == CQ_GATE_ROW && G.dgate && threadIdx.x == 0) {
+      if (P.gate_kind == CQ_GATE_ROW && G.dgate && in && threadIdx.x % NT == 0) {
         float da = P.beta * q * s[2];
         if (P.sigmoid) da *= ga * (1.f - ga);
         elem_store<BK>(G.dgate, t, da);
       }
+    }
 #pragma unroll
-      for (int j = 0; j < C; ++j) {
-        const int c = c0 + j * NT * 8;
-        float w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.f;
-        if (P.w_post) weight_load8<SK, VEC>(P.w_post, P.wf32, c, P.H - c, w);
-        float z[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = ga;
-        if (P.gate_kind == CQ_GATE_ELEM) {
-          float da[8];
-          row_load8<BK, VEC>(P.gate, row + c, P.H - c, z);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            z[i] = P.sigmoid ? sigmoid_of(z[i]) : z[i];
-            da[i] = P.beta * d[j][i] * y[j][i] * q * w[i];
-            if (P.sigmoid) da[i] *= z[i] * (1.f - z[i]);
-          }
-          if (G.dgate) row_store8<BK, VEC>(G.dgate, row + c, P.H - c, da);
-        }
-        float v[8];
+    for (int j = 0; j < C; ++j) {
+      forget_values(R.y[j]);
+      if constexpr (ELEM) forget_values(R.gate[j]);
+      float y[8], w[8], a[8], v[8];
+      factors(j, y, w, a);
+      if (ELEM && G.dgate) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float du = P.beta * z[i] * d[j][i];
-          acc_post[j][i] = fmaf(du, y[j][i] * q, acc_post[j][i]);
-          v[i] = q * fmaf(-back * P.beta, y[j][i], du * w[i]);
+          v[i] = P.beta * d[j][i] * y[i] * q * w[i];
+          if (P.sigmoid) v[i] *= a[i] * (1.f - a[i]);
         }
-        row_store8<BK, VEC>(G.dy, row + c, P.H - c, v);
+        slot_store<BK>(G.dgate, row, slot(j), H, in, v);
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float du = P.beta * a[i] * d[j][i];
+        acc_post[j][i] = fmaf(du, y[i] * q, acc_post[j][i]);
+        v[i] = q * fmaf(-back, y[i], du * w[i]);
+      }
+      slot_store<BK>(G.dy, row, slot(j), H, in, v);
     }
   }
-  // (the workspace's rows are padded to whole groups of eight)
-  const int Hp = (P.H + 7) & ~7;
+  // a workgroup's share: over its rows in LDS (one weight after the other), then to the workspace, rows of whole groups of eight
+  const int Hp = (H + 7) & ~7;
+  auto give = [&](float* part, float (&acc)[C][8]) {
+    if (!part) return;
+    if constexpr (kGroups == 1) {
 #pragma unroll
-  for (int j = 0; j < C; ++j) {
-    const int c = c0 + j * NT * 8;
-    if (G.part_pre) row_store8<CQ_A_F32, true>(G.part_pre, (size_t)blockIdx.x * Hp + c, P.H - c, acc_pre[j]);
-    if (G.part_post) row_store8<CQ_A_F32, true>(G.part_post, (size_t)blockIdx.x * Hp + c, P.H - c, acc_post[j]);
-  }
+      for (int j = 0; j < C; ++j) slot_store<CQ_A_F32>(part, (size_t)blockIdx.x * Hp, slot(j), H, true, acc[j]);
+    } else {
+      static_assert(C == 1, "several rows at a time are rows of one group of eight per thread");
+      const row_slot s = slot(0);
+      __syncthreads();
+      if (s.on) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i >= s.skip) lds[(threadIdx.x / NT * NT) * 8 + s.c + i] = acc[0][i];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < H; c += kThreads) {
+        float v = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) v += lds[g * NT * 8 + c];
+        part[(size_t)blockIdx.x * Hp + c] = v;
+      }
+    }
+  };
+  give(G.part_pre, acc_pre);
+  give(G.part_post, acc_post);
 }
 
+// d_w[c] = sum of the parts in order: 32 columns per workgroup, every eighth of 32 groups of threads takes four of them
 template <int WK>
 __global__ __launch_bounds__(256) void weight_sum_kernel(const float* part_pre, const float* part_post, int parts, int H,
                                                          void* dw_pre, void* dw_post) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= H) return;
-  const int Hp = (H + 7) & ~7;
+  __shared__ float lds[32][33];
   const float* p = blockIdx.y == 0 ? part_pre : part_post;
   void* out = blockIdx.y == 0 ? dw_pre : dw_post;
   if (!out) return;
-  float s = 0.f;
-  for (int b = 0; b < parts; ++b) s += p[(size_t)b * Hp + c];
-  elem_store<WK>(out, c, s);
+  const int Hp = (H + 7) & ~7, c = blockIdx.x * 32 + (threadIdx.x & 7) * 4, g = threadIdx.x >> 3;
+  cq_v4f s = {0.f, 0.f, 0.f, 0.f};
+  if (c < Hp) {   // (what lies between H and Hp is read and not used)
+#pragma unroll 8
+    for (int b = g; b < parts; b += 32) s += *reinterpret_cast<const cq_v4f*>(p + (size_t)b * Hp + c);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds[g][(threadIdx.x & 7) * 4 + i] = s[i];
+  __syncthreads();
+  if (threadIdx.x < 32 && blockIdx.x * 32 + threadIdx.x < H) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += lds[i][threadIdx.x];
+    elem_store<WK>(out, blockIdx.x * 32 + threadIdx.x, v);
+  }
 }
 
 }  // namespace
@@ -222,17 +311,18 @@ extern "C" cq_status cq_block_norm_grad(const cq_block_norm_spec* P, const void*
   a.part_pre = d_w_pre ? (float*)workspace : nullptr;
   a.part_post = d_w_post ? (float*)((char*)workspace + cq_block_norm_grad_workspace_bytes(P, T) / 2) : nullptr;
   if (T > 0) {
-    const bool elem = a.f.gate_kind == CQ_GATE_ELEM;
-    const void* const rows[] = {d_x ? h : nullptr, y, elem ? gate : nullptr, d_h_out, d_x, d_h, y ? d_y : nullptr,
-                                elem ? d_gate : nullptr, d_x ? P->w_pre : nullptr, a.f.w_post};
-    const bool vec = rows_aligned(P->H, rows, 10);
-#define LAUNCH(SK, BK, NT, C, VEC) \
-  hipLaunchKernelGGL((block_norm_grad_kernel<SK, BK, NT, C, VEC>), dim3(a.parts), dim3(NT), 0, s, a)
-    CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, vec, P->H);
+#define LAUNCH(SK, BK, NT, C)                                                                                            \
+  do {                                                                                                                  \
+    if (a.f.gate_kind == CQ_GATE_ELEM)                                                                                  \
+      hipLaunchKernelGGL((block_norm_grad_kernel<SK, BK, NT, C, true>), dim3(a.parts), dim3(kThreads), 0, s, a);         \
+    else                                                                                                                \
+      hipLaunchKernelGGL((block_norm_grad_kernel<SK, BK, NT, C, false>), dim3(a.parts), dim3(kThreads), 0, s, a);        \
+  } while (0)
+    CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, P->H);
 #undef LAUNCH
   }
   if (d_w_pre || d_w_post) {
-    const dim3 grid((P->H + 255) / 256, 2);
+    const dim3 grid((P->H + 31) / 32, 2);
 #define SUM(WK) \
   hipLaunchKernelGGL((weight_sum_kernel<WK>), grid, dim3(256), 0, s, a.part_pre, a.part_post, a.parts, P->H, d_w_pre, d_w_post)
     if (P->weight_kind == CQ_A_F32) SUM(CQ_A_F32);
