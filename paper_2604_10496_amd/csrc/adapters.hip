@@ -6,7 +6,7 @@
 // rows of one token and stores them together.
 //
 // Tokens meet their adapters in one of two ways.  Batches of up to kLeaderTokens tokens (decode steps, in any order): a
-// workgroup per token looks through the ids; the first of every kTile tokens of one adapter takes those tokens, the others'
+// workgroup per token looks through the ids; the first of every 16 tokens of one adapter takes those tokens, the others'
 // workgroups end.  Longer batches are prompts, whose neighbours share an adapter: tiles of neighbouring tokens, adapter by
 // adapter within a tile.  Either way an adapter's weights are read once per tile, and nothing is sorted or kept.
 //
@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kMaxRank = 256;
 constexpr int kLeaderTokens = 1024;
-constexpr int kDownTile = 16, kUpTile = 64;   // tokens per workgroup
+constexpr int kDownTile = 16, kUpTile = 32;   // tokens per workgroup (kUpTile: of prompts; 16 of single tokens)
 constexpr int kDownWaves = 8, kUpWaves = 4;
 constexpr int kRankBlock = 64;                // rows of A per workgroup
 
@@ -45,50 +45,37 @@ __device__ __forceinline__ int adapter_of(const adapter_args& P, int t) {
   return a >= 0 && a < P.n ? a : -1;
 }
 
-// The tokens of this workgroup in LDS: rows[i] (-1: none) and their adapters.  False: nothing to do.  Ends with a barrier.
+// The tokens of a tile: lane i < TILE gets the i-th one's row (-1: none) and adapter.  Every wavefront finds them by itself, the
+// same ones.  False: another tile has them.
 template <int TILE>
-__device__ __forceinline__ bool find_rows(const adapter_args& P, int* rows, int* adapters, int* found) {
+__device__ __forceinline__ bool find_rows(const adapter_args& P, int tile, int& row, int& id) {
   const int lane = threadIdx.x & 63;
-  if (threadIdx.x < 64) {
-    if (P.T > kLeaderTokens) {
-      const int t = blockIdx.x * TILE + lane;
-      const bool ok = lane < TILE && t < P.T;
-      if (lane < TILE) {
-        rows[lane] = ok ? t : -1;
-        adapters[lane] = ok ? adapter_of(P, t) : -1;
-      }
-      if (lane == 0) *found = min(TILE, P.T - (int)blockIdx.x * TILE);
-    } else {
-      const int me = blockIdx.x, mine = adapter_of(P, me);
-      int before = 0, n = 0;
-      bool lead = true;
-      for (int c = 0; c < P.T; c += 64) {
-        const int t = c + lane;
-        const bool same = t < P.T && adapter_of(P, t) == mine;
-        before += __popcll(__ballot(same && t < me));
-        if (c + 64 > me) {
-          if (c <= me) lead = before % TILE == 0;   // (all tokens in front of `me` have been counted)
-          if (!lead) break;
-          const unsigned long long m = __ballot(same && t >= me);
-          const int at = n + __popcll(m & ((1ull << lane) - 1ull));
-          if (same && t >= me && at < TILE) {
-            rows[at] = t;
-            adapters[at] = mine;
-          }
-          n += __popcll(m);
-          if (n >= TILE) break;
-        }
-      }
-      n = lead ? min(n, TILE) : 0;
-      if (lane >= n && lane < TILE) {
-        rows[lane] = -1;
-        adapters[lane] = -1;
-      }
-      if (lane == 0) *found = n;
-    }
+  if (P.T > kLeaderTokens) {
+    const int t = tile * TILE + lane;
+    const bool in = lane < TILE && t < P.T;
+    row = in ? t : -1;
+    id = in ? adapter_of(P, t) : -1;
+    return true;
   }
-  __syncthreads();
-  return *found > 0;
+  const int me = tile, mine = adapter_of(P, me);
+  int before = 0, n = 0;
+  row = -1;
+  for (int c = 0; c < P.T; c += 64) {
+    const int t = c + lane;
+    const bool same = t < P.T && adapter_of(P, t) == mine;
+    before += __popcll(__ballot(same && t < me));
+    if (c + 64 <= me) continue;
+    if (c <= me && before % TILE != 0) return false;   // (all tokens in front of `me` have been counted)
+    const unsigned long long m = __ballot(same && t >= me);
+    const int at = n + __popcll(m & ((1ull << lane) - 1ull));
+    // lane `at` gets t; those without a place send theirs to the last lane, which no tile uses
+    const int got = __builtin_amdgcn_ds_permute((same && t >= me && at < TILE ? at : 63) * 4, t);
+    if (lane >= n && lane < min(n + __popcll(m), TILE)) row = got;
+    n += __popcll(m);
+    if (n >= TILE) break;
+  }
+  id = row >= 0 ? mine : -1;
+  return true;
 }
 
 // An fp32 value as the sum of three values that bf16 holds (8 bits each, cut off, not rounded: no value overflows).
@@ -128,185 +115,273 @@ constexpr int product_path() {
   return XK == WK && XK != CQ_A_F32 ? kSame16 : (XK == CQ_A_F32 && WK == CQ_A_BF16 ? kSplit : kFloat);
 }
 
+// Eight values of a row of K from k on, zero where k >= k_end (the last part's k_end is K, the others' a multiple of 64).  The last
+// eight of a row that is no whole number of eights overlap their neighbours, whose values they hold as zero.
+template <int KIND>
+__device__ __forceinline__ row8<KIND> fetch_k(const void* p, size_t row, int k, int k_end, int K) {
+  if (K < 8) return row_fetch<KIND>(p, row, k == 0 ? K : 0);
+  const int at = min(k, K - 8);
+  row8<KIND> r = fetch8<KIND>(p, row + at, 0, k < k_end);
+  if (K % 8 != 0) keep_values(r, k - at, 8);
+  return r;
+}
+
 // low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of
-// K, which its eight wavefronts share out in steps of 64 and add up in LDS.
-template <int XK, int WK, int RT>
+// K, which its eight wavefronts share out in rounds of STEPS steps of 64 values each and add up in LDS.  Bound by latency: the
+// loads of a round are all asked for before the first product, those of prompts' tokens before the ids are known.
+template <int XK, int WK, int RT, int STEPS>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_args P) {
-  constexpr int RW = RT * 16, LD = RW + 4;
+  constexpr int RW = RT * 16, LD = RW + 4, kRound = 64 * kDownWaves * STEPS;
   __shared__ float lds[kDownWaves][16][LD];
-  __shared__ int rows[kDownTile], adapters[kDownTile], found;
-  if (!find_rows<kDownTile>(P, rows, adapters, &found)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int t = rows[col] >= 0 ? rows[col] : rows[0];
-  const int mine = adapters[col];
+  const int k_first = blockIdx.y * P.kpart, k_end = min(P.K, k_first + P.kpart);
+  const int k_lane = wave * 64 * STEPS + g * 16;   // this lane's eight of the 32 values of a product, twice per step
+  row8<XK> x[STEPS][2];
+  auto fetch_x = [&](int t, int k0) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int k = k0 + k_lane + s * 64 + half * 8;
+        x[s][half] = fetch_k<XK>(P.X, (size_t)t * P.ldx, k, k_end, P.K);
+      }
+  };
+  bool fetched = P.T > kLeaderTokens;   // x holds the first round of this workgroup's tokens
+  if (fetched) fetch_x(min((int)blockIdx.x * kDownTile + col, P.T - 1), k_first);
+  int row, id;
+  if (!find_rows<kDownTile>(P, blockIdx.x, row, id)) return;
+  // (lane 0 has a token; readlane does not depend on which lanes are active)
+  const int token = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0), t = token < 0 ? some : token;
   const int r0 = blockIdx.z * kRankBlock;
-  const int k_end = min(P.K, (int)(blockIdx.y + 1) * P.kpart);
-  unsigned todo = (unsigned)__ballot(rows[col] >= 0 && mine >= 0) & 0xffffu;
+  unsigned todo = (unsigned)__ballot(id >= 0) & 0xffffu;
   while (todo) {
-    const int a = adapters[__ffs(todo) - 1];
-    const bool here = mine == a && rows[col] >= 0;
-    todo &= ~((unsigned)__ballot(here) & 0xffffu);
+    const int a = __builtin_amdgcn_readlane(id, __ffs(todo) - 1);
+    const unsigned match = (unsigned)__ballot(id == a) & 0xffffu;
+    todo &= ~match;
+    if (!fetched) fetch_x(t, k_first);
     const int rank = rank_of(P, a);
-    if (rank <= r0) continue;
     cq_v4f acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    const size_t w_row = ((size_t)a * P.R + r0 + col) * P.K;
-    for (int k0 = blockIdx.y * P.kpart + wave * 64; k0 < k_end; k0 += 64 * kDownWaves) {
+    if (rank > r0) {
+      const size_t w_row = ((size_t)a * P.R + r0 + col) * P.K;
+      for (int k0 = k_first; k0 < k_end; k0 += kRound) {
+        if (k0 > k_first) fetch_x(t, k0);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k = k0 + g * 16 + half * 8, left = k_end - k;   // this lane's eight of the 32 values of a product
-        if constexpr (product_path<XK, WK>() == kSame16) {
-          const cq_v4u x = raw_load8(P.X, (size_t)t * P.ldx + k, left);
+        for (int i = 0; i < RT; ++i) {
+          const bool in = r0 + i * 16 + col < rank;
+          row8<WK> w[STEPS][2];
 #pragma unroll
-          for (int i = 0; i < RT; ++i) {
-            const bool in = r0 + i * 16 + col < rank;
-            const cq_v4u w = raw_load8(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0);
-            if constexpr (XK == CQ_A_BF16)
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w), __builtin_bit_cast(cq_v8bf16, x), acc[i], 0, 0, 0);
-            else
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(cq_v8f16, w), __builtin_bit_cast(cq_v8f16, x), acc[i], 0, 0, 0);
-          }
-        } else {
-          float x[8];
-          row_load8<XK>(P.X, (size_t)t * P.ldx + k, left, x);
-          if constexpr (product_path<XK, WK>() == kSplit) {
-            const split_frag xs = split_pack(x);
+          for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-              const bool in = r0 + i * 16 + col < rank;
-              const cq_v8bf16 w = __builtin_bit_cast(cq_v8bf16, raw_load8(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0));
-#pragma unroll
-              for (int p = 0; p < 3; ++p) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xs.part[p], acc[i], 0, 0, 0);
+            for (int half = 0; half < 2; ++half) {
+              const int k = k0 + k_lane + s * 64 + half * 8;
+              w[s][half] = fetch_k<WK>(P.A, w_row + (size_t)i * 16 * P.K, in ? k : k_end, k_end, P.K);
             }
-          } else {
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-              const bool in = r0 + i * 16 + col < rank;
-              float w[8];
-              row_load8<WK>(P.A, w_row + (size_t)i * 16 * P.K + k, in ? left : 0, w);
+          for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-              for (int q = 0; q < 8; ++q) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[q], x[q], acc[i], 0, 0, 0);
+            for (int half = 0; half < 2; ++half) {
+              if constexpr (product_path<XK, WK>() == kSame16) {
+                if constexpr (XK == CQ_A_BF16)
+                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[s][half].w[0]),
+                                                                   __builtin_bit_cast(cq_v8bf16, x[s][half].w[0]), acc[i], 0, 0, 0);
+                else
+                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(cq_v8f16, w[s][half].w[0]),
+                                                                  __builtin_bit_cast(cq_v8f16, x[s][half].w[0]), acc[i], 0, 0, 0);
+              } else if constexpr (product_path<XK, WK>() == kSplit) {
+                float v[8];
+                row_values<XK>(x[s][half], v);
+                const split_frag xs = split_pack(v);
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[s][half].w[0]), xs.part[p], acc[i], 0, 0, 0);
+              } else {
+                float v[8], u[8];
+                row_values<XK>(x[s][half], v);
+                row_values<WK>(w[s][half], u);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[q], acc[i], 0, 0, 0);
+              }
             }
-          }
         }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
-    __syncthreads();
-    for (int e = threadIdx.x; e < 16 * RW; e += 64 * kDownWaves) {
-      const int tok = e / RW, r = e % RW;
-      if (rows[tok] < 0 || adapters[tok] != a || r0 + r >= P.Rp) continue;
-      float s = 0.f;
+      for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
+      __syncthreads();
+      for (int e = threadIdx.x; e < 16 * RW; e += 64 * kDownWaves) {
+        const int tok = e / RW, r = e % RW;
+        const int to = __shfl(row, tok);
+        if (!(match >> tok & 1u) || r0 + r >= P.Rp) continue;
+        float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < kDownWaves; ++w) s += lds[w][tok][r];
-      P.low[((size_t)blockIdx.y * P.T + rows[tok]) * P.Rp + r0 + r] = s;
+        for (int w = 0; w < kDownWaves; ++w) s += lds[w][tok][r];
+        P.low[((size_t)blockIdx.y * P.T + to) * P.Rp + r0 + r] = s;
+      }
+      __syncthreads();
     }
-    __syncthreads();
+    fetched = k_end - k_first <= kRound;   // one round: x serves the next adapter's tokens as well
   }
 }
 
-// out = base + scale B_a low.  One workgroup: up to 64 tokens (16 at a time) and 256 outputs; a wavefront has 64 of them as
+// out = base + scale B_a low.  One workgroup: 16 SUBS tokens and 256 outputs; a wavefront has 64 of them as
 // four tiles of 16.  The rows of a tile are chosen so that a lane's outputs of one or (16 bits) two tiles are neighbours.
+// Bound by HBM for prompts (base and out), by latency for single tokens: base is asked for first, for prompts before the ids
+// are known, and all loads of 32 ranks before their products.
 template <int OK>
 __device__ __forceinline__ int out_row(int tile, int i) {
   if (OK == CQ_A_F32) return tile * 16 + i;
   return (tile >> 1) * 32 + (i >> 2) * 8 + (tile & 1) * 4 + (i & 3);
 }
 
-template <int WK, int OK>
+template <int WK, int OK, int SUBS>
 __global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args P) {
-  __shared__ int rows[kUpTile], adapters[kUpTile], found;
-  if (!find_rows<kUpTile>(P, rows, adapters, &found)) return;
+  constexpr int kOuts = OK == CQ_A_F32 ? 4 : 2;      // groups of outputs of a lane
+  constexpr int kOut = OK == CQ_A_F32 ? 4 : 8;       // outputs of a group: 16 bytes
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int n0 = (blockIdx.y * kUpWaves + wave) * 64;
+  // Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of
+  // outputs an XCD meets the same rows of B again and again (prefill of 4096 x 4096 values at rank 32: 26.7 instead of 29.9 us).
+  const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), tile = blockIdx.x / blocks;
+  const int n0 = (((int)blockIdx.x - tile * blocks) * kUpWaves + wave) * 64;
   if (n0 >= P.N) return;
-  for (int sub = 0; sub < found; sub += 16) {
-    const int t = rows[sub + col], mine = adapters[sub + col];
-    unsigned todo = (unsigned)__ballot(t >= 0) & 0xffffu;
-    while (todo) {
-      const int a = adapters[sub + __ffs(todo) - 1];
-      const bool here = t >= 0 && mine == a;
-      todo &= ~((unsigned)__ballot(here) & 0xffffu);
-      const int rank = rank_of(P, a);
-      cq_v4f acc[4];
+  auto first_out = [&](int o) { return n0 + (OK == CQ_A_F32 ? out_row<OK>(o, g * 4) : out_row<OK>(2 * o, g * 4)); };
+  cq_v4u base[SUBS][kOuts];
+  auto fetch_base = [&](int sub, int t) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-      for (int rb = 0; rb < rank; rb += 32) {
-        const int r = rb + g * 8;
-        float v[8];
+    for (int o = 0; o < kOuts; ++o) {
+      const int n = first_out(o);
+      base[sub][o] = cq_v4u{0u, 0u, 0u, 0u};
+      if (P.base && t >= 0 && n + kOut <= P.N)
+        base[sub][o] = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(P.base) + ((size_t)t * P.ldb + n) * (OK == CQ_A_F32 ? 4 : 2));
+    }
+  };
+  const bool prompt = P.T > kLeaderTokens;
+  if (prompt) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-        if (here && r < rank) {
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const int t = (tile * SUBS + sub) * 16 + col;
+      fetch_base(sub, t < P.T ? t : -1);
+    }
+  }
+  int row, id;
+  if (!find_rows<16 * SUBS>(P, tile, row, id)) return;
+  int t[SUBS];
+#pragma unroll
+  for (int sub = 0; sub < SUBS; ++sub) {
+    t[sub] = __shfl(row, sub * 16 + col);
+    if (!prompt) fetch_base(sub, t[sub]);
+  }
+  constexpr unsigned long long kRows = (1ull << 16 * SUBS) - 1;
+  unsigned long long todo = __ballot(row >= 0) & kRows;
+  while (todo) {
+    const int a = __builtin_amdgcn_readlane(id, __ffsll((long long)todo) - 1);
+    const unsigned long long match = __ballot(row >= 0 && id == a) & kRows;
+    todo &= ~match;
+    const int rank = rank_of(P, a);
+    const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
+    cq_v4f acc[SUBS][4];
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[sub][j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
+      // The first 32 columns are asked for before the adapter's own rank is known and cleared beyond it: B's rows are short.
+      // (a row that is no whole number of eights: its last eight overlap their neighbours)
+      const int r = rb + g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r;
+      const bool on = r < (rb == 0 ? P.R : rank);
+      const size_t w_row = ((size_t)a * P.N + n0) * P.R;
+      row8<WK> w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int n = out_row<OK>(j, col);
+        if (P.R >= 8) w[j] = fetch8<WK>(P.B, w_row, (uint32_t)(n * P.R + c), on && n0 + n < P.N);
+        else w[j] = row_fetch<WK>(P.B, w_row + n * P.R, on && n0 + n < P.N ? P.R : 0);
+      }
+      float v[SUBS][8];
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[sub][i] = 0.f;
+        if ((match >> (sub * 16 + col) & 1) && on) {
+          const float* from = P.low + (size_t)t[sub] * P.Rp + c;
+#pragma unroll 2
           for (int p = 0; p < P.parts; ++p) {
             float u[8];
-            row_load8<CQ_A_F32>(P.low, ((size_t)p * P.T + t) * P.Rp + r, 8, u);
+            row_values<CQ_A_F32>(fetch8<CQ_A_F32>(from, (size_t)p * P.T * P.Rp, 0, true), u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += u[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = r + i < rank ? v[i] : 0.f;   // (0 times an infinite x is no 0)
-        }
-        if constexpr (WK == CQ_A_BF16) {
-          const split_frag vs = split_pack(v);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int n = n0 + out_row<OK>(j, col);
-            const cq_v4u b = raw_load8(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0);
-            const cq_v8bf16 w = __builtin_bit_cast(cq_v8bf16, b);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, vs.part[p], acc[j], 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int n = n0 + out_row<OK>(j, col);
-            float w[8];
-            row_load8<WK>(P.B, ((size_t)a * P.N + n) * P.R + r, n < P.N ? rank - r : 0, w);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[q], v[q], acc[j], 0, 0, 0);
+            for (int i = 0; i < 8; ++i) v[sub][i] += u[i];
           }
         }
       }
-      if (!here) continue;
-      const float scale = rank > 0 ? (P.scale ? P.scale[a] : 1.f) : 0.f;
-      const size_t o = (size_t)t * P.ldo, b = (size_t)t * P.ldb;
-      if constexpr (OK == CQ_A_F32) {
+      if (rank < rb + 32) {   // what lies beyond the rank may be anything, and 0 times an infinite x is no 0
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int n = n0 + out_row<OK>(j, g * 4), left = P.N - n;
-          if (left >= 4) {
-            typedef cq_v4f cq_v4f_any __attribute__((aligned(4)));
-            cq_v4f v = {0.f, 0.f, 0.f, 0.f};
-            if (P.base) v = *reinterpret_cast<const cq_v4f_any*>(reinterpret_cast<const float*>(P.base) + b + n);
-            if (rank > 0) v += scale * acc[j];
-            *reinterpret_cast<cq_v4f_any*>(reinterpret_cast<float*>(P.out) + o + n) = v;
-          } else {
+        for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
-              if (q >= left) continue;
-              float v = P.base ? elem_load<OK>(P.base, b + n + q) : 0.f;
-              if (rank > 0) v = fmaf(scale, acc[j][q], v);
-              elem_store<OK>(P.out, o + n + q, v);
-            }
+          for (int i = 0; i < 8; ++i) v[sub][i] = c + i >= r && c + i < rank ? v[sub][i] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) keep_values(w[j], r - c, rank - c);
+      }
+#pragma unroll
+      for (int sub = 0; sub < SUBS; ++sub) {
+        if (!(match >> (sub * 16) & 0xffffu)) continue;
+        if constexpr (WK == CQ_A_BF16) {
+          const split_frag vs = split_pack(v[sub]);
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              acc[sub][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[j].w[0]), vs.part[p], acc[sub][j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float u[8];
+            row_values<WK>(w[j], u);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc[sub][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[sub][q], acc[sub][j], 0, 0, 0);
           }
         }
-      } else {
+      }
+    }
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const int n = n0 + out_row<OK>(j, g * 4), left = P.N - n;
-          float v[8];
+    for (int sub = 0; sub < SUBS; ++sub) {
+      if (!(match >> (sub * 16 + col) & 1)) continue;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = 0.f;
-          if (P.base) row_load8<OK>(P.base, b + n, left, v);
-          if (rank > 0) {
+      for (int o = 0; o < kOuts; ++o) {
+        const int n = first_out(o);
+        const size_t at = (size_t)t[sub] * P.ldo + n;
+        float add[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, acc[j + (i >> 2)][i & 3], v[i]);
+        for (int i = 0; i < kOut; ++i) add[i] = acc[sub][o * (kOut / 4) + (i >> 2)][i & 3];
+        if (n + kOut <= P.N) {
+          if constexpr (OK == CQ_A_F32) {
+            cq_v4u v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float b = __uint_as_float(base[sub][o][i]);
+              v[i] = __float_as_uint(rank > 0 ? fmaf(scale, add[i], b) : b);
+            }
+            *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<float*>(P.out) + at) = v;
+          } else {
+            row8<OK> b;
+            b.w[0] = base[sub][o];
+            float v[8];
+            row_values<OK>(b, v);
+            if (rank > 0) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, add[i], v[i]);
+            }
+            row_store8<OK>(P.out, at, 8, v);
           }
-          row_store8<OK>(P.out, o + n, left, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kOut; ++i) {
+            if (n + i >= P.N) continue;
+            float v = P.base ? elem_load<OK>(P.base, (size_t)t[sub] * P.ldb + n + i) : 0.f;
+            if (rank > 0) v = fmaf(scale, add[i], v);
+            elem_store<OK>(P.out, at + i, v);
+          }
         }
       }
     }
@@ -323,29 +398,37 @@ cq_status check_adapters(const cq_adapters* W, int T) {
 
 int padded_rank(int R) { return (R + 15) / 16 * 16; }
 
-// Parts of K: enough workgroups to fill the chip, each with one step of 64 values for every wavefront at least.
-int parts_of(int T, int K) {
-  const int tiles = (T + kDownTile - 1) / kDownTile, most = (K + 64 * kDownWaves - 1) / (64 * kDownWaves);
-  const int want = tiles >= 512 ? 1 : 512 / tiles;
-  const int parts = want < most ? want : most;
-  return parts < 16 ? parts : 16;
+// Steps of 64 values per wavefront and round, and parts of K: as many steps as leave two workgroups per compute unit; parts of
+// whole rounds, at most 16.
+struct down_plan { int steps, parts, kpart; };
+
+down_plan plan_of(int T, int K, int x_kind) {
+  const long tiles = ((long)T + kDownTile - 1) / kDownTile;
+  down_plan d;
+  d.steps = x_kind == CQ_A_F32 ? 2 : 4;
+  auto rounds = [&](int steps) { return ((long)K + 64 * kDownWaves * steps - 1) / (64 * kDownWaves * steps); };
+  while (d.steps > 1 && tiles * rounds(d.steps) < 512) d.steps /= 2;
+  const long n = rounds(d.steps);
+  long parts = tiles >= 512 ? 1 : 512 / tiles;
+  if (parts > n) parts = n;
+  if (parts > 16) parts = 16;
+  d.kpart = (int)((n + parts - 1) / parts) * 64 * kDownWaves * d.steps;
+  d.parts = (K + d.kpart - 1) / d.kpart;
+  return d;
 }
 
 }  // namespace
 
 extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T) {
   if (check_adapters(W, T) != CQ_OK) return 0;
-  // the most that any batch of up to T tokens takes: parts(T) T rises between the steps of parts
-  size_t rows = (size_t)T * 1;
-  for (int p = 2; p <= 16; ++p) {
-    const long last = (long)(512 / p) * kDownTile;   // the longest batch with p parts
-    const int t = T < last ? T : (int)last;
-    if (t > 0) {
-      const size_t need = (size_t)t * parts_of(t, W->K);
-      rows = need > rows ? need : rows;
-    }
+  // no batch of up to T tokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one step
+  const long most = ((long)W->K + 64 * kDownWaves - 1) / (64 * kDownWaves), cap = most < 16 ? most : 16;
+  long rows = T;
+  for (long p = 2; p <= cap; ++p) {
+    const long last = 512 / p * kDownTile, t = T < last ? T : last;   // the longest batch with p parts
+    if (t * p > rows) rows = t * p;
   }
-  return cq_align_up(rows * padded_rank(W->rank) * 4, 256);
+  return cq_align_up((size_t)rows * padded_rank(W->rank) * 4, 256);
 }
 
 extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x_kind, long ldx, const int32_t* adapter_ids, int T,
@@ -374,16 +457,25 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   P.K = W->K;
   P.N = W->N;
   P.T = T;
-  P.parts = parts_of(T, W->K);
-  P.kpart = ((W->K + P.parts - 1) / P.parts + 63) / 64 * 64;
+  const down_plan plan = plan_of(T, W->K, x_kind);
+  P.parts = plan.parts;
+  P.kpart = plan.kpart;
   P.ldx = (size_t)ldx;
   P.ldb = base ? (size_t)ld_base : 0;
   P.ldo = (size_t)ld_out;
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
   const dim3 down(leaders ? T : (T + kDownTile - 1) / kDownTile, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
-  const dim3 up(leaders ? T : (T + kUpTile - 1) / kUpTile, (W->N + 64 * kUpWaves - 1) / (64 * kUpWaves));
-#define DOWN2(XK, WK, RT) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT>), down, dim3(64 * kDownWaves), 0, s, P)
+  const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves), up_tiles = leaders ? T : ((long)T + kUpTile - 1) / kUpTile;
+  if (up_tiles * blocks > 0x7fffffffL) return CQ_ERR_SHAPE;
+  const dim3 up((unsigned)(up_tiles * blocks));
+#define DOWN3(XK, WK, RT, STEPS) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, STEPS>), down, dim3(64 * kDownWaves), 0, s, P)
+#define DOWN2(XK, WK, RT)                                  \
+  do {                                                     \
+    if (plan.steps == 1) DOWN3(XK, WK, RT, 1);             \
+    else if (plan.steps == 2) DOWN3(XK, WK, RT, 2);        \
+    else if constexpr (XK != CQ_A_F32) DOWN3(XK, WK, RT, 4); \
+  } while (0)
 #define DOWN1(XK, WK)                         \
   do {                                        \
     if (W->rank <= 16) DOWN2(XK, WK, 1);      \
@@ -396,7 +488,11 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
     else if (x_kind == CQ_A_F16) DOWN1(CQ_A_F16, WK); \
     else DOWN1(CQ_A_BF16, WK);                        \
   } while (0)
-#define UP2(WK, OK) hipLaunchKernelGGL((adapter_up_kernel<WK, OK>), up, dim3(64 * kUpWaves), 0, s, P)
+#define UP2(WK, OK)                                                                                                   \
+  do {                                                                                                                \
+    if (leaders) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, 1>), up, dim3(64 * kUpWaves), 0, s, P);                \
+    else hipLaunchKernelGGL((adapter_up_kernel<WK, OK, kUpTile / 16>), up, dim3(64 * kUpWaves), 0, s, P);             \
+  } while (0)
 #define UP(WK)                                    \
   do {                                            \
     if (out_kind == CQ_A_F32) UP2(WK, CQ_A_F32);  \

@@ -120,18 +120,38 @@ struct row_slot {
   __device__ __forceinline__ row_slot(int c0, int H) : c(H >= 8 && c0 > H - 8 ? H - 8 : c0), skip(c0 - c), on(c0 < H) {}
 };
 
+// Eight values at `at` + `lane_at` of p (uniform and per lane), zero where `on` is false.
 template <int KIND>
-__device__ __forceinline__ row8<KIND> slot_fetch(const void* p, size_t row, const row_slot& s, int H, bool wanted) {
+__device__ __forceinline__ row8<KIND> fetch8(const void* p, size_t at, uint32_t lane_at, bool on) {
+  constexpr uint32_t kSize = KIND == CQ_A_F32 ? 4 : 2;
   row8<KIND> r;
-  if (H < 8) return row_fetch<KIND>(p, row, s.on && wanted ? H : 0);
 #pragma unroll
   for (int n = 0; n < row8<KIND>::N; ++n) r.w[n] = cq_v4u{0u, 0u, 0u, 0u};
-  if (s.on && wanted) {
-    const cq_v4u_any* q = reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(p) + (row + s.c) * (KIND == CQ_A_F32 ? 4 : 2));
+  if (on) {
+    const cq_v4u_any* q = reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(p) + at * kSize + lane_at * kSize);
 #pragma unroll
     for (int n = 0; n < row8<KIND>::N; ++n) r.w[n] = q[n];
   }
   return r;
+}
+
+template <int KIND>
+__device__ __forceinline__ row8<KIND> slot_fetch(const void* p, size_t row, const row_slot& s, int H, bool wanted) {
+  if (H < 8) return row_fetch<KIND>(p, row, s.on && wanted ? H : 0);
+  return fetch8<KIND>(p, row, (uint32_t)s.c, s.on && wanted);
+}
+
+// raw values from .. to-1 of eight, the others as zero
+template <int KIND>
+__device__ __forceinline__ void keep_values(row8<KIND>& r, int from, int to) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool keep = i >= from && i < to;
+    if constexpr (KIND == CQ_A_F32)
+      r.w[i >> 2][i & 3] = keep ? r.w[i >> 2][i & 3] : 0u;
+    else
+      r.w[0][i >> 1] &= keep ? 0xffffffffu : (i & 1 ? 0x0000ffffu : 0xffff0000u);
+  }
 }
 
 // Makes the compiler take the raw values as new, so that it converts them again instead of keeping the converted ones, twice
