@@ -19,7 +19,8 @@ namespace {
 
 constexpr int kMaxRank = 256;
 constexpr int kLeaderTokens = 1024;
-constexpr int kDownTile = 16, kUpTile = 32;   // tokens per workgroup (kUpTile: of prompts; 16 of single tokens)
+constexpr int kTile = 16;         // tokens of a matrix-core tile
+constexpr int kPromptTiles = 2;   // tiles that a wavefront of the second launch takes one after the other, of prompts
 constexpr int kDownWaves = 8, kUpWaves = 4;
 constexpr int kRankBlock = 64;                // rows of A per workgroup
 
@@ -126,9 +127,50 @@ __device__ __forceinline__ row8<KIND> fetch_k(const void* p, size_t row, int k, 
   return r;
 }
 
+// Steps of a round that a kernel has registers for (256 per lane: two workgroups per compute unit).
+template <int XK, int WK, int RT>
+constexpr int most_steps() {
+  return product_path<XK, WK>() == kSame16 ? 8 : product_path<XK, WK>() == kSplit ? (RT == 4 ? 2 : 4) : (RT == 4 ? 1 : 2);
+}
+
+// A whole round of a lane, eight of the 32 values of a product twice per step: one address and constant offsets.
+template <int KIND, int STEPS>
+__device__ __forceinline__ void fetch_round(const void* p, size_t row, int k, row8<KIND> (&v)[STEPS][2]) {
+  const char* q = reinterpret_cast<const char*>(p) + (row + k) * (KIND == CQ_A_F32 ? 4 : 2);
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) v[s][half] = fetch8<KIND>(q, 0, s * 64 + half * 8, true);
+}
+
+// acc += 16 rows of A times 16 tokens over 32 values of K
+template <int XK, int WK>
+__device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& x, cq_v4f& acc) {
+  if constexpr (product_path<XK, WK>() == kSame16) {
+    if constexpr (XK == CQ_A_BF16)
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w.w[0]), __builtin_bit_cast(cq_v8bf16, x.w[0]), acc, 0, 0, 0);
+    else
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(cq_v8f16, w.w[0]), __builtin_bit_cast(cq_v8f16, x.w[0]), acc, 0, 0, 0);
+  } else {
+    float v[8];
+    row_values<XK>(x, v);
+    if constexpr (product_path<XK, WK>() == kSplit) {
+      const split_frag xs = split_pack(v);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w.w[0]), xs.part[p], acc, 0, 0, 0);
+    } else {
+      float u[8];
+      row_values<WK>(w, u);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[q], acc, 0, 0, 0);
+    }
+  }
+}
+
 // low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of
-// K, which its eight wavefronts share out in rounds of STEPS steps of 64 values each and add up in LDS.  Bound by latency: the
-// loads of a round are all asked for before the first product, those of prompts' tokens before the ids are known.
+// K, which its wavefronts share out in rounds of STEPS steps of 64 values each (what is left in single steps) and add up in LDS.
+// Bound by latency: the loads of a round are all asked for before the first product, those of prompts' tokens before the ids are
+// known.
 template <int XK, int WK, int RT, int STEPS>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_args P) {
   constexpr int RW = RT * 16, LD = RW + 4, kRound = 64 * kDownWaves * STEPS;
@@ -136,254 +178,323 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int k_first = blockIdx.y * P.kpart, k_end = min(P.K, k_first + P.kpart);
-  const int k_lane = wave * 64 * STEPS + g * 16;   // this lane's eight of the 32 values of a product, twice per step
+  const int k_lane = wave * 64 * STEPS + g * 16;
+  const int rounds = P.K % 8 == 0 ? (k_end - k_first) / kRound : 0, k_rest = k_first + rounds * kRound;
+  // Workgroups go to the eight XCDs in turn.  Prompts: an XCD takes neighbouring tiles, which share an adapter in its L2.
+  int tile = blockIdx.x;
+  if (P.T > kLeaderTokens) {
+    const int each = gridDim.x / 8;   // (the grid is a multiple of 8 then)
+    tile = blockIdx.x % 8 * each + blockIdx.x / 8;
+    if (tile * kTile >= P.T) return;
+  }
   row8<XK> x[STEPS][2];
-  auto fetch_x = [&](int t, int k0) {
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k = k0 + k_lane + s * 64 + half * 8;
-        x[s][half] = fetch_k<XK>(P.X, (size_t)t * P.ldx, k, k_end, P.K);
-      }
-  };
-  bool fetched = P.T > kLeaderTokens;   // x holds the first round of this workgroup's tokens
-  if (fetched) fetch_x(min((int)blockIdx.x * kDownTile + col, P.T - 1), k_first);
+  bool fetched = P.T > kLeaderTokens && rounds > 0;   // x holds the first round of this workgroup's tokens
+  if (fetched) fetch_round<XK, STEPS>(P.X, (size_t)min(tile * kTile + col, P.T - 1) * P.ldx, k_first + k_lane, x);
   int row, id;
-  if (!find_rows<kDownTile>(P, blockIdx.x, row, id)) return;
+  if (!find_rows<kTile>(P, tile, row, id)) return;
   // (lane 0 has a token; readlane does not depend on which lanes are active)
-  const int token = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0), t = token < 0 ? some : token;
+  const int token = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0);
+  const size_t x_row = (size_t)(token < 0 ? some : token) * P.ldx;
   const int r0 = blockIdx.z * kRankBlock;
   unsigned todo = (unsigned)__ballot(id >= 0) & 0xffffu;
   while (todo) {
     const int a = __builtin_amdgcn_readlane(id, __ffs(todo) - 1);
     const unsigned match = (unsigned)__ballot(id == a) & 0xffffu;
     todo &= ~match;
-    if (!fetched) fetch_x(t, k_first);
     const int rank = rank_of(P, a);
-    cq_v4f acc[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
     if (rank > r0) {
-      const size_t w_row = ((size_t)a * P.R + r0 + col) * P.K;
-      for (int k0 = k_first; k0 < k_end; k0 += kRound) {
-        if (k0 > k_first) fetch_x(t, k0);
+      cq_v4f acc[RT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          const bool in = r0 + i * 16 + col < rank;
-          row8<WK> w[STEPS][2];
+      for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+      // (rows beyond the adapter's rank repeat its last one: their sums are not used)
+      auto w_row = [&](int i) { return ((size_t)a * P.R + min(r0 + i * 16 + col, rank - 1)) * P.K; };
+#pragma unroll 1
+      for (int n = 0; n < rounds; ++n) {
+        const int k = k_first + n * kRound + k_lane;
+        if (!fetched) fetch_round<XK, STEPS>(P.X, x_row, k, x);
+        fetched = false;
+        // (two tiles of rows at a time, all their loads before the first product: the scheduler would hold the second's back)
+        constexpr int kPair = RT < 2 ? 1 : 2;
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s)
+        for (int i = 0; i < RT; i += kPair) {
+          row8<WK> w[kPair][STEPS][2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const int k = k0 + k_lane + s * 64 + half * 8;
-              w[s][half] = fetch_k<WK>(P.A, w_row + (size_t)i * 16 * P.K, in ? k : k_end, k_end, P.K);
-            }
+          for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k, w[j]);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s)
+          for (int j = 0; j < kPair; ++j)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if constexpr (product_path<XK, WK>() == kSame16) {
-                if constexpr (XK == CQ_A_BF16)
-                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[s][half].w[0]),
-                                                                   __builtin_bit_cast(cq_v8bf16, x[s][half].w[0]), acc[i], 0, 0, 0);
-                else
-                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(cq_v8f16, w[s][half].w[0]),
-                                                                  __builtin_bit_cast(cq_v8f16, x[s][half].w[0]), acc[i], 0, 0, 0);
-              } else if constexpr (product_path<XK, WK>() == kSplit) {
-                float v[8];
-                row_values<XK>(x[s][half], v);
-                const split_frag xs = split_pack(v);
+            for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int p = 0; p < 3; ++p)
-                  acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[s][half].w[0]), xs.part[p], acc[i], 0, 0, 0);
-              } else {
-                float v[8], u[8];
-                row_values<XK>(x[s][half], v);
-                row_values<WK>(w[s][half], u);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[q], acc[i], 0, 0, 0);
-              }
-            }
+              for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[j][s][half], x[s][half], acc[i + j]);
         }
       }
+#pragma unroll 1
+      for (int k = k_rest + wave * 64 + g * 16; k < k_end + g * 16; k += 64 * kDownWaves) {   // (the same count in all lanes)
+        row8<XK> rest[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, x_row, k + half * 8, k_end, P.K);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          row8<WK> w[2];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), k + half * 8, k_end, P.K);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
+        }
+      }
+      fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
       __syncthreads();
       for (int e = threadIdx.x; e < 16 * RW; e += 64 * kDownWaves) {
-        const int tok = e / RW, r = e % RW;
+        const int tok = e / RW, r = r0 + e % RW;
         const int to = __shfl(row, tok);
-        if (!(match >> tok & 1u) || r0 + r >= P.Rp) continue;
+        if (!(match >> tok & 1u) || r >= P.Rp) continue;
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < kDownWaves; ++w) s += lds[w][tok][r];
-        P.low[((size_t)blockIdx.y * P.T + to) * P.Rp + r0 + r] = s;
+        for (int w = 0; w < kDownWaves; ++w) s += lds[w][tok][e % RW];
+        P.low[((size_t)blockIdx.y * P.T + to) * P.Rp + r] = r < rank ? s : 0.f;
       }
       __syncthreads();
     }
-    fetched = k_end - k_first <= kRound;   // one round: x serves the next adapter's tokens as well
   }
 }
 
-// out = base + scale B_a low.  One workgroup: 16 SUBS tokens and 256 outputs; a wavefront has 64 of them as
-// four tiles of 16.  The rows of a tile are chosen so that a lane's outputs of one or (16 bits) two tiles are neighbours.
-// Bound by HBM for prompts (base and out), by latency for single tokens: base is asked for first, for prompts before the ids
-// are known, and all loads of 32 ranks before their products.
+// out = base + scale B_a low.  A workgroup has 256 outputs of its tokens, a wavefront 64 of them as four tiles of 16.  The rows of a
+// tile are chosen so that a lane's outputs of one or (16 bits) two tiles are neighbours.
 template <int OK>
 __device__ __forceinline__ int out_row(int tile, int i) {
   if (OK == CQ_A_F32) return tile * 16 + i;
   return (tile >> 1) * 32 + (i >> 2) * 8 + (tile & 1) * 4 + (i & 3);
 }
 
-template <int WK, int OK, int SUBS>
-__global__ __launch_bounds__(64 * kUpWaves) void adapter_up_kernel(adapter_args P) {
-  constexpr int kOuts = OK == CQ_A_F32 ? 4 : 2;      // groups of outputs of a lane
-  constexpr int kOut = OK == CQ_A_F32 ? 4 : 8;       // outputs of a group: 16 bytes
+template <int OK>
+struct up_lane {   // where a lane's outputs lie: kOuts groups of kOut neighbours, 16 bytes each
+  static constexpr int kOuts = OK == CQ_A_F32 ? 4 : 2, kOut = OK == CQ_A_F32 ? 4 : 8;
+  static __device__ __forceinline__ int first(int o, int g) { return out_row<OK>(OK == CQ_A_F32 ? o : 2 * o, g * 4); }
+};
+
+template <int OK>
+__device__ __forceinline__ void fetch_base(const adapter_args& P, int t, int n0, int g, bool in, cq_v4u (&base)[up_lane<OK>::kOuts]) {
+  using L = up_lane<OK>;
+#pragma unroll
+  for (int o = 0; o < L::kOuts; ++o) {
+    const int n = n0 + L::first(o, g);
+    base[o] = cq_v4u{0u, 0u, 0u, 0u};
+    if (P.base && in && n + L::kOut <= P.N)
+      base[o] = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(P.base) + ((size_t)t * P.ldb + n) * (OK == CQ_A_F32 ? 4 : 2));
+  }
+}
+
+// Columns rb + 8 g .. of B's rows n0 .. n0+63 (four tiles).  c: the first column (a row that is no whole number of eights: its last
+// eight overlap their neighbours); columns from `most` on are not asked for.  SHORT: rows may
+// have fewer than eight.
+template <int WK, int OK, bool SHORT>
+__device__ __forceinline__ void fetch_up(const adapter_args& P, int a, int n0, int col, int r, int c, int most, row8<WK> (&w)[4]) {
+  const size_t w_row = ((size_t)a * P.N + n0) * P.R;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int n = out_row<OK>(j, col);
+    const bool on = r < most && n0 + n < P.N;
+    if (!SHORT || P.R >= 8) w[j] = fetch8<WK>(P.B, w_row, (uint32_t)(n * P.R + c), on);
+    else w[j] = row_fetch<WK>(P.B, w_row + n * P.R, on ? P.R : 0);
+  }
+}
+
+// What lies outside of columns r .. rank-1 may be anything, and 0 times an infinite x is no 0: cleared in both operands.
+template <int WK>
+__device__ __forceinline__ void keep_rank(int r, int c, int rank, row8<WK> (&w)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) keep_values(w[j], r - c, rank - c);
+}
+__device__ __forceinline__ void keep_rank(int r, int c, int rank, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = c + i >= r && c + i < rank ? v[i] : 0.f;
+}
+
+template <int WK>
+__device__ __forceinline__ void up_product(const row8<WK> (&w)[4], const float (&v)[8], cq_v4f (&acc)[4]) {
+  if constexpr (WK == CQ_A_BF16) {
+    const split_frag vs = split_pack(v);
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[j].w[0]), vs.part[p], acc[j], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float u[8];
+      row_values<WK>(w[j], u);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[q], acc[j], 0, 0, 0);
+    }
+  }
+}
+
+template <int OK>
+__device__ __forceinline__ void store_out(const adapter_args& P, int t, int n0, int g, bool any, float scale, const cq_v4f (&acc)[4],
+                                          const cq_v4u (&base)[up_lane<OK>::kOuts]) {
+  using L = up_lane<OK>;
+#pragma unroll
+  for (int o = 0; o < L::kOuts; ++o) {
+    const int n = n0 + L::first(o, g);
+    const size_t at = (size_t)t * P.ldo + n;
+    float add[8];
+#pragma unroll
+    for (int i = 0; i < L::kOut; ++i) add[i] = acc[o * (L::kOut / 4) + (i >> 2)][i & 3];
+    if (n + L::kOut <= P.N) {
+      if constexpr (OK == CQ_A_F32) {
+        cq_v4u v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float b = __uint_as_float(base[o][i]);
+          v[i] = __float_as_uint(any ? fmaf(scale, add[i], b) : b);
+        }
+        *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<float*>(P.out) + at) = v;
+      } else {
+        row8<OK> b;
+        b.w[0] = base[o];
+        float v[8];
+        row_values<OK>(b, v);
+        if (any) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, add[i], v[i]);
+        }
+        row_store8<OK>(P.out, at, 8, v);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L::kOut; ++i) {
+        if (n + i >= P.N) continue;
+        float v = P.base ? elem_load<OK>(P.base, (size_t)t * P.ldb + n + i) : 0.f;
+        if (any) v = fmaf(scale, add[i], v);
+        elem_store<OK>(P.out, at + i, v);
+      }
+    }
+  }
+}
+
+// Single tokens: up to 16 of one adapter per workgroup.  Bound by latency: base, low and the first 32 columns of B are asked for
+// together, the latter before the adapter's own rank is known and cleared beyond it (B's rows are short).
+template <int WK, int OK>
+__global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  // Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of
-  // outputs an XCD meets the same rows of B again and again (prefill of 4096 x 4096 values at rank 32: 26.7 instead of 29.9 us).
   const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), tile = blockIdx.x / blocks;
   const int n0 = (((int)blockIdx.x - tile * blocks) * kUpWaves + wave) * 64;
   if (n0 >= P.N) return;
-  auto first_out = [&](int o) { return n0 + (OK == CQ_A_F32 ? out_row<OK>(o, g * 4) : out_row<OK>(2 * o, g * 4)); };
-  cq_v4u base[SUBS][kOuts];
-  auto fetch_base = [&](int sub, int t) {
-#pragma unroll
-    for (int o = 0; o < kOuts; ++o) {
-      const int n = first_out(o);
-      base[sub][o] = cq_v4u{0u, 0u, 0u, 0u};
-      if (P.base && t >= 0 && n + kOut <= P.N)
-        base[sub][o] = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(P.base) + ((size_t)t * P.ldb + n) * (OK == CQ_A_F32 ? 4 : 2));
-    }
-  };
-  const bool prompt = P.T > kLeaderTokens;
-  if (prompt) {
-#pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub) {
-      const int t = (tile * SUBS + sub) * 16 + col;
-      fetch_base(sub, t < P.T ? t : -1);
-    }
-  }
   int row, id;
-  if (!find_rows<16 * SUBS>(P, tile, row, id)) return;
-  int t[SUBS];
+  if (!find_rows<kTile>(P, tile, row, id)) return;
+  const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
+  cq_v4u base[up_lane<OK>::kOuts];
+  fetch_base<OK>(P, t, n0, g, t >= 0, base);
+  const int rank = rank_of(P, a);
+  const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
+  cq_v4f acc[4];
 #pragma unroll
-  for (int sub = 0; sub < SUBS; ++sub) {
-    t[sub] = __shfl(row, sub * 16 + col);
-    if (!prompt) fetch_base(sub, t[sub]);
-  }
-  constexpr unsigned long long kRows = (1ull << 16 * SUBS) - 1;
-  unsigned long long todo = __ballot(row >= 0) & kRows;
-  while (todo) {
-    const int a = __builtin_amdgcn_readlane(id, __ffsll((long long)todo) - 1);
-    const unsigned long long match = __ballot(row >= 0 && id == a) & kRows;
-    todo &= ~match;
-    const int rank = rank_of(P, a);
-    const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
-    cq_v4f acc[SUBS][4];
+  for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+  for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
+    const int r = rb + g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r, most = rb == 0 ? P.R : rank;
+    row8<WK> w[4];
+    fetch_up<WK, OK, true>(P, a, n0, col, r, c, most, w);
+    float v[8];
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub)
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (t >= 0 && r < most) {
+      const float* from = P.low + (size_t)t * P.Rp + c;
+#pragma unroll 4
+      for (int p = 0; p < P.parts; ++p) {
+        float u[8];
+        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(from, (size_t)p * P.T * P.Rp, 0, true), u);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[sub][j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
-      // The first 32 columns are asked for before the adapter's own rank is known and cleared beyond it: B's rows are short.
-      // (a row that is no whole number of eights: its last eight overlap their neighbours)
-      const int r = rb + g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r;
-      const bool on = r < (rb == 0 ? P.R : rank);
-      const size_t w_row = ((size_t)a * P.N + n0) * P.R;
-      row8<WK> w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int n = out_row<OK>(j, col);
-        if (P.R >= 8) w[j] = fetch8<WK>(P.B, w_row, (uint32_t)(n * P.R + c), on && n0 + n < P.N);
-        else w[j] = row_fetch<WK>(P.B, w_row + n * P.R, on && n0 + n < P.N ? P.R : 0);
-      }
-      float v[SUBS][8];
-#pragma unroll
-      for (int sub = 0; sub < SUBS; ++sub) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[sub][i] = 0.f;
-        if ((match >> (sub * 16 + col) & 1) && on) {
-          const float* from = P.low + (size_t)t[sub] * P.Rp + c;
-#pragma unroll 2
-          for (int p = 0; p < P.parts; ++p) {
-            float u[8];
-            row_values<CQ_A_F32>(fetch8<CQ_A_F32>(from, (size_t)p * P.T * P.Rp, 0, true), u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[sub][i] += u[i];
-          }
-        }
-      }
-      if (rank < rb + 32) {   // what lies beyond the rank may be anything, and 0 times an infinite x is no 0
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[sub][i] = c + i >= r && c + i < rank ? v[sub][i] : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) keep_values(w[j], r - c, rank - c);
-      }
-#pragma unroll
-      for (int sub = 0; sub < SUBS; ++sub) {
-        if (!(match >> (sub * 16) & 0xffffu)) continue;
-        if constexpr (WK == CQ_A_BF16) {
-          const split_frag vs = split_pack(v[sub]);
-#pragma unroll
-          for (int p = 0; p < 3; ++p)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              acc[sub][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[j].w[0]), vs.part[p], acc[sub][j], 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float u[8];
-            row_values<WK>(w[j], u);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) acc[sub][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[sub][q], acc[sub][j], 0, 0, 0);
-          }
-        }
+        for (int i = 0; i < 8; ++i) v[i] += u[i];
       }
     }
+    if (rank < rb + 32) {
+      keep_rank(r, c, rank, v);
+      keep_rank<WK>(r, c, rank, w);
+    }
+    up_product<WK>(w, v, acc);
+  }
+  if (t >= 0) store_out<OK>(P, t, n0, g, rank > 0, scale, acc, base);
+}
+
+// Prompts: four tiles of 16 neighbouring tokens one after the other, the next one's base and low in flight while this one is worked
+// on; the adapter's first 32 NB columns of B stay in registers from tile to tile.  Bound by HBM (base in, out written).
+// Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of outputs
+// an XCD meets the same rows of B again and again.
+// ANY: ranks beyond 32 NB or below 8.
+template <int WK, int OK, int NB, bool ANY>
+__global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ? 2 : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32 ? 4 : 3) void adapter_up_prompt_kernel(adapter_args P) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), chunk = blockIdx.x / blocks;
+  const int n0 = (((int)blockIdx.x - chunk * blocks) * kUpWaves + wave) * 64;
+  if (n0 >= P.N) return;
+  struct ahead {
+    cq_v4u base[up_lane<OK>::kOuts];
+    row8<CQ_A_F32> low[NB];
+  } tiles[kPromptTiles];
+  auto column = [&](int rb) { return !ANY || P.R >= 8 ? min(rb + g * 8, P.R - 8) : rb + g * 8; };
+  const int first = chunk * kPromptTiles;
+  const int mine = first * kTile + lane;
+  const int id = lane < kPromptTiles * kTile && mine < P.T ? adapter_of(P, mine) : -1;
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub) {
-      if (!(match >> (sub * 16 + col) & 1)) continue;
+  for (int i = 0; i < kPromptTiles; ++i) {
+    const int t = (first + i) * kTile + col;
+    fetch_base<OK>(P, t, n0, g, t < P.T, tiles[i].base);
 #pragma unroll
-      for (int o = 0; o < kOuts; ++o) {
-        const int n = first_out(o);
-        const size_t at = (size_t)t[sub] * P.ldo + n;
-        float add[8];
+    for (int b = 0; b < NB; ++b)   // (rows of low hold padded_rank values: columns up to R + 7 are read, those from R on cleared)
+      tiles[i].low[b] = fetch8<CQ_A_F32>(P.low, (size_t)t * P.Rp + column(b * 32), 0, t < P.T && b * 32 + g * 8 < P.R);
+  }
+  int have = -1, rank = 0;
+  float scale = 1.f;
+  row8<WK> w[NB][4];
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) add[i] = acc[sub][o * (kOut / 4) + (i >> 2)][i & 3];
-        if (n + kOut <= P.N) {
-          if constexpr (OK == CQ_A_F32) {
-            cq_v4u v;
+  for (int i = 0; i < kPromptTiles; ++i) {
+    const int t = (first + i) * kTile + col;
+    unsigned todo = (unsigned)(__ballot(mine < P.T) >> (i * kTile)) & 0xffffu;
+    while (todo) {
+      const int a = __builtin_amdgcn_readlane(id, i * kTile + __ffs(todo) - 1);
+      const unsigned match = (unsigned)(__ballot(id == a) >> (i * kTile)) & todo;
+      todo &= ~match;
+      if (a != have) {
+        have = a;
+        rank = rank_of(P, a);
+        scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float b = __uint_as_float(base[sub][o][i]);
-              v[i] = __float_as_uint(rank > 0 ? fmaf(scale, add[i], b) : b);
-            }
-            *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<float*>(P.out) + at) = v;
-          } else {
-            row8<OK> b;
-            b.w[0] = base[sub][o];
-            float v[8];
-            row_values<OK>(b, v);
-            if (rank > 0) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, add[i], v[i]);
-            }
-            row_store8<OK>(P.out, at, 8, v);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kOut; ++i) {
-            if (n + i >= P.N) continue;
-            float v = P.base ? elem_load<OK>(P.base, (size_t)t[sub] * P.ldb + n + i) : 0.f;
-            if (rank > 0) v = fmaf(scale, add[i], v);
-            elem_store<OK>(P.out, at + i, v);
-          }
+        for (int b = 0; b < NB; ++b) {
+          fetch_up<WK, OK, ANY>(P, a, n0, col, b * 32 + g * 8, column(b * 32), a >= 0 ? rank : 0, w[b]);
+          if (rank < b * 32 + 32) keep_rank<WK>(b * 32 + g * 8, column(b * 32), rank, w[b]);
         }
       }
+      cq_v4f acc[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (rank <= b * 32) continue;
+        float v[8];
+        row_values<CQ_A_F32>(tiles[i].low[b], v);
+        if (rank < b * 32 + 32) keep_rank(b * 32 + g * 8, column(b * 32), rank, v);
+        up_product<WK>(w[b], v, acc);
+      }
+#pragma unroll 1
+      for (int rb = NB * 32; ANY && rb < rank; rb += 32) {   // ranks beyond the registers
+        const int r = rb + g * 8, c = column(rb);
+        row8<WK> more[4];
+        fetch_up<WK, OK, ANY>(P, a, n0, col, r, c, rank, more);
+        float v[8];
+        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, (size_t)t * P.Rp + c, 0, t < P.T && r < rank), v);
+        if (rank < rb + 32) {
+          keep_rank(r, c, rank, v);
+          keep_rank<WK>(r, c, rank, more);
+        }
+        up_product<WK>(more, v, acc);
+      }
+      if (match >> col & 1) store_out<OK>(P, t, n0, g, rank > 0, scale, acc, tiles[i].base);
     }
   }
 }
@@ -398,21 +509,28 @@ cq_status check_adapters(const cq_adapters* W, int T) {
 
 int padded_rank(int R) { return (R + 15) / 16 * 16; }
 
-// Steps of 64 values per wavefront and round, and parts of K: as many steps as leave two workgroups per compute unit; parts of
-// whole rounds, at most 16.
+// Steps of 64 values per wavefront and round, and parts of K.  Prompts: one part, 16 KiB of X in flight per wavefront.  Single
+// tokens: parts of whole rounds, as many steps as leave two workgroups per compute unit, at most 16 parts.
 struct down_plan { int steps, parts, kpart; };
 
 down_plan plan_of(int T, int K, int x_kind) {
-  const long tiles = ((long)T + kDownTile - 1) / kDownTile;
   down_plan d;
+  d.parts = 1;
+  d.kpart = K;
+  if (T > kLeaderTokens) {
+    d.steps = x_kind == CQ_A_F32 ? 4 : 8;
+    while (d.steps > 1 && K < 64 * kDownWaves * d.steps) d.steps /= 2;
+    return d;
+  }
   d.steps = x_kind == CQ_A_F32 ? 2 : 4;
-  auto rounds = [&](int steps) { return ((long)K + 64 * kDownWaves * steps - 1) / (64 * kDownWaves * steps); };
+  const int tiles = (T + kTile - 1) / kTile;
+  auto rounds = [&](int steps) { return (K + 64 * kDownWaves * steps - 1) / (64 * kDownWaves * steps); };
   while (d.steps > 1 && tiles * rounds(d.steps) < 512) d.steps /= 2;
-  const long n = rounds(d.steps);
-  long parts = tiles >= 512 ? 1 : 512 / tiles;
+  const int n = rounds(d.steps);
+  int parts = 512 / tiles;
   if (parts > n) parts = n;
   if (parts > 16) parts = 16;
-  d.kpart = (int)((n + parts - 1) / parts) * 64 * kDownWaves * d.steps;
+  d.kpart = (n + parts - 1) / parts * 64 * kDownWaves * d.steps;
   d.parts = (K + d.kpart - 1) / d.kpart;
   return d;
 }
@@ -421,11 +539,13 @@ down_plan plan_of(int T, int K, int x_kind) {
 
 extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T) {
   if (check_adapters(W, T) != CQ_OK) return 0;
-  // no batch of up to T tokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one step
+  // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one step
   const long most = ((long)W->K + 64 * kDownWaves - 1) / (64 * kDownWaves), cap = most < 16 ? most : 16;
   long rows = T;
   for (long p = 2; p <= cap; ++p) {
-    const long last = 512 / p * kDownTile, t = T < last ? T : last;   // the longest batch with p parts
+    long last = 512 / p * kTile;   // the longest batch with p parts
+    if (last > kLeaderTokens) last = kLeaderTokens;
+    const long t = T < last ? T : last;
     if (t * p > rows) rows = t * p;
   }
   return cq_align_up((size_t)rows * padded_rank(W->rank) * 4, 256);
@@ -465,16 +585,19 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   P.ldo = (size_t)ld_out;
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
-  const dim3 down(leaders ? T : (T + kDownTile - 1) / kDownTile, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
-  const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves), up_tiles = leaders ? T : ((long)T + kUpTile - 1) / kUpTile;
+  const dim3 down(leaders ? T : ((T + kTile - 1) / kTile + 7) / 8 * 8, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
+  const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
+  const long up_tiles = leaders ? T : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
   if (up_tiles * blocks > 0x7fffffffL) return CQ_ERR_SHAPE;
   const dim3 up((unsigned)(up_tiles * blocks));
 #define DOWN3(XK, WK, RT, STEPS) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, STEPS>), down, dim3(64 * kDownWaves), 0, s, P)
-#define DOWN2(XK, WK, RT)                                  \
-  do {                                                     \
-    if (plan.steps == 1) DOWN3(XK, WK, RT, 1);             \
-    else if (plan.steps == 2) DOWN3(XK, WK, RT, 2);        \
-    else if constexpr (XK != CQ_A_F32) DOWN3(XK, WK, RT, 4); \
+#define DOWN2(XK, WK, RT)                                                      \
+  do {                                                                         \
+    constexpr int kMost = most_steps<XK, WK, RT>();                            \
+    if (plan.steps == 1 || kMost == 1) DOWN3(XK, WK, RT, 1);                   \
+    else if (plan.steps == 2 || kMost == 2) DOWN3(XK, WK, RT, (kMost < 2 ? kMost : 2)); \
+    else if (plan.steps == 4 || kMost == 4) DOWN3(XK, WK, RT, (kMost < 4 ? kMost : 4)); \
+    else DOWN3(XK, WK, RT, kMost);                                             \
   } while (0)
 #define DOWN1(XK, WK)                         \
   do {                                        \
@@ -488,10 +611,13 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
     else if (x_kind == CQ_A_F16) DOWN1(CQ_A_F16, WK); \
     else DOWN1(CQ_A_BF16, WK);                        \
   } while (0)
-#define UP2(WK, OK)                                                                                                   \
-  do {                                                                                                                \
-    if (leaders) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, 1>), up, dim3(64 * kUpWaves), 0, s, P);                \
-    else hipLaunchKernelGGL((adapter_up_kernel<WK, OK, kUpTile / 16>), up, dim3(64 * kUpWaves), 0, s, P);             \
+#define UP_PROMPT(WK, OK, NB, ANY) hipLaunchKernelGGL((adapter_up_prompt_kernel<WK, OK, NB, ANY>), up, dim3(64 * kUpWaves), 0, s, P)
+#define UP2(WK, OK)                                                                                                     \
+  do {                                                                                                                  \
+    if (leaders) hipLaunchKernelGGL((adapter_up_kernel<WK, OK>), up, dim3(64 * kUpWaves), 0, s, P);                     \
+    else if (W->rank < 8 || W->rank > 64) UP_PROMPT(WK, OK, 1, true);                                                    \
+    else if (W->rank <= 32) UP_PROMPT(WK, OK, 1, false);                                                                \
+    else UP_PROMPT(WK, OK, 2, false);                                                                                   \
   } while (0)
 #define UP(WK)                                    \
   do {                                            \
