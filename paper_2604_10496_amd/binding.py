@@ -717,9 +717,9 @@ def cq_balance_loss(logits, ids, alpha: float, seq_offsets=None, token_mask=None
     nbytes = _BYTES.get(("balance", T, E, S))
     if nbytes is None:
         nbytes = _BYTES["balance", T, E, S] = lib.cq_balance_loss_workspace_bytes(T, E, S)
-    ws = _scratch(logits, nbytes)
+    ws = _scratch(logits, nbytes) if nbytes else None
     st = lib.cq_balance_loss(logits.data_ptr(), kind, ids.data_ptr(), _ptr(seq_offsets), S, _ptr(token_mask), T, E, k, alpha,
-                             loss.data_ptr(), counts.data_ptr(), probs.data_ptr(), tokens.data_ptr(), ws.data_ptr(), nbytes,
+                             loss.data_ptr(), counts.data_ptr(), probs.data_ptr(), tokens.data_ptr(), _ptr(ws), nbytes,
                              _raw_stream(logits))
     if st:
         raise CqError(st)

@@ -38,18 +38,31 @@ __device__ __forceinline__ int offset_at(const balance_args& P, int s) {
   return o < 0 ? 0 : (o > P.T ? P.T : o);
 }
 
-// the last sequence that begins at or before token t (-1: none does); t is the same in the whole wavefront
-__device__ __forceinline__ int sequence_of(const balance_args& P, int t) {
-  if (!P.offsets) return 0;
-  int n = 0;
-  for (int c = 0; c < P.S; c += 64) {
-    const int s = c + (threadIdx.x & 63);
-    const int here = __popcll(__ballot(s < P.S && offset_at(P, s) <= t));
-    n += here;
-    if (here < 64) break;
+// The offsets around a token: sequence_of finds the last sequence that begins at or before token t (-1: none does; t is the same in
+// the whole wavefront) and keeps the 64 offsets it has loaded for offset().
+struct offset_window {
+  const balance_args& P;
+  int base, here;   // offsets base .. base+63, one per lane
+  __device__ __forceinline__ explicit offset_window(const balance_args& args) : P(args) { load(0); }
+  __device__ __forceinline__ void load(int first) {
+    base = first;
+    const int s = first + (int)(threadIdx.x & 63);
+    here = s <= P.S ? offset_at(P, s) : 0x7fffffff;
   }
-  return n - 1;
-}
+  __device__ __forceinline__ int sequence_of(int t) {
+    int n = 0;
+    for (;;) {
+      const int found = __popcll(__ballot(base + (int)(threadIdx.x & 63) < P.S && here <= t));
+      n += found;
+      if (found < 64 || base + 64 >= P.S) return n - 1;
+      load(base + 64);
+    }
+  }
+  __device__ __forceinline__ int offset(int s) {   // 0 <= s <= S, the same in the whole wavefront
+    if (s < base || s >= base + 64) load(s);
+    return __builtin_amdgcn_readlane(here, s - base);
+  }
+};
 
 // four consecutive values, the first `left` of which exist; the others read as -inf
 template <int KIND>
@@ -146,11 +159,26 @@ struct segment_lds {
   int n;
 };
 
+// the sums over a workgroup of what its lanes hold for their experts, into S.p; no barrier
+template <int NT, int L, int C>
+__device__ __forceinline__ void give_probs(const float (&acc)[C][4], segment_lds<NT, L, C>& S) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L) * 4;
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v = acc[j][i];
+#pragma unroll
+      for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+      if (lane < L) S.p[wave][e0 + j * L * 4 + i] = v;
+    }
+}
+
 // Tokens [a, b) of one sequence: probability sums per wavefront, counts and the tokens that count, into LDS.  Ends with a barrier.
 template <int KIND, int NT, int L, int C>
 __device__ __forceinline__ void segment(const balance_args& P, int a, int b, segment_lds<NT, L, C>& S) {
   constexpr int U = C == 1 ? 4 : 1;   // loads in flight
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L) * 4;
+  const int lane = threadIdx.x & 63, e0 = (lane % L) * 4;
   for (int e = threadIdx.x; e < P.E; e += NT) S.c[e] = 0;
   if (threadIdx.x == 0) S.n = P.mask ? 0 : b - a;
   __syncthreads();
@@ -193,35 +221,98 @@ __device__ __forceinline__ void segment(const balance_args& P, int a, int b, seg
     const int id = P.ids[(size_t)a * P.k + i];
     if (id >= 0 && id < P.E) atomicAdd(&S.c[id], 1);
   }
-#pragma unroll
-  for (int j = 0; j < C; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float v = acc[j][i];
-#pragma unroll
-      for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-      if (lane < L) S.p[wave][e0 + j * L * 4 + i] = v;
-    }
+  give_probs<NT, L, C>(acc, S);
   __syncthreads();
 }
 
-template <int KIND, int L, int C>
+template <int L, int C>
+__device__ __forceinline__ void write_slot(const balance_args& P, const balance_ws& W, size_t slot, const segment_lds<256, L, C>& S) {
+  for (int e = threadIdx.x; e < P.E; e += 256) {
+    W.probs[slot * P.E + e] = (S.p[0][e] + S.p[1][e]) + (S.p[2][e] + S.p[3][e]);
+    W.counts[slot * P.E + e] = S.c[e];
+  }
+  if (threadIdx.x == 0) W.tokens[slot] = S.n;
+}
+
+// Tiles of one round of loads: everything a tile reads is asked for at once, before the offsets are known; its sequences then take
+// their tokens out of the registers.
+template <int KIND, int L>
 __global__ __launch_bounds__(256) void balance_tile_kernel(balance_args P, balance_ws W) {
+  constexpr int U = 4, kTokens = U * (256 / L), kIds = 4;
+  __shared__ segment_lds<256, L, 1> lds;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *W.done = 0;
+  const int lane = threadIdx.x & 63, e0 = (lane % L) * 4;
+  const int t0 = blockIdx.x * kTokens, t1 = min(P.T, t0 + kTokens);
+  offset_window offsets(P);
+  float p[U][1][4];
+  bool in[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = t0 + u * (256 / L) + threadIdx.x / L;
+    in[u] = t < t1 && (!P.mask || P.mask[t]);
+    load4<KIND>(P.z, (size_t)t * P.E + e0, t < t1 ? P.E - e0 : 0, p[u][0]);
+  }
+  // the first ids of a thread (all of them for up to 1024 assignments), -1 where the token is left out
+  const int assignments = (t1 - t0) * P.k;
+  auto id_of = [&](int i) {
+    const int id = P.ids[(size_t)t0 * P.k + i];
+    return (!P.mask || P.mask[t0 + i / P.k]) && id >= 0 && id < P.E ? id : -1;
+  };
+  int ids[kIds];
+#pragma unroll
+  for (int n = 0; n < kIds; ++n) ids[n] = (int)threadIdx.x + n * 256 < assignments ? id_of(threadIdx.x + n * 256) : -1;
+#pragma unroll
+  for (int u = 0; u < U; ++u) softmax_token<L, 1>(p[u]);
+  for (int s = max(offsets.sequence_of(t0), 0); s < P.S; ++s) {
+    const int a0 = offsets.offset(s), b0 = offsets.offset(s + 1);
+    if (a0 >= t1) break;
+    const int a = max(a0, t0), b = min(b0, t1);
+    if (a >= b) continue;
+    for (int e = threadIdx.x; e < P.E; e += 256) lds.c[e] = 0;
+    if (threadIdx.x == 0) lds.n = 0;
+    __syncthreads();
+    float acc[1][4] = {{0.f, 0.f, 0.f, 0.f}};
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * (256 / L) + threadIdx.x / L;
+      const bool mine = in[u] && t >= a && t < b;
+      n += __popcll(__ballot(mine && lane % L == 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[0][i] += mine ? p[u][0][i] : 0.f;
+    }
+    if (lane == 0 && n) atomicAdd(&lds.n, n);
+    const int from = (a - t0) * P.k, to = (b - t0) * P.k;
+#pragma unroll
+    for (int q = 0; q < kIds; ++q) {
+      const int i = threadIdx.x + q * 256;
+      if (ids[q] >= 0 && i >= from && i < to) atomicAdd(&lds.c[ids[q]], 1);
+    }
+    for (int i = threadIdx.x + kIds * 256; i < to; i += 256) {
+      const int id = i >= from ? id_of(i) : -1;
+      if (id >= 0) atomicAdd(&lds.c[id], 1);
+    }
+    give_probs<256, L, 1>(acc, lds);
+    __syncthreads();
+    write_slot<L, 1>(P, W, (size_t)blockIdx.x + s, lds);
+    __syncthreads();
+  }
+}
+
+// Tiles of any size, sequence after sequence.
+template <int KIND, int L, int C>
+__global__ __launch_bounds__(256) void balance_long_tile_kernel(balance_args P, balance_ws W) {
   __shared__ segment_lds<256, L, C> lds;
   if (blockIdx.x == 0 && threadIdx.x == 0) *W.done = 0;
   const int t0 = blockIdx.x * P.tile, t1 = min(P.T, t0 + P.tile);
-  for (int s = max(sequence_of(P, t0), 0); s < P.S; ++s) {
-    const int a0 = offset_at(P, s), b0 = offset_at(P, s + 1);
+  offset_window offsets(P);
+  for (int s = max(offsets.sequence_of(t0), 0); s < P.S; ++s) {
+    const int a0 = offsets.offset(s), b0 = offsets.offset(s + 1);
     if (a0 >= t1) break;
     const int a = max(a0, t0), b = min(b0, t1);
     if (a >= b) continue;
     segment<KIND, 256, L, C>(P, a, b, lds);
-    const size_t slot = (size_t)blockIdx.x + s;
-    for (int e = threadIdx.x; e < P.E; e += 256) {
-      W.probs[slot * P.E + e] = (lds.p[0][e] + lds.p[1][e]) + (lds.p[2][e] + lds.p[3][e]);
-      W.counts[slot * P.E + e] = lds.c[e];
-    }
-    if (threadIdx.x == 0) W.tokens[slot] = lds.n;
+    write_slot<L, C>(P, W, (size_t)blockIdx.x + s, lds);
     __syncthreads();
   }
 }
@@ -335,7 +426,7 @@ __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const
                                                            const float* d_loss, void* dz) {
   constexpr int U = C == 1 ? 4 : 1;
   const int e0 = (threadIdx.x % L) * 4, t0 = blockIdx.x * (U * (256 / L));
-  const int s0 = sequence_of(P, t0);
+  offset_window offsets(P);
   float p[U][C][4];
   bool in[U];
 #pragma unroll
@@ -352,7 +443,7 @@ __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const
   const float g = (d_loss ? d_loss[0] : 1.f) * P.alpha * (float)P.E;
   float f[C][4];
   float w = 0.f;
-  int s = s0, have = -2;
+  int s = offsets.sequence_of(t0), have = -2;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int t = t0 + u * (256 / L) + threadIdx.x / L;
@@ -397,11 +488,26 @@ cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, in
   return CQ_OK;
 }
 
-// Tokens per workgroup: one round of loads in flight for up to 64 experts; more where the second launch would have to add more
-// than 512 tiles.
-int tile_of(int T) { return T <= (64 << 9) ? 64 : T <= (128 << 9) ? 128 : 256; }
+// Tokens per workgroup.  One round of loads, about 4096 logits, where that makes no more than kMostTiles tiles; longer batches take
+// as many tokens as make kMostTiles, so that the second launch has no more to add.
+constexpr int kMostTiles = 512;
+constexpr int kMostExpertsInRound = 256;
 
-size_t slots_of(int T, int S) { return (size_t)T / 64 + 1 + S; }   // (never falls as T grows)
+int round_tokens(int E) {
+  int lanes = 1;
+  while (lanes * 4 < E) lanes *= 2;
+  return 4 * (256 / lanes);
+}
+
+bool in_rounds(int T, int E) { return E <= kMostExpertsInRound && ((long)T + round_tokens(E) - 1) / round_tokens(E) <= kMostTiles; }
+
+int tile_of(int T, int E) {
+  if (in_rounds(T, E)) return round_tokens(E);
+  const int tile = (int)(((long)T + kMostTiles - 1) / kMostTiles);
+  return tile < 16 ? 16 : tile;
+}
+
+size_t slots_of(int T, int S) { return (size_t)(T < kMostTiles ? T : kMostTiles) + 1 + S; }   // (never falls as T grows)
 
 bool in_one(int T, int E, int S) { return (long)T * E <= 32768 && S <= 4 && E <= 256; }
 
@@ -426,7 +532,7 @@ bool in_one(int T, int E, int S) { return (long)T * E <= 32768 && S <= 4 && E <=
 }  // namespace
 
 extern "C" size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs) {
-  if (T < 0 || E <= 0 || E > kMaxExperts || n_seqs <= 0) return 0;
+  if (T < 0 || E <= 0 || E > kMaxExperts || n_seqs <= 0 || in_one(T, E, n_seqs)) return 0;
   const size_t slots = slots_of(T, n_seqs);
   return 2 * cq_align_up(slots * E * 4, 256) + cq_align_up(slots * 4, 256) + cq_align_up((size_t)n_seqs * ((E + 31) / 32) * 4, 256) + 256;
 }
@@ -438,9 +544,10 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   const cq_status st = check_balance(logit_kind, seq_offsets, n_seqs, T, E, top_k);
   if (st != CQ_OK) return st;
   if ((T > 0 && (!logits || !topk_ids)) || !loss || !counts || !probs || !tokens) return CQ_ERR_NULL;
-  if (!workspace || workspace_bytes < cq_balance_loss_workspace_bytes(T, E, n_seqs)) return CQ_ERR_WORKSPACE;
+  const size_t need = cq_balance_loss_workspace_bytes(T, E, n_seqs);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T), alpha};
+  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T, E), alpha};
   const size_t slots = slots_of(T, n_seqs);
   balance_ws W;
   char* at = (char*)workspace;
@@ -464,7 +571,12 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
     return cq_check_launch();
   }
   const int tiles = T > 0 ? (T - 1) / P.tile + 1 : 1;
-#define LAUNCH(KIND, L, C) hipLaunchKernelGGL((balance_tile_kernel<KIND, L, C>), dim3(tiles), dim3(256), 0, s, P, W)
+  const bool rounds = in_rounds(T, E);
+#define LAUNCH(KIND, L, C)                                                                                             \
+  do {                                                                                                                 \
+    if (C == 1 && rounds) hipLaunchKernelGGL((balance_tile_kernel<KIND, L>), dim3(tiles), dim3(256), 0, s, P, W);      \
+    else hipLaunchKernelGGL((balance_long_tile_kernel<KIND, L, C>), dim3(tiles), dim3(256), 0, s, P, W);               \
+  } while (0)
   CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
 #undef LAUNCH
   hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seqs, (E + 31) / 32), dim3(1024), 0, s, P, W, counts, probs, tokens, loss);

@@ -132,8 +132,9 @@ def test_balance_refusals():
     assert call(T=-1) == 2 and call(E=0) == 2 and call(E=1025) == 2 and call(k=0) == 2 and call(k=17) == 2 and call(S=0) == 2
     assert call(E=100, k=65) == 2
     assert call(kind=0) == 3 and call(kind=4) == 3
-    need = lib.cq_balance_loss_workspace_bytes(8, 16, 3)
-    assert need > 0 and call(n=need - 1) == 4 and call(ws=None) == 4
+    need = lib.cq_balance_loss_workspace_bytes(4096, 16, 3)
+    assert need > 0 and call(T=4096, n=need - 1) == 4 and call(T=4096, ws=None) == 4
+    assert lib.cq_balance_loss_workspace_bytes(8, 16, 3) == 0      # few logits: one workgroup, no workspace
     assert lib.cq_balance_loss_workspace_bytes(8, 0, 3) == 0
 
     def grad(z=ONE, kind=F32, counts=ONE, tokens=ONE, off=ONE, S=3, T=8, E=16, k=2, out=ONE):
@@ -179,5 +180,6 @@ def test_workspaces_never_fall_as_the_batch_grows():
     for s in (_adapters(), _adapters(rank=200, n=100, K=4096, N=4096)):
         sizes = [lib.cq_adapter_workspace_bytes(ctypes.byref(s), t) for t in T]
         assert sizes == sorted(sizes)
-    sizes = [lib.cq_balance_loss_workspace_bytes(t, 60, 5) for t in T]
-    assert sizes == sorted(sizes)
+    for E, S in ((60, 5), (4, 1), (128, 3), (1000, 2)):
+        sizes = [lib.cq_balance_loss_workspace_bytes(t, E, S) for t in T]
+        assert sizes == sorted(sizes)
