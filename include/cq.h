@@ -378,7 +378,8 @@ cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t
  *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256; K, N <= 2^23.
  *   X [T, K] of x_kind with rows ldx values apart; base [T, N] (NULL: zero) and out [T, N] of out_kind, rows ld_base and ld_out
  *   values apart; out may be base.  adapter_ids [T] on the device, in any order.
- *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, T) bytes, which never falls as T grows.
+ *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, T) bytes, which never falls as T grows (few tokens of low
+ *   rank need none: 0, NULL allowed).
  */
 typedef struct {
   int n, rank, K, N;

@@ -804,9 +804,9 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
     nbytes = adapters._bytes.get(T)
     if nbytes is None:
         nbytes = adapters._bytes[T] = lib.cq_adapter_workspace_bytes(s, T)
-    ws = _scratch(X, nbytes)
+    ws = _scratch(X, nbytes) if nbytes else None
     st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),
-                              _kind(out.dtype, "out"), ldo, ws.data_ptr(), nbytes, _raw_stream(X))
+                              _kind(out.dtype, "out"), ldo, _ptr(ws), nbytes, _raw_stream(X))
     if st:
         raise CqError(st)
     return out

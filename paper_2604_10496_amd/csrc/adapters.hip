@@ -1,8 +1,8 @@
 // Low-rank adapters of many requests beside a projection that they share:
 //   out_t = base_t + scale_a B_a (A_a x_t),  a = ids[t];   a outside [0, n): out_t = base_t.
 //
-// Two launches of matrix-core tiles, low = A_a x (fp32, kept in K parts in the workspace) and out = base + scale B_a low.
-// Both hold tokens as the columns and rows of A or B as the rows of a 16 x 16 result, so that a lane owns four neighbouring
+// Two launches of matrix-core tiles, low = A_a x (fp32, kept in K parts in the workspace) and out = base + scale B_a low; one launch
+// for few tokens of low rank.  They hold tokens as the columns and rows of A or B as the rows of a 16 x 16 result, so that a lane owns four neighbouring
 // rows of one token and stores them together.
 //
 // Tokens meet their adapters in one of two ways.  Batches of up to kLeaderTokens tokens (decode steps, in any order): a
@@ -167,6 +167,55 @@ __device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& 
   }
 }
 
+// A wavefront's share of the sums over k_first .. k_end-1 for one adapter's rows r0 .. and 16 tokens: rounds of STEPS steps of 64 values,
+// what is left in single steps.  x: a round of the tokens' values, the first one's where `fetched`.
+template <int XK, int WK, int RT, int STEPS>
+__device__ __forceinline__ void down_sums(const adapter_args& P, int a, int rank, int r0, size_t x_row, int k_first, int k_end, int rounds,
+                                          bool fetched, row8<XK> (&x)[STEPS][2], cq_v4f (&acc)[RT]) {
+  constexpr int kRound = 64 * kDownWaves * STEPS;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+  const int k_lane = wave * 64 * STEPS + g * 16, k_rest = k_first + rounds * kRound;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+  // (rows beyond the adapter's rank repeat its last one: their sums are not used)
+  auto w_row = [&](int i) { return ((size_t)a * P.R + min(r0 + i * 16 + col, rank - 1)) * P.K; };
+#pragma unroll 1
+  for (int n = 0; n < rounds; ++n) {
+    const int k = k_first + n * kRound + k_lane;
+    if (!fetched) fetch_round<XK, STEPS>(P.X, x_row, k, x);
+    fetched = false;
+    // (two tiles of rows at a time, all their loads before the first product: the scheduler would hold the second's back)
+    constexpr int kPair = RT < 2 ? 1 : 2;
+#pragma unroll
+    for (int i = 0; i < RT; i += kPair) {
+      row8<WK> w[kPair][STEPS][2];
+#pragma unroll
+      for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k, w[j]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < kPair; ++j)
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[j][s][half], x[s][half], acc[i + j]);
+    }
+  }
+#pragma unroll 1
+  for (int k = k_rest + wave * 64 + g * 16; k < k_end + g * 16; k += 64 * kDownWaves) {   // (the same count in all lanes)
+    row8<XK> rest[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, x_row, k + half * 8, k_end, P.K);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      row8<WK> w[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), k + half * 8, k_end, P.K);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
+    }
+  }
+}
+
 // low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of
 // K, which its wavefronts share out in rounds of STEPS steps of 64 values each (what is left in single steps) and add up in LDS.
 // Bound by latency: the loads of a round are all asked for before the first product, those of prompts' tokens before the ids are
@@ -179,7 +228,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
   const int col = lane & 15, g = lane >> 4;
   const int k_first = blockIdx.y * P.kpart, k_end = min(P.K, k_first + P.kpart);
   const int k_lane = wave * 64 * STEPS + g * 16;
-  const int rounds = P.K % 8 == 0 ? (k_end - k_first) / kRound : 0, k_rest = k_first + rounds * kRound;
+  const int rounds = P.K % 8 == 0 ? (k_end - k_first) / kRound : 0;
   // Workgroups go to the eight XCDs in turn.  Prompts: an XCD takes neighbouring tiles, which share an adapter in its L2.
   int tile = blockIdx.x;
   if (P.T > kLeaderTokens) {
@@ -204,45 +253,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
     const int rank = rank_of(P, a);
     if (rank > r0) {
       cq_v4f acc[RT];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-      // (rows beyond the adapter's rank repeat its last one: their sums are not used)
-      auto w_row = [&](int i) { return ((size_t)a * P.R + min(r0 + i * 16 + col, rank - 1)) * P.K; };
-#pragma unroll 1
-      for (int n = 0; n < rounds; ++n) {
-        const int k = k_first + n * kRound + k_lane;
-        if (!fetched) fetch_round<XK, STEPS>(P.X, x_row, k, x);
-        fetched = false;
-        // (two tiles of rows at a time, all their loads before the first product: the scheduler would hold the second's back)
-        constexpr int kPair = RT < 2 ? 1 : 2;
-#pragma unroll
-        for (int i = 0; i < RT; i += kPair) {
-          row8<WK> w[kPair][STEPS][2];
-#pragma unroll
-          for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k, w[j]);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < kPair; ++j)
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[j][s][half], x[s][half], acc[i + j]);
-        }
-      }
-#pragma unroll 1
-      for (int k = k_rest + wave * 64 + g * 16; k < k_end + g * 16; k += 64 * kDownWaves) {   // (the same count in all lanes)
-        row8<XK> rest[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, x_row, k + half * 8, k_end, P.K);
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          row8<WK> w[2];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), k + half * 8, k_end, P.K);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
-        }
-      }
+      down_sums<XK, WK, RT, STEPS>(P, a, rank, r0, x_row, k_first, k_end, rounds, fetched, x, acc);
       fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
@@ -421,6 +432,54 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
   if (t >= 0) store_out<OK>(P, t, n0, g, rank > 0, scale, acc, base);
 }
 
+// Few tokens of low rank in one launch: every workgroup of 512 outputs takes the whole of A_a x_t for itself, so that nothing
+// passes through memory, at the price of reading A (from L2) once per workgroup.  Bound by latency: base and B are asked for
+// before A.
+template <int XK, int WK, int OK, int RT>
+__global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_args P) {
+  constexpr int STEPS = product_path<XK, WK>() == kFloat ? 1 : XK == CQ_A_F32 ? 2 : 4, kRound = 64 * kDownWaves * STEPS, LD = RT * 16 + 4;
+  __shared__ float lds[kDownWaves][16][LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  const int blocks = (P.N + 64 * kDownWaves - 1) / (64 * kDownWaves), tile = blockIdx.x / blocks;
+  const int n0 = (((int)blockIdx.x - tile * blocks) * kDownWaves + wave) * 64;
+  int row, id;
+  if (!find_rows<kTile>(P, tile, row, id)) return;
+  const int t = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0), a = __builtin_amdgcn_readlane(id, 0);
+  const size_t x_row = (size_t)(t < 0 ? some : t) * P.ldx;
+  const int rounds = P.K % 8 == 0 ? P.K / kRound : 0;
+  cq_v4u base[up_lane<OK>::kOuts];
+  fetch_base<OK>(P, t, n0, g, t >= 0, base);
+  const int r = g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r, rank = rank_of(P, a);
+  const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
+  cq_v4f out[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) out[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+  if (rank > 0) {
+    row8<WK> b[4];
+    fetch_up<WK, OK, true>(P, a, n0, col, r, c, rank, b);
+    row8<XK> x[STEPS][2];
+    cq_v4f acc[RT];
+    down_sums<XK, WK, RT, STEPS>(P, a, rank, 0, x_row, 0, P.K, rounds, false, x, acc);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
+    __syncthreads();
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (r < rank) {
+#pragma unroll
+      for (int w = 0; w < kDownWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += lds[w][col][c + i];
+    }
+    keep_rank(r, c, rank, v);
+    keep_rank<WK>(r, c, rank, b);
+    up_product<WK>(b, v, out);
+  }
+  if (t >= 0 && n0 < P.N) store_out<OK>(P, t, n0, g, rank > 0, scale, out, base);
+}
+
 // Prompts: four tiles of 16 neighbouring tokens one after the other, the next one's base and low in flight while this one is worked
 // on; the adapter's first 32 NB columns of B stay in registers from tile to tile.  Bound by HBM (base in, out written).
 // Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of outputs
@@ -535,10 +594,19 @@ down_plan plan_of(int T, int K, int x_kind) {
   return d;
 }
 
+// One launch instead of two where A is small and its copies are few: up to 65536 values per adapter, read by up to 256 workgroups
+// that read 2^23 values between them.  Graph replays, bf16, one / two launches (us): rank 8, K = 2048, N = 2816, 64 tokens 6.6 / 8.4;
+// rank 16, K = N = 4096, 1 token 9.4 / 8.3, 16 tokens 9.6 / 9.3, 64 tokens 12.2 / 10.2; rank 32, 1 token 13.6 / 9.2; called from Python
+// a launch is another 3 us.
+bool takes_few(const cq_adapters* W, int T) {
+  const long values = (long)W->rank * W->K, blocks = ((long)W->N + 64 * kDownWaves - 1) / (64 * kDownWaves);
+  return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23;
+}
+
 }  // namespace
 
 extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T) {
-  if (check_adapters(W, T) != CQ_OK) return 0;
+  if (check_adapters(W, T) != CQ_OK || takes_few(W, T)) return 0;
   // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one step
   const long most = ((long)W->K + 64 * kDownWaves - 1) / (64 * kDownWaves), cap = most < 16 ? most : 16;
   long rows = T;
@@ -560,7 +628,8 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   if (T == 0) return CQ_OK;
   if (!W->A || !W->B || !X || !adapter_ids || !out) return CQ_ERR_NULL;
   if (ldx < W->K || ld_out < W->N || (base && ld_base < W->N)) return CQ_ERR_SHAPE;
-  if (!workspace || workspace_bytes < cq_adapter_workspace_bytes(W, T)) return CQ_ERR_WORKSPACE;
+  const size_t need = cq_adapter_workspace_bytes(W, T);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   adapter_args P;
   P.A = W->A;
   P.B = W->B;
@@ -585,6 +654,31 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   P.ldo = (size_t)ld_out;
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
+  if (takes_few(W, T)) {
+    const dim3 few((unsigned)(T * (((long)W->N + 64 * kDownWaves - 1) / (64 * kDownWaves))));
+#define FEW3(XK, WK, OK, RT) hipLaunchKernelGGL((adapter_few_kernel<XK, WK, OK, RT>), few, dim3(64 * kDownWaves), 0, s, P)
+#define FEW2(XK, WK, OK)                     \
+  do {                                       \
+    if (W->rank <= 16) FEW3(XK, WK, OK, 1);  \
+    else FEW3(XK, WK, OK, 2);                \
+  } while (0)
+#define FEW1(XK, WK)                                     \
+  do {                                                   \
+    if (out_kind == CQ_A_F32) FEW2(XK, WK, CQ_A_F32);    \
+    else if (out_kind == CQ_A_F16) FEW2(XK, WK, CQ_A_F16); \
+    else FEW2(XK, WK, CQ_A_BF16);                        \
+  } while (0)
+#define FEW(XK)                                          \
+  do {                                                   \
+    if (W->kind == CQ_A_F32) FEW1(XK, CQ_A_F32);         \
+    else if (W->kind == CQ_A_F16) FEW1(XK, CQ_A_F16);    \
+    else FEW1(XK, CQ_A_BF16);                            \
+  } while (0)
+    if (x_kind == CQ_A_F32) FEW(CQ_A_F32);
+    else if (x_kind == CQ_A_F16) FEW(CQ_A_F16);
+    else FEW(CQ_A_BF16);
+    return cq_check_launch();
+  }
   const dim3 down(leaders ? T : ((T + kTile - 1) / kTile + 7) / 8 * 8, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
   const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
   const long up_tiles = leaders ? T : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);

@@ -164,9 +164,10 @@ def test_adapter_refusals():
     assert lib.cq_adapter_apply(ctypes.byref(_adapters(n=0)), ONE, F32, 64, ONE, 5, ONE, 32, ONE, F32, 32, ONE, 1 << 30, None) == 2
     assert call(ldx=63) == 2 and call(ldb=31) == 2 and call(ldo=31) == 2
     assert call(kind=0) == 3 and call(xk=0) == 3 and call(ok=5) == 3
-    s = _adapters()
+    s = _adapters(rank=40)
     need = lib.cq_adapter_workspace_bytes(ctypes.byref(s), 5)
-    assert need > 0 and call(n=need - 1) == 4 and call(ws=None) == 4
+    assert need > 0 and call(rank=40, n=need - 1) == 4 and call(rank=40, ws=None) == 4
+    assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters()), 5) == 0      # few tokens of low rank: no workspace
     assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters(rank=300)), 5) == 0
     assert call(T=0, X=None, ids=None, out=None, ws=None) == 0
 
