@@ -167,22 +167,25 @@ __device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& 
   }
 }
 
-// A wavefront's share of the sums over k_first .. k_end-1 for one adapter's rows r0 .. and 16 tokens: rounds of STEPS steps of 64 values,
-// what is left in single steps.  x: a round of the tokens' values, the first one's where `fetched`.
+// A wavefront's share of the sums over k .. k_end-1 for one adapter's rows r0 .. and 16 tokens: rounds of STEPS steps of 64 values per
+// wavefront, then of half as many, down to one; what is no whole step comes last, with bounds.  `x` holds the first round's values of
+// the tokens where `fetched`.
+struct down_place {
+  int a, rank, r0;
+  size_t x_row;
+};
+
 template <int XK, int WK, int RT, int STEPS>
-__device__ __forceinline__ void down_sums(const adapter_args& P, int a, int rank, int r0, size_t x_row, int k_first, int k_end, int rounds,
-                                          bool fetched, row8<XK> (&x)[STEPS][2], cq_v4f (&acc)[RT]) {
+__device__ __forceinline__ void down_rounds(const adapter_args& P, const down_place& at, int k, int k_end, bool fetched,
+                                            row8<XK> (&x)[STEPS][2], cq_v4f (&acc)[RT]) {
   constexpr int kRound = 64 * kDownWaves * STEPS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-  const int k_lane = wave * 64 * STEPS + g * 16, k_rest = k_first + rounds * kRound;
-#pragma unroll
-  for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
   // (rows beyond the adapter's rank repeat its last one: their sums are not used)
-  auto w_row = [&](int i) { return ((size_t)a * P.R + min(r0 + i * 16 + col, rank - 1)) * P.K; };
+  auto w_row = [&](int i) { return ((size_t)at.a * P.R + min(at.r0 + i * 16 + col, at.rank - 1)) * P.K; };
 #pragma unroll 1
-  for (int n = 0; n < rounds; ++n) {
-    const int k = k_first + n * kRound + k_lane;
-    if (!fetched) fetch_round<XK, STEPS>(P.X, x_row, k, x);
+  for (; P.K % 8 == 0 && k_end - k >= kRound; k += kRound) {
+    const int k_lane = k + wave * 64 * STEPS + g * 16;
+    if (!fetched) fetch_round<XK, STEPS>(P.X, at.x_row, k_lane, x);
     fetched = false;
     // (two tiles of rows at a time, all their loads before the first product: the scheduler would hold the second's back)
     constexpr int kPair = RT < 2 ? 1 : 2;
@@ -190,7 +193,7 @@ __device__ __forceinline__ void down_sums(const adapter_args& P, int a, int rank
     for (int i = 0; i < RT; i += kPair) {
       row8<WK> w[kPair][STEPS][2];
 #pragma unroll
-      for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k, w[j]);
+      for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k_lane, w[j]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < kPair; ++j)
@@ -200,18 +203,23 @@ __device__ __forceinline__ void down_sums(const adapter_args& P, int a, int rank
           for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[j][s][half], x[s][half], acc[i + j]);
     }
   }
+  if constexpr (STEPS > 1) {
+    row8<XK> fewer[STEPS / 2][2];
+    down_rounds<XK, WK, RT, STEPS / 2>(P, at, k, k_end, false, fewer, acc);
+  } else {
 #pragma unroll 1
-  for (int k = k_rest + wave * 64 + g * 16; k < k_end + g * 16; k += 64 * kDownWaves) {   // (the same count in all lanes)
-    row8<XK> rest[2];
+    for (int kk = k + wave * 64 + g * 16; kk < k_end + g * 16; kk += kRound) {   // (the same count in all lanes)
+      row8<XK> rest[2];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, x_row, k + half * 8, k_end, P.K);
+      for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, at.x_row, kk + half * 8, k_end, P.K);
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      row8<WK> w[2];
+      for (int i = 0; i < RT; ++i) {
+        row8<WK> w[2];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), k + half * 8, k_end, P.K);
+        for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), kk + half * 8, k_end, P.K);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
+        for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
+      }
     }
   }
 }
@@ -253,7 +261,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
     const int rank = rank_of(P, a);
     if (rank > r0) {
       cq_v4f acc[RT];
-      down_sums<XK, WK, RT, STEPS>(P, a, rank, r0, x_row, k_first, k_end, rounds, fetched, x, acc);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+      down_rounds<XK, WK, RT, STEPS>(P, {a, rank, r0, x_row}, k_first, k_end, fetched, x, acc);
       fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
@@ -437,7 +447,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
 // before A.
 template <int XK, int WK, int OK, int RT>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_args P) {
-  constexpr int STEPS = product_path<XK, WK>() == kFloat ? 1 : XK == CQ_A_F32 ? 2 : 4, kRound = 64 * kDownWaves * STEPS, LD = RT * 16 + 4;
+  constexpr int STEPS = most_steps<XK, WK, RT>(), LD = RT * 16 + 4;
   __shared__ float lds[kDownWaves][16][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
@@ -447,7 +457,6 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_ar
   if (!find_rows<kTile>(P, tile, row, id)) return;
   const int t = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0), a = __builtin_amdgcn_readlane(id, 0);
   const size_t x_row = (size_t)(t < 0 ? some : t) * P.ldx;
-  const int rounds = P.K % 8 == 0 ? P.K / kRound : 0;
   cq_v4u base[up_lane<OK>::kOuts];
   fetch_base<OK>(P, t, n0, g, t >= 0, base);
   const int r = g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r, rank = rank_of(P, a);
@@ -460,7 +469,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_ar
     fetch_up<WK, OK, true>(P, a, n0, col, r, c, rank, b);
     row8<XK> x[STEPS][2];
     cq_v4f acc[RT];
-    down_sums<XK, WK, RT, STEPS>(P, a, rank, 0, x_row, 0, P.K, rounds, false, x, acc);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    down_rounds<XK, WK, RT, STEPS>(P, {a, rank, 0, x_row}, 0, P.K, false, x, acc);
 #pragma unroll
     for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
     __syncthreads();
