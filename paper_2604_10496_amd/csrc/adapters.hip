@@ -21,7 +21,7 @@ constexpr int kMaxRank = 256;
 constexpr int kLeaderTokens = 1024;
 constexpr int kTile = 16;         // tokens of a matrix-core tile
 constexpr int kPromptTiles = 2;   // tiles that a wavefront of the second launch takes one after the other, of prompts
-constexpr int kDownWaves = 8, kUpWaves = 4;
+constexpr int kDownWaves = 4, kPromptDownWaves = 8, kFewWaves = 8, kUpWaves = 4;
 constexpr int kRankBlock = 64;                // rows of A per workgroup
 
 struct adapter_args {
@@ -29,8 +29,8 @@ struct adapter_args {
   const float* scale;
   const int32_t *ranks, *ids;
   void* out;
-  float* low;   // [parts][T][Rp]
-  int n, R, Rp, K, N, T, parts, kpart;
+  float* low;   // [parts][tiles of 16 tokens][Rp], see low_at
+  int n, R, Rp, K, N, T, tiles, parts, kpart;
   size_t ldx, ldb, ldo;
 };
 
@@ -127,21 +127,68 @@ __device__ __forceinline__ row8<KIND> fetch_k(const void* p, size_t row, int k, 
   return r;
 }
 
-// Steps of a round that a kernel has registers for (256 per lane: two workgroups per compute unit).
+// Units of a round that a kernel has registers for (256 per lane: two workgroups of eight wavefronts per compute unit).
 template <int XK, int WK, int RT>
-constexpr int most_steps() {
-  return product_path<XK, WK>() == kSame16 ? 8 : product_path<XK, WK>() == kSplit ? (RT == 4 ? 2 : 4) : (RT == 4 ? 1 : 2);
+constexpr int most_units() {
+  return product_path<XK, WK>() == kSame16 ? (RT == 1 ? 4 : 2) : product_path<XK, WK>() == kSplit && RT == 1 ? 2 : 1;
 }
 
-// A whole round of a lane, eight of the 32 values of a product twice per step: one address and constant offsets.
-template <int KIND, int STEPS>
-__device__ __forceinline__ void fetch_round(const void* p, size_t row, int k, row8<KIND> (&v)[STEPS][2]) {
-  const char* q = reinterpret_cast<const char*>(p) + (row + k) * (KIND == CQ_A_F32 ? 4 : 2);
+// Four neighbouring lanes hand each other their registers: lane q of the four gets, as its value c, value q of lane c.
+__device__ __forceinline__ void quad_transpose(cq_v4u (&r)[4]) {
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s)
+  for (int d = 0; d < 4; ++d) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) v[s][half] = fetch8<KIND>(q, 0, s * 64 + half * 8, true);
+    for (int n = 0; n < 4; n += 2) {
+      const uint32_t a = r[n][d], b = r[n + 1][d];
+      const uint32_t from_b = __builtin_amdgcn_update_dpp(0u, b, 0xb1, 0xf, 0xf, false);   // quad_perm 1 0 3 2
+      const uint32_t from_a = __builtin_amdgcn_update_dpp(0u, a, 0xb1, 0xf, 0xf, false);
+      r[n][d] = odd ? from_b : a;
+      r[n + 1][d] = odd ? b : from_a;
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const uint32_t a = r[n][d], b = r[n + 2][d];
+      const uint32_t from_b = __builtin_amdgcn_update_dpp(0u, b, 0x4e, 0xf, 0xf, false);   // quad_perm 2 3 0 1
+      const uint32_t from_a = __builtin_amdgcn_update_dpp(0u, a, 0x4e, 0xf, 0xf, false);
+      r[n][d] = high ? from_b : a;
+      r[n + 2][d] = high ? b : from_a;
+    }
+  }
 }
+
+// 128 values of K of 16 rows, as operands of four products: a lane of row l % 16 has values (l / 16) * 32 + c * 8 .. +7 as its c-th.
+// The four lanes of rows 4 i .. 4 i + 3 read 64 contiguous bytes of one row after the other and exchange them: lanes that
+// each read their own row take the cache three times as long (out of L2 15 instead of 42 bytes per clock and compute unit).
+template <int KIND>
+struct k_unit {
+  static constexpr int kSize = KIND == CQ_A_F32 ? 4 : 2, kSets = KIND == CQ_A_F32 ? 2 : 1;
+  cq_v4u raw[kSets][4];
+  // row[n]: first value of row 4 i + n, k: first value of the unit
+  __device__ __forceinline__ void fetch(const void* p, const size_t (&row)[4], int k) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const char* q = reinterpret_cast<const char*>(p) + (row[n] + k + (lane >> 4) * 32) * kSize + (lane & 3) * 16;
+#pragma unroll
+      for (int h = 0; h < kSets; ++h) raw[h][n] = reinterpret_cast<const cq_v4u_any*>(q + h * 64)[0];
+    }
+  }
+  __device__ __forceinline__ void exchange() {
+#pragma unroll
+    for (int h = 0; h < kSets; ++h) quad_transpose(raw[h]);
+  }
+  __device__ __forceinline__ row8<KIND> operand(int c) const {
+    row8<KIND> r;
+    if constexpr (KIND == CQ_A_F32) {
+      r.w[0] = raw[c >> 1][2 * (c & 1)];
+      r.w[1] = raw[c >> 1][2 * (c & 1) + 1];
+    } else {
+      r.w[0] = raw[0][c];
+    }
+    return r;
+  }
+};
 
 // acc += 16 rows of A times 16 tokens over 32 values of K
 template <int XK, int WK>
@@ -167,76 +214,115 @@ __device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& 
   }
 }
 
-// A wavefront's share of the sums over k .. k_end-1 for one adapter's rows r0 .. and 16 tokens: rounds of STEPS steps of 64 values per
-// wavefront, then of half as many, down to one; what is no whole step comes last, with bounds.  `x` holds the first round's values of
+// A wavefront's share of the sums over k .. k_end-1 for one adapter's rows r0 .. and 16 tokens: rounds of UNITS units per wavefront,
+// then of half as many, down to one; the values that make no whole unit come last, with bounds.  `x` holds the first round's units of
 // the tokens where `fetched`.
 struct down_place {
   int a, rank, r0;
-  size_t x_row;
+  size_t own_row, x_row[4];   // X of the lane's own token, and of the four tokens that its quad reads
 };
 
-template <int XK, int WK, int RT, int STEPS>
+template <int XK, int WK, int RT, int UNITS, int WAVES>
 __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_place& at, int k, int k_end, bool fetched,
-                                            row8<XK> (&x)[STEPS][2], cq_v4f (&acc)[RT]) {
-  constexpr int kRound = 64 * kDownWaves * STEPS;
+                                            k_unit<XK> (&x)[UNITS], cq_v4f (&acc)[RT]) {
+  constexpr int kRound = 128 * WAVES * UNITS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   // (rows beyond the adapter's rank repeat its last one: their sums are not used)
-  auto w_row = [&](int i) { return ((size_t)at.a * P.R + min(at.r0 + i * 16 + col, at.rank - 1)) * P.K; };
+  auto w_row = [&](int r) { return ((size_t)at.a * P.R + min(at.r0 + r, at.rank - 1)) * P.K; };
+  auto fetch_rows = [&](int i, int kk, k_unit<WK>& w) {
+    const size_t row[4] = {w_row(i * 16 + (col & 12)), w_row(i * 16 + (col & 12) + 1), w_row(i * 16 + (col & 12) + 2), w_row(i * 16 + (col & 12) + 3)};
+    w.fetch(P.A, row, kk);
+  };
 #pragma unroll 1
-  for (; P.K % 8 == 0 && k_end - k >= kRound; k += kRound) {
-    const int k_lane = k + wave * 64 * STEPS + g * 16;
-    if (!fetched) fetch_round<XK, STEPS>(P.X, at.x_row, k_lane, x);
-    fetched = false;
+  for (; k_end - k >= kRound; k += kRound) {
+    const int kk = k + wave * 128 * UNITS;
+    if (!fetched) {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) x[u].fetch(P.X, at.x_row, kk + u * 128);
+    }
     // (two tiles of rows at a time, all their loads before the first product: the scheduler would hold the second's back)
     constexpr int kPair = RT < 2 ? 1 : 2;
 #pragma unroll
     for (int i = 0; i < RT; i += kPair) {
-      row8<WK> w[kPair][STEPS][2];
-#pragma unroll
-      for (int j = 0; j < kPair; ++j) fetch_round<WK, STEPS>(P.A, w_row(i + j), k_lane, w[j]);
-      __builtin_amdgcn_sched_barrier(0);
+      k_unit<WK> w[kPair][UNITS];
 #pragma unroll
       for (int j = 0; j < kPair; ++j)
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+        for (int u = 0; u < UNITS; ++u) fetch_rows(i + j, kk + u * 128, w[j][u]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == 0 && !fetched) {
 #pragma unroll
-          for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[j][s][half], x[s][half], acc[i + j]);
+        for (int u = 0; u < UNITS; ++u) x[u].exchange();
+      }
+#pragma unroll
+      for (int j = 0; j < kPair; ++j)
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          w[j][u].exchange();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) down_product<XK, WK>(w[j][u].operand(c), x[u].operand(c), acc[i + j]);
+        }
     }
+    fetched = false;
   }
-  if constexpr (STEPS > 1) {
-    row8<XK> fewer[STEPS / 2][2];
-    down_rounds<XK, WK, RT, STEPS / 2>(P, at, k, k_end, false, fewer, acc);
+  if constexpr (UNITS > 1) {
+    k_unit<XK> fewer[UNITS / 2];
+    down_rounds<XK, WK, RT, UNITS / 2, WAVES>(P, at, k, k_end, false, fewer, acc);
   } else {
-#pragma unroll 1
-    for (int kk = k + wave * 64 + g * 16; kk < k_end + g * 16; kk += kRound) {   // (the same count in all lanes)
-      row8<XK> rest[2];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) rest[half] = fetch_k<XK>(P.X, at.x_row, kk + half * 8, k_end, P.K);
+    const int kk = k + wave * 128;
+    if (kk + 128 <= k_end) {
+      k_unit<XK> last;   // (x may be wanted again)
+      last.fetch(P.X, at.x_row, kk);
+      last.exchange();
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        row8<WK> w[2];
+        k_unit<WK> w;
+        fetch_rows(i, kk, w);
+        w.exchange();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) w[half] = fetch_k<WK>(P.A, w_row(i), kk + half * 8, k_end, P.K);
+        for (int c = 0; c < 4; ++c) down_product<XK, WK>(w.operand(c), last.operand(c), acc[i]);
+      }
+    } else {
+#pragma unroll 1
+      for (int from = kk; from < k_end; from += 32) {
+        const row8<XK> rest = fetch_k<XK>(P.X, at.own_row, from + g * 8, k_end, P.K);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) down_product<XK, WK>(w[half], rest[half], acc[i]);
+        for (int i = 0; i < RT; ++i) down_product<XK, WK>(fetch_k<WK>(P.A, w_row(i * 16 + col), from + g * 8, k_end, P.K), rest, acc[i]);
       }
     }
   }
 }
 
-// low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of
-// K, which its wavefronts share out in rounds of STEPS steps of 64 values each (what is left in single steps) and add up in LDS.
-// Bound by latency: the loads of a round are all asked for before the first product, those of prompts' tokens before the ids are
-// known.
-template <int XK, int WK, int RT, int STEPS>
-__global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_args P) {
-  constexpr int RW = RT * 16, LD = RW + 4, kRound = 64 * kDownWaves * STEPS;
-  __shared__ float lds[kDownWaves][16][LD];
+// the rows of X that the quad of a lane reads, and the lane's own (lanes without a token: the first lane's, which has one; readlane
+// does not depend on which lanes are active)
+__device__ __forceinline__ void place_tokens(const adapter_args& P, int row, down_place& at) {
+  const int col = threadIdx.x & 15, some = __builtin_amdgcn_readlane(row, 0);
+  auto token = [&](int of) {
+    const int t = __shfl(row, of);
+    return (size_t)(t < 0 ? some : t) * P.ldx;
+  };
+  at.own_row = token(col);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) at.x_row[n] = token((col & 12) + n);
+}
+
+// Where low holds value r of token t: blocks of 16 tokens x 8 values, so that what the four lanes of neighbouring tokens read of
+// it is contiguous.
+__device__ __forceinline__ size_t low_at(const adapter_args& P, int part, int t, int r) {
+  return (((size_t)part * P.tiles + (t >> 4)) * (P.Rp / 8) + (r >> 3)) * 128 + (t & 15) * 8 + (r & 7);
+}
+
+// low[part][t][r] = sum over the part's k of A_a[r, k] x_t[k].  One workgroup: 16 tokens, RT tiles of 16 rows of A, one part of K,
+// which its wavefronts share out and add up in LDS.  Bound by latency and by the traffic out of L2 (every tile reads its adapter's
+// A): the loads of a round are all asked for before the first product, those of prompts' tokens before the ids are known.
+template <int XK, int WK, int RT, int UNITS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(adapter_args P) {
+  constexpr int RW = RT * 16, LD = RW + 4, kRound = 128 * WAVES * UNITS;
+  __shared__ float lds[WAVES][16][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int k_first = blockIdx.y * P.kpart, k_end = min(P.K, k_first + P.kpart);
-  const int k_lane = wave * 64 * STEPS + g * 16;
-  const int rounds = P.K % 8 == 0 ? (k_end - k_first) / kRound : 0;
+  const int rounds = (k_end - k_first) / kRound;
   // Workgroups go to the eight XCDs in turn.  Prompts: an XCD takes neighbouring tiles, which share an adapter in its L2.
   int tile = blockIdx.x;
   if (P.T > kLeaderTokens) {
@@ -244,38 +330,46 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(adapter_a
     tile = blockIdx.x % 8 * each + blockIdx.x / 8;
     if (tile * kTile >= P.T) return;
   }
-  row8<XK> x[STEPS][2];
+  down_place at;
+  k_unit<XK> x[UNITS];
   bool fetched = P.T > kLeaderTokens && rounds > 0;   // x holds the first round of this workgroup's tokens
-  if (fetched) fetch_round<XK, STEPS>(P.X, (size_t)min(tile * kTile + col, P.T - 1) * P.ldx, k_first + k_lane, x);
+  if (fetched) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) at.x_row[n] = (size_t)min(tile * kTile + (col & 12) + n, P.T - 1) * P.ldx;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) x[u].fetch(P.X, at.x_row, k_first + (wave * UNITS + u) * 128);
+  }
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
-  // (lane 0 has a token; readlane does not depend on which lanes are active)
-  const int token = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0);
-  const size_t x_row = (size_t)(token < 0 ? some : token) * P.ldx;
-  const int r0 = blockIdx.z * kRankBlock;
+  place_tokens(P, row, at);
+  if (fetched) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) x[u].exchange();
+  }
+  at.r0 = blockIdx.z * kRankBlock;
   unsigned todo = (unsigned)__ballot(id >= 0) & 0xffffu;
   while (todo) {
-    const int a = __builtin_amdgcn_readlane(id, __ffs(todo) - 1);
-    const unsigned match = (unsigned)__ballot(id == a) & 0xffffu;
+    at.a = __builtin_amdgcn_readlane(id, __ffs(todo) - 1);
+    const unsigned match = (unsigned)__ballot(id == at.a) & 0xffffu;
     todo &= ~match;
-    const int rank = rank_of(P, a);
-    if (rank > r0) {
+    at.rank = rank_of(P, at.a);
+    if (at.rank > at.r0) {
       cq_v4f acc[RT];
 #pragma unroll
       for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-      down_rounds<XK, WK, RT, STEPS>(P, {a, rank, r0, x_row}, k_first, k_end, fetched, x, acc);
+      down_rounds<XK, WK, RT, UNITS, WAVES>(P, at, k_first, k_end, fetched, x, acc);
       fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
       __syncthreads();
-      for (int e = threadIdx.x; e < 16 * RW; e += 64 * kDownWaves) {
-        const int tok = e / RW, r = r0 + e % RW;
+      for (int e = threadIdx.x; e < 16 * RW; e += 64 * WAVES) {
+        const int tok = e / RW, r = at.r0 + e % RW;
         const int to = __shfl(row, tok);
         if (!(match >> tok & 1u) || r >= P.Rp) continue;
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < kDownWaves; ++w) s += lds[w][tok][e % RW];
-        P.low[((size_t)blockIdx.y * P.T + to) * P.Rp + r] = r < rank ? s : 0.f;
+        for (int w = 0; w < WAVES; ++w) s += lds[w][tok][e % RW];
+        P.low[low_at(P, blockIdx.y, to, r)] = r < at.rank ? s : 0.f;
       }
       __syncthreads();
     }
@@ -308,12 +402,36 @@ __device__ __forceinline__ void fetch_base(const adapter_args& P, int t, int n0,
   }
 }
 
-// Columns rb + 8 g .. of B's rows n0 .. n0+63 (four tiles).  c: the first column (a row that is no whole number of eights: its last
-// eight overlap their neighbours); columns from `most` on are not asked for.  SHORT: rows may
-// have fewer than eight.
+// raw values from, from + 1, ... of eight, zeros behind them
+template <int KIND>
+__device__ __forceinline__ void drop_values(row8<KIND>& r, int from) {
+#pragma unroll
+  for (int bit = 1; bit < 8; bit *= 2) {
+    const bool move = from & bit;
+    if constexpr (KIND == CQ_A_F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t next = i + bit < 8 ? r.w[(i + bit) >> 2][(i + bit) & 3] : 0u;
+        r.w[i >> 2][i & 3] = move ? next : r.w[i >> 2][i & 3];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t up = i < 3 ? r.w[0][i + 1 < 4 ? i + 1 : 3] : 0u, far = i < 2 ? r.w[0][i + 2 < 4 ? i + 2 : 3] : 0u;
+        const uint32_t next = bit == 1 ? (r.w[0][i] >> 16 | up << 16) : bit == 2 ? up : far;
+        r.w[0][i] = move ? next : r.w[0][i];
+      }
+    }
+  }
+}
+
+// Columns r .. r+7 of B's rows n0 .. n0+63 (four tiles) where r < most, zeros beyond the row.  A row that is no whole number of
+// eights: its last eight are read and moved into place.  SHORT: rows may have
+// fewer than eight values, or be no whole number of eights.
 template <int WK, int OK, bool SHORT>
-__device__ __forceinline__ void fetch_up(const adapter_args& P, int a, int n0, int col, int r, int c, int most, row8<WK> (&w)[4]) {
+__device__ __forceinline__ void fetch_up(const adapter_args& P, int a, int n0, int col, int r, int most, row8<WK> (&w)[4]) {
   const size_t w_row = ((size_t)a * P.N + n0) * P.R;
+  const int c = !SHORT ? r : P.R >= 8 ? min(r, P.R - 8) : 0;   // (not SHORT: whole eights)
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int n = out_row<OK>(j, col);
@@ -321,17 +439,21 @@ __device__ __forceinline__ void fetch_up(const adapter_args& P, int a, int n0, i
     if (!SHORT || P.R >= 8) w[j] = fetch8<WK>(P.B, w_row, (uint32_t)(n * P.R + c), on);
     else w[j] = row_fetch<WK>(P.B, w_row + n * P.R, on ? P.R : 0);
   }
+  if (SHORT && P.R % 8 != 0 && P.R >= 8) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) drop_values(w[j], r < P.R ? r - c : 0);
+  }
 }
 
-// What lies outside of columns r .. rank-1 may be anything, and 0 times an infinite x is no 0: cleared in both operands.
+// Columns beyond the adapter's rank may be anything, and 0 times an infinite x is no 0: cleared in both operands.
 template <int WK>
-__device__ __forceinline__ void keep_rank(int r, int c, int rank, row8<WK> (&w)[4]) {
+__device__ __forceinline__ void keep_rank(int r, int rank, row8<WK> (&w)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) keep_values(w[j], r - c, rank - c);
+  for (int j = 0; j < 4; ++j) keep_values(w[j], 0, rank - r);
 }
-__device__ __forceinline__ void keep_rank(int r, int c, int rank, float (&v)[8]) {
+__device__ __forceinline__ void keep_rank(int r, int rank, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = c + i >= r && c + i < rank ? v[i] : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] = r + i < rank ? v[i] : 0.f;
 }
 
 template <int WK>
@@ -417,25 +539,24 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
 #pragma unroll
   for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
   for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
-    const int r = rb + g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r, most = rb == 0 ? P.R : rank;
+    const int r = rb + g * 8, most = rb == 0 ? P.R : rank;
     row8<WK> w[4];
-    fetch_up<WK, OK, true>(P, a, n0, col, r, c, most, w);
+    fetch_up<WK, OK, true>(P, a, n0, col, r, most, w);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
     if (t >= 0 && r < most) {
-      const float* from = P.low + (size_t)t * P.Rp + c;
 #pragma unroll 4
       for (int p = 0; p < P.parts; ++p) {
         float u[8];
-        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(from, (size_t)p * P.T * P.Rp, 0, true), u);
+        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, p, t, r), 0, true), u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += u[i];
       }
     }
     if (rank < rb + 32) {
-      keep_rank(r, c, rank, v);
-      keep_rank<WK>(r, c, rank, w);
+      keep_rank(r, rank, v);
+      keep_rank<WK>(r, rank, w);
     }
     up_product<WK>(w, v, acc);
   }
@@ -446,32 +567,36 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
 // passes through memory, at the price of reading A (from L2) once per workgroup.  Bound by latency: base and B are asked for
 // before A.
 template <int XK, int WK, int OK, int RT>
-__global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_args P) {
-  constexpr int STEPS = most_steps<XK, WK, RT>(), LD = RT * 16 + 4;
-  __shared__ float lds[kDownWaves][16][LD];
+__global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_args P) {
+  constexpr int UNITS = most_units<XK, WK, RT>(), LD = RT * 16 + 4;
+  __shared__ float lds[kFewWaves][16][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int blocks = (P.N + 64 * kDownWaves - 1) / (64 * kDownWaves), tile = blockIdx.x / blocks;
-  const int n0 = (((int)blockIdx.x - tile * blocks) * kDownWaves + wave) * 64;
+  const int blocks = (P.N + 64 * kFewWaves - 1) / (64 * kFewWaves), tile = blockIdx.x / blocks;
+  const int n0 = (((int)blockIdx.x - tile * blocks) * kFewWaves + wave) * 64;
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
-  const int t = __shfl(row, col), some = __builtin_amdgcn_readlane(row, 0), a = __builtin_amdgcn_readlane(id, 0);
-  const size_t x_row = (size_t)(t < 0 ? some : t) * P.ldx;
+  const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
+  down_place at;
+  place_tokens(P, row, at);
   cq_v4u base[up_lane<OK>::kOuts];
   fetch_base<OK>(P, t, n0, g, t >= 0, base);
-  const int r = g * 8, c = P.R >= 8 ? min(r, P.R - 8) : r, rank = rank_of(P, a);
+  const int r = g * 8, rank = rank_of(P, a);
   const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
   cq_v4f out[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) out[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
   if (rank > 0) {
     row8<WK> b[4];
-    fetch_up<WK, OK, true>(P, a, n0, col, r, c, rank, b);
-    row8<XK> x[STEPS][2];
+    fetch_up<WK, OK, true>(P, a, n0, col, r, rank, b);
+    at.a = a;
+    at.rank = rank;
+    at.r0 = 0;
+    k_unit<XK> x[UNITS];
     cq_v4f acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    down_rounds<XK, WK, RT, STEPS>(P, {a, rank, 0, x_row}, 0, P.K, false, x, acc);
+    down_rounds<XK, WK, RT, UNITS, kFewWaves>(P, at, 0, P.K, false, x, acc);
 #pragma unroll
     for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
     __syncthreads();
@@ -480,12 +605,12 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_ar
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
     if (r < rank) {
 #pragma unroll
-      for (int w = 0; w < kDownWaves; ++w)
+      for (int w = 0; w < kFewWaves; ++w)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += lds[w][col][c + i];
+        for (int i = 0; i < 8; ++i) v[i] += lds[w][col][r + i];
     }
-    keep_rank(r, c, rank, v);
-    keep_rank<WK>(r, c, rank, b);
+    keep_rank(r, rank, v);
+    keep_rank<WK>(r, rank, b);
     up_product<WK>(b, v, out);
   }
   if (t >= 0 && n0 < P.N) store_out<OK>(P, t, n0, g, rank > 0, scale, out, base);
@@ -495,7 +620,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_few_kernel(adapter_ar
 // on; the adapter's first 32 NB columns of B stay in registers from tile to tile.  Bound by HBM (base in, out written).
 // Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of outputs
 // an XCD meets the same rows of B again and again.
-// ANY: ranks beyond 32 NB or below 8.
+// ANY: ranks beyond 32 NB, below 8, or that are no multiple of 8.
 template <int WK, int OK, int NB, bool ANY>
 __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ? 2 : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32 ? 4 : 3) void adapter_up_prompt_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -507,7 +632,6 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ?
     cq_v4u base[up_lane<OK>::kOuts];
     row8<CQ_A_F32> low[NB];
   } tiles[kPromptTiles];
-  auto column = [&](int rb) { return !ANY || P.R >= 8 ? min(rb + g * 8, P.R - 8) : rb + g * 8; };
   const int first = chunk * kPromptTiles;
   const int mine = first * kTile + lane;
   const int id = lane < kPromptTiles * kTile && mine < P.T ? adapter_of(P, mine) : -1;
@@ -516,8 +640,8 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ?
     const int t = (first + i) * kTile + col;
     fetch_base<OK>(P, t, n0, g, t < P.T, tiles[i].base);
 #pragma unroll
-    for (int b = 0; b < NB; ++b)   // (rows of low hold padded_rank values: columns up to R + 7 are read, those from R on cleared)
-      tiles[i].low[b] = fetch8<CQ_A_F32>(P.low, (size_t)t * P.Rp + column(b * 32), 0, t < P.T && b * 32 + g * 8 < P.R);
+    for (int b = 0; b < NB; ++b)
+      tiles[i].low[b] = fetch8<CQ_A_F32>(P.low, low_at(P, 0, t, b * 32 + g * 8), 0, t < P.T && b * 32 + g * 8 < P.R);
   }
   int have = -1, rank = 0;
   float scale = 1.f;
@@ -536,8 +660,8 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ?
         scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          fetch_up<WK, OK, ANY>(P, a, n0, col, b * 32 + g * 8, column(b * 32), a >= 0 ? rank : 0, w[b]);
-          if (rank < b * 32 + 32) keep_rank<WK>(b * 32 + g * 8, column(b * 32), rank, w[b]);
+          fetch_up<WK, OK, ANY>(P, a, n0, col, b * 32 + g * 8, a >= 0 ? rank : 0, w[b]);
+          if (rank < b * 32 + 32) keep_rank<WK>(b * 32 + g * 8, rank, w[b]);
         }
       }
       cq_v4f acc[4];
@@ -548,19 +672,19 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ?
         if (rank <= b * 32) continue;
         float v[8];
         row_values<CQ_A_F32>(tiles[i].low[b], v);
-        if (rank < b * 32 + 32) keep_rank(b * 32 + g * 8, column(b * 32), rank, v);
+        if (rank < b * 32 + 32) keep_rank(b * 32 + g * 8, rank, v);
         up_product<WK>(w[b], v, acc);
       }
 #pragma unroll 1
       for (int rb = NB * 32; ANY && rb < rank; rb += 32) {   // ranks beyond the registers
-        const int r = rb + g * 8, c = column(rb);
+        const int r = rb + g * 8;
         row8<WK> more[4];
-        fetch_up<WK, OK, ANY>(P, a, n0, col, r, c, rank, more);
+        fetch_up<WK, OK, ANY>(P, a, n0, col, r, rank, more);
         float v[8];
-        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, (size_t)t * P.Rp + c, 0, t < P.T && r < rank), v);
+        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, 0, t, r), 0, t < P.T && r < rank), v);
         if (rank < rb + 32) {
-          keep_rank(r, c, rank, v);
-          keep_rank<WK>(r, c, rank, more);
+          keep_rank(r, rank, v);
+          keep_rank<WK>(r, rank, more);
         }
         up_product<WK>(more, v, acc);
       }
@@ -579,28 +703,24 @@ cq_status check_adapters(const cq_adapters* W, int T) {
 
 int padded_rank(int R) { return (R + 15) / 16 * 16; }
 
-// Steps of 64 values per wavefront and round, and parts of K.  Prompts: one part, 16 KiB of X in flight per wavefront.  Single
-// tokens: parts of whole rounds, as many steps as leave two workgroups per compute unit, at most 16 parts.
-struct down_plan { int steps, parts, kpart; };
+// Units of 128 values per wavefront and round, and parts of K.  Prompts: one part.  Single tokens: parts of whole rounds, as many
+// units as leave two workgroups per compute unit, at most 16 parts.
+struct down_plan { int units, parts, kpart; };
 
-down_plan plan_of(int T, int K, int x_kind) {
+down_plan plan_of(int T, int K) {
   down_plan d;
+  d.units = 4;
   d.parts = 1;
   d.kpart = K;
-  if (T > kLeaderTokens) {
-    d.steps = x_kind == CQ_A_F32 ? 4 : 8;
-    while (d.steps > 1 && K < 64 * kDownWaves * d.steps) d.steps /= 2;
-    return d;
-  }
-  d.steps = x_kind == CQ_A_F32 ? 2 : 4;
+  if (T > kLeaderTokens) return d;
   const int tiles = (T + kTile - 1) / kTile;
-  auto rounds = [&](int steps) { return (K + 64 * kDownWaves * steps - 1) / (64 * kDownWaves * steps); };
-  while (d.steps > 1 && tiles * rounds(d.steps) < 512) d.steps /= 2;
-  const int n = rounds(d.steps);
+  auto rounds = [&](int units) { return (K + 128 * kDownWaves * units - 1) / (128 * kDownWaves * units); };
+  while (d.units > 1 && tiles * rounds(d.units) < 512) d.units /= 2;
+  const int n = rounds(d.units);
   int parts = 512 / tiles;
   if (parts > n) parts = n;
   if (parts > 16) parts = 16;
-  d.kpart = (n + parts - 1) / parts * 64 * kDownWaves * d.steps;
+  d.kpart = (n + parts - 1) / parts * 128 * kDownWaves * d.units;
   d.parts = (K + d.kpart - 1) / d.kpart;
   return d;
 }
@@ -610,7 +730,7 @@ down_plan plan_of(int T, int K, int x_kind) {
 // rank 16, K = N = 4096, 1 token 9.4 / 8.3, 16 tokens 9.6 / 9.3, 64 tokens 12.2 / 10.2; rank 32, 1 token 13.6 / 9.2; called from Python
 // a launch is another 3 us.
 bool takes_few(const cq_adapters* W, int T) {
-  const long values = (long)W->rank * W->K, blocks = ((long)W->N + 64 * kDownWaves - 1) / (64 * kDownWaves);
+  const long values = (long)W->rank * W->K, blocks = ((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves);
   return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23;
 }
 
@@ -618,14 +738,14 @@ bool takes_few(const cq_adapters* W, int T) {
 
 extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T) {
   if (check_adapters(W, T) != CQ_OK || takes_few(W, T)) return 0;
-  // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one step
-  const long most = ((long)W->K + 64 * kDownWaves - 1) / (64 * kDownWaves), cap = most < 16 ? most : 16;
-  long rows = T;
+  // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one unit
+  const long most = ((long)W->K + 128 * kDownWaves - 1) / (128 * kDownWaves), cap = most < 16 ? most : 16;
+  long rows = ((long)T + kTile - 1) / kTile * kTile;
   for (long p = 2; p <= cap; ++p) {
     long last = 512 / p * kTile;   // the longest batch with p parts
     if (last > kLeaderTokens) last = kLeaderTokens;
-    const long t = T < last ? T : last;
-    if (t * p > rows) rows = t * p;
+    const long t = (T < last ? T : last) + kTile - 1;
+    if (t / kTile * kTile * p > rows) rows = t / kTile * kTile * p;
   }
   return cq_align_up((size_t)rows * padded_rank(W->rank) * 4, 256);
 }
@@ -657,7 +777,8 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   P.K = W->K;
   P.N = W->N;
   P.T = T;
-  const down_plan plan = plan_of(T, W->K, x_kind);
+  P.tiles = (T + kTile - 1) / kTile;
+  const down_plan plan = plan_of(T, W->K);
   P.parts = plan.parts;
   P.kpart = plan.kpart;
   P.ldx = (size_t)ldx;
@@ -666,8 +787,8 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
   if (takes_few(W, T)) {
-    const dim3 few((unsigned)(T * (((long)W->N + 64 * kDownWaves - 1) / (64 * kDownWaves))));
-#define FEW3(XK, WK, OK, RT) hipLaunchKernelGGL((adapter_few_kernel<XK, WK, OK, RT>), few, dim3(64 * kDownWaves), 0, s, P)
+    const dim3 few((unsigned)(T * (((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves))));
+#define FEW3(XK, WK, OK, RT) hipLaunchKernelGGL((adapter_few_kernel<XK, WK, OK, RT>), few, dim3(64 * kFewWaves), 0, s, P)
 #define FEW2(XK, WK, OK)                     \
   do {                                       \
     if (W->rank <= 16) FEW3(XK, WK, OK, 1);  \
@@ -695,14 +816,14 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   const long up_tiles = leaders ? T : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
   if (up_tiles * blocks > 0x7fffffffL) return CQ_ERR_SHAPE;
   const dim3 up((unsigned)(up_tiles * blocks));
-#define DOWN3(XK, WK, RT, STEPS) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, STEPS>), down, dim3(64 * kDownWaves), 0, s, P)
-#define DOWN2(XK, WK, RT)                                                      \
-  do {                                                                         \
-    constexpr int kMost = most_steps<XK, WK, RT>();                            \
-    if (plan.steps == 1 || kMost == 1) DOWN3(XK, WK, RT, 1);                   \
-    else if (plan.steps == 2 || kMost == 2) DOWN3(XK, WK, RT, (kMost < 2 ? kMost : 2)); \
-    else if (plan.steps == 4 || kMost == 4) DOWN3(XK, WK, RT, (kMost < 4 ? kMost : 4)); \
-    else DOWN3(XK, WK, RT, kMost);                                             \
+#define DOWN3(XK, WK, RT, UNITS, WAVES) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, UNITS, WAVES>), down, dim3(64 * WAVES), 0, s, P)
+#define DOWN2(XK, WK, RT)                                                              \
+  do {                                                                                 \
+    constexpr int kMost = most_units<XK, WK, RT>(), kTwo = kMost < 2 ? kMost : 2;      \
+    if (!leaders) DOWN3(XK, WK, RT, kMost, kPromptDownWaves);                          \
+    else if (plan.units == 1) DOWN3(XK, WK, RT, 1, kDownWaves);                        \
+    else if (plan.units == 2) DOWN3(XK, WK, RT, kTwo, kDownWaves);                     \
+    else DOWN3(XK, WK, RT, kMost, kDownWaves);                                         \
   } while (0)
 #define DOWN1(XK, WK)                         \
   do {                                        \
@@ -720,7 +841,7 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
 #define UP2(WK, OK)                                                                                                     \
   do {                                                                                                                  \
     if (leaders) hipLaunchKernelGGL((adapter_up_kernel<WK, OK>), up, dim3(64 * kUpWaves), 0, s, P);                     \
-    else if (W->rank < 8 || W->rank > 64) UP_PROMPT(WK, OK, 1, true);                                                    \
+    else if (W->rank % 8 != 0 || W->rank > 64) UP_PROMPT(WK, OK, 1, true);                                                   \
     else if (W->rank <= 32) UP_PROMPT(WK, OK, 1, false);                                                                \
     else UP_PROMPT(WK, OK, 2, false);                                                                                   \
   } while (0)

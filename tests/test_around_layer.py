@@ -399,6 +399,21 @@ def test_adapter_apply(B, T, K, N, R, n, x, w, o):
     assert two.equal(one[p])
 
 
+@pytest.mark.parametrize("T,K,N,R,n", [(1040, 1152, 80, 24, 5), (1100, 2304, 64, 16, 3), (1030, 4224, 40, 40, 4), (1090, 1024, 130, 8, 2), (1026, 1000, 96, 70, 3),
+                                       (30, 4300, 96, 48, 9), (900, 1500, 64, 32, 4), (20, 4096, 600, 12, 20), (3, 2049, 1024, 32, 3)])
+@pytest.mark.parametrize("x,w,o", [("f32", "bf16", "f32"), ("bf16", "bf16", "bf16"), ("f16", "f16", "f16"), ("f32", "f32", "f32")])
+def test_adapter_widths_around_the_rounds_of_the_sum(B, T, K, N, R, n, x, w, o):
+    """K of whole rounds, of rounds and units, of units and a rest; several adapters within a tile share the values of X."""
+    import torch
+    rng = np.random.default_rng(T + K)
+    A, A64, Bm, B64, X, X64, base, base64, scale, scale64, ids, _ = _adapter_inputs(rng, T, K, N, R, n, x, w, o, False)
+    print(f"T={T} K={K} N={N} R={R} n={n} {x} {w} {o}", flush=True)
+    ids[:T // 2] = np.sort(ids[:T // 2])
+    got = B.cq_adapter_apply(B.DeviceAdapters(A, Bm, scale), X, torch.from_numpy(ids).cuda(), base=base)
+    ref, mag = O.adapter_apply(X64, ids, A64, B64, scale64, None, base64)
+    _check_adapter(got, ref, mag, base64, K, R, f"K={K}")
+
+
 def test_adapter_rows_in_wider_rows_and_in_place(B):
     import torch
     rng = np.random.default_rng(31)
