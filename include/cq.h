@@ -378,7 +378,7 @@ cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t
  *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256; K, N <= 2^23.
  *   X [T, K] of x_kind with rows ldx values apart; base [T, N] (NULL: zero) and out [T, N] of out_kind, rows ld_base and ld_out
  *   values apart; out may be base.  adapter_ids [T] on the device, in any order.
- *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, T) bytes, which never falls as T grows (few tokens of low
+ *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, x_kind, T) bytes, which never falls as T grows (few tokens of low
  *   rank need none: 0, NULL allowed).
  */
 typedef struct {
@@ -389,7 +389,7 @@ typedef struct {
   const float* scale;
   const int32_t* ranks;
 } cq_adapters;
-size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T);
+size_t cq_adapter_workspace_bytes(const cq_adapters* W, int x_kind, int T);
 cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x_kind, long ldx, const int32_t* adapter_ids, int T,
                            const void* base, long ld_base, void* out, int out_kind, long ld_out, void* workspace,
                            size_t workspace_bytes, cq_stream stream);

@@ -145,7 +145,7 @@ def load_library() -> ctypes.CDLL:
     lib.cq_balance_loss_grad.restype = ci
     lib.cq_balance_loss_grad.argtypes = [vp, ci, vp, vp, vp, ci, vp, ci, ci, ci, cf, vp, vp, vp]
     lib.cq_adapter_workspace_bytes.restype = sz
-    lib.cq_adapter_workspace_bytes.argtypes = [ad, ci]
+    lib.cq_adapter_workspace_bytes.argtypes = [ad, ci, ci]
     lib.cq_adapter_apply.restype = ci
     lib.cq_adapter_apply.argtypes = [ad, vp, ci, cl, vp, ci, vp, cl, vp, ci, cl, vp, sz, vp]
     lib.cq_stream_read.restype = ci
@@ -760,7 +760,7 @@ class DeviceAdapters:
             _tensor(ranks, "ranks", (self.n,), torch.int32)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
         self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind, _ptr(A), _ptr(B), _ptr(scale), _ptr(ranks))
-        self._bytes: Dict[int, int] = {}
+        self._bytes: Dict[tuple, int] = {}
 
     def struct(self) -> Adapters:
         return self._struct
@@ -801,9 +801,9 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
         ldo = _rows(out, "out", (T, adapters.N))
     ldb = _rows(base, "base", (T, adapters.N), out.dtype) if base is not None else 0
     s = adapters.struct()
-    nbytes = adapters._bytes.get(T)
+    nbytes = adapters._bytes.get((x_kind, T))
     if nbytes is None:
-        nbytes = adapters._bytes[T] = lib.cq_adapter_workspace_bytes(s, T)
+        nbytes = adapters._bytes[x_kind, T] = lib.cq_adapter_workspace_bytes(s, x_kind, T)
     ws = _scratch(X, nbytes) if nbytes else None
     st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),
                               _kind(out.dtype, "out"), ldo, _ptr(ws), nbytes, _raw_stream(X))

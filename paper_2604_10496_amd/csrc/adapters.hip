@@ -726,18 +726,19 @@ down_plan plan_of(int T, int K) {
 }
 
 // One launch instead of two where A is small and its copies are few: up to 65536 values per adapter, read by up to 256 workgroups
-// that read 2^23 values between them.  Graph replays, bf16, one / two launches (us): rank 8, K = 2048, N = 2816, 64 tokens 6.6 / 8.4;
-// rank 16, K = N = 4096, 1 token 9.4 / 8.3, 16 tokens 9.6 / 9.3, 64 tokens 12.2 / 10.2; rank 32, 1 token 13.6 / 9.2; called from Python
-// a launch is another 3 us.
-bool takes_few(const cq_adapters* W, int T) {
+// that read 2^23 values between them; fp32 rows, whose cutting every workgroup repeats, up to 2048 values of K.  Graph replays, bf16
+// rows, one / two launches (us): rank 8, K = 2048, N = 2816, 32 tokens 6.8 / 8.3; rank 16, K = N = 4096, 1 token 8.4 / 8.3, 16 tokens
+// 8.6 / 9.3, 64 tokens 12.2 / 10.2; fp32 rows, 1 token, K = 2048 9.0 / 7.6, K = 4096 13.0 / 8.3.  Called from Python a launch is
+// another 3 us.
+bool takes_few(const cq_adapters* W, int x_kind, int T) {
   const long values = (long)W->rank * W->K, blocks = ((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves);
-  return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23;
+  return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23 && (x_kind != CQ_A_F32 || W->K <= 2048);
 }
 
 }  // namespace
 
-extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int T) {
-  if (check_adapters(W, T) != CQ_OK || takes_few(W, T)) return 0;
+extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int x_kind, int T) {
+  if (check_adapters(W, T) != CQ_OK || !cq_row_kind(x_kind) || takes_few(W, x_kind, T)) return 0;
   // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one unit
   const long most = ((long)W->K + 128 * kDownWaves - 1) / (128 * kDownWaves), cap = most < 16 ? most : 16;
   long rows = ((long)T + kTile - 1) / kTile * kTile;
@@ -759,7 +760,7 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   if (T == 0) return CQ_OK;
   if (!W->A || !W->B || !X || !adapter_ids || !out) return CQ_ERR_NULL;
   if (ldx < W->K || ld_out < W->N || (base && ld_base < W->N)) return CQ_ERR_SHAPE;
-  const size_t need = cq_adapter_workspace_bytes(W, T);
+  const size_t need = cq_adapter_workspace_bytes(W, x_kind, T);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   adapter_args P;
   P.A = W->A;
@@ -786,7 +787,7 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   P.ldo = (size_t)ld_out;
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
-  if (takes_few(W, T)) {
+  if (takes_few(W, x_kind, T)) {
     const dim3 few((unsigned)(T * (((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves))));
 #define FEW3(XK, WK, OK, RT) hipLaunchKernelGGL((adapter_few_kernel<XK, WK, OK, RT>), few, dim3(64 * kFewWaves), 0, s, P)
 #define FEW2(XK, WK, OK)                     \

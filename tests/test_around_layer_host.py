@@ -165,10 +165,10 @@ def test_adapter_refusals():
     assert call(ldx=63) == 2 and call(ldb=31) == 2 and call(ldo=31) == 2
     assert call(kind=0) == 3 and call(xk=0) == 3 and call(ok=5) == 3
     s = _adapters(rank=40)
-    need = lib.cq_adapter_workspace_bytes(ctypes.byref(s), 5)
+    need = lib.cq_adapter_workspace_bytes(ctypes.byref(s), F32, 5)
     assert need > 0 and call(rank=40, n=need - 1) == 4 and call(rank=40, ws=None) == 4
-    assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters()), 5) == 0      # few tokens of low rank: no workspace
-    assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters(rank=300)), 5) == 0
+    assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters()), F32, 5) == 0      # few tokens of low rank: no workspace
+    assert lib.cq_adapter_workspace_bytes(ctypes.byref(_adapters(rank=300)), F32, 5) == 0
     assert call(T=0, X=None, ids=None, out=None, ws=None) == 0
 
 
@@ -179,8 +179,9 @@ def test_workspaces_never_fall_as_the_batch_grows():
         sizes = [lib.cq_block_norm_grad_workspace_bytes(ctypes.byref(s), t) for t in T]
         assert sizes == sorted(sizes)
     for s in (_adapters(), _adapters(rank=200, n=100, K=4096, N=4096)):
-        sizes = [lib.cq_adapter_workspace_bytes(ctypes.byref(s), t) for t in T]
-        assert sizes == sorted(sizes)
+        for kind in (F32, BF16):
+            sizes = [lib.cq_adapter_workspace_bytes(ctypes.byref(s), kind, t) for t in T]
+            assert sizes == sorted(sizes)
     for E, S in ((60, 5), (4, 1), (128, 3), (1000, 2)):
         sizes = [lib.cq_balance_loss_workspace_bytes(t, E, S) for t in T]
         assert sizes == sorted(sizes)
