@@ -376,31 +376,51 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(adapter_args P
   }
 }
 
-// out = base + scale B_a low.  A workgroup has 256 outputs of its tokens, a wavefront 64 of them as four tiles of 16.  The rows of a
-// tile are chosen so that a lane's outputs of one or (16 bits) two tiles are neighbours.
-template <int OK>
-__device__ __forceinline__ int out_row(int tile, int i) {
-  if (OK == CQ_A_F32) return tile * 16 + i;
-  return (tile >> 1) * 32 + (i >> 2) * 8 + (tile & 1) * 4 + (i & 3);
-}
+// out = base + scale B_a low.  A workgroup has 256 outputs of its tokens, a wavefront 64 of them as four tiles of 16, whose rows are
+// chosen so that a lane's 16 outputs are neighbours.
+__device__ __forceinline__ int out_row(int tile, int i) { return (i >> 2) * 16 + tile * 4 + (i & 3); }
 
+// A lane's outputs as kOuts pieces of 16 bytes.  kOuts neighbouring lanes read and write one token after the other, a piece each, and
+// exchange the pieces (k_unit has the reason).
 template <int OK>
-struct up_lane {   // where a lane's outputs lie: kOuts groups of kOut neighbours, 16 bytes each
-  static constexpr int kOuts = OK == CQ_A_F32 ? 4 : 2, kOut = OK == CQ_A_F32 ? 4 : 8;
-  static __device__ __forceinline__ int first(int o, int g) { return out_row<OK>(OK == CQ_A_F32 ? o : 2 * o, g * 4); }
-};
-
-template <int OK>
-__device__ __forceinline__ void fetch_base(const adapter_args& P, int t, int n0, int g, bool in, cq_v4u (&base)[up_lane<OK>::kOuts]) {
-  using L = up_lane<OK>;
+struct out_pieces {
+  static constexpr int kOuts = OK == CQ_A_F32 ? 4 : 2, kOut = OK == CQ_A_F32 ? 4 : 8, kSize = OK == CQ_A_F32 ? 4 : 2;
+  cq_v4u w[kOuts];
+  // the first output of the piece that this lane moves for its neighbours
+  static __device__ __forceinline__ int moved(int n0, int g) { return n0 + g * 16 + (int)(threadIdx.x & (kOuts - 1)) * kOut; }
+  // token[n]: of the n-th of the neighbouring lanes, -1: none
+  __device__ __forceinline__ void fetch(const adapter_args& P, const int (&token)[kOuts], int n0, int g) {
+    const int at = moved(n0, g);
 #pragma unroll
-  for (int o = 0; o < L::kOuts; ++o) {
-    const int n = n0 + L::first(o, g);
-    base[o] = cq_v4u{0u, 0u, 0u, 0u};
-    if (P.base && in && n + L::kOut <= P.N)
-      base[o] = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(P.base) + ((size_t)t * P.ldb + n) * (OK == CQ_A_F32 ? 4 : 2));
+    for (int n = 0; n < kOuts; ++n) {
+      w[n] = cq_v4u{0u, 0u, 0u, 0u};
+      if (P.base && token[n] >= 0 && at + kOut <= P.N)
+        w[n] = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(P.base) + ((size_t)token[n] * P.ldb + at) * kSize);
+    }
   }
-}
+  __device__ __forceinline__ void store(const adapter_args& P, const int (&token)[kOuts], int n0, int g) const {
+    const int at = moved(n0, g);
+#pragma unroll
+    for (int n = 0; n < kOuts; ++n)
+      if (token[n] >= 0 && at + kOut <= P.N)
+        *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<char*>(P.out) + ((size_t)token[n] * P.ldo + at) * kSize) = w[n];
+  }
+  __device__ __forceinline__ void exchange() {
+    if constexpr (kOuts == 4) {
+      quad_transpose(w);
+    } else {
+      const bool odd = threadIdx.x & 1;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t a = w[0][d], b = w[1][d];
+        const uint32_t from_b = __builtin_amdgcn_update_dpp(0u, b, 0xb1, 0xf, 0xf, false);
+        const uint32_t from_a = __builtin_amdgcn_update_dpp(0u, a, 0xb1, 0xf, 0xf, false);
+        w[0][d] = odd ? from_b : a;
+        w[1][d] = odd ? b : from_a;
+      }
+    }
+  }
+};
 
 // raw values from, from + 1, ... of eight, zeros behind them
 template <int KIND>
@@ -434,7 +454,7 @@ __device__ __forceinline__ void fetch_up(const adapter_args& P, int a, int n0, i
   const int c = !SHORT ? r : P.R >= 8 ? min(r, P.R - 8) : 0;   // (not SHORT: whole eights)
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int n = out_row<OK>(j, col);
+    const int n = out_row(j, col);
     const bool on = r < most && n0 + n < P.N;
     if (!SHORT || P.R >= 8) w[j] = fetch8<WK>(P.B, w_row, (uint32_t)(n * P.R + c), on);
     else w[j] = row_fetch<WK>(P.B, w_row + n * P.R, on ? P.R : 0);
@@ -476,47 +496,53 @@ __device__ __forceinline__ void up_product(const row8<WK> (&w)[4], const float (
   }
 }
 
+// out = base + scale acc of the lane's own token t (-1: none), and of its neighbours' (token)
 template <int OK>
-__device__ __forceinline__ void store_out(const adapter_args& P, int t, int n0, int g, bool any, float scale, const cq_v4f (&acc)[4],
-                                          const cq_v4u (&base)[up_lane<OK>::kOuts]) {
-  using L = up_lane<OK>;
+__device__ __forceinline__ void store_out(const adapter_args& P, int t, const int (&token)[out_pieces<OK>::kOuts], int n0, int g, bool any,
+                                          float scale, const cq_v4f (&acc)[4], out_pieces<OK> base) {
+  using L = out_pieces<OK>;
+  base.exchange();
+  L out;
 #pragma unroll
   for (int o = 0; o < L::kOuts; ++o) {
-    const int n = n0 + L::first(o, g);
-    const size_t at = (size_t)t * P.ldo + n;
-    float add[8];
+    float add[8], v[8];
 #pragma unroll
     for (int i = 0; i < L::kOut; ++i) add[i] = acc[o * (L::kOut / 4) + (i >> 2)][i & 3];
-    if (n + L::kOut <= P.N) {
-      if constexpr (OK == CQ_A_F32) {
-        cq_v4u v;
+    if constexpr (OK == CQ_A_F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float b = __uint_as_float(base[o][i]);
-          v[i] = __float_as_uint(any ? fmaf(scale, add[i], b) : b);
-        }
-        *reinterpret_cast<cq_v4u_any*>(reinterpret_cast<float*>(P.out) + at) = v;
-      } else {
-        row8<OK> b;
-        b.w[0] = base[o];
-        float v[8];
-        row_values<OK>(b, v);
-        if (any) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = fmaf(scale, add[i], v[i]);
-        }
-        row_store8<OK>(P.out, at, 8, v);
+      for (int i = 0; i < 4; ++i) {
+        const float b = __uint_as_float(base.w[o][i]);
+        out.w[o][i] = __float_as_uint(any ? fmaf(scale, add[i], b) : b);
       }
     } else {
+      row8<OK> b;
+      b.w[0] = base.w[o];
+      row_values<OK>(b, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t pair = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float x = fmaf(scale, add[2 * i + h], v[2 * i + h]);
+          const uint16_t bits = OK == CQ_A_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)x) : __builtin_bit_cast(uint16_t, (_Float16)x);
+          pair |= (uint32_t)bits << (16 * h);
+        }
+        out.w[o][i] = any ? pair : base.w[o][i];
+      }
+    }
+    const int n = n0 + g * 16 + o * L::kOut;
+    if (n + L::kOut > P.N && t >= 0) {   // the row ends within these outputs
 #pragma unroll
       for (int i = 0; i < L::kOut; ++i) {
         if (n + i >= P.N) continue;
-        float v = P.base ? elem_load<OK>(P.base, (size_t)t * P.ldb + n + i) : 0.f;
-        if (any) v = fmaf(scale, add[i], v);
-        elem_store<OK>(P.out, at + i, v);
+        float x = P.base ? elem_load<OK>(P.base, (size_t)t * P.ldb + n + i) : 0.f;
+        if (any) x = fmaf(scale, add[i], x);
+        elem_store<OK>(P.out, (size_t)t * P.ldo + n + i, x);
       }
     }
   }
+  out.exchange();
+  out.store(P, token, n0, g);
 }
 
 // Single tokens: up to 16 of one adapter per workgroup.  Bound by latency: base, low and the first 32 columns of B are asked for
@@ -531,8 +557,12 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
   const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
-  cq_v4u base[up_lane<OK>::kOuts];
-  fetch_base<OK>(P, t, n0, g, t >= 0, base);
+  constexpr int kOuts = out_pieces<OK>::kOuts;
+  int token[kOuts];
+#pragma unroll
+  for (int n = 0; n < kOuts; ++n) token[n] = __shfl(row, (col & (16 - kOuts)) + n);
+  out_pieces<OK> base;
+  base.fetch(P, token, n0, g);
   const int rank = rank_of(P, a);
   const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
   cq_v4f acc[4];
@@ -560,7 +590,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
     }
     up_product<WK>(w, v, acc);
   }
-  if (t >= 0) store_out<OK>(P, t, n0, g, rank > 0, scale, acc, base);
+  store_out<OK>(P, t, token, n0, g, rank > 0, scale, acc, base);
 }
 
 // Few tokens of low rank in one launch: every workgroup of 512 outputs takes the whole of A_a x_t for itself, so that nothing
@@ -579,8 +609,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
   const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
   down_place at;
   place_tokens(P, row, at);
-  cq_v4u base[up_lane<OK>::kOuts];
-  fetch_base<OK>(P, t, n0, g, t >= 0, base);
+  constexpr int kOuts = out_pieces<OK>::kOuts;
+  int token[kOuts];
+#pragma unroll
+  for (int n = 0; n < kOuts; ++n) token[n] = __shfl(row, (col & (16 - kOuts)) + n);
+  out_pieces<OK> base;
+  base.fetch(P, token, n0, g);
   const int r = g * 8, rank = rank_of(P, a);
   const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
   cq_v4f out[4];
@@ -613,7 +647,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
     keep_rank<WK>(r, rank, b);
     up_product<WK>(b, v, out);
   }
-  if (t >= 0 && n0 < P.N) store_out<OK>(P, t, n0, g, rank > 0, scale, out, base);
+  store_out<OK>(P, t, token, n0, g, rank > 0, scale, out, base);
 }
 
 // Prompts: four tiles of 16 neighbouring tokens one after the other, the next one's base and low in flight while this one is worked
@@ -622,23 +656,28 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
 // an XCD meets the same rows of B again and again.
 // ANY: ranks beyond 32 NB, below 8, or that are no multiple of 8.
 template <int WK, int OK, int NB, bool ANY>
-__global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ? 2 : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32 ? 4 : 3) void adapter_up_prompt_kernel(adapter_args P) {
+__global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && (WK == CQ_A_F32 || OK == CQ_A_F32)) ? 2 : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32 ? 4 : 3) void adapter_up_prompt_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), chunk = blockIdx.x / blocks;
   const int n0 = (((int)blockIdx.x - chunk * blocks) * kUpWaves + wave) * 64;
   if (n0 >= P.N) return;
   struct ahead {
-    cq_v4u base[up_lane<OK>::kOuts];
+    out_pieces<OK> base;
     row8<CQ_A_F32> low[NB];
   } tiles[kPromptTiles];
+  constexpr int kOuts = out_pieces<OK>::kOuts;
   const int first = chunk * kPromptTiles;
+  auto neighbour = [&](int i, int n) { return (first + i) * kTile + (col & (16 - kOuts)) + n; };
   const int mine = first * kTile + lane;
   const int id = lane < kPromptTiles * kTile && mine < P.T ? adapter_of(P, mine) : -1;
 #pragma unroll
   for (int i = 0; i < kPromptTiles; ++i) {
     const int t = (first + i) * kTile + col;
-    fetch_base<OK>(P, t, n0, g, t < P.T, tiles[i].base);
+    int token[kOuts];
+#pragma unroll
+    for (int n = 0; n < kOuts; ++n) token[n] = neighbour(i, n) < P.T ? neighbour(i, n) : -1;
+    tiles[i].base.fetch(P, token, n0, g);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
       tiles[i].low[b] = fetch8<CQ_A_F32>(P.low, low_at(P, 0, t, b * 32 + g * 8), 0, t < P.T && b * 32 + g * 8 < P.R);
@@ -688,7 +727,10 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && WK == CQ_A_F32) ?
         }
         up_product<WK>(more, v, acc);
       }
-      if (match >> col & 1) store_out<OK>(P, t, n0, g, rank > 0, scale, acc, tiles[i].base);
+      int token[kOuts];
+#pragma unroll
+      for (int n = 0; n < kOuts; ++n) token[n] = match >> ((col & (16 - kOuts)) + n) & 1 ? neighbour(i, n) : -1;
+      store_out<OK>(P, match >> col & 1 ? t : -1, token, n0, g, rank > 0, scale, acc, tiles[i].base);
     }
   }
 }
