@@ -302,7 +302,7 @@ cq_status cq_decode_dense(const cq_codebook_weights* W, int g, uint16_t* Wc_bf16
  * The operators that stand around the layer in a model.  Their rows may be fp32, f16 or bf16 (element kinds CQ_A_F32, CQ_A_F16,
  * CQ_A_BF16 as above; stored values are rounded to nearest, ties to even, without saturation), of any width, and need only the
  * alignment of their elements (rows that start on 16 bytes and are whole groups of eight values move 16 bytes at a time).
- * Sums are held in fp32 and added in an order that depends on the sizes alone.  T = 0 is allowed.
+ * Sums are held in fp32 and added in an order that depends on the sizes alone.  0 <= T <= 2^30.
  */
 
 /* the gate of a block: none, one value per token [T], or one per value [T, H]; of the block's kind */
@@ -353,7 +353,7 @@ cq_status cq_block_norm_grad(const cq_block_norm_spec* P, const void* h, const v
  *   token_mask [T] bytes or NULL: tokens whose byte is 0 (padding) are left out, whatever their logits hold.  A token all of whose
  *   logits are -inf counts, with probabilities of 0.
  *   Outputs: loss [1] f32, counts [n_seqs, E] i32, probs [n_seqs, E] f32 (P), tokens [n_seqs + 1] i32 (n_s, then S').
- *   E <= 1024, top_k <= min(E, 64).  workspace: cq_balance_loss_workspace_bytes(T, E, n_seqs) bytes,
+ *   E <= 1024, top_k <= min(E, 64), T top_k < 2^31.  workspace: cq_balance_loss_workspace_bytes(T, E, n_seqs) bytes,
  *   which never falls as T grows (few logits need none: 0, NULL allowed).
  */
 size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs);

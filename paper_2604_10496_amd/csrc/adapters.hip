@@ -19,8 +19,11 @@ namespace {
 
 constexpr int kMaxRank = 256;
 constexpr int kLeaderTokens = 1024;
+// Workgroups of a launch for single tokens, most of which end at once: they are started at about 250 per us (1024 tokens of 16 adapters,
+// K = N = 4096 at rank 32: 96.6 us with 8192 and 16384 workgroups, 55.4 with at most 4096).
+constexpr int kMostGroups = 4096;
 constexpr int kTile = 16;         // tokens of a matrix-core tile
-constexpr int kPromptTiles = 2;   // tiles that a wavefront of the second launch takes one after the other, of prompts
+constexpr int kPromptTiles = 2;   // tiles that a wavefront of the second launch takes, of prompts
 constexpr int kDownWaves = 4, kPromptDownWaves = 8, kFewWaves = 8, kUpWaves = 4;
 constexpr int kRankBlock = 64;                // rows of A per workgroup
 
@@ -31,6 +34,7 @@ struct adapter_args {
   void* out;
   float* low;   // [parts][tiles of 16 tokens][Rp], see low_at
   int n, R, Rp, K, N, T, tiles, parts, kpart;
+  int up_blocks;   // blocks of 256 outputs that a workgroup of the second launch takes, of single tokens
   size_t ldx, ldb, ldo;
 };
 
@@ -547,13 +551,14 @@ __device__ __forceinline__ void store_out(const adapter_args& P, int t, const in
 
 // Single tokens: up to 16 of one adapter per workgroup.  Bound by latency: base, low and the first 32 columns of B are asked for
 // together, the latter before the adapter's own rank is known and cleared beyond it (B's rows are short).
-template <int WK, int OK>
-__global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_args P) {
+// WIDE: several blocks of outputs per workgroup, one after the other.
+template <int WK, int OK, bool WIDE>
+__global__ __launch_bounds__(64 * kUpWaves, WIDE ? 3 : 4) void adapter_up_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), tile = blockIdx.x / blocks;
-  const int n0 = (((int)blockIdx.x - tile * blocks) * kUpWaves + wave) * 64;
-  if (n0 >= P.N) return;
+  const int up_blocks = WIDE ? P.up_blocks : 1, wide = 64 * kUpWaves * up_blocks, blocks = (P.N + wide - 1) / wide, tile = blockIdx.x / blocks;
+  const int first = ((int)blockIdx.x - tile * blocks) * wide + wave * 64;
+  if (first >= P.N) return;
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
   const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
@@ -561,36 +566,41 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void adapter_up_kernel(adapter_ar
   int token[kOuts];
 #pragma unroll
   for (int n = 0; n < kOuts; ++n) token[n] = __shfl(row, (col & (16 - kOuts)) + n);
-  out_pieces<OK> base;
-  base.fetch(P, token, n0, g);
   const int rank = rank_of(P, a);
   const float scale = a >= 0 && P.scale ? P.scale[a] : 1.f;
-  cq_v4f acc[4];
+#pragma unroll 1
+  for (int block = 0; block < up_blocks; ++block) {
+    const int n0 = first + block * 64 * kUpWaves;
+    if (n0 >= P.N) break;
+    out_pieces<OK> base;
+    base.fetch(P, token, n0, g);
+    cq_v4f acc[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-  for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
-    const int r = rb + g * 8, most = rb == 0 ? P.R : rank;
-    row8<WK> w[4];
-    fetch_up<WK, OK, true>(P, a, n0, col, r, most, w);
-    float v[8];
+    for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
+      const int r = rb + g * 8, most = rb == 0 ? P.R : rank;
+      row8<WK> w[4];
+      fetch_up<WK, OK, true>(P, a, n0, col, r, most, w);
+      float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (t >= 0 && r < most) {
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      if (t >= 0 && r < most) {
 #pragma unroll 4
-      for (int p = 0; p < P.parts; ++p) {
-        float u[8];
-        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, p, t, r), 0, true), u);
+        for (int p = 0; p < P.parts; ++p) {
+          float u[8];
+          row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, p, t, r), 0, true), u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += u[i];
+          for (int i = 0; i < 8; ++i) v[i] += u[i];
+        }
       }
+      if (rank < rb + 32) {
+        keep_rank(r, rank, v);
+        keep_rank<WK>(r, rank, w);
+      }
+      up_product<WK>(w, v, acc);
     }
-    if (rank < rb + 32) {
-      keep_rank(r, rank, v);
-      keep_rank<WK>(r, rank, w);
-    }
-    up_product<WK>(w, v, acc);
+    store_out<OK>(P, t, token, n0, g, rank > 0, scale, acc, base);
   }
-  store_out<OK>(P, t, token, n0, g, rank > 0, scale, acc, base);
 }
 
 // Few tokens of low rank in one launch: every workgroup of 512 outputs takes the whole of A_a x_t for itself, so that nothing
@@ -650,13 +660,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
   store_out<OK>(P, t, token, n0, g, rank > 0, scale, out, base);
 }
 
-// Prompts: four tiles of 16 neighbouring tokens one after the other, the next one's base and low in flight while this one is worked
-// on; the adapter's first 32 NB columns of B stay in registers from tile to tile.  Bound by HBM (base in, out written).
+// Prompts: two tiles of 16 neighbouring tokens, whose base and low are asked for before the ids are known; the adapter's first 32 NB
+// columns of B stay in registers from tile to tile.  Bound by HBM (base in, out written).
 // Outputs first, tokens second: workgroups that run together write whole rows, and where there is a multiple of 8 blocks of outputs
 // an XCD meets the same rows of B again and again.
 // ANY: ranks beyond 32 NB, below 8, or that are no multiple of 8.
 template <int WK, int OK, int NB, bool ANY>
-__global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && (WK == CQ_A_F32 || OK == CQ_A_F32)) ? 2 : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32 ? 4 : 3) void adapter_up_prompt_kernel(adapter_args P) {
+__global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && (WK == CQ_A_F32 || OK == CQ_A_F32)) ? 2
+                                            : NB == 1 && WK != CQ_A_F32 && OK != CQ_A_F32          ? 4
+                                                                                                   : 3)
+void adapter_up_prompt_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int blocks = (P.N + 64 * kUpWaves - 1) / (64 * kUpWaves), chunk = blockIdx.x / blocks;
@@ -737,7 +750,7 @@ __global__ __launch_bounds__(64 * kUpWaves, ANY || (NB == 2 && (WK == CQ_A_F32 |
 
 cq_status check_adapters(const cq_adapters* W, int T) {
   if (!W) return CQ_ERR_NULL;
-  if (T < 0 || W->n <= 0 || W->rank <= 0 || W->rank > kMaxRank || W->K <= 0 || W->N <= 0) return CQ_ERR_SHAPE;
+  if (T < 0 || T > 1 << 30 || W->n <= 0 || W->rank <= 0 || W->rank > kMaxRank || W->K <= 0 || W->N <= 0) return CQ_ERR_SHAPE;
   if (W->K > 1 << 23 || W->N > 1 << 23) return CQ_ERR_SHAPE;
   if (!cq_row_kind(W->kind)) return CQ_ERR_UNSUPPORTED;
   return CQ_OK;
@@ -762,6 +775,7 @@ down_plan plan_of(int T, int K) {
   int parts = 512 / tiles;
   if (parts > n) parts = n;
   if (parts > 16) parts = 16;
+  if ((long)parts * T > kMostGroups) parts = kMostGroups / T;
   d.kpart = (n + parts - 1) / parts * 128 * kDownWaves * d.units;
   d.parts = (K + d.kpart - 1) / d.kpart;
   return d;
@@ -856,9 +870,11 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   }
   const dim3 down(leaders ? T : ((T + kTile - 1) / kTile + 7) / 8 * 8, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
   const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
+  P.up_blocks = leaders ? (int)((blocks * T + kMostGroups - 1) / kMostGroups) : 1;
   const long up_tiles = leaders ? T : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
-  if (up_tiles * blocks > 0x7fffffffL) return CQ_ERR_SHAPE;
-  const dim3 up((unsigned)(up_tiles * blocks));
+  const long up_groups = up_tiles * ((blocks + P.up_blocks - 1) / P.up_blocks);
+  if (up_groups > 0x7fffffffL) return CQ_ERR_SHAPE;
+  const dim3 up((unsigned)up_groups);
 #define DOWN3(XK, WK, RT, UNITS, WAVES) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, UNITS, WAVES>), down, dim3(64 * WAVES), 0, s, P)
 #define DOWN2(XK, WK, RT)                                                              \
   do {                                                                                 \
@@ -880,10 +896,12 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
     else if (x_kind == CQ_A_F16) DOWN1(CQ_A_F16, WK); \
     else DOWN1(CQ_A_BF16, WK);                        \
   } while (0)
+#define UP_SINGLE(WK, OK, WIDE) hipLaunchKernelGGL((adapter_up_kernel<WK, OK, WIDE>), up, dim3(64 * kUpWaves), 0, s, P)
 #define UP_PROMPT(WK, OK, NB, ANY) hipLaunchKernelGGL((adapter_up_prompt_kernel<WK, OK, NB, ANY>), up, dim3(64 * kUpWaves), 0, s, P)
 #define UP2(WK, OK)                                                                                                     \
   do {                                                                                                                  \
-    if (leaders) hipLaunchKernelGGL((adapter_up_kernel<WK, OK>), up, dim3(64 * kUpWaves), 0, s, P);                     \
+    if (leaders && P.up_blocks > 1) UP_SINGLE(WK, OK, true);                                                            \
+    else if (leaders) UP_SINGLE(WK, OK, false);                                                                         \
     else if (W->rank % 8 != 0 || W->rank > 64) UP_PROMPT(WK, OK, 1, true);                                                   \
     else if (W->rank <= 32) UP_PROMPT(WK, OK, 1, false);                                                                \
     else UP_PROMPT(WK, OK, 2, false);                                                                                   \

@@ -482,7 +482,8 @@ __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const
 }
 
 cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, int E, int k) {
-  if (T < 0 || E <= 0 || E > kMaxExperts || k <= 0 || k > E || k > 64 || S <= 0) return CQ_ERR_SHAPE;
+  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || k <= 0 || k > E || k > 64 || S <= 0) return CQ_ERR_SHAPE;
+  if ((long)T * k > 0x7fffffffL) return CQ_ERR_SHAPE;   // (counts are 32-bit)
   if (!offsets && S != 1) return CQ_ERR_NULL;
   if (!cq_row_kind(logit_kind)) return CQ_ERR_UNSUPPORTED;
   return CQ_OK;
@@ -490,7 +491,7 @@ cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, in
 
 // Tokens per workgroup.  One round of loads, about 4096 logits, where that makes no more than kMostTiles tiles; longer batches take
 // as many tokens as make kMostTiles, so that the second launch has no more to add.
-constexpr int kMostTiles = 512;
+constexpr int kMostTiles = 2048;
 constexpr int kMostExpertsInRound = 256;
 
 int round_tokens(int E) {
@@ -532,7 +533,7 @@ bool in_one(int T, int E, int S) { return (long)T * E <= 32768 && S <= 4 && E <=
 }  // namespace
 
 extern "C" size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs) {
-  if (T < 0 || E <= 0 || E > kMaxExperts || n_seqs <= 0 || in_one(T, E, n_seqs)) return 0;
+  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || n_seqs <= 0 || in_one(T, E, n_seqs)) return 0;
   const size_t slots = slots_of(T, n_seqs);
   return 2 * cq_align_up(slots * E * 4, 256) + cq_align_up(slots * 4, 256) + cq_align_up((size_t)n_seqs * ((E + 31) / 32) * 4, 256) + 256;
 }

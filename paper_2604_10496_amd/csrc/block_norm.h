@@ -18,7 +18,7 @@ struct norm_args {
 
 inline cq_status check_norm_spec(const cq_block_norm_spec* P, int T) {
   if (!P) return CQ_ERR_NULL;
-  if (T < 0 || P->H <= 0 || P->H > kMaxNormWidth || !(P->eps > 0.f) || !isfinite(P->eps)) return CQ_ERR_SHAPE;
+  if (T < 0 || T > 1 << 30 || P->H <= 0 || P->H > kMaxNormWidth || !(P->eps > 0.f) || !isfinite(P->eps)) return CQ_ERR_SHAPE;
   if (!cq_row_kind(P->stream_kind)) return CQ_ERR_UNSUPPORTED;
   if (P->block_kind != P->stream_kind && P->block_kind != CQ_A_F32) return CQ_ERR_UNSUPPORTED;
   if (P->weight_kind != P->stream_kind && P->weight_kind != CQ_A_F32) return CQ_ERR_UNSUPPORTED;

@@ -54,8 +54,15 @@ __device__ __forceinline__ void fetch_row(const norm_grad_args& G, int t, grad_r
 template <int SK, int BK, int NT, int C, bool ELEM>
 __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_args G) {
   constexpr int kGroups = kThreads / NT;
-  // rows of 32 bits and several groups of eight leave no registers for the next row
-  constexpr bool kAhead = C == 1 && SK != CQ_A_F32 && BK != CQ_A_F32;
+  // rows of 32 bits, of several groups of eight, and the widest of one group with a gate per value leave no registers for the next row
+  constexpr bool kAhead = C == 1 && SK != CQ_A_F32 && BK != CQ_A_F32 && !(ELEM && NT == 1024);
+  // Rows of several groups of eight are read again where they are used again (out of the caches) instead of held.  again(): the
+  // compiler takes the pointer as a new one, so that it does not hold them, or the weights from row to row, after all.
+  constexpr bool kHold = C == 1;
+  auto again = [](const void* p) {
+    asm volatile("" : "+s"(p));
+    return p;
+  };
   const norm_args& P = G.f;
   const int H = P.H;
   // (two sets, used by rows in turn: a row's sums are read while the next row's may be written already)
@@ -71,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else {
-      slot_weights<SK>(w, P.wf32, slot(j), H, v);
+      slot_weights<SK>(again(w), P.wf32, slot(j), H, v);
     }
   };
   if constexpr (C == 1) {
@@ -103,22 +110,37 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
     if constexpr (kAhead) {
       R = next;
       if (first + kGroups * G.parts < P.T) fetch_row<SK, BK, NT, C, ELEM>(G, t + kGroups * G.parts, next);
-    } else {
+    } else if constexpr (kHold) {
       fetch_row<SK, BK, NT, C, ELEM>(G, t, R);
+    } else {
+      R.z = P.gate_kind == CQ_GATE_ROW && t < P.T ? elem_load<BK>(P.gate, t) : 1.f;
     }
     const bool in = t < P.T;
     const size_t row = (size_t)t * H;
     float d[C][8];   // gradient that reaches h'
 #pragma unroll
-    for (int j = 0; j < C; ++j) slot_values<SK>(R.dh[j], slot(j), H, d[j]);
+    for (int j = 0; j < C; ++j) {
+      if constexpr (kHold)
+        slot_values<SK>(R.dh[j], slot(j), H, d[j]);
+      else
+        slot_values<SK>(slot_fetch<SK>(G.dh_out, row, slot(j), H, in && G.dh_out), slot(j), H, d[j]);
+    }
+    auto stream_of = [&](int j, float (&h)[8], float (&dx)[8]) {
+      if constexpr (kHold) {
+        slot_values<SK>(R.h[j], slot(j), H, h);
+        slot_values<BK>(R.dx[j], slot(j), H, dx);
+      } else {
+        slot_values<SK>(slot_fetch<SK>(again(P.h), row, slot(j), H, in), slot(j), H, h);
+        slot_values<BK>(slot_fetch<BK>(again(G.dx), row, slot(j), H, in), slot(j), H, dx);
+      }
+    };
     if (G.dx) {
       float s[2] = {0.f, 0.f};   // h'^2, dx w h'
 #pragma unroll
       for (int j = 0; j < C; ++j) {
         float w[8], h[8], dx[8];
         weights(P.w_pre, 0, j, w);
-        slot_values<SK>(R.h[j], slot(j), H, h);
-        slot_values<BK>(R.dx[j], slot(j), H, dx);
+        stream_of(j, h, dx);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           s[0] = fmaf(h[i], h[i], s[0]);
@@ -130,12 +152,13 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
       const float back = r * r * s[1] * inv_H;   // D = dh' + r (dn - h' r^2 mean(dn h'))
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        forget_values(R.h[j]);
-        forget_values(R.dx[j]);
+        if constexpr (kHold) {
+          forget_values(R.h[j]);
+          forget_values(R.dx[j]);
+        }
         float w[8], h[8], dx[8];
         weights(P.w_pre, 0, j, w);
-        slot_values<SK>(R.h[j], slot(j), H, h);
-        slot_values<BK>(R.dx[j], slot(j), H, dx);
+        stream_of(j, h, dx);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           d[j][i] = fmaf(r, fmaf(-back, h[i], dx[i] * w[i]), d[j][i]);
@@ -155,7 +178,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
     const float ga = P.gate_kind == CQ_GATE_ROW && P.sigmoid ? sigmoid_of(R.z) : R.z;
     // y, u's weight and the gate of eight values
     auto factors = [&](int j, float (&y)[8], float (&w)[8], float (&a)[8]) {
-      slot_values<BK>(R.y[j], slot(j), H, y);
+      if constexpr (kHold)
+        slot_values<BK>(R.y[j], slot(j), H, y);
+      else
+        slot_values<BK>(slot_fetch<BK>(again(P.y), row, slot(j), H, in), slot(j), H, y);
       if (C == 1 || P.w_post) {
         weights(P.w_post, 1, j, w);
       } else {
@@ -163,7 +189,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
         for (int i = 0; i < 8; ++i) w[i] = 1.f;
       }
       if constexpr (ELEM) {
-        row_values<BK>(R.gate[j], a);
+        if constexpr (kHold)
+          row_values<BK>(R.gate[j], a);
+        else
+          row_values<BK>(slot_fetch<BK>(again(P.gate), row, slot(j), H, in), a);
         if (P.sigmoid) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) a[i] = sigmoid_of(a[i]);
@@ -202,8 +231,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
     }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      forget_values(R.y[j]);
-      if constexpr (ELEM) forget_values(R.gate[j]);
+      if constexpr (kHold) {
+        forget_values(R.y[j]);
+        if constexpr (ELEM) forget_values(R.gate[j]);
+      }
       float y[8], w[8], a[8], v[8];
       factors(j, y, w, a);
       if (ELEM && G.dgate) {

@@ -138,7 +138,15 @@ __device__ __forceinline__ row8<KIND> fetch8(const void* p, size_t at, uint32_t 
 template <int KIND>
 __device__ __forceinline__ row8<KIND> slot_fetch(const void* p, size_t row, const row_slot& s, int H, bool wanted) {
   if (H < 8) return row_fetch<KIND>(p, row, s.on && wanted ? H : 0);
-  return fetch8<KIND>(p, row, (uint32_t)s.c, s.on && wanted);
+  row8<KIND> r;
+#pragma unroll
+  for (int n = 0; n < row8<KIND>::N; ++n) r.w[n] = cq_v4u{0u, 0u, 0u, 0u};
+  if (s.on && wanted) {
+    const cq_v4u_any* q = reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(p) + (row + s.c) * (KIND == CQ_A_F32 ? 4 : 2));
+#pragma unroll
+    for (int n = 0; n < row8<KIND>::N; ++n) r.w[n] = q[n];
+  }
+  return r;
 }
 
 // raw values from .. to-1 of eight, the others as zero

@@ -566,3 +566,50 @@ def test_binding_refuses_what_the_kernels_cannot_take(B):
                 lambda: B.cq_adapter_apply(ad, X[:1].expand(3, 16), aid)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_rows_beyond_32_bit_offsets(B):
+    """More than 2^31 values: the rows at the end equal those of a call on them alone."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    T, H, n = 70000, 32768, 3
+    w = torch.rand(H, generator=g, device="cuda") + 0.5
+    norm = B.BlockNorm(w, w, block_dtype=torch.bfloat16)
+    h = torch.ones((T, H), dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn((n, H), generator=g, device="cuda").bfloat16()
+    h[T - n:] = tail
+    print("norm", flush=True)
+    out = B.cq_block_norm(norm, h, h)
+    want = B.cq_block_norm(norm, tail, tail)
+    assert out["h"][T - n:].equal(want["h"]) and out["x"][T - n:].equal(want["x"])
+    got = B.cq_block_norm_grad(norm, h, h, dh=h, dx=h, want_weights=False)
+    want = B.cq_block_norm_grad(norm, tail, tail, dh=tail, dx=tail, want_weights=False)
+    assert got["dh"][T - n:].equal(want["dh"]) and got["dy"][T - n:].equal(want["dy"])
+    del out, got, h
+    print("balance", flush=True)
+    T, E = 2200000, 1024
+    z = torch.zeros((T, E), dtype=torch.float16, device="cuda")
+    z[T - n:] = torch.randn((n, E), generator=g, device="cuda").half()
+    ids = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    ids[T - n:, 0] = torch.arange(n, device="cuda")
+    off = torch.tensor([0, T - n, T], dtype=torch.int32, device="cuda")
+    bal = B.cq_balance_loss(z, ids, 1.0, off)
+    alone = B.cq_balance_loss(z[T - n:].clone(), ids[T - n:].clone(), 1.0)
+    assert bal["counts"][1].equal(alone["counts"][0]) and bal["tokens"].tolist() == [T - n, n, 2]
+    assert (bal["probs"][1] - alone["probs"][0]).abs().max() <= 200 * U * alone["probs"].max()
+    one = torch.tensor([T - n, n, 1], dtype=torch.int32, device="cuda")
+    grad = B.cq_balance_loss_grad(z, bal["counts"], one, 1, 1.0, off)
+    assert grad[T - n:].equal(B.cq_balance_loss_grad(z[T - n:].clone(), alone["counts"], alone["tokens"], 1, 1.0))
+    del z, grad, ids
+    print("adapters", flush=True)
+    T, K = 1100, 1 << 21
+    X = torch.ones((T, K), dtype=torch.bfloat16, device="cuda")
+    X[T - n:] = torch.randn((n, K), generator=g, device="cuda").bfloat16()
+    A = (torch.randn((2, 8, K), generator=g, device="cuda") * K ** -0.5).bfloat16()
+    Bm = torch.randn((2, 64, 8), generator=g, device="cuda").bfloat16()
+    ad = B.DeviceAdapters(A, Bm)
+    ids = torch.ones(T, dtype=torch.int32, device="cuda")
+    got = B.cq_adapter_apply(ad, X, ids)[T - n:].double()
+    low = X[T - n:].double() @ A[1].double().t()
+    mag = X[T - n:].double().abs() @ A[1].double().abs().t() @ Bm[1].double().abs().t()
+    assert ((got - low @ Bm[1].double().t()).abs() <= _adapter_roundings(K, 8) * U * mag).all()

@@ -96,7 +96,7 @@ def test_block_norm_refusals():
     assert lib.cq_block_norm(None, ONE, ONE, None, 4, ONE, ONE, None) == 1
     assert call(h=None) == 1 and call(h_out=None) == 1 and call(y=None, x_out=None) == 1 and call(w_pre=None) == 1
     assert call(gate_kind=1) == 1 and call(gate_kind=2) == 1
-    assert call(T=-1) == 2 and call(H=0) == 2 and call(H=32769) == 2
+    assert call(T=-1) == 2 and call(T=(1 << 30) + 1) == 2 and call(H=0) == 2 and call(H=32769) == 2
     assert call(eps=0.0) == 2 and call(eps=-1.0) == 2 and call(eps=float("nan")) == 2 and call(eps=float("inf")) == 2
     assert call(stream_kind=0) == 3 and call(stream_kind=9) == 3 and call(block_kind=F16) == 3 and call(weight_kind=F16) == 3
     assert call(stream_kind=F32, block_kind=BF16) == 3 and call(gate_kind=3) == 3
@@ -130,7 +130,7 @@ def test_balance_refusals():
     for name in ("z", "ids", "off", "loss", "counts", "probs", "tokens"):
         assert call(**{name: None}) == 1, name
     assert call(T=-1) == 2 and call(E=0) == 2 and call(E=1025) == 2 and call(k=0) == 2 and call(k=17) == 2 and call(S=0) == 2
-    assert call(E=100, k=65) == 2
+    assert call(E=100, k=65) == 2 and call(T=(1 << 30) + 1, k=1) == 2 and call(T=1 << 30, k=2) == 2
     assert call(kind=0) == 3 and call(kind=4) == 3
     need = lib.cq_balance_loss_workspace_bytes(4096, 16, 3)
     assert need > 0 and call(T=4096, n=need - 1) == 4 and call(T=4096, ws=None) == 4
@@ -158,7 +158,7 @@ def test_adapter_refusals():
         return lib.cq_adapter_apply(ctypes.byref(_adapters(**k)), X, xk, ldx, ids, T, base, ldb, out, ok, ldo, ws, n, None)
     assert lib.cq_adapter_apply(None, ONE, F32, 64, ONE, 5, ONE, 32, ONE, F32, 32, ONE, 1 << 30, None) == 1
     assert call(X=None) == 1 and call(ids=None) == 1 and call(out=None) == 1 and call(A=None) == 1 and call(B=None) == 1
-    assert call(T=-1) == 2
+    assert call(T=-1) == 2 and call(T=(1 << 30) + 1) == 2
     for k in (dict(rank=0), dict(rank=257), dict(K=0), dict(N=0)):
         assert call(**k) == 2, k
     assert lib.cq_adapter_apply(ctypes.byref(_adapters(n=0)), ONE, F32, 64, ONE, 5, ONE, 32, ONE, F32, 32, ONE, 1 << 30, None) == 2
