@@ -8,6 +8,7 @@
 // pair to the next in order either the tile or the sequence grows by one at least, so the slots differ, and a second launch
 // adds every sequence's slots in a fixed order; its last workgroup adds the sequences' losses.  Counts are integers added in LDS;
 // no atomics on floats.  Few logits take one workgroup and one launch.
+// 8192 x 64 in 13 sequences 7.5 + 6.2 us (2.3 MB: latency), 64 x 4 5.8 us; the gradient of 65536 x 128 18.4 us for 67 MB = 3.6 TB/s.
 #include <math.h>
 
 #include "cq_rows.h"

@@ -8,6 +8,9 @@
 // a time and asks for the next ones before it works on these, so that loads are in flight across the two barriers of a row sum.
 // The shares of the weights' gradients stay in registers, are added over a workgroup's rows in LDS and go to the workspace
 // once, [parts][H] each; a second launch adds the parts in order.  No atomics: the results do not depend on timing.
+// 8192 x 4096 in bf16 with a gate per value, 537 MB: 107 us = 5.0 TB/s, and 5.0 us for the sum of the parts; without the next rows in
+// flight, one row per workgroup of 512 threads, 141 us.  2048 x 2048: 18.9 and 3.9 us, two rounds of rows, in which the first
+// loads, the weights and the shares at the end weigh as much as the rows.
 #include "block_norm.h"
 
 namespace {
