@@ -21,9 +21,12 @@
 namespace {
 
 constexpr int kMaxRank = 256;
-constexpr int kLeaderTokens = 1024;
-// Workgroups of a launch for single tokens, most of which end at once: they are started at about 250 per us (1024 tokens of 16 adapters,
-// K = N = 4096 at rank 32: 96.6 us with 8192 and 16384 workgroups, 55.4 with at most 4096).
+// Both ways at K = N = 4096, rank 32 (us; 8 adapters in order / in turn, 32 adapters in order / in turn): 257 tokens singly 20 / 22, 22 / 20,
+// as prompts 21 / 72, 31 / 143; 400 tokens 27 / 31, 31 / 25 and 21 / 73, 30 / 142; 512 tokens 36 / 37, 37 / 31 and 14 / 74, 16 / 143.  Decode
+// batches stay below, the usual pieces of prompts above.
+constexpr int kLeaderTokens = 384;
+// Workgroups of a launch for single tokens, most of which end at once: they are started at about 250 per us (1024 tokens of 16 adapters
+// taken singly: 96.6 us with 8192 and 16384 workgroups, 55.4 with at most 4096).
 constexpr int kMostGroups = 4096;
 constexpr int kTile = 16;         // tokens of a matrix-core tile
 constexpr int kPromptTiles = 2;   // tiles that a wavefront of the second launch takes, of prompts
@@ -53,6 +56,13 @@ __device__ __forceinline__ int adapter_of(const adapter_args& P, int t) {
   return a >= 0 && a < P.n ? a : -1;
 }
 
+// The tile of a group of workgroups.  Single tokens: which ones have work depends on the ids (every 16th where neighbours share an
+// adapter, the first ones where they take turns); workgroups go to the eight XCDs in turn, and either pattern is spread over them.
+// (1024 tokens in order, taken singly: 97 us where every 16th workgroup is on the same XCD, 55 spread.)
+__device__ __forceinline__ int tile_of_group(const adapter_args& P, int group) {
+  return P.T > kLeaderTokens ? group : group ^ (group >> 4 & 7);
+}
+
 // The tokens of a tile: lane i < TILE gets the i-th one's row (-1: none) and adapter.  Every wavefront finds them by itself, the
 // same ones.  False: another tile has them.
 template <int TILE>
@@ -65,6 +75,7 @@ __device__ __forceinline__ bool find_rows(const adapter_args& P, int tile, int& 
     id = in ? adapter_of(P, t) : -1;
     return true;
   }
+  if (tile >= P.T) return false;
   const int me = tile, mine = adapter_of(P, me);
   int before = 0, n = 0;
   row = -1;
@@ -331,7 +342,7 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(adapter_args P
   const int k_first = blockIdx.y * P.kpart, k_end = min(P.K, k_first + P.kpart);
   const int rounds = (k_end - k_first) / kRound;
   // Workgroups go to the eight XCDs in turn.  Prompts: an XCD takes neighbouring tiles, which share an adapter in its L2.
-  int tile = blockIdx.x;
+  int tile = tile_of_group(P, blockIdx.x);
   if (P.T > kLeaderTokens) {
     const int each = gridDim.x / 8;   // (the grid is a multiple of 8 then)
     tile = blockIdx.x % 8 * each + blockIdx.x / 8;
@@ -559,8 +570,8 @@ template <int WK, int OK, bool WIDE>
 __global__ __launch_bounds__(64 * kUpWaves, WIDE ? 3 : 4) void adapter_up_kernel(adapter_args P) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int up_blocks = WIDE ? P.up_blocks : 1, wide = 64 * kUpWaves * up_blocks, blocks = (P.N + wide - 1) / wide, tile = blockIdx.x / blocks;
-  const int first = ((int)blockIdx.x - tile * blocks) * wide + wave * 64;
+  const int up_blocks = WIDE ? P.up_blocks : 1, wide = 64 * kUpWaves * up_blocks, blocks = (P.N + wide - 1) / wide, group = blockIdx.x / blocks;
+  const int tile = tile_of_group(P, group), first = ((int)blockIdx.x - group * blocks) * wide + wave * 64;
   if (first >= P.N) return;
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
@@ -615,8 +626,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
   __shared__ float lds[kFewWaves][16][LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int blocks = (P.N + 64 * kFewWaves - 1) / (64 * kFewWaves), tile = blockIdx.x / blocks;
-  const int n0 = (((int)blockIdx.x - tile * blocks) * kFewWaves + wave) * 64;
+  const int blocks = (P.N + 64 * kFewWaves - 1) / (64 * kFewWaves), group = blockIdx.x / blocks;
+  const int tile = tile_of_group(P, group), n0 = (((int)blockIdx.x - group * blocks) * kFewWaves + wave) * 64;
   int row, id;
   if (!find_rows<kTile>(P, tile, row, id)) return;
   const int t = __shfl(row, col), a = __builtin_amdgcn_readlane(id, 0);
@@ -847,7 +858,7 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   hipStream_t s = (hipStream_t)stream;
   const bool leaders = T <= kLeaderTokens;
   if (takes_few(W, x_kind, T)) {
-    const dim3 few((unsigned)(T * (((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves))));
+    const dim3 few((unsigned)((T + 7) / 8 * 8 * (((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves))));
 #define FEW3(XK, WK, OK, RT) hipLaunchKernelGGL((adapter_few_kernel<XK, WK, OK, RT>), few, dim3(64 * kFewWaves), 0, s, P)
 #define FEW2(XK, WK, OK)                     \
   do {                                       \
@@ -871,10 +882,11 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
     else FEW(CQ_A_BF16);
     return cq_check_launch();
   }
-  const dim3 down(leaders ? T : ((T + kTile - 1) / kTile + 7) / 8 * 8, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
+  const int singles = (T + 7) / 8 * 8;   // (tile_of_group stays within eight)
+  const dim3 down(leaders ? singles : ((T + kTile - 1) / kTile + 7) / 8 * 8, P.parts, (W->rank + kRankBlock - 1) / kRankBlock);
   const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
   P.up_blocks = leaders ? (int)((blocks * T + kMostGroups - 1) / kMostGroups) : 1;
-  const long up_tiles = leaders ? T : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
+  const long up_tiles = leaders ? singles : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
   const long up_groups = up_tiles * ((blocks + P.up_blocks - 1) / P.up_blocks);
   if (up_groups > 0x7fffffffL) return CQ_ERR_SHAPE;
   const dim3 up((unsigned)up_groups);

@@ -490,10 +490,12 @@ cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, in
   return CQ_OK;
 }
 
-// Tokens per workgroup.  One round of loads, about 4096 logits, where that makes no more than kMostTiles tiles; longer batches take
-// as many tokens as make kMostTiles, so that the second launch has no more to add.
-constexpr int kMostTiles = 2048;
+// Tokens per workgroup.  One round of loads, about 4096 logits, where that makes no more tiles than the second launch, whose workgroups
+// share out the sequences, adds quickly: 512 per sequence (65536 x 128 in one sequence 21.8 us, with 2048 tiles 27.3; 60000 x 100 in
+// 64 sequences 36.1, with 1875 tiles 27.9).  Longer batches take as many tokens as make that many tiles.
 constexpr int kMostExpertsInRound = 256;
+
+long most_tiles(int S) { return 512 * (S < 4 ? S : 4); }
 
 int round_tokens(int E) {
   int lanes = 1;
@@ -501,17 +503,19 @@ int round_tokens(int E) {
   return 4 * (256 / lanes);
 }
 
-bool in_rounds(int T, int E) { return E <= kMostExpertsInRound && ((long)T + round_tokens(E) - 1) / round_tokens(E) <= kMostTiles; }
+bool in_rounds(int T, int E, int S) { return E <= kMostExpertsInRound && ((long)T + round_tokens(E) - 1) / round_tokens(E) <= most_tiles(S); }
 
-int tile_of(int T, int E) {
-  if (in_rounds(T, E)) return round_tokens(E);
-  const int tile = (int)(((long)T + kMostTiles - 1) / kMostTiles);
+int tile_of(int T, int E, int S) {
+  if (in_rounds(T, E, S)) return round_tokens(E);
+  const int tile = (int)((T + most_tiles(S) - 1) / most_tiles(S));
   return tile < 16 ? 16 : tile;
 }
 
-size_t slots_of(int T, int S) { return (size_t)(T < kMostTiles ? T : kMostTiles) + 1 + S; }   // (never falls as T grows)
+size_t slots_of(int T, int S) { return (size_t)(T < most_tiles(S) ? T : most_tiles(S)) + 1 + S; }   // (never falls as T grows)
 
-bool in_one(int T, int E, int S) { return (long)T * E <= 32768 && S <= 4 && E <= 256; }
+// One workgroup and one launch: 64 x 4 6.2 us (two launches 8.7), 256 x 64 6.2 (10.2), 512 x 64 9.1 (10.2), 1024 x 64 15.0 (10.5); 512 x 64
+// in four sequences, one after the other, 18.6 (10.5).
+bool in_one(int T, int E, int S) { return (long)T * E * S <= 32768 && S <= 2 && E <= 256; }
 
 #define CQ_BALANCE_WIDTHS(LAUNCH, KIND, E)      \
   do {                                          \
@@ -549,7 +553,7 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   const size_t need = cq_balance_loss_workspace_bytes(T, E, n_seqs);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T, E), alpha};
+  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T, E, n_seqs), alpha};
   const size_t slots = slots_of(T, n_seqs);
   balance_ws W;
   char* at = (char*)workspace;
@@ -573,7 +577,7 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
     return cq_check_launch();
   }
   const int tiles = T > 0 ? (T - 1) / P.tile + 1 : 1;
-  const bool rounds = in_rounds(T, E);
+  const bool rounds = in_rounds(T, E, n_seqs);
 #define LAUNCH(KIND, L, C)                                                                                             \
   do {                                                                                                                 \
     if (C == 1 && rounds) hipLaunchKernelGGL((balance_tile_kernel<KIND, L>), dim3(tiles), dim3(256), 0, s, P, W);      \

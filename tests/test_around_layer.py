@@ -400,7 +400,8 @@ def test_adapter_apply(B, T, K, N, R, n, x, w, o):
 
 
 @pytest.mark.parametrize("T,K,N,R,n", [(1040, 1152, 80, 24, 5), (1100, 2304, 64, 16, 3), (1030, 4224, 40, 40, 4), (1090, 1024, 130, 8, 2), (1026, 1000, 96, 70, 3),
-                                       (30, 4300, 96, 48, 9), (900, 1500, 64, 32, 4), (20, 4096, 600, 12, 20), (3, 2049, 1024, 32, 3)])
+                                       (30, 4300, 96, 48, 9), (900, 1500, 64, 32, 4), (20, 4096, 600, 12, 20), (3, 2049, 1024, 32, 3),
+                                       (384, 640, 1100, 16, 30), (385, 640, 1100, 16, 30), (383, 200, 2100, 40, 2)])
 @pytest.mark.parametrize("x,w,o", [("f32", "bf16", "f32"), ("bf16", "bf16", "bf16"), ("f16", "f16", "f16"), ("f32", "f32", "f32")])
 def test_adapter_widths_around_the_rounds_of_the_sum(B, T, K, N, R, n, x, w, o):
     """K of whole rounds, of rounds and units, of units and a rest; several adapters within a tile share the values of X."""
