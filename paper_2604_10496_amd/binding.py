@@ -613,7 +613,8 @@ class BlockNorm:
         if spec is None:
             spec = self._specs[key] = BlockNormSpec(
                 h.shape[1], _kind(h.dtype, "h"), self.block_kind, self.weight_kind, gate_kind, self.gate_sigmoid, self.eps,
-                self.residual_scale, self.branch_scale, _ptr(self.w_pre), _ptr(self.w_post))
+                self.residual_scale, self.branch_scale)
+        spec.w_pre, spec.w_post = _ptr(self.w_pre), _ptr(self.w_post)   # (the tensors may have been replaced)
         return spec
 
     def check(self, h, y, gate):
@@ -759,11 +760,13 @@ class DeviceAdapters:
         if ranks is not None:
             _tensor(ranks, "ranks", (self.n,), torch.int32)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
-        self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind, _ptr(A), _ptr(B), _ptr(scale), _ptr(ranks))
+        self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind)
         self._bytes: Dict[tuple, int] = {}
 
     def struct(self) -> Adapters:
-        return self._struct
+        s = self._struct                              # (the tensors may have been replaced)
+        s.A, s.B, s.scale, s.ranks = self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), _ptr(self.ranks)
+        return s
 
 
 def _rows(t, what: str, shape, dtype=None) -> int:

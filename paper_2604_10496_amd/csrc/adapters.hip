@@ -2,8 +2,8 @@
 //   out_t = base_t + scale_a B_a (A_a x_t),  a = ids[t];   a outside [0, n): out_t = base_t.
 //
 // Two launches of matrix-core tiles, low = A_a x (fp32, kept in K parts in the workspace) and out = base + scale B_a low; one launch
-// for few tokens of low rank.  They hold tokens as the columns and rows of A or B as the rows of a 16 x 16 result, so that a lane owns four neighbouring
-// rows of one token and stores them together.
+// for few tokens of low rank.  They hold tokens as the columns and rows of A or B as the rows of a 16 x 16 result, so that a lane
+// owns four neighbouring rows of one token and stores them together.
 //
 // Tokens meet their adapters in one of two ways.  Batches of up to kLeaderTokens tokens (decode steps, in any order): a
 // workgroup per token looks through the ids; the first of every 16 tokens of one adapter takes those tokens, the others'
@@ -123,9 +123,6 @@ __device__ __forceinline__ split_frag split_pack(const float (&v)[8]) {
   for (int p = 0; p < 3; ++p) f.part[p] = __builtin_bit_cast(cq_v8bf16, w[p]);
   return f;
 }
-
-// Eight consecutive 16-bit values as they are; the first `left` exist, the others are zero.
-__device__ __forceinline__ cq_v4u raw_load8(const void* p, size_t at, int left) { return row_fetch<CQ_A_BF16>(p, at, left).w[0]; }
 
 // How a pair of types is multiplied
 enum { kSame16 = 0, kSplit = 1, kFloat = 2 };

@@ -9,7 +9,6 @@ namespace {
 
 // element kinds are the activation kinds of cq.h: CQ_A_F16, CQ_A_F32, CQ_A_BF16
 inline bool cq_row_kind(int kind) { return kind == CQ_A_F16 || kind == CQ_A_F32 || kind == CQ_A_BF16; }
-inline int cq_row_bytes(int kind) { return kind == CQ_A_F32 ? 4 : 2; }
 
 template <int KIND>
 __device__ __forceinline__ float elem_load(const void* p, size_t at) {
@@ -73,11 +72,6 @@ __device__ __forceinline__ void row_values(const row8<KIND>& r, float (&v)[8]) {
         v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w & 0xffffu));
     }
   }
-}
-
-template <int KIND>
-__device__ __forceinline__ void row_load8(const void* p, size_t at, int left, float (&v)[8]) {
-  row_values<KIND>(row_fetch<KIND>(p, at, left), v);
 }
 
 template <int KIND>

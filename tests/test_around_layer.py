@@ -569,6 +569,22 @@ def test_binding_refuses_what_the_kernels_cannot_take(B):
             bad()
 
 
+def test_tensors_of_a_handle_may_be_replaced(B):
+    """A training step gives the norm and the adapters new tensors: the next call reads those."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(6)
+    h = torch.randn((5, 64), generator=g, device="cuda")
+    norm = B.BlockNorm(torch.ones(64, device="cuda"))
+    first = B.cq_block_norm(norm, h)["x"]
+    norm.w_pre = torch.full((64,), 2.0, device="cuda")
+    assert B.cq_block_norm(norm, h)["x"].equal(2 * first)
+    A, Bm = torch.randn((2, 4, 64), generator=g, device="cuda"), torch.randn((2, 32, 4), generator=g, device="cuda")
+    ad, ids = B.DeviceAdapters(A, Bm), torch.tensor([0, 1, 0, -1, 1], dtype=torch.int32, device="cuda")
+    first = B.cq_adapter_apply(ad, h, ids)
+    ad.B = 2 * Bm
+    assert B.cq_adapter_apply(ad, h, ids).equal(2 * first)
+
+
 def test_rows_beyond_32_bit_offsets(B):
     """More than 2^31 values: the rows at the end equal those of a call on them alone."""
     import torch
