@@ -14,8 +14,8 @@
 // into three bf16 values of 8 bits each, which hold every bit of the fp32 value: three products, each exact in fp32.  The other pairs of
 // types run on the fp32 matrix cores.  Either way A_a x and B_a low are fp32 sums of exact products.
 //
-// 4096 tokens of 9 prompts, K = N = 4096, rank 32, bf16: 18.4 + 18.1 us for 104 MB (2.9 TB/s); 64 requests with adapters of ranks 16 to
-// 64, K = 2048, N = 2816: 6.4 + 10.0 us for 22 MB; one token at rank 16: 4.9 + 6.6 us.
+// 4096 tokens of 9 prompts, K = N = 4096, rank 32, bf16: 19.0 + 18.4 us for 104 MB (2.8 TB/s); 64 requests with adapters of ranks 16 to
+// 64, K = 2048, N = 2816: 6.5 + 10.7 us for 22 MB; one token at rank 16: 4.2 + 7.0 us.
 #include "cq_rows.h"
 
 namespace {
