@@ -183,10 +183,16 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+_raw_stream_of = None
+
+
 def _raw_stream(t) -> int:
     """_stream() for a call on a tensor of the current device, without the Stream object (2.7 us less on the host)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    global _raw_stream_of
+    if _raw_stream_of is None:
+        import torch
+        _raw_stream_of = torch._C._cuda_getCurrentRawStream
+    return _raw_stream_of(t.device.index)
 
 
 def _ws(nbytes: int):
@@ -545,7 +551,6 @@ def cq_mfma_loop(workgroups: int, iters: int):
 # the operators around the layer
 # ------------------------------------------------------------------------------------------------
 _KINDS: Dict[object, int] = {}      # filled once torch is known
-_BYTES: Dict[tuple, int] = {}       # workspace sizes by the sizes that they are functions of
 
 
 def _kind(dtype, what: str) -> int:
@@ -675,9 +680,7 @@ def cq_block_norm_grad(norm: BlockNorm, h, y=None, gate=None, dh=None, dx=None, 
     s = norm.struct(h, gate)
     ws, nbytes = None, 0
     if dw_pre is not None or dw_post is not None:
-        nbytes = _BYTES.get(("norm", T, H))
-        if nbytes is None:
-            nbytes = _BYTES["norm", T, H] = lib.cq_block_norm_grad_workspace_bytes(s, T)
+        nbytes = lib.cq_block_norm_grad_workspace_bytes(s, T)
         ws = _scratch(h, nbytes)
     st = lib.cq_block_norm_grad(s, h.data_ptr(), _ptr(y), _ptr(gate), _ptr(dh), _ptr(dx), T, o_dh.data_ptr(), _ptr(dy), _ptr(dgate),
                                 _ptr(dw_pre), _ptr(dw_post), _ptr(ws), nbytes, _raw_stream(h))
@@ -715,9 +718,7 @@ def cq_balance_loss(logits, ids, alpha: float, seq_offsets=None, token_mask=None
     counts = ids.new_empty((S, E))
     probs = loss.new_empty((S, E))
     tokens = ids.new_empty(S + 1)
-    nbytes = _BYTES.get(("balance", T, E, S))
-    if nbytes is None:
-        nbytes = _BYTES["balance", T, E, S] = lib.cq_balance_loss_workspace_bytes(T, E, S)
+    nbytes = lib.cq_balance_loss_workspace_bytes(T, E, S)
     ws = _scratch(logits, nbytes) if nbytes else None
     st = lib.cq_balance_loss(logits.data_ptr(), kind, ids.data_ptr(), _ptr(seq_offsets), S, _ptr(token_mask), T, E, k, alpha,
                              loss.data_ptr(), counts.data_ptr(), probs.data_ptr(), tokens.data_ptr(), _ptr(ws), nbytes,
@@ -761,7 +762,6 @@ class DeviceAdapters:
             _tensor(ranks, "ranks", (self.n,), torch.int32)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
         self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind)
-        self._bytes: Dict[tuple, int] = {}
 
     def struct(self) -> Adapters:
         s = self._struct                              # (the tensors may have been replaced)
@@ -804,9 +804,7 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
         ldo = _rows(out, "out", (T, adapters.N))
     ldb = _rows(base, "base", (T, adapters.N), out.dtype) if base is not None else 0
     s = adapters.struct()
-    nbytes = adapters._bytes.get((x_kind, T))
-    if nbytes is None:
-        nbytes = adapters._bytes[x_kind, T] = lib.cq_adapter_workspace_bytes(s, x_kind, T)
+    nbytes = lib.cq_adapter_workspace_bytes(s, x_kind, T)
     ws = _scratch(X, nbytes) if nbytes else None
     st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),
                               _kind(out.dtype, "out"), ldo, _ptr(ws), nbytes, _raw_stream(X))
