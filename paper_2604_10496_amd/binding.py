@@ -590,7 +590,9 @@ class BlockNorm:
 
     w_pre [H]: weights of the norm in front of the next block (None: no such norm); w_post [H]: of the norm behind the block
     (None: its output is taken as it is).  block_dtype: type of the block's input, output and gate, float32 (what
-    cq_moe_forward takes and gives) or the residual stream's."""
+    cq_moe_forward takes and gives) or the residual stream's.
+    The weights may be replaced by others of their size and type, and the numbers changed: a call takes what is there, and looks at the
+    weights anew (a tensor's type, size and place may also change in the hands of its owner)."""
 
     def __init__(self, w_pre=None, w_post=None, eps: float = 1e-6, residual_scale: float = 1.0, branch_scale: float = 1.0,
                  gate_sigmoid: bool = False, block_dtype=None):
@@ -605,52 +607,51 @@ class BlockNorm:
                 _tensor(w, name, (self.H,), self.weight_dtype)
         self.w_pre, self.w_post = w_pre, w_post
         self.block_dtype = torch.float32 if block_dtype is None else block_dtype
-        self.weight_kind, self.block_kind = _kind(self.weight_dtype, "weights"), _kind(self.block_dtype, "block_dtype")
+        _kind(self.weight_dtype, "weights"), _kind(self.block_dtype, "block_dtype")
         self.eps, self.residual_scale, self.branch_scale = float(eps), float(residual_scale), float(branch_scale)
         self.gate_sigmoid = bool(gate_sigmoid)
 
-        self._specs: Dict[tuple, BlockNormSpec] = {}
-
-    def struct(self, h, gate=None) -> BlockNormSpec:
-        gate_kind = CQ_GATE_NONE if gate is None else CQ_GATE_ROW if gate.dim() == 1 else CQ_GATE_ELEM
-        key = (h.shape[1], h.dtype, gate_kind)
-        spec = self._specs.get(key)
-        if spec is None:
-            spec = self._specs[key] = BlockNormSpec(
-                h.shape[1], _kind(h.dtype, "h"), self.block_kind, self.weight_kind, gate_kind, self.gate_sigmoid, self.eps,
-                self.residual_scale, self.branch_scale)
-        spec.w_pre, spec.w_post = _ptr(self.w_pre), _ptr(self.w_post)   # (the tensors may have been replaced)
-        return spec
-
-    def check(self, h, y, gate):
-        _tensor(h, "h", (h.shape[0], self.H or h.shape[-1]) if h.dim() == 2 else (None, self.H))
-        if y is None:
+    def struct(self, h, y=None, gate=None) -> BlockNormSpec:
+        """Checks the weights and the arguments against each other; what a call hands to the library."""
+        shape = h.shape
+        if len(shape) != 2:
+            raise ValueError(f"h: shape {tuple(shape)} where {(None, self.H)} is needed")
+        T, H = shape
+        _tensor(h, "h", (T, self.H or H))
+        block = self.block_dtype
+        gate_kind = CQ_GATE_NONE
+        if y is not None:
+            _tensor(y, "y", shape, block)
             if gate is not None:
-                raise ValueError("gate: there is no block output that it could gate")
-            return
-        _tensor(y, "y", h.shape, self.block_dtype)
-        if gate is not None:
-            _tensor(gate, "gate", h.shape[:1] if gate.dim() == 1 else h.shape, self.block_dtype)
+                gate_kind = CQ_GATE_ROW if gate.dim() == 1 else CQ_GATE_ELEM
+                _tensor(gate, "gate", (T,) if gate_kind == CQ_GATE_ROW else shape, block)
+        elif gate is not None:
+            raise ValueError("gate: there is no block output that it could gate")
+        w_pre, w_post, weights = self.w_pre, self.w_post, self.weight_dtype
+        if w_pre is not None:
+            w_pre = _tensor(w_pre, "w_pre", (H,), weights).data_ptr()
+        if w_post is not None:
+            w_post = _tensor(w_post, "w_post", (H,), weights).data_ptr()
+        return BlockNormSpec(H, _kind(h.dtype, "h"), _kind(block, "block_dtype"), _kind(weights, "weights"), gate_kind, self.gate_sigmoid,
+                             self.eps, self.residual_scale, self.branch_scale, w_pre, w_post)
 
 
 def cq_block_norm(norm: BlockNorm, h, y=None, gate=None, h_out=None, x_out=None) -> Dict[str, object]:
     """h' = residual_scale h + branch_scale gate N(y) w_post and x = N(h') w_pre: {"h": h', "x": x or None}.
 
     y None: x = N(h) w_pre alone, and "h" is h itself."""
+    import torch
     lib = _lib or load_library()
-    norm.check(h, y, gate)
+    s = norm.struct(h, y, gate)
     if y is None:
         h_new = h
     else:
-        h_new = h.new_empty(h.shape) if h_out is None else _tensor(h_out, "h_out", h.shape, h.dtype)
+        h_new = torch.empty_like(h) if h_out is None else _tensor(h_out, "h_out", h.shape, h.dtype)
     x = None
-    if norm.w_pre is not None:
-        if x_out is not None:
-            x = _tensor(x_out, "x_out", h.shape, norm.block_dtype)
-        else:
-            x = h.new_empty(h.shape) if h.dtype == norm.block_dtype else h.new_empty(h.shape, dtype=norm.block_dtype)
-    st = lib.cq_block_norm(norm.struct(h, gate), h.data_ptr(), _ptr(y), _ptr(gate), h.shape[0],
-                           None if y is None else h_new.data_ptr(), _ptr(x), _raw_stream(h))
+    if s.w_pre is not None:
+        x = torch.empty_like(h, dtype=norm.block_dtype) if x_out is None else _tensor(x_out, "x_out", h.shape, norm.block_dtype)
+    st = lib.cq_block_norm(s, h.data_ptr(), _ptr(y), _ptr(gate), h.shape[0], None if y is None else h_new.data_ptr(), _ptr(x),
+                           _raw_stream(h))
     if st:
         raise CqError(st)
     return {"h": h_new, "x": x}
@@ -659,25 +660,25 @@ def cq_block_norm(norm: BlockNorm, h, y=None, gate=None, h_out=None, x_out=None)
 def cq_block_norm_grad(norm: BlockNorm, h, y=None, gate=None, dh=None, dx=None, want_weights: bool = True) -> Dict[str, object]:
     """Gradients of cq_block_norm from its h' (with y None: its h), y, gate and the gradients dh of h' and dx of x (None: zero):
     {"dh", "dw_pre", "dgate", "dw_post", "dy"}, None where there is no such input."""
+    import torch
     lib = _lib or load_library()
-    norm.check(h, y, gate)
+    s = norm.struct(h, y, gate)
     if dh is not None:
         _tensor(dh, "dh", h.shape, h.dtype)
     if dx is not None:
         if norm.w_pre is None:
             raise ValueError("dx: there is no norm in front of a next block")
         _tensor(dx, "dx", h.shape, norm.block_dtype)
-    T, H = h.shape
-    o_dh, dw_pre, dgate, dw_post, dy = h.new_empty(h.shape), None, None, None, None
+    T = h.shape[0]
+    o_dh, dw_pre, dgate, dw_post, dy = torch.empty_like(h), None, None, None, None
     if y is not None:
-        dy = y.new_empty(y.shape)
+        dy = torch.empty_like(y)
         if gate is not None:
-            dgate = gate.new_empty(gate.shape)
+            dgate = torch.empty_like(gate)
         if want_weights and norm.w_post is not None:
-            dw_post = norm.w_post.new_empty(H)
+            dw_post = torch.empty_like(norm.w_post)
     if want_weights and dx is not None:
-        dw_pre = norm.w_pre.new_empty(H)
-    s = norm.struct(h, gate)
+        dw_pre = torch.empty_like(norm.w_pre)
     ws, nbytes = None, 0
     if dw_pre is not None or dw_post is not None:
         nbytes = lib.cq_block_norm_grad_workspace_bytes(s, T)
@@ -747,26 +748,33 @@ def cq_balance_loss_grad(logits, counts, tokens, top_k: int, alpha: float, seq_o
 
 
 class DeviceAdapters:
-    """Low-rank adapters on the device: A [n, rank, K], B [n, N, rank], scale [n] f32 or None, ranks [n] i32 or None."""
+    """Low-rank adapters on the device: A [n, rank, K], B [n, N, rank], scale [n] f32 or None, ranks [n] i32 or None.
+
+    The tensors may be replaced by others of their size and type (a bank of another size is another handle): a call takes what
+    is there, and looks at them anew (a tensor's type, size and place may also change in the hands of its owner)."""
 
     def __init__(self, A, B, scale=None, ranks=None):
         import torch
         _tensor(A, "A", (None, None, None))
         self.n, self.rank, self.K = A.shape
-        self.kind = _kind(A.dtype, "A")
+        kind = _kind(A.dtype, "A")
         _tensor(B, "B", (self.n, None, self.rank), A.dtype)
         self.N = B.shape[1]
-        if scale is not None:
-            _tensor(scale, "scale", (self.n,), torch.float32)
-        if ranks is not None:
-            _tensor(ranks, "ranks", (self.n,), torch.int32)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
-        self._struct = Adapters(self.n, self.rank, self.K, self.N, self.kind)
+        self._layout = self.n, self.rank, self.K, self.N, kind, A.dtype, torch.float32, torch.int32
+        self.struct()
 
     def struct(self) -> Adapters:
-        s = self._struct                              # (the tensors may have been replaced)
-        s.A, s.B, s.scale, s.ranks = self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), _ptr(self.ranks)
-        return s
+        """Checks the tensors; what a call hands to the library."""
+        n, rank, K, N, kind, dtype, f32, i32 = self._layout
+        A = _tensor(self.A, "A", (n, rank, K), dtype).data_ptr()
+        B = _tensor(self.B, "B", (n, N, rank), dtype).data_ptr()
+        scale, ranks = self.scale, self.ranks
+        if scale is not None:
+            scale = _tensor(scale, "scale", (n,), f32).data_ptr()
+        if ranks is not None:
+            ranks = _tensor(ranks, "ranks", (n,), i32).data_ptr()
+        return Adapters(n, rank, K, N, kind, A, B, scale, ranks)
 
 
 def _rows(t, what: str, shape, dtype=None) -> int:
@@ -792,18 +800,22 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
     output's type.  X, base and out may be slices of wider rows."""
     import torch
     lib = _lib or load_library()
-    T = X.shape[0]
-    ldx = _rows(X, "X", (T, adapters.K))
+    s = adapters.struct()
+    T, N = X.shape[0], s.N
+    ldx = _rows(X, "X", (T, s.K))
     x_kind = _kind(X.dtype, "X")
     _tensor(ids, "ids", (T,), torch.int32)
-    if out is None:
+    shape = T, N
+    ldb = ldo = 0
+    if base is not None:
+        ldb = _rows(base, "base", shape, None if out is None else out.dtype)
+    if out is None and base is not None and base.is_contiguous():
+        out, ldo = torch.empty_like(base), N
+    elif out is None:
         dtype = base.dtype if base is not None else (out_dtype or torch.float32)
-        out = torch.empty((T, adapters.N), dtype=dtype, device=X.device)
-        ldo = adapters.N
+        out, ldo = torch.empty(shape, dtype=dtype, device=X.device), N
     else:
-        ldo = _rows(out, "out", (T, adapters.N))
-    ldb = _rows(base, "base", (T, adapters.N), out.dtype) if base is not None else 0
-    s = adapters.struct()
+        ldo = ldb if out is base else _rows(out, "out", shape)
     nbytes = lib.cq_adapter_workspace_bytes(s, x_kind, T)
     ws = _scratch(X, nbytes) if nbytes else None
     st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),

@@ -74,3 +74,103 @@ def test_batch_sizes_leave_nothing_behind(lib):
     for T in range(4, 40):
         calls(T)
     assert sizes() == before
+
+
+def _norm_calls(norm, h, y, gate):
+    return (lambda: B.cq_block_norm(norm, h, y, gate), lambda: B.cq_block_norm_grad(norm, h, y, gate, dh=h, dx=y))
+
+
+@pytest.mark.parametrize("bad", [card(64, dtype=torch.bfloat16), card(63), card(65), card(1), card(1, 64), card(64, 2)[:, 0], torch.zeros(64)])
+@pytest.mark.parametrize("name", ["w_pre", "w_post"])
+def test_replaced_weights_are_checked(lib, name, bad):
+    """By another tensor, and by other contents of the same one."""
+    h, y, gate = card(3, 64, dtype=torch.bfloat16), card(3, 64), card(3)
+    norm = B.BlockNorm(card(64), card(64))
+    for call in _norm_calls(norm, h, y, gate):
+        call()
+        with pytest.raises(ValueError):
+            setattr(norm, name, bad)
+            call()
+        setattr(norm, name, card(64))
+        call()
+    norm = B.BlockNorm(card(64), card(64))
+    if bad.is_cuda:
+        getattr(norm, name).data = bad
+        for call in _norm_calls(norm, h, y, gate):
+            with pytest.raises(ValueError):
+                call()
+    assert all(handle.w_pre and handle.w_post for _, handle, _ in lib.calls)
+
+
+def test_a_handle_without_weights_takes_those_that_fit(lib):
+    h, y = card(3, 64, dtype=torch.bfloat16), card(3, 64)
+    norm = B.BlockNorm()
+    assert B.cq_block_norm(norm, h, y)["x"] is None
+    norm.w_pre = card(64)
+    assert B.cq_block_norm(norm, h, y)["x"].shape == (3, 64)
+    norm.w_pre = None
+    assert B.cq_block_norm(norm, h, y)["x"] is None
+    norm.w_pre = card(32)
+    with pytest.raises(ValueError):
+        B.cq_block_norm(norm, h, y)
+
+
+def test_changed_numbers_of_a_norm_take_effect(lib):
+    h, y = card(3, 64, dtype=torch.bfloat16), card(3, 64)
+    norm = B.BlockNorm(card(64), eps=1.0, residual_scale=2.0, branch_scale=3.0)
+    for call in _norm_calls(norm, h, y, None):
+        call()
+        got = lib.calls[-1][1]
+        assert (got.eps, got.residual_scale, got.branch_scale, got.gate_sigmoid, got.block_kind) == (1.0, 2.0, 3.0, 0, B.CQ_A_F32)
+        norm.eps, norm.residual_scale, norm.branch_scale, norm.gate_sigmoid = 0.5, 4.0, 0.25, True
+        call()
+        got = lib.calls[-1][1]
+        assert (got.eps, got.residual_scale, got.branch_scale, got.gate_sigmoid) == (0.5, 4.0, 0.25, 1)
+        norm.eps, norm.residual_scale, norm.branch_scale, norm.gate_sigmoid = 1.0, 2.0, 3.0, False
+    norm.block_dtype = torch.bfloat16
+    with pytest.raises(ValueError):
+        B.cq_block_norm(norm, h, y)
+    B.cq_block_norm(norm, h, y.bfloat16())
+    assert lib.calls[-1][1].block_kind == B.CQ_A_BF16
+
+
+@pytest.mark.parametrize("name,bad", [("A", card(3, 4, 16, dtype=torch.bfloat16)), ("A", card(2, 4, 16)), ("A", card(4, 4, 16)), ("A", card(3, 8, 16)),
+                                      ("A", card(3, 4, 8)), ("A", card(3, 16, 4).transpose(1, 2)), ("A", torch.zeros(3, 4, 16)),
+                                      ("B", card(3, 10, 4, dtype=torch.float16)), ("B", card(2, 10, 4)), ("B", card(3, 9, 4)), ("B", card(3, 10, 2)),
+                                      ("B", card(3, 4, 10).transpose(1, 2)), ("scale", card(2)), ("scale", card(3, dtype=torch.float64)),
+                                      ("scale", torch.zeros(3)), ("ranks", card(3)), ("ranks", card(2, dtype=torch.int32)),
+                                      ("ranks", card(3, dtype=torch.int64))])
+def test_replaced_adapters_are_checked(lib, name, bad):
+    def handle():
+        return B.DeviceAdapters(card(3, 4, 16), card(3, 10, 4), card(3), card(3, dtype=torch.int32))
+    X, ids = card(5, 16), card(5, dtype=torch.int32)
+    ad = handle()
+    B.cq_adapter_apply(ad, X, ids)
+    with pytest.raises(ValueError):
+        setattr(ad, name, bad)
+        B.cq_adapter_apply(ad, X, ids)
+    ad = handle()
+    if bad.is_cuda:
+        getattr(ad, name).data = bad
+        with pytest.raises(ValueError):
+            B.cq_adapter_apply(ad, X, ids)
+    assert len(lib.calls) == 1
+    ad = handle()
+    ad.scale = ad.ranks = None
+    B.cq_adapter_apply(ad, X, ids)
+    got = lib.calls[-1][1]
+    assert (got.n, got.rank, got.K, got.N, got.scale, got.ranks) == (3, 4, 16, 10, None, None)
+
+
+def test_outputs_of_adapters_are_laid_out_like_rows(lib):
+    """What the call allocates is contiguous, whatever the base's rows are."""
+    ad, X, ids = B.DeviceAdapters(card(3, 4, 16), card(3, 10, 4)), card(5, 16), card(5, dtype=torch.int32)
+    wide = card(5, 30, dtype=torch.bfloat16)
+    for base, ldb in ((wide[:, 3:13], 30), (card(5, 10, dtype=torch.bfloat16), 10)):
+        out = B.cq_adapter_apply(ad, X, ids, base=base)
+        args = lib.calls[-1][2]
+        assert out.is_contiguous() and out.dtype == torch.bfloat16 and (args[6], args[9]) == (ldb, 10)
+        assert B.cq_adapter_apply(ad, X, ids, base=base, out=base) is base and (lib.calls[-1][2][6], lib.calls[-1][2][9]) == (ldb, ldb)
+    assert B.cq_adapter_apply(ad, X, ids).dtype == torch.float32
+    with pytest.raises(ValueError):
+        B.cq_adapter_apply(ad, X, ids, base=wide[:, :10], out=card(5, 10))
