@@ -61,8 +61,8 @@ def block_norm_grad(h, y, gate, dh, dx, w_pre, w_post, eps, rho, beta, use_sigmo
         da, mda = e * u, me * np.abs(u)
         if gate.ndim == 1:
             da, mda = da.sum(axis=1, keepdims=True), mda.sum(axis=1, keepdims=True)
-        slope = a * (1.0 - a) if use_sigmoid else 1.0
-        da, mda = da * slope, mda * (a if use_sigmoid else 1.0)   # (1 - a is a difference)
+        slope = a * _gate(-gate, True) if use_sigmoid else 1.0    # (s(-z) = 1 - s(z), without the difference)
+        da, mda = da * slope, mda * slope
         out["dgate"] = da[:, 0] if gate.ndim == 1 else da
         mag["dgate"] = mda[:, 0] if gate.ndim == 1 else mda
         e, me = e * a, me * np.abs(a)

@@ -54,6 +54,14 @@ __device__ __forceinline__ void slot_weights(const void* w, int wf32, const row_
 
 __device__ __forceinline__ float sigmoid_of(float z) { return 1.f / (1.f + expf(-z)); }
 
+// The same with its slope s (1 - s) = s(z) s(-z) = e / (1 + e)^2, e = exp(-|z|): no difference, which would leave nothing of the slope
+// of a gate that is nearly open (s - s^2: 1 % off at z = 12, 0 from z = 17).
+__device__ __forceinline__ float sigmoid_of(float z, float& slope) {
+  const float e = expf(-fabsf(z)), r = 1.f / (1.f + e), er = e * r;
+  slope = er * r;
+  return z >= 0.f ? r : er;
+}
+
 }  // namespace
 
 // Runs LAUNCH(SK, BK, NT, C) for the kinds and the width of a call.  A row belongs to NT threads, each of which holds C groups

@@ -178,9 +178,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
       slot_store<SK>(G.dh, row, slot(j), H, in, v);
     }
     if (!P.y) continue;
-    const float ga = P.gate_kind == CQ_GATE_ROW && P.sigmoid ? sigmoid_of(R.z) : R.z;
-    // y, u's weight and the gate of eight values
-    auto factors = [&](int j, float (&y)[8], float (&w)[8], float (&a)[8]) {
+    float row_slope = 1.f;
+    const float ga = P.gate_kind == CQ_GATE_ROW && P.sigmoid ? sigmoid_of(R.z, row_slope) : R.z;
+    // y, u's weight and the gate of eight values with its slope
+    auto factors = [&](int j, float (&y)[8], float (&w)[8], float (&a)[8], float (&slope)[8]) {
       if constexpr (kHold)
         slot_values<BK>(R.y[j], slot(j), H, y);
       else
@@ -196,9 +197,11 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
           row_values<BK>(R.gate[j], a);
         else
           row_values<BK>(slot_fetch<BK>(again(P.gate), row, slot(j), H, in), a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) slope[i] = 1.f;
         if (P.sigmoid) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) a[i] = sigmoid_of(a[i]);
+          for (int i = 0; i < 8; ++i) a[i] = sigmoid_of(a[i], slope[i]);
         }
       } else {
 #pragma unroll
@@ -211,8 +214,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
       float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        float y[8], w[8], a[8];
-        factors(j, y, w, a);
+        float y[8], w[8], a[8], slope[8];
+        factors(j, y, w, a, slope);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float dw = d[j][i] * w[i];
@@ -227,9 +230,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
         back = P.beta * q * q * s[1] * inv_H;
       }
       if (P.gate_kind == CQ_GATE_ROW && G.dgate && in && threadIdx.x % NT == 0) {
-        float da = P.beta * q * s[2];
-        if (P.sigmoid) da *= ga * (1.f - ga);
-        elem_store<BK>(G.dgate, t, da);
+        const float da = P.beta * q * s[2];
+        elem_store<BK>(G.dgate, t, da * row_slope);
       }
     }
 #pragma unroll
@@ -238,14 +240,11 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
         forget_values(R.y[j]);
         if constexpr (ELEM) forget_values(R.gate[j]);
       }
-      float y[8], w[8], a[8], v[8];
-      factors(j, y, w, a);
+      float y[8], w[8], a[8], slope[8], v[8];
+      factors(j, y, w, a, slope);
       if (ELEM && G.dgate) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[i] = P.beta * d[j][i] * y[i] * q * w[i];
-          if (P.sigmoid) v[i] *= a[i] * (1.f - a[i]);
-        }
+        for (int i = 0; i < 8; ++i) v[i] = P.beta * d[j][i] * y[i] * q * w[i] * slope[i];
         slot_store<BK>(G.dgate, row, slot(j), H, in, v);
       }
 #pragma unroll
