@@ -761,20 +761,17 @@ class DeviceAdapters:
         _tensor(B, "B", (self.n, None, self.rank), A.dtype)
         self.N = B.shape[1]
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
-        self._layout = self.n, self.rank, self.K, self.N, kind, A.dtype, torch.float32, torch.int32
+        self._layout = self.n, self.rank, self.K, self.N, kind
+        self._tensors = A.dtype, A.shape, B.shape, torch.float32, torch.int32, A.shape[:1]
         self.struct()
 
     def struct(self) -> Adapters:
         """Checks the tensors; what a call hands to the library."""
-        n, rank, K, N, kind, dtype, f32, i32 = self._layout
-        A = _tensor(self.A, "A", (n, rank, K), dtype).data_ptr()
-        B = _tensor(self.B, "B", (n, N, rank), dtype).data_ptr()
+        dtype, a, b, f32, i32, row = self._tensors
         scale, ranks = self.scale, self.ranks
-        if scale is not None:
-            scale = _tensor(scale, "scale", (n,), f32).data_ptr()
-        if ranks is not None:
-            ranks = _tensor(ranks, "ranks", (n,), i32).data_ptr()
-        return Adapters(n, rank, K, N, kind, A, B, scale, ranks)
+        return Adapters(*self._layout, _tensor(self.A, "A", a, dtype).data_ptr(), _tensor(self.B, "B", b, dtype).data_ptr(),
+                        None if scale is None else _tensor(scale, "scale", row, f32).data_ptr(),
+                        None if ranks is None else _tensor(ranks, "ranks", row, i32).data_ptr())
 
 
 def _rows(t, what: str, shape, dtype=None) -> int:
@@ -798,28 +795,30 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
 
     base: the shared projection's output [T, N] (None: zero); out may be base.  Without either, out_dtype (float32) is the
     output's type.  X, base and out may be slices of wider rows."""
-    import torch
     lib = _lib or load_library()
     s = adapters.struct()
-    T, N = X.shape[0], s.N
-    ldx = _rows(X, "X", (T, s.K))
-    x_kind = _kind(X.dtype, "X")
-    _tensor(ids, "ids", (T,), torch.int32)
+    _, _, K, N, _ = adapters._layout
+    T = X.shape[0]
     shape = T, N
+    ldx = _rows(X, "X", (T, K))
+    x_kind = _kind(X.dtype, "X")
+    _tensor(ids, "ids", (T,), adapters._tensors[4])
     ldb = ldo = 0
     if base is not None:
         ldb = _rows(base, "base", shape, None if out is None else out.dtype)
-    if out is None and base is not None and base.is_contiguous():
-        out, ldo = torch.empty_like(base), N
-    elif out is None:
-        dtype = base.dtype if base is not None else (out_dtype or torch.float32)
-        out, ldo = torch.empty(shape, dtype=dtype, device=X.device), N
+    if out is None:
+        import torch
+        ldo = N
+        if ldb == N:      # (the base is contiguous)
+            out = torch.empty_like(base)
+        else:
+            out = torch.empty(shape, dtype=base.dtype if base is not None else out_dtype or torch.float32, device=X.device)
     else:
         ldo = ldb if out is base else _rows(out, "out", shape)
     nbytes = lib.cq_adapter_workspace_bytes(s, x_kind, T)
-    ws = _scratch(X, nbytes) if nbytes else None
-    st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, _ptr(base), ldb, out.data_ptr(),
-                              _kind(out.dtype, "out"), ldo, _ptr(ws), nbytes, _raw_stream(X))
+    ws = ids.new_empty((nbytes + 3) // 4) if nbytes else None
+    st = lib.cq_adapter_apply(s, X.data_ptr(), x_kind, ldx, ids.data_ptr(), T, None if base is None else base.data_ptr(), ldb,
+                              out.data_ptr(), _kind(out.dtype, "out"), ldo, None if ws is None else ws.data_ptr(), nbytes, _raw_stream(X))
     if st:
         raise CqError(st)
     return out
