@@ -35,3 +35,43 @@ def test_gradients_of_gates_far_from_zero(B, stream, block, gate, H):  # noqa: F
     A._check_norm(got, c.backward(out["h"].double().cpu().numpy()), T, "backward")
     near = c.gate.abs() <= 20          # (at 80 a value may lie below a type's smallest)
     assert (got["dgate"][near] != 0).all()
+
+
+# ------------------------------------------------------------------------------------------------
+# the balance loss along its gradient
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,E,k,S,padded", [(50, 9, 2, 1, False), (120, 16, 3, 5, True), (700, 64, 6, 3, True), (60, 300, 8, 2, False)])
+def test_balance_gradient_along_itself(B, T, E, k, S, padded):  # noqa: F811
+    """(L(z + s v) - L(z - s v)) / 2s of the forward kernel against |gradient|, v the gradient's direction, and against the gradient
+    along the part of it that each sequence has.  Truncation: along v a token's sum of f p has the third derivative
+    E[f' v'^3] - 3 E[f' v'] E[v'^2] (f', v' centred, expectations under p), at most 4 F V^3 with F and V the ranges of f and v over the
+    experts.  Rounding: both losses by the roundings that test_around_layer derives, and z + s v by half a step of fp32 times the
+    gradient.  The bound is small beside what it is held against: a gradient of zero, of the wrong sign or off by a tenth fails."""
+    import torch
+    rng = np.random.default_rng(T)
+    alpha, step = 3.0, 2.0 ** -4
+    z, z64, ids = A._routing(rng, T, E, k, torch.float32)
+    off = A._offsets(rng, T, S) if S > 1 else None
+    mask = rng.random(T) < 0.8 if padded else None
+    dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    t_ids, t_off, t_mask = dev(ids), dev(off), dev(mask)
+    out = B.cq_balance_loss(z, t_ids, alpha, t_off, t_mask)
+    g = B.cq_balance_loss_grad(z, out["counts"], out["tokens"], k, alpha, t_off, t_mask).double().cpu().numpy()
+    seqs = [m for m in O.members(T, off, mask) if len(m)]
+    counts = [c for c, n in zip(out["counts"].cpu().numpy(), out["tokens"].cpu().numpy()[:-1]) if n]
+    loss = lambda s, v: float(B.cq_balance_loss(z + dev((s * v).astype(np.float32)), t_ids, alpha, t_off, t_mask)["loss"])
+    parts = [np.arange(T)] + (seqs if len(seqs) > 1 else [])
+    for part in parts:
+        v = np.zeros((T, E))
+        v[part] = g[part]
+        v = (v / np.linalg.norm(v)).astype(np.float32).astype(np.float64)
+        diff, got = (loss(step, v) - loss(-step, v)) / (2 * step), float((g * v).sum())
+        cut = 0.0
+        for at, c in zip(seqs, counts):
+            F, V = np.ptp(c) / (k * len(at)), np.ptp(v[at], axis=1)
+            cut += alpha * E / (len(seqs) * len(at)) * 4 * F * (V ** 3).sum() * step ** 2 / 6
+        roundings = 256 + T // 64 + S
+        bound = cut + roundings * U * float(out["loss"]) / step + U * (np.abs(g) * (np.abs(z64) + 1)).sum() / step
+        print(f"{diff:.6g} {got:.6g} bound {bound:.3g}", flush=True)
+        assert bound < 0.1 * got
+        assert abs(diff - got) <= bound
