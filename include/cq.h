@@ -353,7 +353,7 @@ cq_status cq_block_norm_grad(const cq_block_norm_spec* P, const void* h, const v
  *   token_mask [T] bytes or NULL: tokens whose byte is 0 (padding) are left out, whatever their logits hold.  A token all of whose
  *   logits are -inf counts, with probabilities of 0.
  *   Outputs: loss [1] f32, counts [n_seqs, E] i32, probs [n_seqs, E] f32 (P), tokens [n_seqs + 1] i32 (n_s, then S').
- *   E <= 1024, top_k <= min(E, 64), T top_k < 2^31.  workspace: cq_balance_loss_workspace_bytes(T, E, n_seqs) bytes,
+ *   E <= 1024, top_k <= min(E, 64), T top_k < 2^31, n_seqs <= 2^26.  workspace: cq_balance_loss_workspace_bytes(T, E, n_seqs) bytes,
  *   which never falls as T grows (few logits need none: 0, NULL allowed).
  */
 size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs);

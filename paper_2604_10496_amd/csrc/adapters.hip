@@ -802,10 +802,18 @@ bool takes_few(const cq_adapters* W, int x_kind, int T) {
   return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23 && (x_kind != CQ_A_F32 || W->K <= 2048);
 }
 
+// Tokens of one pair of launches (at least 8192); longer batches take several.
+int most_tokens(const cq_adapters* W) {
+  const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
+  const long down = kMostThreads / (64 * kPromptDownWaves) * kTile, up = kMostThreads / (64 * kUpWaves) / blocks * kTile * kPromptTiles;
+  return (int)(down < up ? down : up);
+}
+
 }  // namespace
 
 extern "C" size_t cq_adapter_workspace_bytes(const cq_adapters* W, int x_kind, int T) {
   if (check_adapters(W, T) != CQ_OK || !cq_row_kind(x_kind) || takes_few(W, x_kind, T)) return 0;
+  if (T > most_tokens(W)) T = most_tokens(W);
   // no batch of T <= kLeaderTokens has more parts than 512 over its tiles, nor than 16, nor than there are rounds of one unit
   const long most = ((long)W->K + 128 * kDownWaves - 1) / (128 * kDownWaves), cap = most < 16 ? most : 16;
   long rows = ((long)T + kTile - 1) / kTile * kTile;
@@ -829,6 +837,15 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   if (ldx < W->K || ld_out < W->N || (base && ld_base < W->N)) return CQ_ERR_SHAPE;
   const size_t need = cq_adapter_workspace_bytes(W, x_kind, T);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
+  const int most = most_tokens(W);
+  if (T > most) {
+    cq_status done = CQ_OK;
+    for (int t = 0; t < T && done == CQ_OK; t += most)
+      done = cq_adapter_apply(W, row_at(X, x_kind, (size_t)t * ldx), x_kind, ldx, adapter_ids + t, T - t < most ? T - t : most,
+                              row_at(base, out_kind, (size_t)t * ld_base), ld_base, row_at(out, out_kind, (size_t)t * ld_out), out_kind,
+                              ld_out, workspace, workspace_bytes, stream);
+    return done;
+  }
   adapter_args P;
   P.A = W->A;
   P.B = W->B;
@@ -884,9 +901,7 @@ extern "C" cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x
   const long blocks = ((long)W->N + 64 * kUpWaves - 1) / (64 * kUpWaves);
   P.up_blocks = leaders ? (int)((blocks * T + kMostGroups - 1) / kMostGroups) : 1;
   const long up_tiles = leaders ? singles : ((long)T + kTile * kPromptTiles - 1) / (kTile * kPromptTiles);
-  const long up_groups = up_tiles * ((blocks + P.up_blocks - 1) / P.up_blocks);
-  if (up_groups > 0x7fffffffL) return CQ_ERR_SHAPE;
-  const dim3 up((unsigned)up_groups);
+  const dim3 up((unsigned)(up_tiles * ((blocks + P.up_blocks - 1) / P.up_blocks)));
 #define DOWN3(XK, WK, RT, UNITS, WAVES) hipLaunchKernelGGL((adapter_down_kernel<XK, WK, RT, UNITS, WAVES>), down, dim3(64 * WAVES), 0, s, P)
 #define DOWN2(XK, WK, RT)                                                              \
   do {                                                                                 \

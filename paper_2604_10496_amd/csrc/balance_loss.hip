@@ -16,12 +16,14 @@
 namespace {
 
 constexpr int kMaxExperts = 1024;
+constexpr int kMostSequences = 1 << 26;   // (their workgroups of the second launch are counted in 32 bits)
 
 struct balance_args {
   const void* z;
   const int32_t *ids, *offsets;
   const uint8_t* mask;
   int T, E, k, S, tile;
+  int first;   // first workgroup of this launch (the gradient, the sums over sequences)
   float alpha;
 };
 
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(1024) void balance_sequence_kernel(balance_args P, 
   __shared__ int lds_n;
   __shared__ bool last;
   __shared__ float sums[16];
-  const int s = blockIdx.x, x = threadIdx.x & 31, y = threadIdx.x >> 5, e = blockIdx.y * 32 + x;
+  const int s = P.first + blockIdx.x, x = threadIdx.x & 31, y = threadIdx.x >> 5, e = blockIdx.y * 32 + x;
   const int a = offset_at(P, s), b = offset_at(P, s + 1);
   const int i0 = a / P.tile, i1 = b > a ? (b - 1) / P.tile : i0 - 1;
   if (threadIdx.x == 0) lds_n = 0;
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(1024) void balance_sequence_kernel(balance_args P, 
       __hip_atomic_store(&W.loss[(size_t)s * gridDim.y + blockIdx.y], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (blockIdx.y == 0) __hip_atomic_store(&tokens[s], n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       const uint32_t before = __hip_atomic_fetch_add(W.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-      last = before == gridDim.x * gridDim.y - 1;
+      last = before == (uint32_t)P.S * gridDim.y - 1;
     }
   }
   __syncthreads();
@@ -426,7 +428,7 @@ template <int KIND, int L, int C>
 __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const int32_t* counts, const int32_t* tokens,
                                                            const float* d_loss, void* dz) {
   constexpr int U = C == 1 ? 4 : 1;
-  const int e0 = (threadIdx.x % L) * 4, t0 = blockIdx.x * (U * (256 / L));
+  const int e0 = (threadIdx.x % L) * 4, t0 = (P.first + blockIdx.x) * (U * (256 / L));
   offset_window offsets(P);
   float p[U][C][4];
   bool in[U];
@@ -483,7 +485,7 @@ __global__ __launch_bounds__(256) void balance_grad_kernel(balance_args P, const
 }
 
 cq_status check_balance(int logit_kind, const int32_t* offsets, int S, int T, int E, int k) {
-  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || k <= 0 || k > E || k > 64 || S <= 0) return CQ_ERR_SHAPE;
+  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || k <= 0 || k > E || k > 64 || S <= 0 || S > kMostSequences) return CQ_ERR_SHAPE;
   if ((long)T * k > 0x7fffffffL) return CQ_ERR_SHAPE;   // (counts are 32-bit)
   if (!offsets && S != 1) return CQ_ERR_NULL;
   if (!cq_row_kind(logit_kind)) return CQ_ERR_UNSUPPORTED;
@@ -538,7 +540,7 @@ bool in_one(int T, int E, int S) { return (long)T * E * S <= 32768 && S <= 2 && 
 }  // namespace
 
 extern "C" size_t cq_balance_loss_workspace_bytes(int T, int E, int n_seqs) {
-  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || n_seqs <= 0 || in_one(T, E, n_seqs)) return 0;
+  if (T < 0 || T > 1 << 30 || E <= 0 || E > kMaxExperts || n_seqs <= 0 || n_seqs > kMostSequences || in_one(T, E, n_seqs)) return 0;
   const size_t slots = slots_of(T, n_seqs);
   return 2 * cq_align_up(slots * E * 4, 256) + cq_align_up(slots * 4, 256) + cq_align_up((size_t)n_seqs * ((E + 31) / 32) * 4, 256) + 256;
 }
@@ -553,7 +555,7 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   const size_t need = cq_balance_loss_workspace_bytes(T, E, n_seqs);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T, E, n_seqs), alpha};
+  balance_args P = {logits, topk_ids, seq_offsets, token_mask, T, E, top_k, n_seqs, tile_of(T, E, n_seqs), 0, alpha};
   const size_t slots = slots_of(T, n_seqs);
   balance_ws W;
   char* at = (char*)workspace;
@@ -585,8 +587,14 @@ extern "C" cq_status cq_balance_loss(const void* logits, int logit_kind, const i
   } while (0)
   CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
 #undef LAUNCH
-  hipLaunchKernelGGL(balance_sequence_kernel, dim3(n_seqs, (E + 31) / 32), dim3(1024), 0, s, P, W, counts, probs, tokens, loss);
-  return cq_check_launch();
+  cq_status launched = cq_check_launch();
+  constexpr int kMost = (int)(kMostThreads / 1024);
+  for (; P.first < n_seqs && launched == CQ_OK; P.first += kMost) {
+    const int seqs = n_seqs - P.first < kMost ? n_seqs - P.first : kMost;
+    hipLaunchKernelGGL(balance_sequence_kernel, dim3(seqs, (E + 31) / 32), dim3(1024), 0, s, P, W, counts, probs, tokens, loss);
+    launched = cq_check_launch();
+  }
+  return launched;
 }
 
 extern "C" cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t* counts, const int32_t* tokens,
@@ -596,14 +604,20 @@ extern "C" cq_status cq_balance_loss_grad(const void* logits, int logit_kind, co
   if (st != CQ_OK) return st;
   if (T == 0) return CQ_OK;
   if (!logits || !counts || !tokens || !d_logits) return CQ_ERR_NULL;
-  const balance_args P = {logits, nullptr, seq_offsets, token_mask, T, E, top_k, n_seqs, 0, alpha};
-#define LAUNCH(KIND, L, C)                                                                                                       \
-  do {                                                                                                                           \
-    constexpr int kTokens = (C == 1 ? 4 : 1) * (256 / L);                                                                        \
-    hipLaunchKernelGGL((balance_grad_kernel<KIND, L, C>), dim3((T - 1) / kTokens + 1), dim3(256), 0, (hipStream_t)stream, P, counts, \
-                       tokens, d_loss, d_logits);                                                                                \
+  balance_args P = {logits, nullptr, seq_offsets, token_mask, T, E, top_k, n_seqs, 0, 0, alpha};
+  cq_status launched = CQ_OK;
+#define LAUNCH(KIND, L, C)                                                                                                          \
+  do {                                                                                                                              \
+    constexpr int kMost = (int)(kMostThreads / 256), kTokens = (C == 1 ? 4 : 1) * (256 / L);                                        \
+    const int groups = (T - 1) / kTokens + 1;                                                                                       \
+    for (; P.first < groups && launched == CQ_OK; P.first += kMost) {                                                               \
+      const int now = groups - P.first < kMost ? groups - P.first : kMost;                                                          \
+      hipLaunchKernelGGL((balance_grad_kernel<KIND, L, C>), dim3(now), dim3(256), 0, (hipStream_t)stream, P, counts, tokens, d_loss, \
+                         d_logits);                                                                                                 \
+      launched = cq_check_launch();                                                                                                 \
+    }                                                                                                                               \
   } while (0)
   CQ_BALANCE_DISPATCH(LAUNCH, logit_kind, E);
 #undef LAUNCH
-  return cq_check_launch();
+  return launched;
 }

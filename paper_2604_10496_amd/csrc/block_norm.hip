@@ -92,10 +92,19 @@ extern "C" cq_status cq_block_norm(const cq_block_norm_spec* P, const void* h, c
   if (T == 0) return CQ_OK;
   if (!h || (!y && !x_out) || (y && !h_out) || (x_out && !P->w_pre)) return CQ_ERR_NULL;
   if (y && P->gate_kind != CQ_GATE_NONE && !gate) return CQ_ERR_NULL;
-  const norm_args a = make_norm_args(P, T, h, y, gate);
-#define LAUNCH(SK, BK, NT, C)                                                                                  \
-  hipLaunchKernelGGL((block_norm_kernel<SK, BK, NT, C>), dim3(T), dim3(NT), 0, (hipStream_t)stream, a, h_out, x_out)
-  CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, P->H);
+  constexpr int kMostRows = (int)(kMostThreads / 1024);   // (of the widest rows' workgroups)
+  for (int t = 0; t < T; t += kMostRows) {
+    const int rows = T - t < kMostRows ? T - t : kMostRows;
+    const size_t at = (size_t)t * P->H;
+    const norm_args a = make_norm_args(P, rows, row_at(h, P->stream_kind, at), row_at(y, P->block_kind, at),
+                                       row_at(gate, P->block_kind, P->gate_kind == CQ_GATE_ROW ? (size_t)t : at));
+    void *const h_new = row_at(h_out, P->stream_kind, at), *const x = row_at(x_out, P->block_kind, at);
+#define LAUNCH(SK, BK, NT, C) \
+  hipLaunchKernelGGL((block_norm_kernel<SK, BK, NT, C>), dim3(rows), dim3(NT), 0, (hipStream_t)stream, a, h_new, x)
+    CQ_NORM_DISPATCH(LAUNCH, P->stream_kind, P->block_kind, P->H);
 #undef LAUNCH
-  return cq_check_launch();
+    const cq_status launched = cq_check_launch();
+    if (launched != CQ_OK) return launched;
+  }
+  return CQ_OK;
 }

@@ -10,6 +10,16 @@ namespace {
 // element kinds are the activation kinds of cq.h: CQ_A_F16, CQ_A_F32, CQ_A_BF16
 inline bool cq_row_kind(int kind) { return kind == CQ_A_F16 || kind == CQ_A_F32 || kind == CQ_A_BF16; }
 
+// The threads along a dimension of a launch are counted in 32 bits, and what does not fit is cut off without an error (2^26 + 3 rows of
+// 64 threads: 3 rows were worked on): larger batches take several launches.
+constexpr long kMostThreads = 1l << 31;
+
+// p moved on by `values` elements (a null pointer stays one)
+template <typename P>
+inline P* row_at(P* p, int kind, size_t values) {
+  return p ? (P*)((uintptr_t)p + values * (kind == CQ_A_F32 ? 4 : 2)) : nullptr;
+}
+
 template <int KIND>
 __device__ __forceinline__ float elem_load(const void* p, size_t at) {
   if constexpr (KIND == CQ_A_F32) return reinterpret_cast<const float*>(p)[at];

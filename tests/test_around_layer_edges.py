@@ -75,3 +75,95 @@ def test_balance_gradient_along_itself(B, T, E, k, S, padded):  # noqa: F811
         print(f"{diff:.6g} {got:.6g} bound {bound:.3g}", flush=True)
         assert bound < 0.1 * got
         assert abs(diff - got) <= bound
+
+
+# ------------------------------------------------------------------------------------------------
+# batches beyond one launch, whose threads along a dimension are counted in 32 bits
+# ------------------------------------------------------------------------------------------------
+def _around(step, T):
+    """Rows on either side of every boundary between launches, and the last ones."""
+    import torch
+    at = [t + d for t in range(0, T, step) for d in (-1, 0, 1)] + [T - 2, T - 1]
+    return torch.tensor(sorted({t for t in at if 0 <= t < T}), device="cuda")
+
+
+def test_norm_of_more_rows_than_one_launch_takes(B):  # noqa: F811
+    import torch
+    T, H = (1 << 26) + 3, 2
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.randn((T, H), generator=g, device="cuda").bfloat16()
+    y = torch.randn((T, H), generator=g, device="cuda").bfloat16()
+    gate = torch.randn(T, generator=g, device="cuda").bfloat16()
+    w = torch.tensor([0.5, 2.0], device="cuda")
+    norm = B.BlockNorm(w, w, gate_sigmoid=True, block_dtype=torch.bfloat16)
+    h_out, x_out = torch.full_like(h, float("nan")), torch.full_like(h, float("nan"))
+    print("rows", flush=True)
+    B.cq_block_norm(norm, h, y, gate, h_out=h_out, x_out=x_out)
+    assert h_out.isfinite().all() and x_out.isfinite().all()
+    at = _around(1 << 21, T)
+    for gates in (gate, y):
+        if gates is y:
+            print("a gate per value", flush=True)
+            B.cq_block_norm(norm, h, y, y, h_out=h_out, x_out=x_out)
+        want = B.cq_block_norm(norm, h[at], y[at], gates[at])
+        assert h_out[at].equal(want["h"]) and x_out[at].equal(want["x"])
+    print("without a block", flush=True)
+    assert B.cq_block_norm(norm, h, x_out=x_out)["x"][at].equal(B.cq_block_norm(norm, h[at])["x"])
+
+
+def test_balance_gradient_of_more_tokens_than_one_launch_takes(B):  # noqa: F811
+    import torch
+    T, E = (1 << 26) + 5, 257
+    g = torch.Generator(device="cuda").manual_seed(2)
+    at = _around(1 << 25, T)
+    z = torch.zeros((T, E), dtype=torch.float16, device="cuda")
+    z[at] = torch.randn((len(at), E), generator=g, device="cuda").half()
+    counts = torch.randint(0, 1000, (1, E), generator=g, device="cuda", dtype=torch.int32)
+    tokens = torch.tensor([100, 1], dtype=torch.int32, device="cuda")
+    print("gradient", flush=True)
+    got = B.cq_balance_loss_grad(z, counts, tokens, 2, 1.0)
+    assert got[at].equal(B.cq_balance_loss_grad(z[at], counts, tokens, 2, 1.0))
+    assert got[12345].equal(got[T - 12345])
+    del z, got
+    torch.cuda.empty_cache()
+
+
+def test_balance_loss_of_more_sequences_than_one_launch_takes(B):  # noqa: F811
+    """One token each, and one sequence without any."""
+    import torch
+    T, E = (1 << 22) + 2, 4
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn((T, E), generator=g, device="cuda")
+    ids = torch.randint(0, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)
+    off = torch.cat([torch.arange(T + 1, device="cuda"), torch.tensor([T], device="cuda")]).int()
+    print("loss", flush=True)
+    out = B.cq_balance_loss(z, ids, 1.0, off)
+    p = torch.softmax(z.double(), dim=1)
+    one = torch.nn.functional.one_hot(ids[:, 0].long(), E)
+    assert out["counts"][:T].equal(one.int()) and not out["counts"][T].any()
+    assert out["tokens"][:T].eq(1).all() and out["tokens"][T:].tolist() == [0, T]
+    assert ((out["probs"][:T].double() - p).abs() <= 128 * U * p).all() and not out["probs"][T].any()
+    want = E * (p * one).sum().item() / T
+    assert abs(out["loss"].item() - want) <= (256 + T // 1024) * U * want
+
+
+def test_adapters_of_more_tokens_than_one_launch_takes(B):  # noqa: F811
+    import torch
+    T, K, N, n = (1 << 27) + 40, 2, 3, 5
+    g = torch.Generator(device="cuda").manual_seed(4)
+    A_, Bm = torch.randn((n, 1, K), generator=g, device="cuda").bfloat16(), torch.randn((n, N, 1), generator=g, device="cuda").bfloat16()
+    X = torch.randn((T, K), generator=g, device="cuda").bfloat16()
+    base = torch.randn((T, N), generator=g, device="cuda").bfloat16()
+    ids = torch.randint(-1, n, (T,), generator=g, device="cuda", dtype=torch.int32)
+    print("adapters", flush=True)
+    got = B.cq_adapter_apply(B.DeviceAdapters(A_, Bm), X, ids, base=base)
+    for t in range(0, T, 1 << 24):
+        a = ids[t:t + (1 << 24)].long()
+        on, a = (a >= 0)[:, None], a.clamp(min=0)
+        x, b = X[t:t + (1 << 24)].double(), base[t:t + (1 << 24)].double()
+        up = Bm[a, :, 0].double()
+        want = b + on * (A_[a, 0].double() * x).sum(1, keepdim=True) * up
+        mag = b.abs() + (A_[a, 0].double() * x).abs().sum(1, keepdim=True) * up.abs()
+        bound = A._adapter_roundings(K, 1) * U * mag
+        bound = bound + torch.finfo(torch.bfloat16).eps / 2 * (want.abs() + bound) + 1e-40
+        assert ((got[t:t + (1 << 24)].double() - want).abs() <= bound).all(), t

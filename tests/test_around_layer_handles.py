@@ -174,3 +174,20 @@ def test_outputs_of_adapters_are_laid_out_like_rows(lib):
     assert B.cq_adapter_apply(ad, X, ids).dtype == torch.float32
     with pytest.raises(ValueError):
         B.cq_adapter_apply(ad, X, ids, base=wide[:, :10], out=card(5, 10))
+
+
+def test_sequences_beyond_those_that_can_be_counted_are_refused():
+    real = B.load_library()
+    one = ctypes.c_void_p(256)     # a non-null dummy that must never be dereferenced
+    S = (1 << 26) + 1
+    assert real.cq_balance_loss(one, B.CQ_A_F32, one, one, S, None, 8, 4, 1, 0.1, one, one, one, one, one, 1 << 60, None) == 2
+    assert real.cq_balance_loss_grad(one, B.CQ_A_F32, one, one, one, S, None, 8, 4, 1, 0.1, None, one, None) == 2
+    assert real.cq_balance_loss_workspace_bytes(8, 4, S) == 0 and real.cq_balance_loss_workspace_bytes(8, 4, S - 1) > 0
+
+
+def test_workspace_of_adapters_ends_with_the_longest_launch():
+    real = B.load_library()
+    for N, most in ((3, 1 << 26), (256, 1 << 26), (1 << 23, 8192)):
+        s = B.Adapters(2, 16, 8, N, B.CQ_A_BF16, 256, 256, None, None)
+        at = lambda T: real.cq_adapter_workspace_bytes(ctypes.byref(s), B.CQ_A_BF16, T)
+        assert at(most - 1) <= at(most) == at(most + 1) == at(1 << 30) == most * 16 * 4
