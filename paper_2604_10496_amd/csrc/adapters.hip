@@ -16,6 +16,8 @@
 //
 // 4096 tokens of 9 prompts, K = N = 4096, rank 32, bf16: 19.0 + 18.4 us for 104 MB (2.8 TB/s); 64 requests with adapters of ranks 16 to
 // 64, K = 2048, N = 2816: 6.5 + 10.7 us for 22 MB; one token at rank 16: 4.2 + 7.0 us.
+#include <type_traits>
+
 #include "cq_rows.h"
 
 namespace {
@@ -97,7 +99,8 @@ __device__ __forceinline__ bool find_rows(const adapter_args& P, int tile, int& 
   return true;
 }
 
-// An fp32 value as the sum of three values that bf16 holds (8 bits each, cut off, not rounded: no value overflows).
+// An fp32 value as the sum of three values that bf16 holds (8 bits each, cut off, not rounded: no value overflows; what is below
+// bf16's smallest, 2^-133, is lost).  An infinity is its own first part.
 __device__ __forceinline__ void split3(float x, uint32_t& a, uint32_t& b, uint32_t& c) {
   a = __float_as_uint(x) & 0xffff0000u;
   float rest = x - __uint_as_float(a);
@@ -122,6 +125,27 @@ __device__ __forceinline__ split_frag split_pack(const float (&v)[8]) {
 #pragma unroll
   for (int p = 0; p < 3; ++p) f.part[p] = __builtin_bit_cast(cq_v8bf16, w[p]);
   return f;
+}
+
+// The second and third parts of a value are often 0, and 0 times an infinite weight makes a NaN of what should be an infinite product.
+// Sums that come out as NaN are therefore taken again (FINITE below) with those parts against finite_weights: infinities and NaN as the
+// largest finite value of their sign.  The first part, which has the value's sign and is 0 only with it (from 2^-133 on), meets the weight
+// itself, and what a finite weight adds to that has the same sign.  4096 tokens of fp32 rows at rank 64: 59.8 us without either, 60.1 with
+// the second look at NaN, 64.2 with finite weights at all times.
+__device__ __forceinline__ cq_v8bf16 finite_weights(const cq_v4u& w) {
+  typedef __attribute__((__vector_size__(16))) uint16_t v8u;
+  typedef __attribute__((__vector_size__(16))) int16_t v8i;
+  const v8u bits = __builtin_elementwise_min(__builtin_bit_cast(v8u, w), (v8u)(v8u{} + (uint16_t)0xff7f));   // negative ones
+  const v8i both = __builtin_elementwise_min(__builtin_bit_cast(v8i, bits), (v8i)(v8i{} + (int16_t)0x7f7f));
+  return __builtin_bit_cast(cq_v8bf16, both);
+}
+
+template <int N>
+__device__ __forceinline__ bool any_nan(const cq_v4f (&acc)[N]) {   // in the wavefront; true at times where infinities of both signs meet
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += (acc[i][0] + acc[i][1]) + (acc[i][2] + acc[i][3]);
+  return __ballot(s != s) != 0;
 }
 
 // How a pair of types is multiplied
@@ -206,7 +230,7 @@ struct k_unit {
 };
 
 // acc += 16 rows of A times 16 tokens over 32 values of K
-template <int XK, int WK>
+template <int XK, int WK, bool FINITE>
 __device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& x, cq_v4f& acc) {
   if constexpr (product_path<XK, WK>() == kSame16) {
     if constexpr (XK == CQ_A_BF16)
@@ -218,8 +242,10 @@ __device__ __forceinline__ void down_product(const row8<WK>& w, const row8<XK>& 
     row_values<XK>(x, v);
     if constexpr (product_path<XK, WK>() == kSplit) {
       const split_frag xs = split_pack(v);
-#pragma unroll
-      for (int p = 0; p < 3; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w.w[0]), xs.part[p], acc, 0, 0, 0);
+      const cq_v8bf16 rest = FINITE ? finite_weights(w.w[0]) : __builtin_bit_cast(cq_v8bf16, w.w[0]);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w.w[0]), xs.part[0], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, xs.part[1], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, xs.part[2], acc, 0, 0, 0);
     } else {
       float u[8];
       row_values<WK>(w, u);
@@ -237,7 +263,7 @@ struct down_place {
   size_t own_row, x_row[4];   // X of the lane's own token, and of the four tokens that its quad reads
 };
 
-template <int XK, int WK, int RT, int UNITS, int WAVES>
+template <int XK, int WK, int RT, int UNITS, int WAVES, bool FINITE>
 __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_place& at, int k, int k_end, bool fetched,
                                             k_unit<XK> (&x)[UNITS], cq_v4f (&acc)[RT]) {
   constexpr int kRound = 128 * WAVES * UNITS;
@@ -275,14 +301,14 @@ __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_pl
         for (int u = 0; u < UNITS; ++u) {
           w[j][u].exchange();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) down_product<XK, WK>(w[j][u].operand(c), x[u].operand(c), acc[i + j]);
+          for (int c = 0; c < 4; ++c) down_product<XK, WK, FINITE>(w[j][u].operand(c), x[u].operand(c), acc[i + j]);
         }
     }
     fetched = false;
   }
   if constexpr (UNITS > 1) {
     k_unit<XK> fewer[UNITS / 2];
-    down_rounds<XK, WK, RT, UNITS / 2, WAVES>(P, at, k, k_end, false, fewer, acc);
+    down_rounds<XK, WK, RT, UNITS / 2, WAVES, FINITE>(P, at, k, k_end, false, fewer, acc);
   } else {
     const int kk = k + wave * 128;
     if (kk + 128 <= k_end) {
@@ -295,16 +321,27 @@ __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_pl
         fetch_rows(i, kk, w);
         w.exchange();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) down_product<XK, WK>(w.operand(c), last.operand(c), acc[i]);
+        for (int c = 0; c < 4; ++c) down_product<XK, WK, FINITE>(w.operand(c), last.operand(c), acc[i]);
       }
     } else {
 #pragma unroll 1
       for (int from = kk; from < k_end; from += 32) {
         const row8<XK> rest = fetch_k<XK>(P.X, at.own_row, from + g * 8, k_end, P.K);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) down_product<XK, WK>(fetch_k<WK>(P.A, w_row(i * 16 + col), from + g * 8, k_end, P.K), rest, acc[i]);
+        for (int i = 0; i < RT; ++i) down_product<XK, WK, FINITE>(fetch_k<WK>(P.A, w_row(i * 16 + col), from + g * 8, k_end, P.K), rest, acc[i]);
       }
     }
+  }
+}
+
+// acc again, where it holds a NaN that finite_weights may spare (x then holds the first round of these tokens, as before)
+template <int XK, int WK, int RT, int UNITS, int WAVES>
+__device__ __forceinline__ void down_again(const adapter_args& P, const down_place& at, int k, int k_end, k_unit<XK> (&x)[UNITS], cq_v4f (&acc)[RT]) {
+  if constexpr (product_path<XK, WK>() == kSplit) {
+    if (__builtin_expect(!any_nan(acc), 1)) return;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    down_rounds<XK, WK, RT, UNITS, WAVES, true>(P, at, k, k_end, false, x, acc);
   }
 }
 
@@ -372,7 +409,8 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(adapter_args P
       cq_v4f acc[RT];
 #pragma unroll
       for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-      down_rounds<XK, WK, RT, UNITS, WAVES>(P, at, k_first, k_end, fetched, x, acc);
+      down_rounds<XK, WK, RT, UNITS, WAVES, false>(P, at, k_first, k_end, fetched, x, acc);
+      down_again<XK, WK, RT, UNITS, WAVES>(P, at, k_first, k_end, x, acc);
       fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
@@ -491,10 +529,21 @@ __device__ __forceinline__ void keep_rank(int r, int rank, float (&v)[8]) {
   for (int i = 0; i < 8; ++i) v[i] = r + i < rank ? v[i] : 0.f;
 }
 
-template <int WK>
+template <int WK, bool FINITE>
 __device__ __forceinline__ void up_product(const row8<WK> (&w)[4], const float (&v)[8], cq_v4f (&acc)[4]) {
   if constexpr (WK == CQ_A_BF16) {
     const split_frag vs = split_pack(v);
+    if constexpr (FINITE) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {   // (one after the other: the rare form adds few registers)
+        const cq_v8bf16 rest = finite_weights(w[j].w[0]);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, w[j].w[0]), vs.part[0], acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, vs.part[1], acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, vs.part[2], acc[j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return;
+    }
 #pragma unroll
     for (int p = 0; p < 3; ++p)
 #pragma unroll
@@ -508,6 +557,20 @@ __device__ __forceinline__ void up_product(const row8<WK> (&w)[4], const float (
 #pragma unroll
       for (int q = 0; q < 8; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[q], v[q], acc[j], 0, 0, 0);
     }
+  }
+}
+
+// acc = sum<FINITE>(acc) on zeros, see finite_weights
+template <int WK, typename SUM>
+__device__ __forceinline__ void up_sums(cq_v4f (&acc)[4], SUM&& sum) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+  sum(std::false_type{});
+  if constexpr (WK == CQ_A_BF16) {
+    if (__builtin_expect(!any_nan(acc), 1)) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    sum(std::true_type{});
   }
 }
 
@@ -586,30 +649,30 @@ __global__ __launch_bounds__(64 * kUpWaves, WIDE ? 3 : 4) void adapter_up_kernel
     out_pieces<OK> base;
     base.fetch(P, token, n0, g);
     cq_v4f acc[4];
+    up_sums<WK>(acc, [&](auto finite) {
+      for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
+        const int r = rb + g * 8, most = rb == 0 ? P.R : rank;
+        row8<WK> w[4];
+        fetch_up<WK, OK, true>(P, a, n0, col, r, most, w);
+        float v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    for (int rb = 0; a >= 0 && (rb == 0 || rb < rank); rb += 32) {
-      const int r = rb + g * 8, most = rb == 0 ? P.R : rank;
-      row8<WK> w[4];
-      fetch_up<WK, OK, true>(P, a, n0, col, r, most, w);
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-      if (t >= 0 && r < most) {
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        if (t >= 0 && r < most) {
 #pragma unroll 4
-        for (int p = 0; p < P.parts; ++p) {
-          float u[8];
-          row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, p, t, r), 0, true), u);
+          for (int p = 0; p < P.parts; ++p) {
+            float u[8];
+            row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, p, t, r), 0, true), u);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += u[i];
+            for (int i = 0; i < 8; ++i) v[i] += u[i];
+          }
         }
+        if (rank < rb + 32) {
+          keep_rank(r, rank, v);
+          keep_rank<WK>(r, rank, w);
+        }
+        up_product<WK, finite.value>(w, v, acc);
       }
-      if (rank < rb + 32) {
-        keep_rank(r, rank, v);
-        keep_rank<WK>(r, rank, w);
-      }
-      up_product<WK>(w, v, acc);
-    }
+    });
     store_out<OK>(P, t, token, n0, g, rank > 0, scale, acc, base);
   }
 }
@@ -651,7 +714,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
     cq_v4f acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    down_rounds<XK, WK, RT, UNITS, kFewWaves>(P, at, 0, P.K, false, x, acc);
+    down_rounds<XK, WK, RT, UNITS, kFewWaves, false>(P, at, 0, P.K, false, x, acc);
+    down_again<XK, WK, RT, UNITS, kFewWaves>(P, at, 0, P.K, x, acc);
 #pragma unroll
     for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
     __syncthreads();
@@ -666,7 +730,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
     }
     keep_rank(r, rank, v);
     keep_rank<WK>(r, rank, b);
-    up_product<WK>(b, v, out);
+    up_sums<WK>(out, [&](auto finite) { up_product<WK, finite.value>(b, v, out); });
   }
   store_out<OK>(P, t, token, n0, g, rank > 0, scale, out, base);
 }
@@ -728,29 +792,29 @@ void adapter_up_prompt_kernel(adapter_args P) {
         }
       }
       cq_v4f acc[4];
+      up_sums<WK>(acc, [&](auto finite) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if (rank <= b * 32) continue;
-        float v[8];
-        row_values<CQ_A_F32>(tiles[i].low[b], v);
-        if (rank < b * 32 + 32) keep_rank(b * 32 + g * 8, rank, v);
-        up_product<WK>(w[b], v, acc);
-      }
-#pragma unroll 1
-      for (int rb = NB * 32; ANY && rb < rank; rb += 32) {   // ranks beyond the registers
-        const int r = rb + g * 8;
-        row8<WK> more[4];
-        fetch_up<WK, OK, ANY>(P, a, n0, col, r, rank, more);
-        float v[8];
-        row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, 0, t, r), 0, t < P.T && r < rank), v);
-        if (rank < rb + 32) {
-          keep_rank(r, rank, v);
-          keep_rank<WK>(r, rank, more);
+        for (int b = 0; b < NB; ++b) {
+          if (rank <= b * 32) continue;
+          float v[8];
+          row_values<CQ_A_F32>(tiles[i].low[b], v);
+          if (rank < b * 32 + 32) keep_rank(b * 32 + g * 8, rank, v);
+          up_product<WK, finite.value>(w[b], v, acc);
         }
-        up_product<WK>(more, v, acc);
-      }
+#pragma unroll 1
+        for (int rb = NB * 32; ANY && rb < rank; rb += 32) {   // ranks beyond the registers
+          const int r = rb + g * 8;
+          row8<WK> more[4];
+          fetch_up<WK, OK, ANY>(P, a, n0, col, r, rank, more);
+          float v[8];
+          row_values<CQ_A_F32>(fetch8<CQ_A_F32>(P.low, low_at(P, 0, t, r), 0, t < P.T && r < rank), v);
+          if (rank < rb + 32) {
+            keep_rank(r, rank, v);
+            keep_rank<WK>(r, rank, more);
+          }
+          up_product<WK, finite.value>(more, v, acc);
+        }
+      });
       int token[kOuts];
 #pragma unroll
       for (int n = 0; n < kOuts; ++n) token[n] = match >> ((col & (16 - kOuts)) + n) & 1 ? neighbour(i, n) : -1;

@@ -167,3 +167,37 @@ def test_adapters_of_more_tokens_than_one_launch_takes(B):  # noqa: F811
         bound = A._adapter_roundings(K, 1) * U * mag
         bound = bound + torch.finfo(torch.bfloat16).eps / 2 * (want.abs() + bound) + 1e-40
         assert ((got[t:t + (1 << 24)].double() - want).abs() <= bound).all(), t
+
+
+# ------------------------------------------------------------------------------------------------
+# adapters with infinite weights
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [1, 5, 80, 1100])
+@pytest.mark.parametrize("R,K", [(8, 64), (12, 300), (16, 4096), (40, 1111), (100, 640)])
+@pytest.mark.parametrize("x,w,o", [("f32", "bf16", "f32"), ("f32", "bf16", "bf16"), ("bf16", "bf16", "bf16"), ("f16", "f16", "f32"), ("f32", "f32", "f32"),
+                                   ("bf16", "f32", "f16")])
+def test_adapters_with_infinite_weights(B, T, R, K, x, w, o):  # noqa: F811
+    """An infinite weight makes the infinities that the definition gives, and NaN only where that has 0 times infinity or a difference of
+    infinities.  Small whole numbers: every sum is exact, so everything else is equal to the last bit."""
+    import torch
+    rng = np.random.default_rng(R + K)
+    n, N = 5, 70
+    A_, Bm = rng.integers(-2, 3, (n, R, K)).astype(float), rng.integers(-1, 2, (n, N, R)).astype(float)
+    A_[:, :, rng.random(K) < 0.9] = 0.0                # (sums stay small enough for every type)
+    X, base = rng.integers(-1, 2, (T, K)).astype(float), rng.integers(-3, 4, (T, N)).astype(float)
+    ids = rng.integers(-1, n, T).astype(np.int32)
+    ids[0] = 0
+    ranks = np.array([R, R, max(1, R - 3), R, 1], dtype=np.int32)
+    for a, k in ((0, K - 1), (1, 0), (2, K // 2)):
+        A_[a, ranks[a] - 1, k] = np.inf if a else -np.inf
+    Bm[1, 3, 0], Bm[3, N - 1, R - 1], Bm[3, 5, 0], Bm[4, 0, 0] = np.inf, -np.inf, np.inf, np.inf
+    X[1::7, K - 1], X[0, K - 1] = 0.0, 1.0
+    with np.errstate(invalid="ignore"):
+        want, _ = O.adapter_apply(X, ids, A_, Bm, None, ranks, base)
+    put = lambda v, d: torch.from_numpy(v).to(A._dt(d)).cuda()
+    print(f"T={T} R={R} K={K} {x} {w} {o}", flush=True)
+    ad = B.DeviceAdapters(put(A_, w), put(Bm, w), None, torch.from_numpy(ranks).cuda())
+    for order in (np.arange(T), np.argsort(ids, kind="stable")):
+        got = B.cq_adapter_apply(ad, put(X[order], x), torch.from_numpy(ids[order]).cuda(), base=put(base[order], o))
+        ref = torch.from_numpy(want[order]).to(A._dt(o))
+        assert ((got.cpu() == ref) | (got.cpu().isnan() & ref.isnan())).all()
