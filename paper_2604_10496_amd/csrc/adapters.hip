@@ -199,7 +199,9 @@ __device__ __forceinline__ void quad_transpose(cq_v4u (&r)[4]) {
 // 128 values of K of 16 rows, as operands of four products: a lane of row l % 16 has values (l / 16) * 32 + c * 8 .. +7 as its c-th.
 // The four lanes of rows 4 i .. 4 i + 3 read 64 contiguous bytes of one row after the other and exchange them: lanes that
 // each read their own row take the cache three times as long (out of L2 15 instead of 42 bytes per clock and compute unit).
-template <int KIND>
+// OWN: each lane reads its own row all the same, and exchanges nothing (fp32 rows of few tokens, whose exchange costs more than their
+// loads: one token at rank 16, K = N = 4096 in one launch 10.9 instead of 13.5 us).
+template <int KIND, bool OWN = false>
 struct k_unit {
   static constexpr int kSize = KIND == CQ_A_F32 ? 4 : 2, kSets = KIND == CQ_A_F32 ? 2 : 1;
   cq_v4u raw[kSets][4];
@@ -208,14 +210,17 @@ struct k_unit {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const char* q = reinterpret_cast<const char*>(p) + (row[n] + k + (lane >> 4) * 32) * kSize + (lane & 3) * 16;
+      const size_t from = OWN ? row[0] : row[n];
+      const char* q = reinterpret_cast<const char*>(p) + (from + k + (lane >> 4) * 32) * kSize + (OWN ? n : lane & 3) * 16;
 #pragma unroll
       for (int h = 0; h < kSets; ++h) raw[h][n] = reinterpret_cast<const cq_v4u_any*>(q + h * 64)[0];
     }
   }
   __device__ __forceinline__ void exchange() {
+    if constexpr (!OWN) {
 #pragma unroll
-    for (int h = 0; h < kSets; ++h) quad_transpose(raw[h]);
+      for (int h = 0; h < kSets; ++h) quad_transpose(raw[h]);
+    }
   }
   __device__ __forceinline__ row8<KIND> operand(int c) const {
     row8<KIND> r;
@@ -263,9 +268,9 @@ struct down_place {
   size_t own_row, x_row[4];   // X of the lane's own token, and of the four tokens that its quad reads
 };
 
-template <int XK, int WK, int RT, int UNITS, int WAVES, bool FINITE>
+template <int XK, int WK, int RT, int UNITS, int WAVES, bool FINITE, bool OWN>
 __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_place& at, int k, int k_end, bool fetched,
-                                            k_unit<XK> (&x)[UNITS], cq_v4f (&acc)[RT]) {
+                                            k_unit<XK, OWN> (&x)[UNITS], cq_v4f (&acc)[RT]) {
   constexpr int kRound = 128 * WAVES * UNITS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   // (rows beyond the adapter's rank repeat its last one: their sums are not used)
@@ -307,12 +312,12 @@ __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_pl
     fetched = false;
   }
   if constexpr (UNITS > 1) {
-    k_unit<XK> fewer[UNITS / 2];
-    down_rounds<XK, WK, RT, UNITS / 2, WAVES, FINITE>(P, at, k, k_end, false, fewer, acc);
+    k_unit<XK, OWN> fewer[UNITS / 2];
+    down_rounds<XK, WK, RT, UNITS / 2, WAVES, FINITE, OWN>(P, at, k, k_end, false, fewer, acc);
   } else {
     const int kk = k + wave * 128;
     if (kk + 128 <= k_end) {
-      k_unit<XK> last;   // (x may be wanted again)
+      k_unit<XK, OWN> last;   // (x may be wanted again)
       last.fetch(P.X, at.x_row, kk);
       last.exchange();
 #pragma unroll
@@ -335,13 +340,14 @@ __device__ __forceinline__ void down_rounds(const adapter_args& P, const down_pl
 }
 
 // acc again, where it holds a NaN that finite_weights may spare (x then holds the first round of these tokens, as before)
-template <int XK, int WK, int RT, int UNITS, int WAVES>
-__device__ __forceinline__ void down_again(const adapter_args& P, const down_place& at, int k, int k_end, k_unit<XK> (&x)[UNITS], cq_v4f (&acc)[RT]) {
+template <int XK, int WK, int RT, int UNITS, int WAVES, bool OWN>
+__device__ __forceinline__ void down_again(const adapter_args& P, const down_place& at, int k, int k_end, k_unit<XK, OWN> (&x)[UNITS],
+                                           cq_v4f (&acc)[RT]) {
   if constexpr (product_path<XK, WK>() == kSplit) {
     if (__builtin_expect(!any_nan(acc), 1)) return;
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    down_rounds<XK, WK, RT, UNITS, WAVES, true>(P, at, k, k_end, false, x, acc);
+    down_rounds<XK, WK, RT, UNITS, WAVES, true, OWN>(P, at, k, k_end, false, x, acc);
   }
 }
 
@@ -409,8 +415,8 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(adapter_args P
       cq_v4f acc[RT];
 #pragma unroll
       for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-      down_rounds<XK, WK, RT, UNITS, WAVES, false>(P, at, k_first, k_end, fetched, x, acc);
-      down_again<XK, WK, RT, UNITS, WAVES>(P, at, k_first, k_end, x, acc);
+      down_rounds<XK, WK, RT, UNITS, WAVES, false, false>(P, at, k_first, k_end, fetched, x, acc);
+      down_again<XK, WK, RT, UNITS, WAVES, false>(P, at, k_first, k_end, x, acc);
       fetched = rounds == 1;   // x serves the next adapter's tokens as well
 #pragma unroll
       for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
@@ -710,12 +716,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void adapter_few_kernel(adapter_arg
     at.a = a;
     at.rank = rank;
     at.r0 = 0;
-    k_unit<XK> x[UNITS];
+    constexpr bool kOwn = XK == CQ_A_F32;
+    if (kOwn) at.x_row[0] = at.own_row;
+    k_unit<XK, kOwn> x[UNITS];
     cq_v4f acc[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[i] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-    down_rounds<XK, WK, RT, UNITS, kFewWaves, false>(P, at, 0, P.K, false, x, acc);
-    down_again<XK, WK, RT, UNITS, kFewWaves>(P, at, 0, P.K, x, acc);
+    down_rounds<XK, WK, RT, UNITS, kFewWaves, false, kOwn>(P, at, 0, P.K, false, x, acc);
+    down_again<XK, WK, RT, UNITS, kFewWaves, kOwn>(P, at, 0, P.K, x, acc);
 #pragma unroll
     for (int i = 0; i < RT; ++i) *reinterpret_cast<cq_v4f*>(&lds[wave][col][i * 16 + g * 4]) = acc[i];
     __syncthreads();
@@ -856,14 +864,21 @@ down_plan plan_of(int T, int K) {
   return d;
 }
 
-// One launch instead of two where A is small and its copies are few: up to 65536 values per adapter, read by up to 256 workgroups
-// that read 2^23 values between them; fp32 rows, whose cutting every workgroup repeats, up to 2048 values of K.  Graph replays, bf16
-// rows, one / two launches (us): rank 8, K = 2048, N = 2816, 32 tokens 6.8 / 8.3; rank 16, K = N = 4096, 1 token 8.4 / 8.3, 16 tokens
-// 8.6 / 9.3, 64 tokens 12.2 / 10.2; fp32 rows, 1 token, K = 2048 9.0 / 7.6, K = 4096 13.0 / 8.3.  Called from Python a launch is
-// another 3 us.
+// One launch instead of two where A is small and its copies are few: up to 65536 values per adapter, read by up to 256 workgroups that
+// read 2^23 values between them.  Every workgroup repeats the products of A, so K times the tiles of 16 ranks is bounded by what a product
+// costs: 8192 for 16-bit types, 4096 for cut fp32 rows, 2048 on the fp32 matrix cores.  The bounds stand where the one launch's own time has
+// caught up with the two's (graph replays); called from Python a launch is another 3 us.  One token, N = 2048 to 4096, one / two
+// launches (us), graph, then Python:
+//   bf16 rows, bf16 weights   rank 16, K = 2048  6.4 / 8.2, 8.5 / 12.6   rank 16, 4096  8.3 / 9.2, 8.5 / 12.5   rank 8, 8192  11.6 / 11.2, 11.6 / 12.5
+//                             rank 4, 16384  19.5 / 13.1, 19.5 / 13.4
+//   fp32 rows, bf16 weights   rank 16, K = 2048  7.9 / 9.2, 8.3 / 12.1   rank 16, 4096  10.9 / 10.6, 10.8 / 12.3   rank 8, 5120  12.0 / 10.9, 11.8 / 12.6
+//                             rank 8, 8192  16.5 / 12.3, 16.3 / 12.7
+//   bf16 rows, fp32 weights   rank 16, K = 2048  10.4 / 9.4, 10.3 / 12.7   rank 32, 2048  15.6 / 10.8, 15.3 / 12.6   rank 16, 4096  15.2 / 10.5, 15.0 / 12.7
 bool takes_few(const cq_adapters* W, int x_kind, int T) {
   const long values = (long)W->rank * W->K, blocks = ((long)W->N + 64 * kFewWaves - 1) / (64 * kFewWaves);
-  return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23 && (x_kind != CQ_A_F32 || W->K <= 2048);
+  const int path = x_kind == W->kind && x_kind != CQ_A_F32 ? kSame16 : x_kind == CQ_A_F32 && W->kind == CQ_A_BF16 ? kSplit : kFloat;
+  const long most = path == kSame16 ? 8192 : path == kSplit ? 4096 : 2048;
+  return W->rank <= 32 && values <= 65536 && blocks * T <= 256 && values * blocks * T <= 1l << 23 && (long)W->K * ((W->rank + 15) / 16) <= most;
 }
 
 // Tokens of one pair of launches (at least 8192); longer batches take several.

@@ -191,3 +191,20 @@ def test_workspace_of_adapters_ends_with_the_longest_launch():
         s = B.Adapters(2, 16, 8, N, B.CQ_A_BF16, 256, 256, None, None)
         at = lambda T: real.cq_adapter_workspace_bytes(ctypes.byref(s), B.CQ_A_BF16, T)
         assert at(most - 1) <= at(most) == at(most + 1) == at(1 << 30) == most * 16 * 4
+
+
+def test_few_tokens_take_one_launch_where_it_is_the_faster_form():
+    """No workspace: one launch.  A's products are repeated by every workgroup of it, and cost the more the wider the types."""
+    real = B.load_library()
+    F16, F32, BF16 = B.CQ_A_F16, B.CQ_A_F32, B.CQ_A_BF16
+
+    def one(x, w, T, K, N, R):
+        s = B.Adapters(4, R, K, N, w, 256, 256, None, None)
+        return real.cq_adapter_workspace_bytes(ctypes.byref(s), x, T) == 0
+    for same in (F16, BF16):
+        assert one(same, same, 1, 4096, 4096, 16) and one(same, same, 1, 8192, 2048, 8) and one(same, same, 16, 2048, 2048, 32)
+        assert not one(same, same, 1, 16384, 2048, 4)
+    assert one(F32, BF16, 1, 4096, 4096, 16) and one(F32, BF16, 16, 2048, 2048, 32) and not one(F32, BF16, 1, 5120, 2048, 8)
+    for x, w in ((F32, F32), (BF16, F32), (F16, BF16), (F32, F16)):
+        assert one(x, w, 1, 2048, 2048, 16) and not one(x, w, 1, 2048, 2048, 32) and not one(x, w, 1, 4096, 4096, 16)
+    assert not one(BF16, BF16, 400, 2048, 2048, 16) and not one(BF16, BF16, 1, 512, 512, 33)
