@@ -317,6 +317,7 @@ enum { CQ_GATE_NONE = 0, CQ_GATE_ROW = 1, CQ_GATE_ELEM = 2 };
  *   CQ_A_F32 (what cq_moe_forward takes and gives) or stream_kind.  w_pre, w_post [H] of weight_kind: CQ_A_F32 or stream_kind.
  *   y NULL: x = N(h) * w_pre alone (in front of the first block); h_out is then not written.
  *   x_out NULL: h' alone (behind the last block).  h_out may be h, and x_out may be y if their kinds agree.
+ *   A row whose sum of squares leaves fp32's range has a norm of zeros (NaN where the row is infinite).
  *   1 <= H <= 32768; 0 < eps < inf.
  */
 typedef struct {
@@ -378,7 +379,7 @@ cq_status cq_balance_loss_grad(const void* logits, int logit_kind, const int32_t
  *   rows of A and columns of B, what lies beyond is not used.  1 <= rank <= 256; K, N <= 2^23.
  *   X [T, K] of x_kind with rows ldx values apart; base [T, N] (NULL: zero) and out [T, N] of out_kind, rows ld_base and ld_out
  *   values apart; out may be base.  adapter_ids [T] on the device, in any order.
- *   A_a x_t is held in fp32.  workspace: cq_adapter_workspace_bytes(W, x_kind, T) bytes, which never falls as T grows (few tokens of low
+ *   A_a x_t is held in fp32; infinite weights give the infinities of this definition.  workspace: cq_adapter_workspace_bytes(W, x_kind, T) bytes, which never falls as T grows (few tokens of low
  *   rank need none: 0, NULL allowed).
  */
 typedef struct {

@@ -14,8 +14,8 @@
 // into three bf16 values of 8 bits each, which hold every bit of the fp32 value: three products, each exact in fp32.  The other pairs of
 // types run on the fp32 matrix cores.  Either way A_a x and B_a low are fp32 sums of exact products.
 //
-// 4096 tokens of 9 prompts, K = N = 4096, rank 32, bf16: 19.0 + 18.4 us for 104 MB (2.8 TB/s); 64 requests with adapters of ranks 16 to
-// 64, K = 2048, N = 2816: 6.5 + 10.7 us for 22 MB; one token at rank 16: 4.2 + 7.0 us.
+// 4096 tokens of 9 prompts, K = N = 4096, rank 32, bf16: 18.4 + 18.2 us for 104 MB (2.8 TB/s); 64 requests with adapters of ranks 16 to
+// 64, K = 2048, N = 2816: 7.6 + 10.2 us for 22 MB; one token of fp32 rows at rank 16: 11.5 us in one launch.
 #include <type_traits>
 
 #include "cq_rows.h"
@@ -166,7 +166,7 @@ __device__ __forceinline__ row8<KIND> fetch_k(const void* p, size_t row, int k, 
   return r;
 }
 
-// Units of a round that a kernel has registers for (256 per lane: two workgroups of eight wavefronts per compute unit).
+// Units of a round that a kernel has registers for (256 per lane: one workgroup of eight wavefronts per compute unit, or two of four).
 template <int XK, int WK, int RT>
 constexpr int most_units() {
   return product_path<XK, WK>() == kSame16 ? (RT == 1 ? 4 : 2) : product_path<XK, WK>() == kSplit && RT == 1 ? 2 : 1;

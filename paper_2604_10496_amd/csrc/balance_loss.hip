@@ -2,13 +2,14 @@
 //   p_t = softmax(z_t),  f_se = c_se / (k n_s),  P_se = mean of p_te over the n_s tokens of sequence s that count,
 //   L = alpha / S' sum_s E sum_e f_se P_se (S' sequences with a token),   dz_te = g alpha E / (S' n_s) p_te (f_se - sum_j f_sj p_tj).
 // One pass over the logits in either direction, bound by HBM for long batches and by latency for the others.  L lanes share a
-// token (four neighbouring experts each), so that a wavefront reads 64 / L tokens in one contiguous load, and works on several
-// loads at a time.
+// token (four neighbouring experts each), so that a wavefront reads 64 / L tokens in one contiguous load, and works on the logits of
+// several loads at a time (asked for one behind the other without a mask; with one, each waits for its tokens' mask bytes).
 // Forward: tokens are taken in tiles.  A tile's share of a sequence goes to slot  tile + sequence  of the workspace: from one
 // pair to the next in order either the tile or the sequence grows by one at least, so the slots differ, and a second launch
 // adds every sequence's slots in a fixed order; its last workgroup adds the sequences' losses.  Counts are integers added in LDS;
 // no atomics on floats.  Few logits take one workgroup and one launch.
-// 8192 x 64 in 13 sequences 7.5 + 6.2 us (2.3 MB: latency), 64 x 4 5.8 us; the gradient of 65536 x 128 18.4 us for 67 MB = 3.6 TB/s.
+// 8192 x 64 in 13 sequences with padding 8.4 + 5.4 us (2.3 MB: latency), 64 x 4 5.9 us; the gradient of 65536 x 128 18.3 us for 67 MB =
+// 3.7 TB/s.
 #include <math.h>
 
 #include "cq_rows.h"
@@ -237,8 +238,9 @@ __device__ __forceinline__ void write_slot(const balance_args& P, const balance_
   if (threadIdx.x == 0) W.tokens[slot] = S.n;
 }
 
-// Tiles of one round of loads: everything a tile reads is asked for at once, before the offsets are known; its sequences then take
-// their tokens out of the registers.
+// Tiles of one round of loads: a tile's logits and ids are read once, in front of its sequences, which then take their tokens out of
+// the registers.  Bound by latency, and by more of it than two dependent loads: the offsets, each of four mask bytes and each of four ids
+// (and its token's mask byte) are tested inside a branch of their own, and waited for there.
 template <int KIND, int L>
 __global__ __launch_bounds__(256) void balance_tile_kernel(balance_args P, balance_ws W) {
   constexpr int U = 4, kTokens = U * (256 / L), kIds = 4;

@@ -5,12 +5,14 @@
 // The sums of squares are taken again, together with mean(dn h') in the first of two row sums and with the sum behind a row's
 // gate in the second, so that the forward pass keeps no statistics.
 // Bound by HBM (five or six rows in, two or three out).  One workgroup of 1024 threads per compute unit takes 1024 / NT rows at
-// a time and asks for the next ones before it works on these, so that loads are in flight across the two barriers of a row sum.
+// a time and, where registers allow it (16-bit stream and block, up to 8192 values), asks for the next ones before it works on these, so
+// that loads are in flight across the two barriers of a row sum.  A gate per token is waited for in front of its row's loads.
 // The shares of the weights' gradients stay in registers, are added over a workgroup's rows in LDS and go to the workspace
 // once, [parts][H] each; a second launch adds the parts in order.  No atomics: the results do not depend on timing.
-// 8192 x 4096 in bf16 with a gate per value, 537 MB: 107 us = 5.0 TB/s, and 5.0 us for the sum of the parts; without the next rows in
-// flight, one row per workgroup of 512 threads, 141 us.  2048 x 2048: 18.9 and 3.9 us, two rounds of rows, in which the first
-// loads, the weights and the shares at the end weigh as much as the rows.
+// 8192 x 4096 in bf16 with a gate per value, 537 MB: 106 us = 5.1 TB/s, and 4.8 us for the sum of the parts; a sigmoid gate's
+// exponentials and quotients make it 136 together.  Without the next rows in flight, one row per workgroup of 512 threads, 141 us.
+// 2048 x 2048: 19.0 and 3.9 us (with a gate per token 1.4 more), two rounds of rows, in which the first loads, the weights and the
+// shares at the end weigh as much as the rows.  4096 x 4096, bf16 stream, fp32 block, gate per token (no rows in flight), 302 MB: 69 us.
 #include "block_norm.h"
 
 namespace {
@@ -60,7 +62,9 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_kernel(norm_grad_arg
   // rows of 32 bits, of several groups of eight, and the widest of one group with a gate per value leave no registers for the next row
   constexpr bool kAhead = C == 1 && SK != CQ_A_F32 && BK != CQ_A_F32 && !(ELEM && NT == 1024);
   // Rows of several groups of eight are read again where they are used again (out of the caches) instead of held.  again(): the
-  // compiler takes the pointer as a new one, so that it does not hold them, or the weights from row to row, after all.
+  // compiler takes the pointer as a new one, so that it does not hold them, or the weights from row to row, after all.  The shares
+  // of the weights' gradients and the row's own gradient still need more than the 128 registers of a lane: 116 to 188 bytes of a lane
+  // spill up to 16384 values, 560 to 750 beyond (1024 x 16384, both norms: 125 us for a floor of 39).
   constexpr bool kHold = C == 1;
   auto again = [](const void* p) {
     asm volatile("" : "+s"(p));
