@@ -763,15 +763,20 @@ class DeviceAdapters:
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
         self._layout = self.n, self.rank, self.K, self.N, kind
         self._tensors = A.dtype, A.shape, B.shape, torch.float32, torch.int32, A.shape[:1]
+        self._struct = None, None
         self.struct()
 
     def struct(self) -> Adapters:
         """Checks the tensors; what a call hands to the library."""
         dtype, a, b, f32, i32, row = self._tensors
         scale, ranks = self.scale, self.ranks
-        return Adapters(*self._layout, _tensor(self.A, "A", a, dtype).data_ptr(), _tensor(self.B, "B", b, dtype).data_ptr(),
-                        None if scale is None else _tensor(scale, "scale", row, f32).data_ptr(),
-                        None if ranks is None else _tensor(ranks, "ranks", row, i32).data_ptr())
+        at = (_tensor(self.A, "A", a, dtype).data_ptr(), _tensor(self.B, "B", b, dtype).data_ptr(),
+              None if scale is None else _tensor(scale, "scale", row, f32).data_ptr(),
+              None if ranks is None else _tensor(ranks, "ranks", row, i32).data_ptr())
+        kept = self._struct              # (never written to again: a call of another thread may be reading it)
+        if kept[0] != at:
+            kept = self._struct = at, Adapters(*self._layout, *at)
+        return kept[1]
 
 
 def _rows(t, what: str, shape, dtype=None) -> int:
