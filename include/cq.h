@@ -395,6 +395,118 @@ cq_status cq_adapter_apply(const cq_adapters* W, const void* X, int x_kind, long
                            const void* base, long ld_base, void* out, int out_kind, long ld_out, void* workspace,
                            size_t workspace_bytes, cq_stream stream);
 
+/*
+ * What lies between a block's Q/K/V projection (cq_codebook_grouped_gemm with one group) and its output projection: heads with a norm and
+ * the rotation by position, the paged cache of keys and values, and the attention of single tokens over it.
+ *
+ * Heads are rows of D values of `kind`, n for each token, the rows token_stride (tokens) and head_stride (heads of a token) values apart:
+ * slices of a fused projection's rows need no copy.  They may start on any element.  What is read may overlap (strides of 0 repeat rows);
+ * what is written may not, but may be what is read at the same place.  n <= 16384.  Sums and angles as below; stored values are
+ * rounded to nearest, ties to even, without saturation (saturated to +-448 in a cache of 8 bits).
+ */
+typedef struct {
+  void* p;
+  int kind; /* CQ_A_F32, CQ_A_F16, CQ_A_BF16 */
+  int n;
+  long token_stride, head_stride;
+} cq_heads;
+
+/*
+ * Norms of queries and keys for each head and the rotation by position t (either may be missing):
+ *     N(x) = x / sqrt(mean(x^2) + eps) * w          (w NULL: N(x) = x)
+ *     pairs (a, b) of the first `rot` of D values:  a' = a c - b s,  b' = b c + a s,   (c, s) = rot_scale (cos, sin)(t freq[i])
+ *   pair i is (i, i + rot/2), or with `interleaved` (2i, 2i + 1); the other values are not rotated.  freq [rot/2] f64: radians per
+ *   position; t freq is taken modulo a revolution in 64 bits, so that any 32-bit position keeps the accuracy of fp32.
+ *   w_q, w_k [D] of weight_kind: CQ_A_F32, CQ_A_F16 or CQ_A_BF16.  1 <= D <= 256, rot even, 0 <= rot <= D; 0 < eps < inf.
+ */
+typedef struct {
+  int D, rot, interleaved;
+  int weight_kind;
+  float eps, rot_scale;
+  const double* freq;
+  const void* w_q;
+  const void* w_k;
+} cq_head_spec;
+
+/*
+ * q and k (either may be NULL) of T tokens at positions [T] i32 (NULL with rot = 0) -> q_out, k_out, of the rows' kind or, from fp32
+ * rows, of any.  q_out may be q, and k_out k.  0 <= T <= 2^30.
+ */
+cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, const cq_heads* k, const int32_t* positions, int T,
+                       const cq_heads* q_out, const cq_heads* k_out, cq_stream stream);
+/*
+ * Its gradients, from q and k as the forward pass took them (not read where there is no norm: NULL allowed) and the gradients of its
+ * results (either may be NULL: then that side is left out).  d_q, d_k of the rows' kind; d_w_q, d_w_k [D] of weight_kind (NULL: not
+ * wanted).  Sums in fp32 in an order that depends on the sizes alone.  d_q may be d_q_out, and d_k d_k_out, of one kind.
+ *   workspace: cq_head_norm_grad_workspace_bytes(P, T) bytes, which never falls as T grows; not needed without d_w_q and d_w_k.
+ */
+size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int T);
+cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q, const cq_heads* k, const int32_t* positions, int T,
+                            const cq_heads* d_q_out, const cq_heads* d_k_out, const cq_heads* d_q, const cq_heads* d_k, void* d_w_q,
+                            void* d_w_k, void* workspace, size_t workspace_bytes, cq_stream stream);
+
+/*
+ * A paged cache: `pages` pages of page_size slots, each with a row of D values for every key head, in k and in v alike; page, slot and
+ * head strides in values (heads may lie inside slots or slots inside heads).  kind: CQ_A_F16, CQ_A_BF16 or CQ_C_E4M3 (8-bit floats
+ * of 4 exponent bits without infinities, largest value 448; they stand for k_scale[h] resp. v_scale[h] [heads] f32 times their value, NULL: 1).
+ * Rows are moved 16 bytes at a time: D and the strides are multiples of 8 values (16 of CQ_C_E4M3), D <= 256.
+ */
+enum { CQ_C_E4M3 = 4 };
+typedef struct {
+  int kind;
+  int heads, D, page_size, pages;
+  long page_stride, slot_stride, head_stride;
+  void* k;
+  void* v;
+  const float* k_scale;
+  const float* v_scale;
+} cq_cache;
+/*
+ * The sequences of a call: position p of sequence s lies in slot p % page_size of page page_table[s * stride + p / page_size].  Entries
+ * outside [0, pages) are pages that are not there: nothing is written to or read from them.  lengths [n]: tokens of each sequence, the new ones of
+ * this call among them (the same array serves the append and the attention behind it).  width * page_size <= 2^30.
+ */
+typedef struct {
+  int n, width;
+  long stride;
+  const int32_t* page_table;
+  const int32_t* lengths;
+} cq_sequences;
+
+/*
+ * Keys and values of T new tokens into the cache, keys with P's norm and rotation on the way (P NULL: as they are), and the queries
+ * beside them, if any, into q_out (of q's kind): what cq_head_norm does, in the same launch.  k and v have the cache's heads.
+ *   seq_offsets [S->n + 1] i32, non-decreasing: tokens seq_offsets[s] .. seq_offsets[s+1]-1 are the last ones of sequence s, at positions
+ *   lengths[s] - n_s .. lengths[s] - 1; tokens outside all of them (padding behind the last) are left out and their rows of q_out left as they
+ *   were.  NULL with T = S->n: one new token of every sequence.  Tokens before position 0 or beyond the table's row are left out too;
+ *   those whose page is not there write no key or value.
+ *   positions [T] i32 or NULL: rotate by these instead of by the positions in the cache.
+ *   Two tokens of a call must not share a slot (a page that stands twice among the entries that it writes to): one of the two, or a mixture, would remain.
+ */
+cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, const cq_head_spec* P, const cq_heads* q, const cq_heads* k,
+                          const cq_heads* v, const int32_t* seq_offsets, const int32_t* positions, int T, const cq_heads* q_out,
+                          cq_stream stream);
+
+/*
+ * Attention of one new token per sequence: token s with queries q[s] over the first lengths[s] positions of sequence s; each of the
+ * cache's heads serves q->n / heads queries one after another:
+ *     z_j = scale q.k_j,  softcap > 0: z_j = softcap tanh(z_j / softcap);   window > 0: the last `window` positions only
+ *     out = sum_j e^(z_j) v_j / (sum_j e^(z_j) + e^(sinks[head])),  lse = log of the denominator        (sinks [q->n] f32; NULL: none)
+ *   Positions whose page is not there do not take part; a row without any that does, or all of whose scores are -inf, gives zeros and the
+ *   lse of its sink (-inf without).  What lies behind a sequence's length is not read.  out [S->n, q->n] of any kind; lse [S->n, q->n] f32 or
+ *   NULL.  Scores, softmax and sums in fp32; the products' operands carry 16 bits at least, 22 where q or out is fp32.
+ *   max_length: what the lengths are expected to reach.  The cache is cut into parts for it; longer sequences take longer, no more.
+ *   workspace: cq_cache_attention_workspace_bytes() bytes (0: none needed).
+ */
+typedef struct {
+  float scale, softcap;
+  int window, max_length;
+  const float* sinks;
+} cq_attention_spec;
+size_t cq_cache_attention_workspace_bytes(const cq_cache* C, int n_seqs, int n_query_heads, int max_length, int window);
+cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S, const cq_attention_spec* P, const cq_heads* q, const cq_heads* out,
+                             float* lse, void* workspace, size_t workspace_bytes, cq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

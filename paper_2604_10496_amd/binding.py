@@ -19,6 +19,7 @@ CQ_A_INT8_CODES, CQ_A_F16, CQ_A_F32, CQ_A_BF16 = 0, 1, 2, 3
 CQ_EPI_NONE, CQ_EPI_SWIGLU = 0, 1
 CQ_OUT_F32, CQ_OUT_F16 = 0, 1
 CQ_GATE_NONE, CQ_GATE_ROW, CQ_GATE_ELEM = 0, 1, 2
+CQ_C_E4M3 = 4
 
 EXPORTS = [
     "cq_status_string", "cq_rotate_quant_workspace_bytes", "cq_rotate_quant",
@@ -30,6 +31,8 @@ EXPORTS = [
     "cq_codebook_grouped_gemm_lut", "cq_expand_centroid_budget",
     "cq_block_norm", "cq_block_norm_grad_workspace_bytes", "cq_block_norm_grad", "cq_balance_loss_workspace_bytes",
     "cq_balance_loss", "cq_balance_loss_grad", "cq_adapter_workspace_bytes", "cq_adapter_apply",
+    "cq_head_norm", "cq_head_norm_grad_workspace_bytes", "cq_head_norm_grad", "cq_cache_append", "cq_cache_attention_workspace_bytes",
+    "cq_cache_attention",
 ]
 
 
@@ -63,6 +66,33 @@ class BlockNormSpec(ctypes.Structure):
 class Adapters(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int), ("rank", ctypes.c_int), ("K", ctypes.c_int), ("N", ctypes.c_int), ("kind", ctypes.c_int),
                 ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ranks", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("kind", ctypes.c_int), ("n", ctypes.c_int), ("token_stride", ctypes.c_long),
+                ("head_stride", ctypes.c_long)]
+
+
+class HeadSpec(ctypes.Structure):
+    _fields_ = [("D", ctypes.c_int), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int), ("weight_kind", ctypes.c_int),
+                ("eps", ctypes.c_float), ("rot_scale", ctypes.c_float), ("freq", ctypes.c_void_p), ("w_q", ctypes.c_void_p),
+                ("w_k", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("heads", ctypes.c_int), ("D", ctypes.c_int), ("page_size", ctypes.c_int), ("pages", ctypes.c_int),
+                ("page_stride", ctypes.c_long), ("slot_stride", ctypes.c_long), ("head_stride", ctypes.c_long), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class Sequences(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("width", ctypes.c_int), ("stride", ctypes.c_long), ("page_table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p)]
+
+
+class AttentionSpec(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int), ("max_length", ctypes.c_int),
+                ("sinks", ctypes.c_void_p)]
 
 
 _lib = None
@@ -152,6 +182,19 @@ def load_library() -> ctypes.CDLL:
     lib.cq_stream_read.argtypes = [vp, sz, vp, vp]
     lib.cq_mfma_loop.restype = ci
     lib.cq_mfma_loop.argtypes = [ci, ci, vp, vp]
+    heads, spec, cache, seqs = (ctypes.POINTER(t) for t in (Heads, HeadSpec, Cache, Sequences))
+    lib.cq_head_norm.restype = ci
+    lib.cq_head_norm.argtypes = [spec, heads, heads, vp, ci, heads, heads, vp]
+    lib.cq_head_norm_grad_workspace_bytes.restype = sz
+    lib.cq_head_norm_grad_workspace_bytes.argtypes = [spec, ci]
+    lib.cq_head_norm_grad.restype = ci
+    lib.cq_head_norm_grad.argtypes = [spec, heads, heads, vp, ci, heads, heads, heads, heads, vp, vp, vp, sz, vp]
+    lib.cq_cache_append.restype = ci
+    lib.cq_cache_append.argtypes = [cache, seqs, spec, heads, heads, heads, vp, vp, ci, heads, vp]
+    lib.cq_cache_attention_workspace_bytes.restype = sz
+    lib.cq_cache_attention_workspace_bytes.argtypes = [cache, ci, ci, ci, ci]
+    lib.cq_cache_attention.restype = ci
+    lib.cq_cache_attention.argtypes = [cache, seqs, ctypes.POINTER(AttentionSpec), heads, heads, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -827,3 +870,247 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
     if st:
         raise CqError(st)
     return out
+
+
+# ------------------------------------------------------------------------------------------------
+# heads, the paged cache and attention over it
+# ------------------------------------------------------------------------------------------------
+def _heads(t, what: str, shape, dtype, device) -> Heads:
+    """Checks heads [T, n, D] (None: any number) on the GPU, a head's values one after another; what a call hands to the library."""
+    if not t.is_cuda:
+        raise ValueError(f"{what}: not on the GPU")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device} where {device} is needed")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype} where {dtype} is needed")
+    if t.dim() != 3 or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    token, head, one = t.stride()
+    if one != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what}: a head's values are {one} apart")
+    return Heads(t.data_ptr(), _kind(t.dtype, what), t.shape[1], token, head)
+
+
+def _out_heads(t, what: str, like, dtype):
+    """The output of rows like these: a tensor of the caller's whose rows do not overlap, or a new one."""
+    import torch
+    if t is None:
+        t = torch.empty(like.shape, dtype=dtype, device=like.device)
+        T, n, D = like.shape
+        return t, Heads(t.data_ptr(), _kind(dtype, what), n, n * D, D)
+    h = _heads(t, what, like.shape, dtype, like.device)
+    T, n, D = t.shape
+    a, b = sorted(((h.token_stride, T), (h.head_stride, n)))
+    # (the nearer of the two steps over a row, the farther over all rows of the nearer)
+    if T > 1 and n > 1 and (a[0] < D or b[0] < (a[1] - 1) * a[0] + D):
+        raise ValueError(f"{what}: rows of strides {t.stride()} overlap")
+    return t, h
+
+
+def _on_device(call, device, *args):
+    """call(*args, stream) on the current stream of that device, whichever device is the current one."""
+    import torch
+    index = device.index
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            st = call(*args, torch.cuda.current_stream(index).cuda_stream)
+    else:
+        st = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st:
+        raise CqError(st)
+
+
+def _ints(t, what: str, shape, device, dtype=None):
+    """The address of a contiguous i32 tensor on that device (None: 0)."""
+    import torch
+    if t is None:
+        return None
+    _tensor(t, what, shape, torch.int32 if dtype is None else dtype)
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device} where {device} is needed")
+    return t.data_ptr()
+
+
+class HeadNorm:
+    """Norms of queries and keys for each head of D values, and the rotation by position (cq_head_spec).
+
+    w_q, w_k [D]: the norms' weights (None: no such norm).  freq [rot / 2] f64: radians per position of each pair of the first rot
+    values (None: no rotation); pairs are (i, i + rot / 2), or with interleaved (2i, 2i + 1); rot_scale: factor on cosine and sine.
+    The tensors may be replaced by others of their size and type, and the numbers changed: a call takes what is there, and looks at the
+    tensors anew."""
+
+    def __init__(self, D: int, w_q=None, w_k=None, eps: float = 1e-6, freq=None, interleaved: bool = False, rot_scale: float = 1.0):
+        self.D, self.eps, self.interleaved, self.rot_scale = int(D), float(eps), bool(interleaved), float(rot_scale)
+        self.w_q, self.w_k, self.freq = w_q, w_k, freq
+        some = w_q if w_q is not None else w_k
+        if some is not None:
+            self.struct(some.device)
+        elif freq is not None:
+            self.struct(freq.device)
+
+    def struct(self, device) -> HeadSpec:
+        """Checks the tensors; what a call hands to the library."""
+        import torch
+        shape, some, rot = (self.D,), self.w_q if self.w_q is not None else self.w_k, 0
+        if self.freq is not None:
+            _ints(self.freq, "freq", (None,), device, torch.float64)
+            rot = 2 * self.freq.shape[0]
+        weights = CQ_A_F32 if some is None else _kind(some.dtype, "weights")
+        return HeadSpec(self.D, rot, self.interleaved, weights, self.eps, self.rot_scale, self.freq.data_ptr() if rot else None,
+                        None if self.w_q is None else _ints(self.w_q, "w_q", shape, device, some.dtype),
+                        None if self.w_k is None else _ints(self.w_k, "w_k", shape, device, some.dtype))
+
+
+def cq_head_norm(norm: HeadNorm, q=None, k=None, positions=None, q_out=None, k_out=None, out_dtype=None) -> Dict[str, object]:
+    """Norm and rotation of queries q [T, Hq, D] and keys k [T, Hk, D] (either may be None) at positions [T] i32: {"q", "k"}.
+
+    q and k may be slices of a fused projection's rows.  out_dtype: of new outputs (None: the rows'); fp32 rows may become any type.
+    q_out may be q, and k_out k."""
+    lib = _lib or load_library()
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q, k: there are neither queries nor keys")
+    device, T = some.device, some.shape[0]
+    spec = norm.struct(device)
+    positions = _ints(positions, "positions", (T,), device)
+    args, out = [], {"q": None, "k": None}
+    for name, x, given in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            args.append((None, None))
+            continue
+        h = _heads(x, name, (T, None, norm.D), some.dtype, device)
+        out[name], o = _out_heads(given, name + "_out", x, out_dtype or (x.dtype if given is None else given.dtype))
+        args.append((h, o))
+    (hq, oq), (hk, ok) = args
+    _on_device(lib.cq_head_norm, device, spec, hq, hk, positions, T, oq, ok)
+    return out
+
+
+def cq_head_norm_grad(norm: HeadNorm, q=None, k=None, positions=None, dq=None, dk=None, want_weights: bool = True) -> Dict[str, object]:
+    """Gradients of cq_head_norm from its q and k and the gradients dq, dk of its results (either may be None): {"dq", "dk", "dw_q", "dw_k"},
+    of the types of q, k and the weights; None where there is no such input.  q and k give the types also where there is no norm."""
+    import torch
+    lib = _lib or load_library()
+    some = dq if dq is not None else dk
+    if some is None:
+        raise ValueError("dq, dk: there are no gradients")
+    device, T = some.device, some.shape[0]
+    spec = norm.struct(device)
+    positions = _ints(positions, "positions", (T,), device)
+    out = {"dq": None, "dk": None, "dw_q": None, "dw_k": None}
+    x_of, d_of, o_of, w_of, dtype = [None] * 2, [None] * 2, [None] * 2, [None] * 2, None
+    for i, (name, x, d, w) in enumerate((("q", q, dq, norm.w_q), ("k", k, dk, norm.w_k))):
+        if d is None:
+            continue
+        if x is None:
+            raise ValueError(f"{name}: its gradient needs it")
+        dtype = dtype or x.dtype
+        x_of[i] = _heads(x, name, (T, None, norm.D), dtype, device)
+        d_of[i] = _heads(d, "d" + name, tuple(x.shape), some.dtype, device)
+        out["d" + name], o_of[i] = _out_heads(None, "d" + name, x, dtype)
+        if want_weights and w is not None:
+            out["dw_" + name] = w_of[i] = torch.empty_like(w)
+    ws, nbytes = None, 0
+    if w_of[0] is not None or w_of[1] is not None:
+        nbytes = lib.cq_head_norm_grad_workspace_bytes(spec, T)
+        ws = _scratch(some, nbytes)
+    _on_device(lib.cq_head_norm_grad, device, spec, x_of[0], x_of[1], positions, T, d_of[0], d_of[1], o_of[0], o_of[1], _ptr(w_of[0]),
+               _ptr(w_of[1]), _ptr(ws), nbytes)
+    return out
+
+
+class PagedCache:
+    """A paged cache of keys and values (cq_cache): k, v [pages, page_size, heads, D] of float16, bfloat16 or float8_e4m3fn, alike in strides, a
+    row's D values one after another (a permuted view of pages with heads outside slots will do).  k_scale, v_scale [heads] f32 (None: 1):
+    what the values of an 8-bit cache are to be multiplied by.
+
+    The tensors may be replaced by others of their size and type: a call takes what is there, and looks at them anew."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct()
+
+    def struct(self) -> Cache:
+        """Checks the tensors; what a call hands to the library."""
+        import torch
+        k, v = self.k, self.v
+        kind = {torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16, torch.float8_e4m3fn: CQ_C_E4M3}.get(k.dtype)
+        if kind is None:
+            raise ValueError(f"k: {k.dtype} is not one of float16, bfloat16, float8_e4m3fn")
+        if not k.is_cuda or v.device != k.device:
+            raise ValueError("k, v: not on one GPU")
+        stride = k.stride()
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != stride or stride[3] != 1:
+            raise ValueError(f"k, v: {k.dtype} {tuple(k.shape)} {stride} and {v.dtype} {tuple(v.shape)} {v.stride()} are not pages of one layout")
+        pages, size, heads, D = k.shape
+        f32 = torch.float32
+        return Cache(kind, heads, D, size, pages, stride[0], stride[1], stride[2], k.data_ptr(), v.data_ptr(),
+                     None if self.k_scale is None else _ints(self.k_scale, "k_scale", (heads,), k.device, f32),
+                     None if self.v_scale is None else _ints(self.v_scale, "v_scale", (heads,), k.device, f32))
+
+
+def _sequences(page_table, lengths, device) -> Sequences:
+    width = _rows_of_table(page_table, device)
+    S = page_table.shape[0]
+    return Sequences(S, page_table.shape[1], width, page_table.data_ptr(), _ints(lengths, "lengths", (S,), device))
+
+
+def _rows_of_table(t, device) -> int:
+    import torch
+    if t.device != device:
+        raise ValueError(f"page_table: on {t.device} where {device} is needed")
+    return _rows(t, "page_table", (None, None), torch.int32)
+
+
+def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=None, positions=None, norm: Optional[HeadNorm] = None, q=None,
+                    q_out=None):
+    """Keys and values k, v [T, heads, D] of new tokens into the cache, keys with norm and rotation on the way; returns the queries q [T, Hq, D]
+    with theirs (None without).
+
+    page_table [S, width] i32, lengths [S] i32 with the new tokens counted; seq_offsets [S + 1] i32: the new tokens of each sequence (None:
+    one each); positions [T] i32: rotate by these instead of by the positions in the cache.  Rows of tokens outside all sequences are
+    not written (in a new q_out they hold anything)."""
+    lib = _lib or load_library()
+    device, T = k.device, k.shape[0]
+    c = cache.struct()
+    if cache.k.device != device:
+        raise ValueError(f"k: on {device}, the cache on {cache.k.device}")
+    s = _sequences(page_table, lengths, device)
+    spec = None if norm is None else norm.struct(device)
+    shape, dtype = (T, c.heads, c.D), k.dtype
+    hk, hv = _heads(k, "k", shape, dtype, device), _heads(v, "v", shape, dtype, device)
+    hq = oq = None
+    if q is not None:
+        hq = _heads(q, "q", (T, None, c.D), dtype, device)
+        q_out, oq = _out_heads(q_out, "q_out", q, dtype)
+    _on_device(lib.cq_cache_append, device, c, s, spec, hq, hk, hv, _ints(seq_offsets, "seq_offsets", (s.n + 1,), device),
+               _ints(positions, "positions", (T,), device), T, oq)
+    return q_out if q is not None else None
+
+
+def cq_cache_attention(cache: PagedCache, q, page_table, lengths, scale: Optional[float] = None, max_length: Optional[int] = None,
+                       window: int = 0, softcap: float = 0.0, sinks=None, out=None, out_dtype=None, want_lse: bool = True) -> Dict[str, object]:
+    """Attention of one new token per sequence, queries q [S, Hq, D], over the first lengths[s] positions (window > 0: the last ones) of
+    the cache: {"out" [S, Hq, D], "lse" [S, Hq] f32 or None}.
+
+    scale: D ** -0.5 if None.  max_length: what the lengths are expected to reach (None: all that the page table's rows can hold).  sinks
+    [Hq] f32: logits that join the denominator."""
+    import torch
+    lib = _lib or load_library()
+    device = q.device
+    c = cache.struct()
+    if cache.k.device != device:
+        raise ValueError(f"q: on {device}, the cache on {cache.k.device}")
+    s = _sequences(page_table, lengths, device)
+    hq = _heads(q, "q", (s.n, None, c.D), None, device)
+    S, Hq = s.n, hq.n
+    if max_length is None:
+        max_length = s.width * c.page_size
+    spec = AttentionSpec(c.D ** -0.5 if scale is None else scale, softcap, window, max_length,
+                         None if sinks is None else _ints(sinks, "sinks", (Hq,), device, torch.float32))
+    out, ho = _out_heads(out, "out", q, out_dtype or (q.dtype if out is None else out.dtype))
+    lse = torch.empty((S, Hq), dtype=torch.float32, device=device) if want_lse else None
+    nbytes = lib.cq_cache_attention_workspace_bytes(c, S, Hq, max_length, window)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _on_device(lib.cq_cache_attention, device, c, s, spec, hq, ho, _ptr(lse), _ptr(ws), nbytes)
+    return {"out": out, "lse": lse}

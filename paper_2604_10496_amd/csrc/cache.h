@@ -1,0 +1,66 @@
+// The paged cache of keys and values as the operators that fill and read it see it (gfx950 only): checks and addresses.
+#ifndef CQ_CACHE_H_
+#define CQ_CACHE_H_
+
+#include "heads.h"
+
+namespace {
+
+inline int cache_elem(int kind) { return kind == CQ_C_E4M3 ? 1 : 2; }
+
+inline cq_status check_cache(const cq_cache* C) {
+  if (!C) return CQ_ERR_NULL;
+  if (C->kind != CQ_A_F16 && C->kind != CQ_A_BF16 && C->kind != CQ_C_E4M3) return CQ_ERR_UNSUPPORTED;
+  const int whole = 16 / cache_elem(C->kind);   // rows are moved in pieces of 16 bytes
+  if (C->D <= 0 || C->D > kMaxHeadWidth || C->D % whole != 0) return CQ_ERR_SHAPE;
+  if (C->heads <= 0 || C->heads > kMaxHeads || C->page_size <= 0 || C->pages < 0) return CQ_ERR_SHAPE;
+  if (C->page_stride < 0 || C->slot_stride < C->D || C->head_stride < C->D) return CQ_ERR_SHAPE;
+  if (C->page_stride % whole != 0 || C->slot_stride % whole != 0 || C->head_stride % whole != 0) return CQ_ERR_SHAPE;
+  if (((uintptr_t)C->k | (uintptr_t)C->v) % 16 != 0) return CQ_ERR_SHAPE;
+  if (C->kind != CQ_C_E4M3 && (C->k_scale || C->v_scale)) return CQ_ERR_UNSUPPORTED;
+  if (C->pages > 0 && (!C->k || !C->v)) return CQ_ERR_NULL;
+  return CQ_OK;
+}
+
+inline cq_status check_sequences(const cq_sequences* S, const cq_cache* C) {
+  if (!S) return CQ_ERR_NULL;
+  if (S->n < 0 || S->width < 0 || S->stride < 0 || (S->n > 1 && S->stride < S->width)) return CQ_ERR_SHAPE;
+  if ((long)S->width * C->page_size > 1l << 30) return CQ_ERR_SHAPE;   // (positions are counted in 32 bits)
+  if (S->n > 0 && (!S->lengths || (S->width > 0 && !S->page_table))) return CQ_ERR_NULL;
+  return CQ_OK;
+}
+
+struct cache_args {
+  int heads, D, page_size, pages;
+  long page, slot, head;   // values between pages, slots and heads
+  void *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t *table, *lengths;
+  int n_seqs, width;
+  long table_stride;
+};
+
+inline cache_args make_cache_args(const cq_cache* C, const cq_sequences* S) {
+  cache_args a;
+  a.heads = C->heads;
+  a.D = C->D;
+  a.page_size = C->page_size;
+  a.pages = C->pages;
+  a.page = C->page_stride;
+  a.slot = C->slot_stride;
+  a.head = C->head_stride;
+  a.k = C->k;
+  a.v = C->v;
+  a.k_scale = C->k_scale;
+  a.v_scale = C->v_scale;
+  a.table = S->page_table;
+  a.lengths = S->lengths;
+  a.n_seqs = S->n;
+  a.width = S->width;
+  a.table_stride = S->stride;
+  return a;
+}
+
+}  // namespace
+
+#endif  // CQ_CACHE_H_

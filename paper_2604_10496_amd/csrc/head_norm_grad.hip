@@ -1,0 +1,228 @@
+// Gradients of the norms of queries and keys for each head with the rotation, from the rows as the forward pass took them and the
+// gradients of its results.  Per row, with r = 1 / sqrt(mean x^2 + eps):
+//     g = the rotation's transpose of dy,   dw += g x r,   dx = r (g w - x r^2 mean(g w x));   without a norm dx = g.
+// Both sums of a row are taken in one pass.  Bound by HBM (two rows in, one out; one in without a norm).  The shares of the weights'
+// gradients stay in registers, are added over a workgroup's rows in LDS and go to the workspace once; a second launch adds the
+// workgroups' in order.  No atomics: the results do not depend on timing.
+#include "heads.h"
+
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kMostParts = 256;   // one workgroup per compute unit
+constexpr int kRows = 2;          // rows of a lane in flight
+
+inline int weight_parts(int T) { return T < kMostParts ? T : kMostParts; }
+inline size_t weight_row(int D) { return cq_align_up((size_t)D, 8); }
+
+struct head_grad_args {
+  head_layout L;
+  int T, split, rows_per_unit, wkind;   // a unit: one token, rows_per_unit of its heads; split units per token
+  float eps, rot_scale, inv_D;
+  const double* freq;
+  const void *w_q, *w_k;
+  const int32_t* positions;
+  head_rows q, k, dq_out, dk_out, dq, dk;
+  float* part;   // [workgroups][2][D], NULL: not wanted
+};
+
+template <int XK, int OK, int LANES>
+__global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
+  constexpr int kAtOnce = 64 / LANES;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const head_slot s(A.L, lane % LANES);
+  float w_q[8], w_k[8], acc_q[8], acc_k[8];
+  head_weights(A.w_q, A.wkind, s, w_q);
+  head_weights(A.w_k, A.wkind, s, w_k);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc_q[e] = acc_k[e] = 0.f;
+  const int rows = A.q.n + A.k.n;
+  const long units = (long)A.T * A.split;
+  // the workgroups take units in turn, so that few tokens spread out
+  for (long unit = (long)wave * gridDim.x + blockIdx.x; unit < units; unit += (long)kWaves * gridDim.x) {
+    const int t = (int)(unit / A.split), from = (int)(unit - (long)t * A.split) * A.rows_per_unit;
+    const int end = min(rows, from + A.rows_per_unit);
+    head_raw<XK> raw_x[kRows];
+    head_raw<OK> raw_d[kRows];
+    auto fetch = [&](int first) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int r = first + i * kAtOnce;
+        const bool key = r >= A.q.n;
+        const int h = key ? r - A.q.n : r;
+        const bool norm = key ? A.w_k != nullptr : A.w_q != nullptr;
+        raw_d[i] = head_fetch<OK>(key ? A.dk_out.p : A.dq_out.p, t * (key ? A.dk_out.token : A.dq_out.token) + h * (key ? A.dk_out.head : A.dq_out.head),
+                                  s, r < end);
+        raw_x[i] = head_fetch<XK>(key ? A.k.p : A.q.p, t * (key ? A.k.token : A.q.token) + h * (key ? A.k.head : A.q.head), s, r < end && norm);
+      }
+    };
+    int row = from + lane / LANES;
+    fetch(row);
+    const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.L.rot ? A.positions[t] : 0);
+    for (int first = from; first < end; first += kRows * kAtOnce, row += kRows * kAtOnce) {
+      float x[kRows][8], g[kRows][8];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        head_values<XK>(raw_x[i], x[i]);
+        head_values<OK>(raw_d[i], g[i]);
+      }
+      if (first + kRows * kAtOnce < end) fetch(row + kRows * kAtOnce);
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int r = row + i * kAtOnce;
+        const bool key = r >= A.q.n;
+        const int h = key ? r - A.q.n : r;
+        turn_values<true>(A.L, s, turn, g[i]);
+        if (A.w_q || A.w_k) {
+          float w[8], ss = 0.f, gx = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = key ? w_k[e] : w_q[e];
+            ss = fmaf(x[i][e], x[i][e], ss);
+            gx = fmaf(g[i][e] * w[e], x[i][e], gx);
+          }
+          const float rn = 1.f / sqrtf(row_sum<LANES>(ss) * A.inv_D + A.eps);
+          const float back = rn * rn * (row_sum<LANES>(gx) * A.inv_D);
+          if (key ? A.w_k != nullptr : A.w_q != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float share = g[i][e] * (x[i][e] * rn);   // (0 where the row is not there: both were read as 0)
+              acc_q[e] += key ? 0.f : share;
+              acc_k[e] += key ? share : 0.f;
+              g[i][e] = rn * fmaf(-back, x[i][e], g[i][e] * w[e]);
+            }
+          }
+        }
+        if (r < end)
+          head_store<XK>(const_cast<void*>(key ? A.dk.p : A.dq.p), t * (key ? A.dk.token : A.dq.token) + h * (key ? A.dk.head : A.dq.head), s, g[i]);
+      }
+    }
+  }
+  if (!A.part) return;
+  __shared__ float lds[kWaves][2 * kMaxHeadWidth];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2) {
+      acc_q[e] += __shfl_xor(acc_q[e], d);
+      acc_k[e] += __shfl_xor(acc_k[e], d);
+    }
+  }
+  if (lane < LANES) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = (e < 4 ? s.a : s.b) + (e & 3);
+      if ((e & 3) < (e < 4 ? s.na : s.nb)) {
+        lds[wave][c] = acc_q[e];
+        lds[wave][A.L.D + c] = acc_k[e];
+      }
+    }
+  }
+  __syncthreads();
+  const int Dp = (A.L.D + 7) & ~7;
+  for (int c = threadIdx.x; c < 2 * A.L.D; c += kThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int n = 0; n < kWaves; ++n) v += lds[n][c];
+    const int key = c >= A.L.D;
+    A.part[(size_t)blockIdx.x * 2 * Dp + key * Dp + c - key * A.L.D] = v;
+  }
+}
+
+// d_w[c] = sum of the parts in order: 32 columns per workgroup, every eighth of 32 groups of threads takes four of them
+template <int WK>
+__global__ __launch_bounds__(256) void head_weight_sum_kernel(const float* part, int parts, int D, void* dw_q, void* dw_k) {
+  __shared__ float lds[32][33];
+  void* out = blockIdx.y == 0 ? dw_q : dw_k;
+  if (!out) return;
+  const int Dp = (D + 7) & ~7, c = blockIdx.x * 32 + (threadIdx.x & 7) * 4, g = threadIdx.x >> 3;
+  const float* p = part + (size_t)blockIdx.y * Dp;
+  cq_v4f s = {0.f, 0.f, 0.f, 0.f};
+  if (c < Dp) {   // (what lies between D and Dp is read and not used)
+#pragma unroll 8
+    for (int b = g; b < parts; b += 32) s += *reinterpret_cast<const cq_v4f*>(p + (size_t)b * 2 * Dp + c);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lds[g][(threadIdx.x & 7) * 4 + i] = s[i];
+  __syncthreads();
+  if (threadIdx.x < 32 && blockIdx.x * 32 + threadIdx.x < D) {
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += lds[i][threadIdx.x];
+    elem_store<WK>(out, blockIdx.x * 32 + threadIdx.x, v);
+  }
+}
+
+}  // namespace
+
+extern "C" size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int T) {
+  if (check_head_spec(P) != CQ_OK || T < 0) return 0;
+  return cq_align_up((size_t)(weight_parts(T)) * 2 * weight_row(P->D) * 4, 256);
+}
+
+extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q, const cq_heads* k, const int32_t* positions, int T,
+                                       const cq_heads* d_q_out, const cq_heads* d_k_out, const cq_heads* d_q, const cq_heads* d_k,
+                                       void* d_w_q, void* d_w_k, void* workspace, size_t workspace_bytes, cq_stream stream) {
+  cq_status st = check_head_spec(P);
+  if (st != CQ_OK) return st;
+  if (T < 0 || T > 1 << 30) return CQ_ERR_SHAPE;
+  if ((!d_q_out && !d_k_out) || (d_q_out && !d_q) || (d_k_out && !d_k)) return CQ_ERR_NULL;
+  const bool norm_q = d_q_out && P->w_q, norm_k = d_k_out && P->w_k;
+  if ((norm_q && !q) || (norm_k && !k) || (d_w_q && !norm_q) || (d_w_k && !norm_k)) return CQ_ERR_NULL;
+  if ((st = check_heads(d_q_out, T)) != CQ_OK || (st = check_heads(d_k_out, T)) != CQ_OK) return st;
+  if ((st = check_heads_out(d_q_out, d_q, T, P->D)) != CQ_OK || (st = check_heads_out(d_k_out, d_k, T, P->D)) != CQ_OK) return st;
+  if (norm_q && ((st = check_heads(q, T)) != CQ_OK || (st = q->n == d_q->n ? CQ_OK : CQ_ERR_SHAPE) != CQ_OK)) return st;
+  if (norm_k && ((st = check_heads(k, T)) != CQ_OK || (st = k->n == d_k->n ? CQ_OK : CQ_ERR_SHAPE) != CQ_OK)) return st;
+  const int kind = d_q_out ? d_q->kind : d_k->kind, out = d_q_out ? d_q_out->kind : d_k_out->kind;
+  if ((d_q_out && d_k_out && (d_k->kind != kind || d_k_out->kind != out)) || (out != kind && kind != CQ_A_F32)) return CQ_ERR_UNSUPPORTED;
+  if ((norm_q && q->kind != kind) || (norm_k && k->kind != kind)) return CQ_ERR_UNSUPPORTED;
+  const bool weights = d_w_q || d_w_k;
+  if (weights && (!workspace || workspace_bytes < cq_head_norm_grad_workspace_bytes(P, T))) return CQ_ERR_WORKSPACE;
+  if (T > 0 && P->rot > 0 && !positions) return CQ_ERR_NULL;
+  if (T == 0 && !weights) return CQ_OK;
+  hipStream_t str = (hipStream_t)stream;
+  head_grad_args a;
+  a.L = make_head_layout(P->D, P->rot, P->interleaved != 0);
+  a.T = T;
+  a.wkind = P->weight_kind;
+  a.eps = P->eps;
+  a.rot_scale = P->rot_scale;
+  a.inv_D = 1.f / (float)P->D;
+  a.freq = P->freq;
+  a.w_q = norm_q ? P->w_q : nullptr;
+  a.w_k = norm_k ? P->w_k : nullptr;
+  a.positions = positions;
+  a.q = make_head_rows(norm_q ? q : nullptr);
+  a.k = make_head_rows(norm_k ? k : nullptr);
+  a.dq_out = make_head_rows(d_q_out);
+  a.dk_out = make_head_rows(d_k_out);
+  a.dq = make_head_rows(d_q_out ? d_q : nullptr);
+  a.dk = make_head_rows(d_k_out ? d_k : nullptr);
+  a.q.n = a.dq.n;   // (the rows are counted there, also where they are not read)
+  a.k.n = a.dk.n;
+  a.part = weights ? (float*)workspace : nullptr;
+  const int parts = weight_parts(T);
+  if (T > 0) {
+    const int rows = a.q.n + a.k.n, step = kRows * 64 / a.L.lanes;
+    int split = 1;
+    while (split * 2 * step <= rows + step && (long)T * split < 2 * kMostParts * kWaves) split *= 2;
+    a.rows_per_unit = (int)cq_align_up((size_t)((rows + split - 1) / split), step);
+    a.split = (rows + a.rows_per_unit - 1) / a.rows_per_unit;
+#define LAUNCH(XK, OK, LANES) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES>), dim3(parts), dim3(kThreads), 0, str, a)
+    if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F16, CQ_A_F16);
+    else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_BF16, CQ_A_BF16);
+    else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F32);
+    else if (out == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F16);
+    else CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_BF16);
+#undef LAUNCH
+  }
+  if (weights) {
+    const dim3 grid((P->D + 31) / 32, 2);
+#define SUM(WK) hipLaunchKernelGGL((head_weight_sum_kernel<WK>), grid, dim3(256), 0, str, a.part, T > 0 ? parts : 0, P->D, d_w_q, d_w_k)
+    if (P->weight_kind == CQ_A_F32) SUM(CQ_A_F32);
+    else if (P->weight_kind == CQ_A_F16) SUM(CQ_A_F16);
+    else SUM(CQ_A_BF16);
+#undef SUM
+  }
+  return cq_check_launch();
+}

@@ -1,0 +1,336 @@
+// Heads of queries, keys and values as the operators behind the Q/K/V projection see them (gfx950 only): rows of D values, one per
+// token and head, with a norm and a rotation by the token's position:
+//     r = 1 / sqrt(mean x^2 + eps),  n = x r w,   pairs (a, b) of the first `rot` values:  a' = n_a c - n_b s,  b' = n_b c + n_a s,
+//     (c, s) = m (cos, sin)(position freq_i)
+// A row belongs to 8, 16, 32 or 64 neighbouring lanes, each of which holds eight values in two quads that are chosen so that both
+// values of a pair lie in the same lane: four values and their partners half a rotation further, or eight neighbours.  What is not
+// rotated follows in lanes of eight neighbours.  The angle is taken modulo one revolution in 64 bits: in 32 bits a position of 10^5
+// would leave it 2^-8 radians off.
+#ifndef CQ_HEADS_H_
+#define CQ_HEADS_H_
+
+#include <math.h>
+
+#include "cq_rows.h"
+
+namespace {
+
+constexpr int kMaxHeadWidth = 256;
+constexpr int kMaxHeads = 1 << 14;
+constexpr float kMostE4M3 = 448.f;
+
+// ---- host side --------------------------------------------------------------------------------
+
+// how the lanes of a row share its values
+struct head_layout {
+  int D, rot, inter;
+  int turned;   // lanes that hold rotated values
+  int lanes;    // 8, 16, 32 or 64
+};
+
+inline head_layout make_head_layout(int D, int rot, int inter) {
+  head_layout L;
+  L.D = D;
+  L.rot = rot;
+  L.inter = inter;
+  L.turned = inter ? (rot + 7) / 8 : (rot / 2 + 3) / 4;
+  const int need = L.turned + (D - rot + 7) / 8;
+  L.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : 64;
+  return L;
+}
+
+inline cq_status check_head_spec(const cq_head_spec* P) {
+  if (!P) return CQ_ERR_NULL;
+  if (P->D <= 0 || P->D > kMaxHeadWidth || P->rot < 0 || P->rot > P->D || P->rot % 2 != 0) return CQ_ERR_SHAPE;
+  if (!isfinite(P->rot_scale)) return CQ_ERR_SHAPE;
+  if ((P->w_q || P->w_k) && (!(P->eps > 0.f) || !isfinite(P->eps))) return CQ_ERR_SHAPE;
+  if (P->rot > 0 && !P->freq) return CQ_ERR_NULL;
+  if ((P->w_q || P->w_k) && !cq_row_kind(P->weight_kind)) return CQ_ERR_UNSUPPORTED;
+  return CQ_OK;
+}
+
+// rows that a call reads (NULL: there are none)
+inline cq_status check_heads(const cq_heads* h, int T) {
+  if (!h) return CQ_OK;
+  if (h->n <= 0 || h->n > kMaxHeads) return CQ_ERR_SHAPE;
+  if (!cq_row_kind(h->kind)) return CQ_ERR_UNSUPPORTED;
+  if (T > 0 && !h->p) return CQ_ERR_NULL;
+  return CQ_OK;
+}
+
+// rows that a call writes: as many heads, none on another's place
+inline cq_status check_heads_out(const cq_heads* in, const cq_heads* out, int T, int D) {
+  if (!in) return CQ_OK;
+  if (!out) return CQ_ERR_NULL;
+  const cq_status st = check_heads(out, T);
+  if (st != CQ_OK) return st;
+  if (out->n != in->n || (out->n > 1 && out->head_stride < D) || (T > 1 && out->token_stride < D)) return CQ_ERR_SHAPE;
+  return CQ_OK;
+}
+
+struct head_rows {
+  const void* p;
+  long token, head;   // values between tokens and between heads
+  int n;
+};
+
+inline head_rows make_head_rows(const cq_heads* h) {
+  head_rows r = {nullptr, 0, 0, 0};
+  if (h) r = {h->p, h->token_stride, h->head_stride, h->n};
+  return r;
+}
+
+inline head_rows rows_from(head_rows r, int kind, long token) {
+  r.p = row_at(r.p, kind, (size_t)(token * r.token));
+  return r;
+}
+
+// ---- device side ------------------------------------------------------------------------------
+
+// four consecutive values as they lie in memory, on any element
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t cq_v2u;
+typedef cq_v2u cq_v2u_any __attribute__((aligned(2)));
+
+template <int KIND>
+struct quad {
+  static constexpr int N = KIND == CQ_A_F32 ? 4 : 2;
+  uint32_t w[N];
+};
+
+template <int KIND>
+__device__ __forceinline__ quad<KIND> quad_fetch(const void* p, long at, int n) {
+  quad<KIND> q;
+#pragma unroll
+  for (int i = 0; i < quad<KIND>::N; ++i) q.w[i] = 0u;
+  const char* b = reinterpret_cast<const char*>(p) + at * (KIND == CQ_A_F32 ? 4 : 2);
+  if (n == 4) {
+    if constexpr (KIND == CQ_A_F32) {
+      const cq_v4u v = *reinterpret_cast<const cq_v4u_any*>(b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q.w[i] = v[i];
+    } else {
+      const cq_v2u v = *reinterpret_cast<const cq_v2u_any*>(b);
+      q.w[0] = v[0];
+      q.w[1] = v[1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (i < n) {
+        if constexpr (KIND == CQ_A_F32)
+          q.w[i] = reinterpret_cast<const uint32_t*>(b)[i];
+        else
+          q.w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(b)[i] << (16 * (i & 1));
+      }
+    }
+  }
+  return q;
+}
+
+template <int KIND>
+__device__ __forceinline__ float quad_value(const quad<KIND>& q, int i) {
+  if constexpr (KIND == CQ_A_F32) return __uint_as_float(q.w[i]);
+  const uint32_t w = q.w[KIND == CQ_A_F32 ? 0 : i >> 1];
+  if constexpr (KIND == CQ_A_BF16) return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w & 0xffffu));
+}
+
+template <int KIND>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint16_t a, b;
+  if constexpr (KIND == CQ_A_BF16) {
+    a = __builtin_bit_cast(uint16_t, (__bf16)lo);
+    b = __builtin_bit_cast(uint16_t, (__bf16)hi);
+  } else {
+    a = __builtin_bit_cast(uint16_t, (_Float16)lo);
+    b = __builtin_bit_cast(uint16_t, (_Float16)hi);
+  }
+  return (uint32_t)a | ((uint32_t)b << 16);
+}
+
+// The four e4m3 codes of four values, rounded to nearest, ties to even; beyond +-448 saturated (NaN stays NaN).
+__device__ __forceinline__ uint32_t pack_e4m3(const float (&v)[4]) {
+  float c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = v[i] != v[i] ? v[i] : fminf(fmaxf(v[i], -kMostE4M3), kMostE4M3);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], w, true);
+}
+
+template <int KIND>
+__device__ __forceinline__ void quad_store(void* p, long at, int n, const float (&v)[4]) {
+  char* b = reinterpret_cast<char*>(p) + at * (KIND == CQ_A_F32 ? 4 : KIND == CQ_C_E4M3 ? 1 : 2);
+  if constexpr (KIND == CQ_C_E4M3) {
+    typedef uint32_t word_any __attribute__((aligned(1)));
+    const uint32_t w = pack_e4m3(v);
+    if (n == 4) {
+      *reinterpret_cast<word_any*>(b) = w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < n) reinterpret_cast<uint8_t*>(b)[i] = (uint8_t)(w >> (8 * i));
+    }
+  } else if (n == 4) {
+    if constexpr (KIND == CQ_A_F32)
+      *reinterpret_cast<cq_v4u_any*>(b) =
+          cq_v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else
+      *reinterpret_cast<cq_v2u_any*>(b) = cq_v2u{pack2<KIND>(v[0], v[1]), pack2<KIND>(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < n) elem_store<KIND>(b, i, v[i]);
+  }
+}
+
+// which values a lane holds: na from column a, nb from column b; turned: they are rotated, as pairs first .. first+3
+struct head_slot {
+  int a, b, na, nb, first;
+  bool turned;
+  __device__ __forceinline__ head_slot(const head_layout& L, int j) {
+    turned = j < L.turned;
+    first = 4 * j;
+    int from, end;
+    if (turned && !L.inter) {
+      const int half = L.rot >> 1;
+      from = 4 * j;
+      end = half;
+      a = from;
+      b = half + from;
+      na = nb = end - from < 4 ? end - from : 4;
+      return;
+    }
+    from = turned ? 8 * j : L.rot + 8 * (j - L.turned);
+    end = turned ? L.rot : L.D;
+    const int left = end - from;
+    a = from;
+    b = from + 4;
+    na = left < 0 ? 0 : left < 4 ? left : 4;
+    nb = left < 4 ? 0 : left < 8 ? left - 4 : 4;
+  }
+};
+
+template <int KIND>
+struct head_raw {
+  quad<KIND> a, b;
+};
+
+template <int KIND>
+__device__ __forceinline__ head_raw<KIND> head_fetch(const void* p, long at, const head_slot& s, bool on) {
+  head_raw<KIND> r;
+  r.a = quad_fetch<KIND>(p, at + s.a, on ? s.na : 0);
+  r.b = quad_fetch<KIND>(p, at + s.b, on ? s.nb : 0);
+  return r;
+}
+
+template <int KIND>
+__device__ __forceinline__ void head_values(const head_raw<KIND>& r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = quad_value<KIND>(r.a, i);
+    v[4 + i] = quad_value<KIND>(r.b, i);
+  }
+}
+
+template <int KIND>
+__device__ __forceinline__ void head_store(void* p, long at, const head_slot& s, const float (&v)[8]) {
+  const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+  quad_store<KIND>(p, at + s.a, s.na, a);
+  quad_store<KIND>(p, at + s.b, s.nb, b);
+}
+
+// a lane's share of a norm's weights (ones without a norm)
+__device__ __forceinline__ void head_weights(const void* w, int kind, const head_slot& s, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 1.f;
+  if (!w) return;
+  if (kind == CQ_A_F32)
+    head_values<CQ_A_F32>(head_fetch<CQ_A_F32>(w, 0, s, true), v);
+  else if (kind == CQ_A_F16)
+    head_values<CQ_A_F16>(head_fetch<CQ_A_F16>(w, 0, s, true), v);
+  else
+    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16>(w, 0, s, true), v);
+}
+
+// cosines and sines of a lane's four pairs
+struct head_turn {
+  float c[4], s[4];
+};
+
+// position freq / (2 pi) modulo 1, in -1/2 .. 1/2.  The product and the quotient keep what their roundings leave over: at position 2^31
+// these are 2^-22 radians each, more than fp32 sines and cosines are off by.
+__device__ __forceinline__ float revolutions(int position, double freq) {
+  constexpr double kHi = 0.15915494309189533577, kLo = -9.839338337591243e-18;   // 1 / (2 pi), and what 64 bits leave of it
+  const double t = (double)position * freq, dt = fma((double)position, freq, -t);
+  const double rev = t * kHi, rest = fma(t, kHi, -rev) + fma(t, kLo, dt * kHi);
+  return (float)((rev - rint(rev)) + rest);
+}
+
+__device__ __forceinline__ head_turn turn_of(const head_layout& L, const head_slot& s, const double* freq, float rot_scale, int position) {
+  head_turn t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    t.c[i] = 1.f;
+    t.s[i] = 0.f;
+    if (s.turned && s.first + i < (L.rot >> 1)) {
+      sincospif(2.f * revolutions(position, freq[s.first + i]), &t.s[i], &t.c[i]);
+      t.c[i] *= rot_scale;
+      t.s[i] *= rot_scale;
+    }
+  }
+  return t;
+}
+
+// a' = a c - b s, b' = b c + a s; back: by the angle's negative
+template <bool BACK>
+__device__ __forceinline__ void turn_values(const head_layout& L, const head_slot& s, const head_turn& t, float (&v)[8]) {
+  if (!s.turned) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float sn = BACK ? -t.s[i] : t.s[i];
+    if (L.inter) {
+      const float a = v[2 * i], b = v[2 * i + 1];
+      v[2 * i] = fmaf(a, t.c[i], -(b * sn));
+      v[2 * i + 1] = fmaf(b, t.c[i], a * sn);
+    } else {
+      const float a = v[i], b = v[4 + i];
+      v[i] = fmaf(a, t.c[i], -(b * sn));
+      v[4 + i] = fmaf(b, t.c[i], a * sn);
+    }
+  }
+}
+
+// sum over the LANES neighbouring lanes of a row, the same in each, in a fixed order
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v) {
+  v = add_dpp<0xb1, 0xf>(v);     // quad_perm 1 0 3 2
+  v = add_dpp<0x4e, 0xf>(v);     // quad_perm 2 3 0 1
+  v = add_dpp<0x141, 0xf>(v);    // row_half_mirror
+  if constexpr (LANES >= 16) v = add_dpp<0x140, 0xf>(v);   // row_mirror
+  if constexpr (LANES >= 32) v += __shfl_xor(v, 16);
+  if constexpr (LANES >= 64) v += __shfl_xor(v, 32);
+  return v;
+}
+
+template <int LANES>
+__device__ __forceinline__ void head_normed(float (&v)[8], const float (&w)[8], float inv_D, float eps) {
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+  const float r = 1.f / sqrtf(row_sum<LANES>(ss) * inv_D + eps);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = v[i] * r * w[i];
+}
+
+}  // namespace
+
+// Runs LAUNCH(..., LANES) for the lanes of a row.
+#define CQ_HEAD_LANES(LAUNCH, lanes, ...)              \
+  do {                                                 \
+    if ((lanes) == 8) LAUNCH(__VA_ARGS__, 8);          \
+    else if ((lanes) == 16) LAUNCH(__VA_ARGS__, 16);   \
+    else if ((lanes) == 32) LAUNCH(__VA_ARGS__, 32);   \
+    else LAUNCH(__VA_ARGS__, 64);                      \
+  } while (0)
+
+#endif  // CQ_HEADS_H_
