@@ -875,90 +875,125 @@ def cq_adapter_apply(adapters: DeviceAdapters, X, ids, base=None, out=None, out_
 # ------------------------------------------------------------------------------------------------
 # heads, the paged cache and attention over it
 # ------------------------------------------------------------------------------------------------
-def _heads(t, what: str, shape, dtype, device) -> Heads:
-    """Checks heads [T, n, D] (None: any number) on the GPU, a head's values one after another; what a call hands to the library."""
+# (a call of these takes a single token's time on the host: what is right is seen in as few operations as there are, what is wrong is told by
+# functions of their own; tensors are compared by their device's number, which is -1 off the GPU)
+_DTYPES: Dict[str, object] = {}      # filled once torch is known
+
+
+def _dtypes() -> Dict[str, object]:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update(i32=torch.int32, f32=torch.float32, f64=torch.float64, empty=torch.empty, empty_like=torch.empty_like)
+        _DTYPES.update(current=torch._C._cuda_getDevice, stream=torch._C._cuda_getCurrentRawStream)
+        _DTYPES["cache"] = {torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16, torch.float8_e4m3fn: CQ_C_E4M3}
+        _kind(torch.float32, "")
+    return _DTYPES
+
+
+def _gpu_of(t, what: str) -> int:
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{what}: not on the GPU")
+    return index
+
+
+def _wrong(t, what: str, shape, dtype, index: int):
+    """What is wrong with a tensor that does not have this type and shape (None in it: any size) on this GPU."""
     if not t.is_cuda:
         raise ValueError(f"{what}: not on the GPU")
-    if t.device != device:
-        raise ValueError(f"{what}: on {t.device} where {device} is needed")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: {t.dtype} where {dtype} is needed")
-    if t.dim() != 3 or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
-    token, head, one = t.stride()
-    if one != 1 and t.shape[2] > 1:
-        raise ValueError(f"{what}: a head's values are {one} apart")
-    return Heads(t.data_ptr(), _kind(t.dtype, what), t.shape[1], token, head)
+    if t.get_device() != index:
+        raise ValueError(f"{what}: on {t.device} where cuda:{index} is needed")
+    raise ValueError(f"{what}: not contiguous")
 
 
-def _out_heads(t, what: str, like, dtype):
-    """The output of rows like these: a tensor of the caller's whose rows do not overlap, or a new one."""
-    import torch
-    if t is None:
-        t = torch.empty(like.shape, dtype=dtype, device=like.device)
-        T, n, D = like.shape
-        return t, Heads(t.data_ptr(), _kind(dtype, what), n, n * D, D)
-    h = _heads(t, what, like.shape, dtype, like.device)
-    T, n, D = t.shape
-    a, b = sorted(((h.token_stride, T), (h.head_stride, n)))
-    # (the nearer of the two steps over a row, the farther over all rows of the nearer)
-    if T > 1 and n > 1 and (a[0] < D or b[0] < (a[1] - 1) * a[0] + D):
-        raise ValueError(f"{what}: rows of strides {t.stride()} overlap")
-    return t, h
-
-
-def _on_device(call, device, *args):
-    """call(*args, stream) on the current stream of that device, whichever device is the current one."""
-    import torch
-    index = device.index
-    if torch.cuda.current_device() != index:
-        with torch.cuda.device(index):
-            st = call(*args, torch.cuda.current_stream(index).cuda_stream)
-    else:
-        st = call(*args, torch._C._cuda_getCurrentRawStream(index))
-    if st:
-        raise CqError(st)
-
-
-def _ints(t, what: str, shape, device, dtype=None):
-    """The address of a contiguous i32 tensor on that device (None: 0)."""
-    import torch
+def _at(t, what: str, shape, dtype, index: int) -> Optional[int]:
+    """The address of a contiguous tensor of that type and shape on that GPU (None: None)."""
     if t is None:
         return None
-    _tensor(t, what, shape, torch.int32 if dtype is None else dtype)
-    if t.device != device:
-        raise ValueError(f"{what}: on {t.device} where {device} is needed")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
+    _wrong(t, what, shape, dtype, index)
+
+
+def _heads(t, what: str, T, n, D, dtype, index: int) -> Heads:
+    """Checks heads [T, n, D] (n None: any number; dtype None: any) on that GPU, a head's values one after another; what a call hands on."""
+    shape, stride = t.shape, t.stride()
+    if t.get_device() != index or len(shape) != 3 or shape[0] != T or n is not None and shape[1] != n or shape[2] != D or (
+            dtype is not None and t.dtype is not dtype):
+        _wrong(t, what, (T, n, D), dtype, index)
+    if stride[2] != 1 and D > 1:
+        raise ValueError(f"{what}: a head's values are {stride[2]} apart")
+    return Heads(t.data_ptr(), _KINDS.get(t.dtype) or _kind(t.dtype, what), shape[1], stride[0], stride[1])
+
+
+def _new_heads(like, h: Heads, dtype):
+    """New rows for these: the tensor, and what a call hands on."""
+    T, n, D = like.shape
+    if dtype is like.dtype and like.is_contiguous():
+        t = _DTYPES["empty_like"](like)
+    else:
+        t = _DTYPES["empty"]((T, n, D), dtype=dtype, device=like.device)
+    return t, Heads(t.data_ptr(), _KINDS.get(dtype) or _kind(dtype, "out_dtype"), n, n * D, D)
+
+
+def _out_heads(t, what: str, like, h: Heads, dtype, index: int):
+    """The output of rows like these: a tensor of the caller's whose rows do not overlap, or a new one."""
+    if t is None:
+        return _new_heads(like, h, dtype)
+    T, n, D = like.shape
+    o = _heads(t, what, T, n, D, dtype, index)
+    (near, count), (far, _) = sorted(((o.token_stride, T), (o.head_stride, n)))
+    # (the nearer of the two steps over a row, the farther over all rows of the nearer)
+    if T > 1 and n > 1 and (near < D or far < (count - 1) * near + D):
+        raise ValueError(f"{what}: rows of strides {t.stride()} overlap")
+    return t, o
+
+
+def _on_device(call, index: int, *args):
+    """call(*args, stream) on the current stream of that GPU, whichever GPU is the current one."""
+    if _DTYPES["current"]() == index:
+        st = call(*args, _DTYPES["stream"](index))
+    else:
+        import torch
+        with torch.cuda.device(index):
+            st = call(*args, _DTYPES["stream"](index))
+    if st:
+        raise CqError(st)
 
 
 class HeadNorm:
     """Norms of queries and keys for each head of D values, and the rotation by position (cq_head_spec).
 
-    w_q, w_k [D]: the norms' weights (None: no such norm).  freq [rot / 2] f64: radians per position of each pair of the first rot
-    values (None: no rotation); pairs are (i, i + rot / 2), or with interleaved (2i, 2i + 1); rot_scale: factor on cosine and sine.
-    The tensors may be replaced by others of their size and type, and the numbers changed: a call takes what is there, and looks at the
-    tensors anew."""
+    w_q, w_k [D]: the norms' weights, of one type (None: no such norm).  freq [rot / 2] f64: radians per position of each pair of the first
+    rot values (None: no rotation); pairs are (i, i + rot / 2), or with interleaved (2i, 2i + 1); rot_scale: factor on cosine and sine.
+    The tensors may be replaced by others, and the numbers changed: a call takes what is there, and looks at the tensors anew."""
 
     def __init__(self, D: int, w_q=None, w_k=None, eps: float = 1e-6, freq=None, interleaved: bool = False, rot_scale: float = 1.0):
         self.D, self.eps, self.interleaved, self.rot_scale = int(D), float(eps), bool(interleaved), float(rot_scale)
         self.w_q, self.w_k, self.freq = w_q, w_k, freq
+        for name, some in (("w_q", w_q), ("w_k", w_k), ("freq", freq)):
+            if some is not None:
+                _gpu_of(some, name)
+                self.struct(some.get_device())
+                break
+
+    def struct(self, index: int) -> HeadSpec:
+        """Checks the tensors; what a call on that GPU hands to the library."""
+        kinds = _DTYPES or _dtypes()
+        w_q, w_k, freq, shape, rot, kind = self.w_q, self.w_k, self.freq, (self.D,), 0, CQ_A_F32
         some = w_q if w_q is not None else w_k
         if some is not None:
-            self.struct(some.device)
-        elif freq is not None:
-            self.struct(freq.device)
-
-    def struct(self, device) -> HeadSpec:
-        """Checks the tensors; what a call hands to the library."""
-        import torch
-        shape, some, rot = (self.D,), self.w_q if self.w_q is not None else self.w_k, 0
-        if self.freq is not None:
-            _ints(self.freq, "freq", (None,), device, torch.float64)
-            rot = 2 * self.freq.shape[0]
-        weights = CQ_A_F32 if some is None else _kind(some.dtype, "weights")
-        return HeadSpec(self.D, rot, self.interleaved, weights, self.eps, self.rot_scale, self.freq.data_ptr() if rot else None,
-                        None if self.w_q is None else _ints(self.w_q, "w_q", shape, device, some.dtype),
-                        None if self.w_k is None else _ints(self.w_k, "w_k", shape, device, some.dtype))
+            dtype = some.dtype
+            kind = _KINDS.get(dtype) or _kind(dtype, "weights")
+            w_q, w_k = _at(w_q, "w_q", shape, dtype, index), _at(w_k, "w_k", shape, dtype, index)
+        if freq is not None:
+            rot = 2 * freq.shape[0] if freq.dim() == 1 else _wrong(freq, "freq", (None,), kinds["f64"], index)
+            freq = _at(freq, "freq", freq.shape, kinds["f64"], index)
+        return HeadSpec(self.D, rot, self.interleaved, kind, self.eps, self.rot_scale, freq, w_q, w_k)
 
 
 def cq_head_norm(norm: HeadNorm, q=None, k=None, positions=None, q_out=None, k_out=None, out_dtype=None) -> Dict[str, object]:
@@ -970,53 +1005,48 @@ def cq_head_norm(norm: HeadNorm, q=None, k=None, positions=None, q_out=None, k_o
     some = q if q is not None else k
     if some is None:
         raise ValueError("q, k: there are neither queries nor keys")
-    device, T = some.device, some.shape[0]
-    spec = norm.struct(device)
-    positions = _ints(positions, "positions", (T,), device)
-    args, out = [], {"q": None, "k": None}
-    for name, x, given in (("q", q, q_out), ("k", k, k_out)):
-        if x is None:
-            args.append((None, None))
-            continue
-        h = _heads(x, name, (T, None, norm.D), some.dtype, device)
-        out[name], o = _out_heads(given, name + "_out", x, out_dtype or (x.dtype if given is None else given.dtype))
-        args.append((h, o))
-    (hq, oq), (hk, ok) = args
-    _on_device(lib.cq_head_norm, device, spec, hq, hk, positions, T, oq, ok)
-    return out
+    index, T, D, dtype = _gpu_of(some, "q" if q is not None else "k"), some.shape[0], norm.D, some.dtype
+    spec = norm.struct(index)
+    hq = oq = hk = ok = None
+    if q is not None:
+        hq = _heads(q, "q", T, None, D, dtype, index)
+        q_out, oq = _out_heads(q_out, "q_out", q, hq, out_dtype or (dtype if q_out is None else q_out.dtype), index)
+    if k is not None:
+        hk = _heads(k, "k", T, None, D, dtype, index)
+        k_out, ok = _out_heads(k_out, "k_out", k, hk, out_dtype or (dtype if k_out is None else k_out.dtype), index)
+    _on_device(lib.cq_head_norm, index, spec, hq, hk, _at(positions, "positions", (T,), _DTYPES["i32"], index), T, oq, ok)
+    return {"q": q_out if q is not None else None, "k": k_out if k is not None else None}
 
 
 def cq_head_norm_grad(norm: HeadNorm, q=None, k=None, positions=None, dq=None, dk=None, want_weights: bool = True) -> Dict[str, object]:
     """Gradients of cq_head_norm from its q and k and the gradients dq, dk of its results (either may be None): {"dq", "dk", "dw_q", "dw_k"},
     of the types of q, k and the weights; None where there is no such input.  q and k give the types also where there is no norm."""
-    import torch
     lib = _lib or load_library()
     some = dq if dq is not None else dk
     if some is None:
         raise ValueError("dq, dk: there are no gradients")
-    device, T = some.device, some.shape[0]
-    spec = norm.struct(device)
-    positions = _ints(positions, "positions", (T,), device)
-    out = {"dq": None, "dk": None, "dw_q": None, "dw_k": None}
-    x_of, d_of, o_of, w_of, dtype = [None] * 2, [None] * 2, [None] * 2, [None] * 2, None
+    index, T, D, d_dtype = _gpu_of(some, "dq" if dq is not None else "dk"), some.shape[0], norm.D, some.dtype
+    spec = norm.struct(index)
+    like = _DTYPES["empty_like"]
+    x_of, d_of, o_of, out_of, w_of, dtype = [None] * 2, [None] * 2, [None] * 2, [None] * 2, [None] * 2, None
     for i, (name, x, d, w) in enumerate((("q", q, dq, norm.w_q), ("k", k, dk, norm.w_k))):
         if d is None:
             continue
         if x is None:
             raise ValueError(f"{name}: its gradient needs it")
         dtype = dtype or x.dtype
-        x_of[i] = _heads(x, name, (T, None, norm.D), dtype, device)
-        d_of[i] = _heads(d, "d" + name, tuple(x.shape), some.dtype, device)
-        out["d" + name], o_of[i] = _out_heads(None, "d" + name, x, dtype)
+        x_of[i] = h = _heads(x, name, T, None, D, dtype, index)
+        d_of[i] = _heads(d, "d" + name, T, h.n, D, d_dtype, index)
+        out_of[i], o_of[i] = _new_heads(x, h, dtype)
         if want_weights and w is not None:
-            out["dw_" + name] = w_of[i] = torch.empty_like(w)
+            w_of[i] = like(w)
     ws, nbytes = None, 0
     if w_of[0] is not None or w_of[1] is not None:
         nbytes = lib.cq_head_norm_grad_workspace_bytes(spec, T)
-        ws = _scratch(some, nbytes)
-    _on_device(lib.cq_head_norm_grad, device, spec, x_of[0], x_of[1], positions, T, d_of[0], d_of[1], o_of[0], o_of[1], _ptr(w_of[0]),
-               _ptr(w_of[1]), _ptr(ws), nbytes)
-    return out
+        ws = _DTYPES["empty"](nbytes >> 2, dtype=_DTYPES["f32"], device=some.device)
+    _on_device(lib.cq_head_norm_grad, index, spec, x_of[0], x_of[1], _at(positions, "positions", (T,), _DTYPES["i32"], index), T, d_of[0],
+               d_of[1], o_of[0], o_of[1], _ptr(w_of[0]), _ptr(w_of[1]), _ptr(ws), nbytes)
+    return {"dq": out_of[0], "dk": out_of[1], "dw_q": w_of[0], "dw_k": w_of[1]}
 
 
 class PagedCache:
@@ -1024,42 +1054,46 @@ class PagedCache:
     row's D values one after another (a permuted view of pages with heads outside slots will do).  k_scale, v_scale [heads] f32 (None: 1):
     what the values of an 8-bit cache are to be multiplied by.
 
-    The tensors may be replaced by others of their size and type: a call takes what is there, and looks at them anew."""
+    The tensors may be replaced by others: a call takes what is there, and looks at them anew."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.struct()
+        if k.dtype not in _dtypes()["cache"]:
+            self._wrong()
+        self.struct(_gpu_of(k, "k"))
 
-    def struct(self) -> Cache:
-        """Checks the tensors; what a call hands to the library."""
-        import torch
+    def _wrong(self):
         k, v = self.k, self.v
-        kind = {torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16, torch.float8_e4m3fn: CQ_C_E4M3}.get(k.dtype)
-        if kind is None:
+        if k.dtype not in _DTYPES["cache"]:
             raise ValueError(f"k: {k.dtype} is not one of float16, bfloat16, float8_e4m3fn")
-        if not k.is_cuda or v.device != k.device:
+        if v.get_device() != k.get_device():
             raise ValueError("k, v: not on one GPU")
-        stride = k.stride()
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != stride or stride[3] != 1:
-            raise ValueError(f"k, v: {k.dtype} {tuple(k.shape)} {stride} and {v.dtype} {tuple(v.shape)} {v.stride()} are not pages of one layout")
-        pages, size, heads, D = k.shape
-        f32 = torch.float32
-        return Cache(kind, heads, D, size, pages, stride[0], stride[1], stride[2], k.data_ptr(), v.data_ptr(),
-                     None if self.k_scale is None else _ints(self.k_scale, "k_scale", (heads,), k.device, f32),
-                     None if self.v_scale is None else _ints(self.v_scale, "v_scale", (heads,), k.device, f32))
+        raise ValueError(f"k, v: {k.dtype} {tuple(k.shape)} {k.stride()} and {v.dtype} {tuple(v.shape)} {v.stride()} are not pages of one layout")
+
+    def struct(self, index: int) -> Cache:
+        """Checks the tensors; what a call on that GPU hands to the library."""
+        k, v, types = self.k, self.v, _DTYPES or _dtypes()
+        shape, stride, kind = k.shape, k.stride(), types["cache"].get(k.dtype)
+        if kind is None or len(shape) != 4 or v.shape != shape or v.stride() != stride or v.dtype is not k.dtype or stride[3] != 1 or (
+                v.get_device() != k.get_device()):
+            self._wrong()
+        if k.get_device() != index:
+            raise ValueError(f"cache: on {k.device} where cuda:{index} is needed")
+        pages, size, heads, D = shape
+        k_scale, v_scale = self.k_scale, self.v_scale
+        if k_scale is not None:
+            k_scale = _at(k_scale, "k_scale", (heads,), types["f32"], index)
+        if v_scale is not None:
+            v_scale = _at(v_scale, "v_scale", (heads,), types["f32"], index)
+        return Cache(kind, heads, D, size, pages, stride[0], stride[1], stride[2], k.data_ptr(), v.data_ptr(), k_scale, v_scale)
 
 
-def _sequences(page_table, lengths, device) -> Sequences:
-    width = _rows_of_table(page_table, device)
-    S = page_table.shape[0]
-    return Sequences(S, page_table.shape[1], width, page_table.data_ptr(), _ints(lengths, "lengths", (S,), device))
-
-
-def _rows_of_table(t, device) -> int:
-    import torch
-    if t.device != device:
-        raise ValueError(f"page_table: on {t.device} where {device} is needed")
-    return _rows(t, "page_table", (None, None), torch.int32)
+def _sequences(page_table, lengths, index: int) -> Sequences:
+    i32, shape = _DTYPES["i32"], page_table.shape
+    if len(shape) != 2 or page_table.dtype is not i32 or page_table.get_device() != index:
+        _wrong(page_table, "page_table", (None, None), i32, index)
+    S, width = shape
+    return Sequences(S, width, _rows(page_table, "page_table", shape), page_table.data_ptr(), _at(lengths, "lengths", (S,), i32, index))
 
 
 def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=None, positions=None, norm: Optional[HeadNorm] = None, q=None,
@@ -1071,20 +1105,17 @@ def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=No
     one each); positions [T] i32: rotate by these instead of by the positions in the cache.  Rows of tokens outside all sequences are
     not written (in a new q_out they hold anything)."""
     lib = _lib or load_library()
-    device, T = k.device, k.shape[0]
-    c = cache.struct()
-    if cache.k.device != device:
-        raise ValueError(f"k: on {device}, the cache on {cache.k.device}")
-    s = _sequences(page_table, lengths, device)
-    spec = None if norm is None else norm.struct(device)
-    shape, dtype = (T, c.heads, c.D), k.dtype
-    hk, hv = _heads(k, "k", shape, dtype, device), _heads(v, "v", shape, dtype, device)
+    index, T, dtype = _gpu_of(k, "k"), k.shape[0], k.dtype
+    c = cache.struct(index)
+    s = _sequences(page_table, lengths, index)
+    n, D, i32 = c.heads, c.D, _DTYPES["i32"]
+    hk, hv = _heads(k, "k", T, n, D, dtype, index), _heads(v, "v", T, n, D, dtype, index)
     hq = oq = None
     if q is not None:
-        hq = _heads(q, "q", (T, None, c.D), dtype, device)
-        q_out, oq = _out_heads(q_out, "q_out", q, dtype)
-    _on_device(lib.cq_cache_append, device, c, s, spec, hq, hk, hv, _ints(seq_offsets, "seq_offsets", (s.n + 1,), device),
-               _ints(positions, "positions", (T,), device), T, oq)
+        hq = _heads(q, "q", T, None, D, dtype, index)
+        q_out, oq = _out_heads(q_out, "q_out", q, hq, dtype, index)
+    _on_device(lib.cq_cache_append, index, c, s, None if norm is None else norm.struct(index), hq, hk, hv,
+               _at(seq_offsets, "seq_offsets", (s.n + 1,), i32, index), _at(positions, "positions", (T,), i32, index), T, oq)
     return q_out if q is not None else None
 
 
@@ -1095,22 +1126,22 @@ def cq_cache_attention(cache: PagedCache, q, page_table, lengths, scale: Optiona
 
     scale: D ** -0.5 if None.  max_length: what the lengths are expected to reach (None: all that the page table's rows can hold).  sinks
     [Hq] f32: logits that join the denominator."""
-    import torch
     lib = _lib or load_library()
-    device = q.device
-    c = cache.struct()
-    if cache.k.device != device:
-        raise ValueError(f"q: on {device}, the cache on {cache.k.device}")
-    s = _sequences(page_table, lengths, device)
-    hq = _heads(q, "q", (s.n, None, c.D), None, device)
-    S, Hq = s.n, hq.n
+    index = _gpu_of(q, "q")
+    c = cache.struct(index)
+    s = _sequences(page_table, lengths, index)
+    S, D, f32 = s.n, c.D, _DTYPES["f32"]
+    hq = _heads(q, "q", S, None, D, None, index)
+    Hq = hq.n
     if max_length is None:
         max_length = s.width * c.page_size
-    spec = AttentionSpec(c.D ** -0.5 if scale is None else scale, softcap, window, max_length,
-                         None if sinks is None else _ints(sinks, "sinks", (Hq,), device, torch.float32))
-    out, ho = _out_heads(out, "out", q, out_dtype or (q.dtype if out is None else out.dtype))
-    lse = torch.empty((S, Hq), dtype=torch.float32, device=device) if want_lse else None
+    spec = AttentionSpec(D ** -0.5 if scale is None else scale, softcap, window, max_length, _at(sinks, "sinks", (Hq,), f32, index))
+    out, ho = _out_heads(out, "out", q, hq, out_dtype or (q.dtype if out is None else out.dtype), index)
+    empty, lse, ws = _DTYPES["empty"], None, None
+    if want_lse:
+        lse = empty((S, Hq), dtype=f32, device=q.device)
     nbytes = lib.cq_cache_attention_workspace_bytes(c, S, Hq, max_length, window)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _on_device(lib.cq_cache_attention, device, c, s, spec, hq, ho, _ptr(lse), _ptr(ws), nbytes)
+    if nbytes:
+        ws = empty(nbytes >> 2, dtype=f32, device=q.device)
+    _on_device(lib.cq_cache_attention, index, c, s, spec, hq, ho, _ptr(lse), _ptr(ws), nbytes)
     return {"out": out, "lse": lse}

@@ -177,7 +177,7 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
   if ((d_q_out && d_k_out && (d_k->kind != kind || d_k_out->kind != out)) || (out != kind && kind != CQ_A_F32)) return CQ_ERR_UNSUPPORTED;
   if ((norm_q && q->kind != kind) || (norm_k && k->kind != kind)) return CQ_ERR_UNSUPPORTED;
   const bool weights = d_w_q || d_w_k;
-  if (weights && (!workspace || workspace_bytes < cq_head_norm_grad_workspace_bytes(P, T))) return CQ_ERR_WORKSPACE;
+  if (weights && T > 0 && (!workspace || workspace_bytes < cq_head_norm_grad_workspace_bytes(P, T))) return CQ_ERR_WORKSPACE;
   if (T > 0 && P->rot > 0 && !positions) return CQ_ERR_NULL;
   if (T == 0 && !weights) return CQ_OK;
   hipStream_t str = (hipStream_t)stream;

@@ -195,7 +195,7 @@ def test_binding_refuses_what_is_not_on_the_gpu():
         B.cq_head_norm(B.HeadNorm(64))
     with pytest.raises(ValueError, match="no gradients"):
         B.cq_head_norm_grad(B.HeadNorm(64))
-    with pytest.raises(ValueError, match="not on one GPU"):
+    with pytest.raises(ValueError, match="k: not on the GPU"):
         B.PagedCache(torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="float16, bfloat16"):
         B.PagedCache(torch.zeros(2, 16, 2, 64), torch.zeros(2, 16, 2, 64))
