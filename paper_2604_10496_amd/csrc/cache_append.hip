@@ -5,11 +5,11 @@
 
 namespace {
 
-constexpr int kRows = 4;   // rows of a lane in flight
+constexpr int kGroups = 2;   // groups of rows in flight
 
 struct append_args {
   head_layout L;
-  int T, first, parts, rows_per_part, wkind;   // tokens first .. first + T - 1
+  int T, first, parts, per_part, groups_q, groups_k, groups, wkind;   // tokens first .. first + T - 1
   float eps, rot_scale, inv_D;
   const double* freq;
   const void *w_q, *w_k;
@@ -57,78 +57,69 @@ __device__ __forceinline__ place place_of(const append_args& A, int t, int lane)
   return p;
 }
 
-template <int XK, int CK, int LANES>
+template <int XK, int CK, int LANES, bool WHOLE, bool INTER>
 __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
   constexpr int kAtOnce = 64 / LANES;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  const int in_launch = unit / A.parts, part = unit - in_launch * A.parts;
+  const int in_launch = unit / A.parts;
   if (in_launch >= A.T) return;
   const int t = A.first + in_launch;
-  const int lane = threadIdx.x & 63;
+  int group = (unit - in_launch * A.parts) * A.per_part;
+  const int end = min(A.groups, group + A.per_part);
+  const int lane = threadIdx.x & 63, sub = lane / LANES;
   const head_slot s(A.L, lane % LANES);
-  const int first_v = A.q.n + A.k.n, rows = first_v + A.v.n, end = min(rows, (part + 1) * A.rows_per_part);
-  int row = part * A.rows_per_part + lane / LANES;
-  head_raw<XK> raw[kRows];
+  // which rows a group holds: 0 queries, 1 keys, 2 values, from head h0 on
+  auto what = [&](int g, int& h0) {
+    const int which = g < A.groups_q ? 0 : g < A.groups_k ? 1 : 2;
+    h0 = (g - (which == 0 ? 0 : which == 1 ? A.groups_q : A.groups_k)) * kAtOnce;
+    return which;
+  };
+  head_raw<XK> raw[kGroups];
   auto fetch = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = first + i * kAtOnce;
-      const bool key = r >= A.q.n, value = r >= first_v;
-      const void* p = value ? A.v.p : key ? A.k.p : A.q.p;
-      const long at = value ? t * A.v.token + (r - first_v) * A.v.head
-                            : key ? t * A.k.token + (r - A.q.n) * A.k.head : t * A.q.token + r * A.q.head;
-      raw[i] = head_fetch<XK>(p, at, s, r < end);
+    for (int i = 0; i < kGroups; ++i) {
+      int h0;
+      const int which = what(first + i, h0);
+      const head_rows& R = which == 0 ? A.q : which == 1 ? A.k : A.v;
+      raw[i] = head_fetch<XK, WHOLE>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
-  fetch(row);
+  fetch(group);
   const place to = place_of(A, t, lane);
   if (to.seq < 0) return;   // (nothing is written, the queries neither)
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.positions ? A.positions[t] : to.position);
   float w_q[8], w_k[8];
-  head_weights(A.w_q, A.wkind, s, w_q);
-  head_weights(A.w_k, A.wkind, s, w_k);
+  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
   const long at = to.page * A.C.page + to.slot * A.C.slot;
-  for (int first = part * A.rows_per_part; first < end; first += kRows * kAtOnce, row += kRows * kAtOnce) {
-    float v[kRows][8];
+  for (; group < end; group += kGroups) {
+    float v[kGroups][8];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) head_values<XK>(raw[i], v[i]);
-    if (first + kRows * kAtOnce < end) fetch(row + kRows * kAtOnce);
+    for (int i = 0; i < kGroups; ++i) head_values<XK>(raw[i], v[i]);
+    if (group + kGroups < end) fetch(group + kGroups);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = row + i * kAtOnce;
-      const bool key = r >= A.q.n, value = r >= first_v;
-      float plain[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) plain[e] = v[i][e];
-      if (A.w_q || A.w_k) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = key ? w_k[e] : w_q[e];
-        head_normed<LANES>(v[i], w, A.inv_D, A.eps);
-        if (!(key ? A.w_k : A.w_q)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[i][e] = plain[e];
-        }
+    for (int i = 0; i < kGroups; ++i) {
+      int h0;
+      const int which = what(group + i, h0), h = h0 + sub;
+      if (which == 0) {
+        if (A.w_q) head_normed<LANES>(v[i], w_q, A.inv_D, A.eps);
+      } else if (which == 1) {
+        if (A.w_k) head_normed<LANES>(v[i], w_k, A.inv_D, A.eps);
       }
-      turn_values<false>(A.L, s, turn, v[i]);
-      if (r >= end) continue;
-      if (!key) {
-        head_store<XK>(const_cast<void*>(A.q_out.p), t * A.q_out.token + r * A.q_out.head, s, v[i]);
-      } else if (to.page >= 0) {
-        const int h = value ? r - first_v : r - A.q.n;
-        if (value) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[i][e] = plain[e];
-        }
+      if (which < 2) turn_values<INTER, false>(s, turn, v[i]);
+      if (group + i >= end) break;
+      if (which == 0) {
+        if (h < A.q.n) head_store<XK, WHOLE>(const_cast<void*>(A.q_out.p), t * A.q_out.token + h * A.q_out.head, s, v[i]);
+      } else if (to.page >= 0 && h < A.C.heads) {
         if constexpr (CK == CQ_C_E4M3) {
-          const float* scale = value ? A.C.v_scale : A.C.k_scale;
+          const float* scale = which == 2 ? A.C.v_scale : A.C.k_scale;
           if (scale) {
             const float sc = scale[h];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] /= sc;
           }
         }
-        head_store<CK>(value ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
+        head_store<CK, WHOLE>(which == 2 ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
       }
     }
   }
@@ -170,24 +161,22 @@ extern "C" cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, c
   a.k = make_head_rows(k);
   a.v = make_head_rows(v);
   a.q_out = make_head_rows(q ? q_out : nullptr);
-  // Few tokens: their heads on several wavefronts, one instruction's rows at a time.
-  const int rows = a.q.n + a.k.n + a.v.n, at_once = 64 / a.L.lanes;
-  int parts = 1;
-  while (parts * 2 * at_once <= rows + at_once && (long)T * parts < 2048) parts *= 2;
-  a.rows_per_part = (int)cq_align_up((size_t)((rows + parts - 1) / parts), at_once);
-  a.parts = (rows + a.rows_per_part - 1) / a.rows_per_part;
+  a.groups_q = head_groups(a.q.n, a.L);
+  a.groups_k = a.groups_q + head_groups(a.k.n, a.L);
+  a.groups = a.groups_k + head_groups(a.v.n, a.L);
+  share_groups(a.groups, T, 2048, a.per_part, a.parts);
   const long most = (kMostThreads / 64 / a.parts) & ~3l;
   for (long from = 0; from < T; from += most) {
     append_args b = a;
     b.first = (int)from;
     b.T = (int)(T - from < most ? T - from : most);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, CK, LANES) hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES>), grid, dim3(256), 0, (hipStream_t)stream, b)
+#define LAUNCH(XK, CK, LANES, WHOLE, INTER) hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES, WHOLE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
 #define KINDS(XK)                                                              \
   do {                                                                         \
-    if (C->kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, XK, CQ_A_F16);   \
-    else if (C->kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, XK, CQ_A_BF16); \
-    else CQ_HEAD_LANES(LAUNCH, a.L.lanes, XK, CQ_C_E4M3);                      \
+    if (C->kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, XK, CQ_A_F16);   \
+    else if (C->kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, XK, CQ_A_BF16); \
+    else CQ_HEAD_LANES(LAUNCH, a.L, XK, CQ_C_E4M3);                      \
   } while (0)
     if (k->kind == CQ_A_F32) KINDS(CQ_A_F32);
     else if (k->kind == CQ_A_F16) KINDS(CQ_A_F16);

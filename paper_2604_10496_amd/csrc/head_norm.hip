@@ -4,11 +4,11 @@
 
 namespace {
 
-constexpr int kRows = 4;   // rows of a lane in flight
+constexpr int kGroups = 2;   // groups of rows in flight
 
 struct head_norm_args {
   head_layout L;
-  int T, parts, rows_per_part, wkind;
+  int T, parts, per_part, groups_q, groups, wkind;
   float eps, rot_scale, inv_D;
   const double* freq;
   const void *w_q, *w_k;
@@ -16,59 +16,48 @@ struct head_norm_args {
   head_rows q, k, q_out, k_out;
 };
 
-template <int XK, int OK, int LANES>
+template <int XK, int OK, int LANES, bool WHOLE, bool INTER>
 __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
   constexpr int kAtOnce = 64 / LANES;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  const int t = unit / A.parts, part = unit - t * A.parts;
+  const int t = unit / A.parts;
   if (t >= A.T) return;
-  const int lane = threadIdx.x & 63;
+  int group = (unit - t * A.parts) * A.per_part;
+  const int end = min(A.groups, group + A.per_part);
+  const int lane = threadIdx.x & 63, sub = lane / LANES;
   const head_slot s(A.L, lane % LANES);
-  const int rows = A.q.n + A.k.n, end = min(rows, (part + 1) * A.rows_per_part);
-  int row = part * A.rows_per_part + lane / LANES;
-  head_raw<XK> raw[kRows];
+  head_raw<XK> raw[kGroups];
   auto fetch = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = first + i * kAtOnce;
-      const bool key = r >= A.q.n;
-      const long at = key ? t * A.k.token + (r - A.q.n) * A.k.head : t * A.q.token + r * A.q.head;
-      raw[i] = head_fetch<XK>(key ? A.k.p : A.q.p, at, s, r < end);
+    for (int i = 0; i < kGroups; ++i) {
+      const bool key = first + i >= A.groups_q;
+      const head_rows& R = key ? A.k : A.q;
+      const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
+      raw[i] = head_fetch<XK, WHOLE>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
-  fetch(row);
+  fetch(group);
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.L.rot ? A.positions[t] : 0);
   float w_q[8], w_k[8];
-  head_weights(A.w_q, A.wkind, s, w_q);
-  head_weights(A.w_k, A.wkind, s, w_k);
-  // (the condition is the wavefront's, so that all lanes of a row sum are there)
-  for (int first = part * A.rows_per_part; first < end; first += kRows * kAtOnce, row += kRows * kAtOnce) {
-    float v[kRows][8];
+  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
+  for (; group < end; group += kGroups) {
+    float v[kGroups][8];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) head_values<XK>(raw[i], v[i]);
-    if (first + kRows * kAtOnce < end) fetch(row + kRows * kAtOnce);
+    for (int i = 0; i < kGroups; ++i) head_values<XK>(raw[i], v[i]);
+    if (group + kGroups < end) fetch(group + kGroups);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = row + i * kAtOnce;
-      const bool key = r >= A.q.n;
-      if (A.w_q || A.w_k) {
-        float w[8], plain[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = key ? w_k[e] : w_q[e];
-          plain[e] = v[i][e];
-        }
-        head_normed<LANES>(v[i], w, A.inv_D, A.eps);
-        if (!(key ? A.w_k : A.w_q)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[i][e] = plain[e];
-        }
+    for (int i = 0; i < kGroups; ++i) {
+      const bool key = group + i >= A.groups_q;
+      const head_rows& R = key ? A.k_out : A.q_out;
+      const int h0 = (group + i - (key ? A.groups_q : 0)) * kAtOnce;
+      if (key ? A.w_k : A.w_q) {
+        if (key) head_normed<LANES>(v[i], w_k, A.inv_D, A.eps);
+        else head_normed<LANES>(v[i], w_q, A.inv_D, A.eps);
       }
-      turn_values<false>(A.L, s, turn, v[i]);
-      if (r < end) {
-        const long at = key ? t * A.k_out.token + (r - A.q.n) * A.k_out.head : t * A.q_out.token + r * A.q_out.head;
-        head_store<OK>(const_cast<void*>(key ? A.k_out.p : A.q_out.p), at, s, v[i]);
-      }
+      turn_values<INTER, false>(s, turn, v[i]);
+      if (group + i < end && h0 + sub < R.n)
+        head_store<OK, WHOLE>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, v[i]);
     }
   }
 }
@@ -100,12 +89,9 @@ extern "C" cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, cons
   a.k = make_head_rows(k);
   a.q_out = make_head_rows(q ? q_out : nullptr);
   a.k_out = make_head_rows(k ? k_out : nullptr);
-  // Few tokens: their heads on several wavefronts, one instruction's rows at a time.
-  const int rows = a.q.n + a.k.n, at_once = 64 / a.L.lanes;
-  int parts = 1;
-  while (parts * 2 * at_once <= rows + at_once && (long)T * parts < 2048) parts *= 2;
-  a.rows_per_part = (int)((cq_align_up((size_t)((rows + parts - 1) / parts), at_once)));
-  a.parts = (rows + a.rows_per_part - 1) / a.rows_per_part;
+  a.groups_q = head_groups(a.q.n, a.L);
+  a.groups = a.groups_q + head_groups(a.k.n, a.L);
+  share_groups(a.groups, T, 2048, a.per_part, a.parts);
   const long most = (kMostThreads / 64 / a.parts) & ~3l;
   for (long from = 0; from < T; from += most) {
     head_norm_args b = a;
@@ -116,12 +102,12 @@ extern "C" cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, cons
     b.q_out = rows_from(a.q_out, out, from);
     b.k_out = rows_from(a.k_out, out, from);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, OK, LANES) hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES>), grid, dim3(256), 0, (hipStream_t)stream, b)
-    if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F16, CQ_A_F16);
-    else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_BF16, CQ_A_BF16);
-    else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F32);
-    else if (out == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F16);
-    else CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_BF16);
+#define LAUNCH(XK, OK, LANES, WHOLE, INTER) hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES, WHOLE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
+    if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
+    else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
+    else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F32);
+    else if (out == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F16);
+    else CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_BF16);
 #undef LAUNCH
   }
   return cq_check_launch();

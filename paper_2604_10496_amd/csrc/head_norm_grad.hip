@@ -10,14 +10,14 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMostParts = 256;   // one workgroup per compute unit
-constexpr int kRows = 2;          // rows of a lane in flight
+constexpr int kGroups = 2;        // groups of rows in flight
 
 inline int weight_parts(int T) { return T < kMostParts ? T : kMostParts; }
 inline size_t weight_row(int D) { return cq_align_up((size_t)D, 8); }
 
 struct head_grad_args {
   head_layout L;
-  int T, split, rows_per_unit, wkind;   // a unit: one token, rows_per_unit of its heads; split units per token
+  int T, split, per_unit, groups_q, groups, wkind;   // a unit: one token, per_unit groups of its heads; split units per token
   float eps, rot_scale, inv_D;
   const double* freq;
   const void *w_q, *w_k;
@@ -26,75 +26,78 @@ struct head_grad_args {
   float* part;   // [workgroups][2][D], NULL: not wanted
 };
 
-template <int XK, int OK, int LANES>
+// g: the gradient behind a row's norm -> in front of it; its share of the weight's gradient
+template <int LANES>
+__device__ __forceinline__ void head_back(const float (&x)[8], float (&g)[8], const float (&w)[8], float (&acc)[8], float inv_D, float eps) {
+  float ss = 0.f, gx = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    ss = fmaf(x[e], x[e], ss);
+    gx = fmaf(g[e] * w[e], x[e], gx);
+  }
+  const float r = 1.f / sqrtf(row_sum<LANES>(ss) * inv_D + eps);
+  const float back = r * r * (row_sum<LANES>(gx) * inv_D);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    acc[e] = fmaf(g[e], x[e] * r, acc[e]);
+    g[e] = r * fmaf(-back, x[e], g[e] * w[e]);
+  }
+}
+
+template <int XK, int OK, int LANES, bool WHOLE, bool INTER>
 __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
   constexpr int kAtOnce = 64 / LANES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const head_slot s(A.L, lane % LANES);
   float w_q[8], w_k[8], acc_q[8], acc_k[8];
-  head_weights(A.w_q, A.wkind, s, w_q);
-  head_weights(A.w_k, A.wkind, s, w_k);
+  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc_q[e] = acc_k[e] = 0.f;
-  const int rows = A.q.n + A.k.n;
+  const int sub = lane / LANES;
   const long units = (long)A.T * A.split;
   // the workgroups take units in turn, so that few tokens spread out
   for (long unit = (long)wave * gridDim.x + blockIdx.x; unit < units; unit += (long)kWaves * gridDim.x) {
-    const int t = (int)(unit / A.split), from = (int)(unit - (long)t * A.split) * A.rows_per_unit;
-    const int end = min(rows, from + A.rows_per_unit);
-    head_raw<XK> raw_x[kRows];
-    head_raw<OK> raw_d[kRows];
+    const int t = (int)(unit / A.split);
+    int group = (int)(unit - (long)t * A.split) * A.per_unit;
+    const int end = min(A.groups, group + A.per_unit);
+    head_raw<XK> raw_x[kGroups];
+    head_raw<OK> raw_d[kGroups];
     auto fetch = [&](int first) {
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const int r = first + i * kAtOnce;
-        const bool key = r >= A.q.n;
-        const int h = key ? r - A.q.n : r;
-        const bool norm = key ? A.w_k != nullptr : A.w_q != nullptr;
-        raw_d[i] = head_fetch<OK>(key ? A.dk_out.p : A.dq_out.p, t * (key ? A.dk_out.token : A.dq_out.token) + h * (key ? A.dk_out.head : A.dq_out.head),
-                                  s, r < end);
-        raw_x[i] = head_fetch<XK>(key ? A.k.p : A.q.p, t * (key ? A.k.token : A.q.token) + h * (key ? A.k.head : A.q.head), s, r < end && norm);
+      for (int i = 0; i < kGroups; ++i) {
+        const bool key = first + i >= A.groups_q;
+        const head_rows &X = key ? A.k : A.q, &G = key ? A.dk_out : A.dq_out;
+        const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
+        const bool on = first + i < end && h0 + sub < G.n;
+        raw_d[i] = head_fetch<OK, WHOLE>(G.p, t * G.token + h0 * G.head + sub * G.head, s, on);
+        raw_x[i] = head_fetch<XK, WHOLE>(X.p, t * X.token + h0 * X.head + sub * X.head, s, on && (key ? A.w_k : A.w_q));
       }
     };
-    int row = from + lane / LANES;
-    fetch(row);
+    fetch(group);
     const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.L.rot ? A.positions[t] : 0);
-    for (int first = from; first < end; first += kRows * kAtOnce, row += kRows * kAtOnce) {
-      float x[kRows][8], g[kRows][8];
+    for (; group < end; group += kGroups) {
+      float x[kGroups][8], g[kGroups][8];
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
+      for (int i = 0; i < kGroups; ++i) {
         head_values<XK>(raw_x[i], x[i]);
         head_values<OK>(raw_d[i], g[i]);
       }
-      if (first + kRows * kAtOnce < end) fetch(row + kRows * kAtOnce);
+      if (group + kGroups < end) fetch(group + kGroups);
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const int r = row + i * kAtOnce;
-        const bool key = r >= A.q.n;
-        const int h = key ? r - A.q.n : r;
-        turn_values<true>(A.L, s, turn, g[i]);
-        if (A.w_q || A.w_k) {
-          float w[8], ss = 0.f, gx = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            w[e] = key ? w_k[e] : w_q[e];
-            ss = fmaf(x[i][e], x[i][e], ss);
-            gx = fmaf(g[i][e] * w[e], x[i][e], gx);
-          }
-          const float rn = 1.f / sqrtf(row_sum<LANES>(ss) * A.inv_D + A.eps);
-          const float back = rn * rn * (row_sum<LANES>(gx) * A.inv_D);
-          if (key ? A.w_k != nullptr : A.w_q != nullptr) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float share = g[i][e] * (x[i][e] * rn);   // (0 where the row is not there: both were read as 0)
-              acc_q[e] += key ? 0.f : share;
-              acc_k[e] += key ? share : 0.f;
-              g[i][e] = rn * fmaf(-back, x[i][e], g[i][e] * w[e]);
-            }
-          }
+      for (int i = 0; i < kGroups; ++i) {
+        const bool key = group + i >= A.groups_q;
+        const head_rows& R = key ? A.dk : A.dq;
+        const int h0 = (group + i - (key ? A.groups_q : 0)) * kAtOnce;
+        turn_values<INTER, true>(s, turn, g[i]);
+        // (rows that are not there were read as zeros and add nothing)
+        if (key) {
+          if (A.w_k) head_back<LANES>(x[i], g[i], w_k, acc_k, A.inv_D, A.eps);
+        } else {
+          if (A.w_q) head_back<LANES>(x[i], g[i], w_q, acc_q, A.inv_D, A.eps);
         }
-        if (r < end)
-          head_store<XK>(const_cast<void*>(key ? A.dk.p : A.dq.p), t * (key ? A.dk.token : A.dq.token) + h * (key ? A.dk.head : A.dq.head), s, g[i]);
+        if (group + i < end && h0 + sub < R.n)
+          head_store<XK, WHOLE>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, g[i]);
       }
     }
   }
@@ -198,22 +201,18 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
   a.dk_out = make_head_rows(d_k_out);
   a.dq = make_head_rows(d_q_out ? d_q : nullptr);
   a.dk = make_head_rows(d_k_out ? d_k : nullptr);
-  a.q.n = a.dq.n;   // (the rows are counted there, also where they are not read)
-  a.k.n = a.dk.n;
   a.part = weights ? (float*)workspace : nullptr;
   const int parts = weight_parts(T);
   if (T > 0) {
-    const int rows = a.q.n + a.k.n, step = kRows * 64 / a.L.lanes;
-    int split = 1;
-    while (split * 2 * step <= rows + step && (long)T * split < 2 * kMostParts * kWaves) split *= 2;
-    a.rows_per_unit = (int)cq_align_up((size_t)((rows + split - 1) / split), step);
-    a.split = (rows + a.rows_per_unit - 1) / a.rows_per_unit;
-#define LAUNCH(XK, OK, LANES) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES>), dim3(parts), dim3(kThreads), 0, str, a)
-    if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F16, CQ_A_F16);
-    else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_BF16, CQ_A_BF16);
-    else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F32);
-    else if (out == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_F16);
-    else CQ_HEAD_LANES(LAUNCH, a.L.lanes, CQ_A_F32, CQ_A_BF16);
+    a.groups_q = head_groups(a.dq.n, a.L);
+    a.groups = a.groups_q + head_groups(a.dk.n, a.L);
+    share_groups(a.groups, T, 2 * kMostParts * kWaves, a.per_unit, a.split);
+#define LAUNCH(XK, OK, LANES, WHOLE, INTER) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES, WHOLE, INTER>), dim3(parts), dim3(kThreads), 0, str, a)
+    if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
+    else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
+    else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F32);
+    else if (out == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F16);
+    else CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_BF16);
 #undef LAUNCH
   }
   if (weights) {

@@ -25,17 +25,20 @@ constexpr float kMostE4M3 = 448.f;
 struct head_layout {
   int D, rot, inter;
   int turned;   // lanes that hold rotated values
+  int used;     // lanes that hold any
   int lanes;    // 8, 16, 32 or 64
+  bool whole;   // each of them holds eight
 };
 
 inline head_layout make_head_layout(int D, int rot, int inter) {
   head_layout L;
   L.D = D;
   L.rot = rot;
-  L.inter = inter;
+  L.inter = inter && rot > 0;
   L.turned = inter ? (rot + 7) / 8 : (rot / 2 + 3) / 4;
-  const int need = L.turned + (D - rot + 7) / 8;
-  L.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : 64;
+  L.used = L.turned + (D - rot + 7) / 8;
+  L.lanes = L.used <= 8 ? 8 : L.used <= 16 ? 16 : L.used <= 32 ? 32 : 64;
+  L.whole = L.used * 8 == D;
   return L;
 }
 
@@ -80,6 +83,17 @@ inline head_rows make_head_rows(const cq_heads* h) {
   return r;
 }
 
+// the groups of rows that a wavefront takes in one instruction: heads of one kind, so that what depends on the kind is the same in every lane
+inline int head_groups(int n, const head_layout& L) { return (n + 64 / L.lanes - 1) / (64 / L.lanes); }
+
+// Groups per wavefront and wavefronts per token: one, or several where there are few tokens (at most `most` wavefronts come of that).
+inline void share_groups(int groups, long T, long most, int& per_part, int& parts) {
+  parts = 1;
+  while (parts * 2 <= groups && T * parts * 2 <= most) parts *= 2;
+  per_part = (groups + parts - 1) / parts;
+  parts = (groups + per_part - 1) / per_part;
+}
+
 inline head_rows rows_from(head_rows r, int kind, long token) {
   r.p = row_at(r.p, kind, (size_t)(token * r.token));
   return r;
@@ -93,27 +107,26 @@ typedef cq_v2u cq_v2u_any __attribute__((aligned(2)));
 
 template <int KIND>
 struct quad {
-  static constexpr int N = KIND == CQ_A_F32 ? 4 : 2;
-  uint32_t w[N];
+  static constexpr int N = 2;
+  cq_v2u w;
+};
+template <>
+struct quad<CQ_A_F32> {
+  static constexpr int N = 4;
+  cq_v4u w;
 };
 
-template <int KIND>
+template <int KIND, bool WHOLE>
 __device__ __forceinline__ quad<KIND> quad_fetch(const void* p, long at, int n) {
   quad<KIND> q;
-#pragma unroll
-  for (int i = 0; i < quad<KIND>::N; ++i) q.w[i] = 0u;
+  q.w = decltype(q.w){};
   const char* b = reinterpret_cast<const char*>(p) + at * (KIND == CQ_A_F32 ? 4 : 2);
   if (n == 4) {
-    if constexpr (KIND == CQ_A_F32) {
-      const cq_v4u v = *reinterpret_cast<const cq_v4u_any*>(b);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q.w[i] = v[i];
-    } else {
-      const cq_v2u v = *reinterpret_cast<const cq_v2u_any*>(b);
-      q.w[0] = v[0];
-      q.w[1] = v[1];
-    }
-  } else {
+    if constexpr (KIND == CQ_A_F32)
+      q.w = *reinterpret_cast<const cq_v4u_any*>(b);
+    else
+      q.w = *reinterpret_cast<const cq_v2u_any*>(b);
+  } else if constexpr (!WHOLE) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       if (i < n) {
@@ -188,25 +201,17 @@ struct head_slot {
   int a, b, na, nb, first;
   bool turned;
   __device__ __forceinline__ head_slot(const head_layout& L, int j) {
+    const int half = L.rot >> 1;
+    const bool apart = j < L.turned && !L.inter;
     turned = j < L.turned;
     first = 4 * j;
-    int from, end;
-    if (turned && !L.inter) {
-      const int half = L.rot >> 1;
-      from = 4 * j;
-      end = half;
-      a = from;
-      b = half + from;
-      na = nb = end - from < 4 ? end - from : 4;
-      return;
-    }
-    from = turned ? 8 * j : L.rot + 8 * (j - L.turned);
-    end = turned ? L.rot : L.D;
-    const int left = end - from;
+    const int from = apart ? 4 * j : turned ? 8 * j : L.rot + 8 * (j - L.turned);
+    const int left = (apart ? half : turned ? L.rot : L.D) - from;   // of which there are
+    const int more = apart ? left : left - 4;
     a = from;
-    b = from + 4;
+    b = apart ? half + from : from + 4;
     na = left < 0 ? 0 : left < 4 ? left : 4;
-    nb = left < 4 ? 0 : left < 8 ? left - 4 : 4;
+    nb = more < 0 ? 0 : more < 4 ? more : 4;
   }
 };
 
@@ -215,11 +220,19 @@ struct head_raw {
   quad<KIND> a, b;
 };
 
-template <int KIND>
+// WHOLE: the layout's lanes hold eight values or none, and the code for fewer, ten times as long, is left out (what single tokens wait
+// for is instructions: 1 token of 40 heads 6.6 us with it)
+template <int KIND, bool WHOLE>
 __device__ __forceinline__ head_raw<KIND> head_fetch(const void* p, long at, const head_slot& s, bool on) {
   head_raw<KIND> r;
-  r.a = quad_fetch<KIND>(p, at + s.a, on ? s.na : 0);
-  r.b = quad_fetch<KIND>(p, at + s.b, on ? s.nb : 0);
+  if constexpr (WHOLE) {
+    const bool there = on && s.na;
+    r.a = quad_fetch<KIND, WHOLE>(p, at + s.a, there ? 4 : 0);
+    r.b = quad_fetch<KIND, WHOLE>(p, at + s.b, there ? 4 : 0);
+  } else {
+    r.a = quad_fetch<KIND, WHOLE>(p, at + s.a, on ? s.na : 0);
+    r.b = quad_fetch<KIND, WHOLE>(p, at + s.b, on ? s.nb : 0);
+  }
   return r;
 }
 
@@ -232,24 +245,32 @@ __device__ __forceinline__ void head_values(const head_raw<KIND>& r, float (&v)[
   }
 }
 
-template <int KIND>
+template <int KIND, bool WHOLE>
 __device__ __forceinline__ void head_store(void* p, long at, const head_slot& s, const float (&v)[8]) {
   const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-  quad_store<KIND>(p, at + s.a, s.na, a);
-  quad_store<KIND>(p, at + s.b, s.nb, b);
+  if constexpr (WHOLE) {
+    if (s.na) {
+      quad_store<KIND>(p, at + s.a, 4, a);
+      quad_store<KIND>(p, at + s.b, 4, b);
+    }
+  } else {
+    quad_store<KIND>(p, at + s.a, s.na, a);
+    quad_store<KIND>(p, at + s.b, s.nb, b);
+  }
 }
 
 // a lane's share of a norm's weights (ones without a norm)
+template <bool WHOLE>
 __device__ __forceinline__ void head_weights(const void* w, int kind, const head_slot& s, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 1.f;
   if (!w) return;
   if (kind == CQ_A_F32)
-    head_values<CQ_A_F32>(head_fetch<CQ_A_F32>(w, 0, s, true), v);
+    head_values<CQ_A_F32>(head_fetch<CQ_A_F32, WHOLE>(w, 0, s, true), v);
   else if (kind == CQ_A_F16)
-    head_values<CQ_A_F16>(head_fetch<CQ_A_F16>(w, 0, s, true), v);
+    head_values<CQ_A_F16>(head_fetch<CQ_A_F16, WHOLE>(w, 0, s, true), v);
   else
-    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16>(w, 0, s, true), v);
+    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16, WHOLE>(w, 0, s, true), v);
 }
 
 // cosines and sines of a lane's four pairs
@@ -266,6 +287,19 @@ __device__ __forceinline__ float revolutions(int position, double freq) {
   return (float)((rev - rint(rev)) + rest);
 }
 
+// Cosine and sine of x revolutions, |x| <= 1/2 and a little: by quarters, of which the rest is at most pi/4, with the series of both to
+// where the next term is under 2^-29 (sine) and 2^-33 (cosine).  (The library's function for this keeps its results in scratch memory.)
+__device__ __forceinline__ void turn_by(float x, float& c, float& s) {
+  const float quarter = rintf(4.f * x);
+  const float t = 6.28318530717958647693f * fmaf(-0.25f, quarter, x), t2 = t * t;
+  const float sn = fmaf(t * t2, fmaf(t2, fmaf(t2, fmaf(t2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), t);
+  const float cs = fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, fmaf(t2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const int n = (int)quarter;
+  const float a = n & 1 ? sn : cs, b = n & 1 ? cs : sn;
+  c = (n + 1) & 2 ? -a : a;
+  s = n & 2 ? -b : b;
+}
+
 __device__ __forceinline__ head_turn turn_of(const head_layout& L, const head_slot& s, const double* freq, float rot_scale, int position) {
   head_turn t;
 #pragma unroll
@@ -273,7 +307,7 @@ __device__ __forceinline__ head_turn turn_of(const head_layout& L, const head_sl
     t.c[i] = 1.f;
     t.s[i] = 0.f;
     if (s.turned && s.first + i < (L.rot >> 1)) {
-      sincospif(2.f * revolutions(position, freq[s.first + i]), &t.s[i], &t.c[i]);
+      turn_by(revolutions(position, freq[s.first + i]), t.c[i], t.s[i]);
       t.c[i] *= rot_scale;
       t.s[i] *= rot_scale;
     }
@@ -282,13 +316,13 @@ __device__ __forceinline__ head_turn turn_of(const head_layout& L, const head_sl
 }
 
 // a' = a c - b s, b' = b c + a s; back: by the angle's negative
-template <bool BACK>
-__device__ __forceinline__ void turn_values(const head_layout& L, const head_slot& s, const head_turn& t, float (&v)[8]) {
+template <bool INTER, bool BACK>
+__device__ __forceinline__ void turn_values(const head_slot& s, const head_turn& t, float (&v)[8]) {
   if (!s.turned) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float sn = BACK ? -t.s[i] : t.s[i];
-    if (L.inter) {
+    if constexpr (INTER) {
       const float a = v[2 * i], b = v[2 * i + 1];
       v[2 * i] = fmaf(a, t.c[i], -(b * sn));
       v[2 * i + 1] = fmaf(b, t.c[i], a * sn);
@@ -324,13 +358,22 @@ __device__ __forceinline__ void head_normed(float (&v)[8], const float (&w)[8], 
 
 }  // namespace
 
-// Runs LAUNCH(..., LANES) for the lanes of a row.
-#define CQ_HEAD_LANES(LAUNCH, lanes, ...)              \
-  do {                                                 \
-    if ((lanes) == 8) LAUNCH(__VA_ARGS__, 8);          \
-    else if ((lanes) == 16) LAUNCH(__VA_ARGS__, 16);   \
-    else if ((lanes) == 32) LAUNCH(__VA_ARGS__, 32);   \
-    else LAUNCH(__VA_ARGS__, 64);                      \
+// Runs LAUNCH(..., LANES, WHOLE, INTER) for the lanes of a row (64 of them are never all whole: that would take 512 values).  Pairs of
+// neighbours and pairs apart are two kernels: in one the compiler reads a row's values by index, from scratch memory.
+#define CQ_HEAD_WIDTHS(LAUNCH, L, INTER, ...)                                   \
+  do {                                                                          \
+    if ((L).whole && (L).lanes == 8) LAUNCH(__VA_ARGS__, 8, true, INTER);       \
+    else if ((L).whole && (L).lanes == 16) LAUNCH(__VA_ARGS__, 16, true, INTER); \
+    else if ((L).whole) LAUNCH(__VA_ARGS__, 32, true, INTER);                   \
+    else if ((L).lanes == 8) LAUNCH(__VA_ARGS__, 8, false, INTER);              \
+    else if ((L).lanes == 16) LAUNCH(__VA_ARGS__, 16, false, INTER);            \
+    else if ((L).lanes == 32) LAUNCH(__VA_ARGS__, 32, false, INTER);            \
+    else LAUNCH(__VA_ARGS__, 64, false, INTER);                                 \
+  } while (0)
+#define CQ_HEAD_LANES(LAUNCH, L, ...)                              \
+  do {                                                             \
+    if ((L).inter) CQ_HEAD_WIDTHS(LAUNCH, L, true, __VA_ARGS__);   \
+    else CQ_HEAD_WIDTHS(LAUNCH, L, false, __VA_ARGS__);            \
   } while (0)
 
 #endif  // CQ_HEADS_H_
