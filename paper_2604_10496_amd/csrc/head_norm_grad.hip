@@ -10,7 +10,6 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMostParts = 256;   // one workgroup per compute unit
-constexpr int kGroups = 2;        // groups of rows in flight
 
 inline int weight_parts(int T) { return T < kMostParts ? T : kMostParts; }
 inline size_t weight_row(int D) { return cq_align_up((size_t)D, 8); }
@@ -47,6 +46,7 @@ __device__ __forceinline__ void head_back(const float (&x)[8], float (&g)[8], co
 template <int XK, int OK, int LANES, bool WHOLE, bool INTER>
 __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
   constexpr int kAtOnce = 64 / LANES;
+  constexpr int kGroups = XK == CQ_A_F32 ? 1 : 2;   // groups of rows in flight (two of fp32 take more registers than there are)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const head_slot s(A.L, lane % LANES);
   float w_q[8], w_k[8], acc_q[8], acc_k[8];
