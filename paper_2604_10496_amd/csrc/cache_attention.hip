@@ -12,31 +12,80 @@
 // Operands are of the cache's type (f16 for e4m3, which it holds exactly).  P, and queries of another type, are split into parts
 // that add up to 16 bits at least, 22 where queries or results are fp32: rounded once to 8 bits, P alone would cost the result
 // as much as its own rounding.
-// The cache is cut along its length into parts, so that few sequences fill the chip; a second launch joins them in order.
+// The work is cut into equal shares: the steps of all sequences, one sequence behind the other, are divided among as many wavefronts as
+// the chip holds, whatever the lengths; a share may begin and end inside a sequence and hold several.  A sequence inside one share is
+// finished there; the others' parts are joined, in order, by a second launch.  The four wavefronts of a workgroup take neighbouring
+// heads, whose rows lie side by side.
+#include <type_traits>
+
 #include "cache.h"
 
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kTile = 32;         // positions of a wavefront's step
-constexpr int kMostSplits = 1024;
+constexpr int kWaves = 4;         // of a workgroup, each by itself
 
 struct attention_args {
   cache_args C;
   int G, tiles;          // queries of a key head, groups of 16 of them
   int q_kind, out_kind, shift;   // shift: log2 of the page size, -1 where it is no power of two
-  int splits, split_len, window, first_seq;
+  int window, shares;    // shares of the work of a head
+  int blocks;            // workgroups, a multiple of eight
+  uint32_t page16, slot16;   // strides in units of 16 bytes
   float scale, softcap;
   const float* sinks;
   head_rows q, out;
-  float *lse, *part, *stat;
+  float *lse, *part, *stat;   // part [shares + sequences][query heads][D], stat [..][2]: the maximum and the sum behind it
 };
 
 __device__ __forceinline__ void span_of(const cache_args& C, int window, int s, int& begin, int& end) {
   const long most = (long)C.width * C.page_size;
   const int len = C.lengths[s];
-  end = len < 0 ? 0 : len > most ? (int)most : len;
+  end = len < 0 || C.pages == 0 ? 0 : len > most ? (int)most : len;
   begin = window > 0 && end > window ? end - window : 0;
+}
+
+// 64 sequences at a time, one per lane: what each reads, and the steps up to and with it.
+struct sequences {
+  int base;            // of the first
+  int begin, end, steps;
+  uint32_t upto;
+};
+
+__device__ __forceinline__ int steps_of(int begin, int end) { return (end - begin + kTile - 1) / kTile; }
+
+// (wave_sum's exchanges, as a running sum over the lanes)
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t n) {
+#define CQ_STEP(CTRL, ROWS) n += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)n, CTRL, ROWS, 0xf, false)
+  CQ_STEP(0x111, 0xf);   // row_shr:1
+  CQ_STEP(0x112, 0xf);   // row_shr:2
+  CQ_STEP(0x114, 0xf);   // row_shr:4
+  CQ_STEP(0x118, 0xf);   // row_shr:8
+  CQ_STEP(0x142, 0xa);   // row_bcast:15 into rows 1 and 3
+  CQ_STEP(0x143, 0xc);   // row_bcast:31 into rows 2 and 3
+#undef CQ_STEP
+  return n;
+}
+
+__device__ __forceinline__ sequences look_at(const attention_args& A, int lane, int base, uint32_t before) {
+  sequences q;
+  q.base = base;
+  q.begin = q.end = 0;
+  if (base + lane < A.C.n_seqs) span_of(A.C, A.window, base + lane, q.begin, q.end);
+  q.steps = steps_of(q.begin, q.end);
+  q.upto = before + sum_up_to((uint32_t)q.steps);
+  return q;
+}
+
+// The steps of all sequences; q: the last 64 of them (all, if there are no more).
+__device__ __forceinline__ uint32_t all_steps(const attention_args& A, int lane, sequences& q) {
+  uint32_t total = 0;
+  for (int base = 0; base < A.C.n_seqs; base += 64) {
+    q = look_at(A, lane, base, total);
+    total = (uint32_t)__builtin_amdgcn_readlane((int)q.upto, 63);
+  }
+  return total;
 }
 
 // results of a row: maximum (base 2) and sum of its exponentials, with the sink
@@ -107,8 +156,14 @@ __device__ __forceinline__ uint32_t two_f16(uint32_t codes) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)codes, 1.f, HI));
 }
 
-template <int CK, int DPAD, int WAVES, bool HIGH>
-__global__ __launch_bounds__(WAVES * 64) void cache_attention_kernel(attention_args A) {
+// Wavefronts of a SIMD that share the work: as many as ask for 16 KB at a time, which is a step of 128 dims of 16 bits.  With one of those
+// 48 sequences of up to 4096 positions take 78 us and their join 5.6, with two 80 and 6.5, with four 84 and 6.8; 64 dims of 8 bits
+// 33 with two, 30 with four, 35 with eight.
+constexpr int resident(int kind, int dpad) { return dpad >= 256 ? 1 : (kind == CQ_C_E4M3 ? 2 : 1) * 128 / dpad; }
+inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+template <int CK, int DPAD, bool HIGH>
+__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && DPAD == 64 ? 4 : 2) void cache_attention_kernel(attention_args A) {
   constexpr bool k8 = CK == CQ_C_E4M3;
   constexpr int kSize = k8 ? 1 : 2;
   constexpr int kSteps = DPAD / 32;                  // products over a row's dims
@@ -118,36 +173,135 @@ __global__ __launch_bounds__(WAVES * 64) void cache_attention_kernel(attention_a
   constexpr int kP = HIGH ? operand<CK>::kQuery : 2;
   constexpr int kKWords = k8 ? DPAD / 64 : DPAD / 32;            // 16-byte pieces of a row of K per lane
   constexpr int kVWords = kE * kSize / 4;                        // words of a row of V per lane and chunk
-  extern __shared__ __align__(16) float lds[];
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int unit = blockIdx.x;
-  const int split = unit % A.splits;
-  unit /= A.splits;
-  const int h = unit % A.C.heads;
-  unit /= A.C.heads;
-  const int tile = unit % A.tiles, s = A.first_seq + unit / A.tiles;
-  const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16;
-  int begin, end;
-  span_of(A.C, A.window, s, begin, end);
-  begin += split * A.split_len;   // (at most splits * split_len < 2^31: checked on the host)
-  if (split + 1 < A.splits) end = min(end, begin + A.split_len);
-  if (A.splits > 1 && begin >= end) return;
   const int D = A.C.D;
+  const bool whole = D == DPAD;
+  // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
+  const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
+  const int unit = __builtin_amdgcn_readfirstlane(block * kWaves + (threadIdx.x >> 6));
+  const int columns = A.C.heads * A.tiles, number = unit / columns, column = unit - number * columns;
+  if (number >= A.shares) return;
+  const int tile = column / A.C.heads, h = column - tile * A.C.heads;
+  const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16, heads = A.G * A.C.heads;
+  sequences near;
+  const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
+  const uint32_t from_step = number * share, to_step = min(total, from_step + share);
+  if (from_step >= to_step) return;
+  if (A.C.n_seqs > 64) near = look_at(A, lane, 0, 0u);
+  // the sequence in which the share begins
+  int s = 0;
+  for (;;) {
+    const uint64_t behind = __ballot(near.upto > from_step);
+    s = near.base + (behind ? __builtin_ctzll(behind) : 64);
+    if (behind) break;
+    near = look_at(A, lane, near.base + 64, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));   // (from_step < total: one follows)
+  }
+  const char* const K = reinterpret_cast<const char*>(A.C.k) + (long)h * A.C.head * kSize + g * 16;
+  const char* const V = reinterpret_cast<const char*>(A.C.v) + (long)h * A.C.head * kSize + (c * kE < D ? c * kE : 0) * kSize;
 
-  // the queries: column c of the product's second operand
+  for (; s < A.C.n_seqs; ++s) {
+  if (s - near.base == 64) near = look_at(A, lane, s, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));
+  const int steps = __builtin_amdgcn_readlane(near.steps, s - near.base);
+  const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, s - near.base) - steps;
+  if (before >= to_step) break;
+  if (steps == 0) continue;
+  const int first = from_step > before ? (int)(from_step - before) : 0, last = min((int)(to_step - before), steps);
+  const int start = __builtin_amdgcn_readlane(near.begin, s - near.base);
+  const int begin = start + first * kTile, end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + last * kTile);
+
+  const int32_t* table = A.C.table + (long)s * A.C.table_stride;
+  // the page of position from + lane % 32 (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
+  // are not there are read from page 0 and left out afterwards, so that no load stands behind a branch.
+  auto page_of = [&](int from) {
+    const int p = min(from + (lane & 31), end - 1);
+    return table[A.shift >= 0 ? p >> A.shift : p / A.C.page_size];
+  };
+  auto row_of = [&](int from, int page, uint32_t& there) {
+    const int p = from + (lane & 31);
+    const int slot = A.shift >= 0 ? p & (A.C.page_size - 1) : p % A.C.page_size;
+    const bool on = p < end && (uint32_t)page < (uint32_t)A.C.pages;
+    there = (uint32_t)__ballot(on);
+    return on ? (uint32_t)page * A.page16 + (uint32_t)slot * A.slot16 : 0u;
+  };
+  cq_v4u k[2][kKWords];                     // K: rows c and 16 + c
+  uint32_t v[kChunks][8][kVWords];          // V: dims kE c .. of rows 4g .. 4g+3 and 16 + 4g ..
+  auto load_k = [&](uint32_t at) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const char* p = K + ((size_t)(uint32_t)__shfl((int)at, n * 16 + c) << 4);
+#pragma unroll
+      for (int i = 0; i < kKWords; ++i) {
+        constexpr int kStep = 64;           // bytes between a lane's pieces
+        // (a lane without dims in a piece reads the row's first ones, which its queries' zeros do not meet: see below)
+        k[n][i] = *reinterpret_cast<const cq_v4u*>(p + (whole || (i * kStep + g * 16) < D * kSize ? i * kStep : -g * 16));
+      }
+    }
+  };
+  auto load_v = [&](uint32_t at) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* p = V + ((size_t)(uint32_t)__shfl((int)at, (j >> 2) * 16 + g * 4 + (j & 3)) << 4);
+#pragma unroll
+      for (int n = 0; n < kChunks; ++n) {
+        // (lanes without dims read others, for results that are not stored)
+        const char* x = p + (n == 0 || whole || c * kE + 128 < D ? n * 128 * kSize : 0);
+        if constexpr (kVWords == 4) {
+          const cq_v4u w = *reinterpret_cast<const cq_v4u*>(x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[n][j][i] = w[i];
+        } else if constexpr (kVWords == 2) {
+          const cq_v2u w = *reinterpret_cast<const cq_v2u*>(x);
+          v[n][j][0] = w[0];
+          v[n][j][1] = w[1];
+        } else {
+          v[n][j][0] = *reinterpret_cast<const uint32_t*>(x);
+        }
+      }
+    }
+  };
+
+  cq_v4f O[kChunks][kE];
+#pragma unroll
+  for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+    for (int d = 0; d < kE; ++d) O[n][d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;   // of query c; l: this lane's share
+  const float cap2 = A.softcap > 0.f ? 2.f * kLog2e / A.softcap : 0.f;
+
+  // what does not wait for anything first: pages, queries, then K and V; the queries become operands while those are under way
+  uint32_t there;
+  const int page0 = page_of(begin);
+  int page = page_of(begin + kTile);
+  cq_v4u raw[kSteps][2];
+  {
+    const size_t size = A.q_kind == CQ_A_F32 ? 4 : 2;
+    const char* row = reinterpret_cast<const char*>(A.q.p) + ((long)s * A.q.token + (long)(first_head + c) * A.q.head) * size;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int d = k8 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8;
+      raw[i][0] = raw[i][1] = cq_v4u{0u, 0u, 0u, 0u};
+      if (c < rows && d < D) {
+        const cq_v4u_any* p = reinterpret_cast<const cq_v4u_any*>(row + d * size);
+        raw[i][0] = p[0];
+        if (A.q_kind == CQ_A_F32) raw[i][1] = p[1];
+      }
+    }
+  }
+  {
+    const uint32_t at = row_of(begin, page0, there);
+    load_k(at);
+    load_v(at);
+  }
+  // column c of the product's second operand
   cq_v4u Q[kSteps][kQ];
   float back = 1.f;   // what the queries were divided by
   {
     float v[kSteps][8], most = 0.f;
-    const long row = (long)s * A.q.token + (long)(first_head + c) * A.q.head;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const int d = k8 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8;
-      const bool on = c < rows && d < D;
-      if (A.q_kind == CQ_A_F32) row_values<CQ_A_F32>(row_fetch<CQ_A_F32>(A.q.p, row + d, on ? 8 : 0), v[i]);
-      else if (A.q_kind == CQ_A_F16) row_values<CQ_A_F16>(row_fetch<CQ_A_F16>(A.q.p, row + d, on ? 8 : 0), v[i]);
-      else row_values<CQ_A_BF16>(row_fetch<CQ_A_BF16>(A.q.p, row + d, on ? 8 : 0), v[i]);
+      if (A.q_kind == CQ_A_F32) row_values<CQ_A_F32>(row8<CQ_A_F32>{{raw[i][0], raw[i][1]}}, v[i]);
+      else if (A.q_kind == CQ_A_F16) row_values<CQ_A_F16>(row8<CQ_A_F16>{{raw[i][0]}}, v[i]);
+      else row_values<CQ_A_BF16>(row8<CQ_A_BF16>{{raw[i][0]}}, v[i]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
     }
@@ -169,69 +323,20 @@ __global__ __launch_bounds__(WAVES * 64) void cache_attention_kernel(attention_a
   }
   const float factor = A.scale * back * (k8 && A.C.k_scale ? A.C.k_scale[h] : 1.f);
 
-  const int32_t* table = A.C.table + (long)s * A.C.table_stride;
-  const char* K = reinterpret_cast<const char*>(A.C.k) + (long)h * A.C.head * kSize;
-  const char* V = reinterpret_cast<const char*>(A.C.v) + (long)h * A.C.head * kSize;
-  // where the row of position from + lane % 32 lies, in bytes; -1: it has none
-  auto row_at = [&](int from) -> long {
-    const int p = from + (lane & 31);
-    if (p >= end) return -1;
-    const int column = A.shift >= 0 ? p >> A.shift : p / A.C.page_size;
-    const int page = table[column];
-    if (page < 0 || page >= A.C.pages) return -1;
-    return (page * A.C.page + (p - column * A.C.page_size) * A.C.slot) * kSize;
-  };
 
-  cq_v4f O[kChunks][kE];
+  // K of the next positions is asked for when this step's scores are there, V when its products are: a step's rows are under way
+  // during the half of a step behind it, in the registers that have just been read.  Its pages are asked for a step earlier.
+  for (int from = begin; from < end; from += kTile) {
+    const uint32_t mine = there;
+    const uint32_t at = row_of(from + kTile, page, there);
+    page = page_of(from + 2 * kTile);
+    if (!whole) {
 #pragma unroll
-  for (int n = 0; n < kChunks; ++n)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-    for (int d = 0; d < kE; ++d) O[n][d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;   // of query c; l: this lane's share
-
-  int from = begin + wave * kTile;
-  long at = from < end ? row_at(from) : -1;
-  for (; from < end; from += WAVES * kTile) {
-    const uint32_t there = (uint32_t)__ballot(at >= 0);
-    // K: rows c and 16 + c
-    cq_v4u k[2][kKWords];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const long row = __shfl(at, n * 16 + c);
-#pragma unroll
-      for (int i = 0; i < kKWords; ++i) {
-        const int d = k8 ? i * 64 + g * 16 : i * 32 + g * 8;
-        k[n][i] = cq_v4u{0u, 0u, 0u, 0u};
-        if (row >= 0 && d < D) k[n][i] = *reinterpret_cast<const cq_v4u*>(K + row + d * kSize);
-      }
+        for (int i = 0; i < kKWords; ++i)
+          if (i * 64 + g * 16 >= D * kSize) k[n][i] = cq_v4u{0u, 0u, 0u, 0u};
     }
-    // V: dims kE c .. of rows 4g .. 4g+3 and 16 + 4g ..
-    uint32_t v[kChunks][8][kVWords];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const long row = __shfl(at, (j >> 2) * 16 + g * 4 + (j & 3));
-#pragma unroll
-      for (int n = 0; n < kChunks; ++n) {
-        const int d = n * 128 + c * kE;
-#pragma unroll
-        for (int w = 0; w < kVWords; ++w) v[n][j][w] = 0u;
-        if (row >= 0 && d < D) {
-          const char* p = V + row + d * kSize;
-          if constexpr (kVWords == 4) {
-            const cq_v4u x = *reinterpret_cast<const cq_v4u*>(p);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) v[n][j][w] = x[w];
-          } else if constexpr (kVWords == 2) {
-            const cq_v2u x = *reinterpret_cast<const cq_v2u*>(p);
-            v[n][j][0] = x[0];
-            v[n][j][1] = x[1];
-          } else {
-            v[n][j][0] = *reinterpret_cast<const uint32_t*>(p);
-          }
-        }
-      }
-    }
-    if (from + WAVES * kTile < end) at = row_at(from + WAVES * kTile);
     // scores of query c at positions 4g + r and 16 + 4g + r
     float z[8];
 #pragma unroll
@@ -253,15 +358,24 @@ __global__ __launch_bounds__(WAVES * 64) void cache_attention_kernel(attention_a
 #pragma unroll
       for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r] * factor;
     }
+    if (from + kTile < end) load_k(at);
     if (A.softcap > 0.f) {
-      const float inv = 1.f / A.softcap;
+      // tanh x = 1 - 2 / (1 + e^(2x)), off by some units of the last place of 1
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = A.softcap * tanhf(z[j] * inv);
+      for (int j = 0; j < 8; ++j) z[j] = A.softcap * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z[j] * cap2)), 1.f);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[j] *= kLog2e;
-      if (there != 0xffffffffu) z[j] = there >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1u ? z[j] : -INFINITY;
+    for (int j = 0; j < 8; ++j) z[j] *= kLog2e;
+    if (mine != 0xffffffffu) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool on = mine >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1u;
+        z[j] = on ? z[j] : -INFINITY;
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+          for (int w = 0; w < kVWords; ++w) v[n][j][w] = on ? v[n][j][w] : 0u;
+      }
     }
     float top = m;
 #pragma unroll
@@ -311,131 +425,122 @@ __global__ __launch_bounds__(WAVES * 64) void cache_attention_kernel(attention_a
         }
       }
     }
+    if (from + kTile < end) load_v(at);
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-
-  // the wavefronts' shares, [WAVES][rows][DPAD + 4], and their maxima and sums behind them
-  constexpr int kPitch = DPAD + 4;
-  float* stats = lds + WAVES * rows * kPitch;   // [rows][WAVES][2]
   if (c < rows) {
-    float* o = lds + (wave * rows + c) * kPitch;
+    const int head = first_head + c;
+    float* stat = A.stat + ((size_t)(number + s) * heads + head) * 2;
+    float* part = A.part + ((size_t)(number + s) * heads + head) * D;
+    const bool all = first == 0 && last == steps;
+    float f = 1.f, lse;
+    if (all) {
+      close_row(m, l, A.sinks, head, f, lse);
+      if (k8 && A.C.v_scale) f *= A.C.v_scale[h];
+      if (g == 0 && A.lse) A.lse[(size_t)s * heads + head] = lse;
+    } else if (g == 0) {
+      stat[0] = m;
+      stat[1] = l;
+    }
+    const long to = (long)s * A.out.token + (long)head * A.out.head;
 #pragma unroll
     for (int n = 0; n < kChunks; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r) {
+        const int d0 = n * 128 + (g * 4 + r) * kE;
+        if (d0 >= D) continue;
 #pragma unroll
-        for (int d = 0; d < kE; d += 4)
-          *reinterpret_cast<cq_v4f*>(o + n * 128 + (g * 4 + r) * kE + d) = cq_v4f{O[n][d][r], O[n][d + 1][r], O[n][d + 2][r], O[n][d + 3][r]};
-    if (g == 0) {
-      stats[(c * WAVES + wave) * 2] = m;
-      stats[(c * WAVES + wave) * 2 + 1] = l;
-    }
-  }
-  __syncthreads();
-  const int quads = D >> 2;
-  for (int i = threadIdx.x; i < rows * quads; i += WAVES * 64) {
-    const int row = i / quads, d = (i - row * quads) * 4;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stats[(row * WAVES + w) * 2]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    cq_v4f o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float f = __builtin_amdgcn_exp2f(stats[(row * WAVES + w) * 2] - base);
-      sum = fmaf(stats[(row * WAVES + w) * 2 + 1], f, sum);
-      o += *reinterpret_cast<const cq_v4f*>(lds + (w * rows + row) * kPitch + d) * f;
-    }
-    const int head = first_head + row;
-    const size_t line = (size_t)s * A.G * A.C.heads + head;
-    if (A.splits > 1) {
-      *reinterpret_cast<cq_v4f*>(A.part + (line * A.splits + split) * D + d) = o;
-      if (d == 0) {
-        A.stat[(line * A.splits + split) * 2] = top;
-        A.stat[(line * A.splits + split) * 2 + 1] = sum;
+        for (int d = 0; d < kE; d += 4) {
+          const float o[4] = {O[n][d][r] * f, O[n][d + 1][r] * f, O[n][d + 2][r] * f, O[n][d + 3][r] * f};
+          if (all)
+            store4(const_cast<void*>(A.out.p), A.out_kind, to + d0 + d, o);
+          else
+            *reinterpret_cast<cq_v4f*>(part + d0 + d) = cq_v4f{o[0], o[1], o[2], o[3]};
+        }
       }
-    } else {
-      float f, lse;
-      close_row(top, sum, A.sinks, head, f, lse);
-      if (k8 && A.C.v_scale) f *= A.C.v_scale[h];
-      const float r[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
-      store4(const_cast<void*>(A.out.p), A.out_kind, (long)s * A.out.token + (long)head * A.out.head + d, r);
-      if (d == 0 && A.lse) A.lse[line] = lse;
-    }
+  }
   }
 }
 
-// joins the parts of a row in order: thread (quad of dims, every n-th part)
-__global__ __launch_bounds__(256) void attention_join_kernel(attention_args A) {
-  __shared__ float weight[kMostSplits];
-  __shared__ float red[8];
-  __shared__ cq_v4f sums[256];
-  const int heads = A.G * A.C.heads, s = A.first_seq + blockIdx.x / heads, head = blockIdx.x % heads, tid = threadIdx.x;
-  const size_t line = (size_t)s * heads + head;
-  int begin, end;
-  span_of(A.C, A.window, s, begin, end);
-  const int parts = min(A.splits, (end - begin + A.split_len - 1) / A.split_len);
-  const float* stat = A.stat + line * A.splits * 2;
-  float top = -INFINITY;
-  for (int i = tid; i < parts; i += 256) top = fmaxf(top, stat[2 * i]);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  if ((tid & 63) == 0) red[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-  for (int i = tid; i < parts; i += 256) {
-    const float f = __builtin_amdgcn_exp2f(stat[2 * i] - base);
-    weight[i] = f;
-    sum = fmaf(stat[2 * i + 1], f, sum);
+// Joins the parts of sequences that lie in several shares, in order: a group of threads takes every n-th part of a row (or of 32 of its
+// dims: `quads` of four each) with a running maximum, then the groups in order.  Rows of sequences without positions are written here too.
+template <int kJoin>
+__global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A, int first_row, int quads) {
+  __shared__ cq_v4f sums[kJoin];
+  __shared__ float stats[kJoin][2];
+  const int heads = A.G * A.C.heads, row = first_row + blockIdx.x, s = row / heads, head = row - s * heads, tid = threadIdx.x, lane = tid & 63;
+  sequences near;
+  const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
+  if (near.base > s || s >= near.base + 64) {
+    uint32_t before = 0;
+    for (int base = 0; base <= s; base += 64) {
+      near = look_at(A, lane, base, before);
+      before = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63);
+    }
   }
-  sum = wave_sum(sum);
-  if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
-  __syncthreads();
-  sum = red[4] + red[5] + red[6] + red[7];
-  const int D = A.C.D, quads = D >> 2, groups = 256 / quads, group = tid / quads, d = (tid - group * quads) * 4;
+  const int steps = __builtin_amdgcn_readlane(near.steps, s - near.base);
+  const uint32_t upto = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, s - near.base);
+  int first = 0, last = -1;
+  if (steps > 0) {
+    first = (int)((upto - steps) / share);
+    last = (int)((upto - 1) / share);
+    if (first == last) return;   // (it has been finished where it was)
+  }
+  const int D = A.C.D, groups = kJoin / quads, group = tid / quads, d = (blockIdx.y * quads + tid - group * quads) * 4;
+  float m = -INFINITY, l = 0.f;
   cq_v4f o = {0.f, 0.f, 0.f, 0.f};
-  if (group < groups) {
-    const float* part = A.part + line * A.splits * D + d;
+  if (group < groups && d < D) {
 #pragma unroll 4
-    for (int i = group; i < parts; i += groups) o += *reinterpret_cast<const cq_v4f*>(part + (size_t)i * D) * weight[i];
+    for (int i = first + group; i <= last; i += groups) {
+      const size_t line = (size_t)(i + s) * heads + head;
+      const float pm = A.stat[line * 2], pl = A.stat[line * 2 + 1];
+      const cq_v4f p = *reinterpret_cast<const cq_v4f*>(A.part + line * D + d);
+      const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.f : top;
+      const float a = __builtin_amdgcn_exp2f(m - base), b = __builtin_amdgcn_exp2f(pm - base);
+      o = o * a + p * b;
+      l = fmaf(l, a, pl * b);
+      m = top;
+    }
   }
   sums[tid] = o;
+  stats[tid][0] = m;
+  stats[tid][1] = l;
   __syncthreads();
-  if (group > 0) return;
-  for (int n = 1; n < groups; ++n) o += sums[n * quads + tid];
+  if (group > 0 || d >= D) return;
+  const int used = min(groups, last - first + 1);   // groups that had a part
+  float top = m;
+  for (int n = 1; n < used; ++n) top = fmaxf(top, stats[n * quads + tid][0]);
+  const float base = top == -INFINITY ? 0.f : top;
+  const float own = __builtin_amdgcn_exp2f(m - base);
+  o *= own;
+  l *= own;
+#pragma unroll 4
+  for (int n = 1; n < used; ++n) {
+    const float f = __builtin_amdgcn_exp2f(stats[n * quads + tid][0] - base);
+    o += sums[n * quads + tid] * f;
+    l = fmaf(stats[n * quads + tid][1], f, l);
+  }
   float f, lse;
-  close_row(top, sum, A.sinks, head, f, lse);
+  close_row(top, l, A.sinks, head, f, lse);
   if (A.C.v_scale) f *= A.C.v_scale[head / A.G];
   const float r[4] = {o[0] * f, o[1] * f, o[2] * f, o[3] * f};
   store4(const_cast<void*>(A.out.p), A.out_kind, (long)s * A.out.token + (long)head * A.out.head + d, r);
-  if (tid == 0 && A.lse) A.lse[line] = lse;
+  if (d == 0 && A.lse) A.lse[row] = lse;
 }
 
-struct plan {
-  int waves, splits, split_len;
-};
-
-// How many parts the sequences are cut into: about as many workgroups as the chip holds at once.
-inline plan plan_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
-  plan p;
-  const int G = Hq / C->heads;
-  const long units = (long)n_seqs * C->heads * ((G + 15) / 16);
+// Shares of a head's work: about as many wavefronts as the chip holds at once, at least one for every sequence, and no more than there
+// are steps where the lengths are as expected.
+inline long shares_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
+  const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
   const long span = window > 0 && window < max_length ? window : max_length;
-  p.waves = 4;
-  const long quantum = p.waves * kTile;
-  long splits = units > 0 ? (1024 + units - 1) / units : 1;
-  if (splits > (span + quantum - 1) / quantum) splits = (span + quantum - 1) / quantum;
-  if (splits > kMostSplits) splits = kMostSplits;
-  if (splits < 1) splits = 1;
-  p.split_len = (int)(((span + splits - 1) / splits + quantum - 1) / quantum * quantum);
-  if (p.split_len < quantum) p.split_len = (int)quantum;
-  p.splits = (int)((span + p.split_len - 1) / p.split_len);
-  if (p.splits < 1) p.splits = 1;
-  return p;
+  const long steps = ((span + kTile - 1) / kTile > 0 ? (span + kTile - 1) / kTile : 1) * n_seqs;
+  const long held = 1024l * resident(C->kind, padded(C->D));
+  long shares = (held + columns - 1) / columns;
+  if (shares < n_seqs) shares = n_seqs;
+  const long most = (kMostThreads / 64 / columns) & ~7l;   // (a launch's threads are counted in 32 bits)
+  if (shares > most) shares = most;
+  return shares < steps ? shares : steps;
 }
 
 inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_length) {
@@ -449,9 +554,8 @@ inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_
 
 extern "C" size_t cq_cache_attention_workspace_bytes(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
   if (check_attention(C, n_seqs, Hq, max_length) != CQ_OK) return 0;
-  const plan p = plan_of(C, n_seqs, Hq, max_length, window);
-  if (p.splits == 1) return 0;
-  return (size_t)n_seqs * Hq * p.splits * (C->D + 2) * 4;
+  if (n_seqs == 0) return 0;
+  return ((size_t)shares_of(C, n_seqs, Hq, max_length, window) + n_seqs) * Hq * (C->D + 2) * 4;
 }
 
 extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S, const cq_attention_spec* P, const cq_heads* q,
@@ -462,10 +566,16 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if ((st = check_heads(q, S->n)) != CQ_OK || (st = check_heads_out(q, out, S->n, C->D)) != CQ_OK) return st;
   if ((st = check_attention(C, S->n, q->n, P->max_length)) != CQ_OK) return st;
   if (!isfinite(P->scale) || !(P->softcap >= 0.f) || !isfinite(P->softcap) || P->window < 0) return CQ_ERR_SHAPE;
+  // (rows are found by 32-bit numbers of 16 bytes: caches of up to 64 GB each for keys and values)
+  if (C->pages > 0 &&
+      ((C->pages - 1) * (double)C->page_stride + (C->page_size - 1) * (double)C->slot_stride) * cache_elem(C->kind) / 16 >= 4294967295.)
+    return CQ_ERR_SHAPE;
+  // (rows and steps are counted in 32 bits)
+  if ((long)S->n * q->n > 1l << 30 || (double)S->n * S->width * C->page_size > 64e9) return CQ_ERR_SHAPE;
   if (S->n == 0) return CQ_OK;
-  const plan p = plan_of(C, S->n, q->n, P->max_length, P->window);
   const size_t need = cq_cache_attention_workspace_bytes(C, S->n, q->n, P->max_length, P->window);
-  if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < need) return CQ_ERR_WORKSPACE;
+  const long shares = shares_of(C, S->n, q->n, P->max_length, P->window);
   attention_args a;
   a.C = make_cache_args(C, S);
   a.G = q->n / C->heads;
@@ -475,9 +585,11 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.shift = -1;
   for (int i = 0; i < 31; ++i)
     if (C->page_size == 1 << i) a.shift = i;
-  a.splits = p.splits;
-  a.split_len = p.split_len;
+  a.shares = (int)shares;
   a.window = P->window;
+  const long unit = 16 / cache_elem(C->kind);
+  a.page16 = (uint32_t)(C->page_stride / unit);
+  a.slot16 = (uint32_t)(C->slot_stride / unit);
   a.scale = P->scale;
   a.softcap = P->softcap;
   a.sinks = P->sinks;
@@ -485,26 +597,12 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.out = make_head_rows(out);
   a.lse = lse;
   a.part = (float*)workspace;
-  a.stat = a.part + (size_t)S->n * q->n * p.splits * C->D;
+  a.stat = a.part + ((size_t)shares + S->n) * q->n * C->D;
   const bool high = q->kind == CQ_A_F32 || out->kind == CQ_A_F32 || (C->kind == CQ_A_BF16 && q->kind == CQ_A_F16);
-  const int dpad = C->D <= 64 ? 64 : C->D <= 128 ? 128 : 256;
-  const int rows = a.G < 16 ? a.G : 16;
-  const int lds = (p.waves * rows * (dpad + 4) + rows * p.waves * 2) * 4;
-  // sequences of a launch: its threads are counted in 32 bits
-  const long per_seq = (long)p.splits * C->heads * a.tiles;
-  const long most = (1l << 22) / (per_seq > q->n ? per_seq : q->n) > 0 ? (1l << 22) / (per_seq > q->n ? per_seq : q->n) : 1;
-  for (long from = 0; from < S->n; from += most) {
-    const long n = S->n - from < most ? S->n - from : most;
-    a.first_seq = (int)from;
-    const dim3 grid((unsigned)(n * per_seq));
-#define LAUNCH(CK, DPAD, HIGH)                                                                                              \
-  do {                                                                                                                      \
-    static std::atomic<bool> done{false};                                                                                   \
-    if (lds > 64 * 1024 - 1024 &&                                                                                           \
-        cq_configure_lds(cache_attention_kernel<CK, DPAD, 4, HIGH>, 4 * (16 * (DPAD + 4) + 32) * 4, done, false) != CQ_OK)  \
-      return CQ_ERR_HIP;                                                                                                    \
-    hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, 4, HIGH>), grid, dim3(256), lds, (hipStream_t)stream, a);          \
-  } while (0)
+  const int dpad = padded(C->D);
+  a.blocks = (int)cq_align_up((size_t)((shares * C->heads * a.tiles + kWaves - 1) / kWaves), 8);
+#define LAUNCH(CK, DPAD, HIGH) \
+  hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(kWaves * 64), 0, (hipStream_t)stream, a)
 #define WIDTHS(CK, HIGH)                      \
   do {                                        \
     if (dpad == 64) LAUNCH(CK, 64, HIGH);     \
@@ -516,13 +614,20 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
     if (high) WIDTHS(CK, true);  \
     else WIDTHS(CK, false);      \
   } while (0)
-    if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
-    else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
-    else KINDS(CQ_C_E4M3);
+  if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
+  else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
+  else KINDS(CQ_C_E4M3);
 #undef KINDS
 #undef WIDTHS
 #undef LAUNCH
-    if (p.splits > 1) hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)(n * q->n)), dim3(256), 0, (hipStream_t)stream, a);
+  // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
+  const bool many = shares >= 16l * S->n;
+  const int quads = many && C->D > 32 ? 8 : C->D / 4, threads = many ? 256 : 64;
+  const long all = (long)S->n * q->n, at_once = kMostThreads / threads;
+  for (long from = 0; from < all; from += at_once) {
+    const dim3 grid((unsigned)(all - from < at_once ? all - from : at_once), (C->D / 4 + quads - 1) / quads);
+    if (many) hipLaunchKernelGGL((attention_join_kernel<256>), grid, dim3(256), 0, (hipStream_t)stream, a, (int)from, quads);
+    else hipLaunchKernelGGL((attention_join_kernel<64>), grid, dim3(64), 0, (hipStream_t)stream, a, (int)from, quads);
   }
   return cq_check_launch();
 }

@@ -404,6 +404,31 @@ def test_attention_lengths_beyond_what_was_expected(cq, max_length):
     _check_attention(cq, cache, _rows(g, 4, 4, 64, "f16"), table, lens, max_length=max_length)
 
 
+@pytest.mark.parametrize("S,longest,Hk", [(64, 40, 1), (65, 300, 2), (200, 70, 1), (1000, 90, 1), (130, 2000, 1)])
+def test_attention_many_sequences(cq, S, longest, Hk):
+    """More sequences than a wavefront has lanes, many of them empty, in shares that hold several."""
+    import torch
+    g = torch.Generator().manual_seed(S)
+    lengths = torch.randint(0, longest + 1, (S,), generator=g)
+    lengths[torch.rand(S, generator=g) < 0.3] = 0
+    lengths[:3] = lengths[-2:] = 0
+    cache, table, lens = _paged(cq, g, lengths.tolist(), 16, Hk, 64, "bf16")
+    for window in (0, 50):
+        got = _check_attention(cq, cache, _rows(g, S, 2 * Hk, 64, "bf16"), table, lens, window=window, max_length=longest)
+        assert not got["out"][lens == 0].any()
+
+
+def test_attention_all_empty(cq):
+    import torch
+    g = torch.Generator().manual_seed(24)
+    cache, table, lens = _paged(cq, g, [0, 0, 0], 16, 1, 64, "bf16")
+    _check_attention(cq, cache, _rows(g, 3, 2, 64, "bf16"), table, lens)
+    none = cq.PagedCache(cache.k[:0], cache.v[:0])                       # a cache without pages
+    _check_attention(cq, none, _rows(g, 3, 2, 64, "bf16"), table, torch.full_like(lens, 9))
+    out = cq.cq_cache_attention(cache, _rows(g, 0, 2, 64, "bf16"), table[:0], lens[:0])
+    assert out["out"].shape == (0, 2, 64) and out["lse"].shape == (0, 2)
+
+
 def test_attention_long(cq):
     import torch
     g = torch.Generator().manual_seed(12)

@@ -177,7 +177,9 @@ def test_cache_attention_refusals():
     need = lib.cq_cache_attention_workspace_bytes(_cache(), 4, 2, 1 << 16, 0)
     assert need > 0 and call(max_length=1 << 16, n=need - 1) == 4 and call(max_length=1 << 16, ws=None) == 4
     assert lib.cq_cache_attention_workspace_bytes(_cache(D=60), 4, 2, 1 << 16, 0) == 0
-    assert lib.cq_cache_attention_workspace_bytes(_cache(), 4, 2, 1 << 16, 32) == 0       # a short window needs no parts
+    assert lib.cq_cache_attention_workspace_bytes(_cache(), 0, 2, 1 << 16, 0) == 0
+    assert call(c=dict(pages=1 << 30, page_stride=1 << 20)) == 2                          # rows beyond 64 GB
+    assert call(s=dict(n=1 << 30, width=1, stride=1)) == 2
     assert call(s=dict(n=0, page_table=None, lengths=None)) == 0
 
 
