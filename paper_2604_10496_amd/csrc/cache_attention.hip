@@ -162,13 +162,33 @@ __device__ __forceinline__ uint32_t two_f16(uint32_t codes) {
 constexpr int resident(int kind, int dpad) { return dpad >= 256 ? 1 : (kind == CQ_C_E4M3 ? 2 : 1) * 128 / dpad; }
 inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-template <int CK, int DPAD, bool HIGH>
-__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && DPAD == 64 ? 4 : 2) void cache_attention_kernel(attention_args A) {
+// What a kernel's lanes hold of a row's results: query c's at dims 128 n + kE (4 g + r) + d, unscaled, the maximum (base 2) of its scores
+// and the sum of the exponentials behind it (this lane's positions).
+template <int DPAD>
+struct row_state {
+  static constexpr int kE = DPAD >= 128 ? 8 : DPAD / 16;    // neighbouring dims of a lane in V
+  static constexpr int kChunks = DPAD / (16 * kE);
+  cq_v4f O[kChunks][kE];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+      for (int d = 0; d < kE; ++d) O[n][d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// One wavefront's attention of the queries first_head .. first_head + rows - 1 of sequence s over the positions begin .. end-1 (there is
+// one), 32 at a time, of which it takes every NEXT / 32nd 32.
+template <int CK, int DPAD, bool HIGH, int NEXT>
+__device__ __forceinline__ void attend(const attention_args& A, int s, int h, int first_head, int rows, int begin, int end,
+                                       row_state<DPAD>& state) {
   constexpr bool k8 = CK == CQ_C_E4M3;
-  constexpr int kSize = k8 ? 1 : 2;
+  constexpr int kSize = k8 ? 1 : 2, kNext = NEXT;
   constexpr int kSteps = DPAD / 32;                  // products over a row's dims
-  constexpr int kE = DPAD >= 128 ? 8 : DPAD / 16;    // neighbouring dims of a lane in V
-  constexpr int kChunks = DPAD / (16 * kE);
+  constexpr int kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
   constexpr int kQ = HIGH ? operand<CK>::kQuery : 1;
   constexpr int kP = HIGH ? operand<CK>::kQuery : 2;
   constexpr int kKWords = k8 ? DPAD / 64 : DPAD / 32;            // 16-byte pieces of a row of K per lane
@@ -176,39 +196,10 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int D = A.C.D;
   const bool whole = D == DPAD;
-  // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
-  const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
-  const int unit = __builtin_amdgcn_readfirstlane(block * kWaves + (threadIdx.x >> 6));
-  const int columns = A.C.heads * A.tiles, number = unit / columns, column = unit - number * columns;
-  if (number >= A.shares) return;
-  const int tile = column / A.C.heads, h = column - tile * A.C.heads;
-  const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16, heads = A.G * A.C.heads;
-  sequences near;
-  const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
-  const uint32_t from_step = number * share, to_step = min(total, from_step + share);
-  if (from_step >= to_step) return;
-  if (A.C.n_seqs > 64) near = look_at(A, lane, 0, 0u);
-  // the sequence in which the share begins
-  int s = 0;
-  for (;;) {
-    const uint64_t behind = __ballot(near.upto > from_step);
-    s = near.base + (behind ? __builtin_ctzll(behind) : 64);
-    if (behind) break;
-    near = look_at(A, lane, near.base + 64, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));   // (from_step < total: one follows)
-  }
+  auto& O = state.O;
+  float &m = state.m, &l = state.l;
   const char* const K = reinterpret_cast<const char*>(A.C.k) + (long)h * A.C.head * kSize + g * 16;
   const char* const V = reinterpret_cast<const char*>(A.C.v) + (long)h * A.C.head * kSize + (c * kE < D ? c * kE : 0) * kSize;
-
-  for (; s < A.C.n_seqs; ++s) {
-  if (s - near.base == 64) near = look_at(A, lane, s, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));
-  const int steps = __builtin_amdgcn_readlane(near.steps, s - near.base);
-  const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, s - near.base) - steps;
-  if (before >= to_step) break;
-  if (steps == 0) continue;
-  const int first = from_step > before ? (int)(from_step - before) : 0, last = min((int)(to_step - before), steps);
-  const int start = __builtin_amdgcn_readlane(near.begin, s - near.base);
-  const int begin = start + first * kTile, end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + last * kTile);
-
   const int32_t* table = A.C.table + (long)s * A.C.table_stride;
   // the page of position from + lane % 32 (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
   // are not there are read from page 0 and left out afterwards, so that no load stands behind a branch.
@@ -260,18 +251,12 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
     }
   };
 
-  cq_v4f O[kChunks][kE];
-#pragma unroll
-  for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-    for (int d = 0; d < kE; ++d) O[n][d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;   // of query c; l: this lane's share
   const float cap2 = A.softcap > 0.f ? 2.f * kLog2e / A.softcap : 0.f;
 
   // what does not wait for anything first: pages, queries, then K and V; the queries become operands while those are under way
   uint32_t there;
   const int page0 = page_of(begin);
-  int page = page_of(begin + kTile);
+  int page = page_of(begin + kNext);
   cq_v4u raw[kSteps][2];
   {
     const size_t size = A.q_kind == CQ_A_F32 ? 4 : 2;
@@ -326,10 +311,10 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
 
   // K of the next positions is asked for when this step's scores are there, V when its products are: a step's rows are under way
   // during the half of a step behind it, in the registers that have just been read.  Its pages are asked for a step earlier.
-  for (int from = begin; from < end; from += kTile) {
+  for (int from = begin; from < end; from += kNext) {
     const uint32_t mine = there;
-    const uint32_t at = row_of(from + kTile, page, there);
-    page = page_of(from + 2 * kTile);
+    const uint32_t at = row_of(from + kNext, page, there);
+    page = page_of(from + 2 * kNext);
     if (!whole) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -358,7 +343,7 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
 #pragma unroll
       for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r] * factor;
     }
-    if (from + kTile < end) load_k(at);
+    if (from + kNext < end) load_k(at);
     if (A.softcap > 0.f) {
       // tanh x = 1 - 2 / (1 + e^(2x)), off by some units of the last place of 1
 #pragma unroll
@@ -425,42 +410,134 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
         }
       }
     }
-    if (from + kTile < end) load_v(at);
+    if (from + kNext < end) load_v(at);
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (c < rows) {
-    const int head = first_head + c;
-    float* stat = A.stat + ((size_t)(number + s) * heads + head) * 2;
-    float* part = A.part + ((size_t)(number + s) * heads + head) * D;
-    const bool all = first == 0 && last == steps;
-    float f = 1.f, lse;
-    if (all) {
-      close_row(m, l, A.sinks, head, f, lse);
-      if (k8 && A.C.v_scale) f *= A.C.v_scale[h];
-      if (g == 0 && A.lse) A.lse[(size_t)s * heads + head] = lse;
-    } else if (g == 0) {
-      stat[0] = m;
-      stat[1] = l;
-    }
-    const long to = (long)s * A.out.token + (long)head * A.out.head;
+}
+
+// A row's results: finished, or as part `line` of those that the second launch joins.
+template <int CK, int DPAD>
+__device__ __forceinline__ void put_rows(const attention_args& A, int s, int h, int first_head, int rows, bool all, size_t number,
+                                         const row_state<DPAD>& state) {
+  constexpr int kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, D = A.C.D, head = first_head + c, heads = A.G * A.C.heads;
+  if (c >= rows) return;
+  const size_t line = number * heads + head;
+  float f = 1.f, lse;
+  if (all) {
+    close_row(state.m, state.l, A.sinks, head, f, lse);
+    if (CK == CQ_C_E4M3 && A.C.v_scale) f *= A.C.v_scale[h];
+    if (g == 0 && A.lse) A.lse[(size_t)s * heads + head] = lse;
+  } else if (g == 0) {
+    A.stat[line * 2] = state.m;
+    A.stat[line * 2 + 1] = state.l;
+  }
+  const long to = (long)s * A.out.token + (long)head * A.out.head;
+  float* part = A.part + line * D;
 #pragma unroll
-    for (int n = 0; n < kChunks; ++n)
+  for (int n = 0; n < kChunks; ++n)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d0 = n * 128 + (g * 4 + r) * kE;
-        if (d0 >= D) continue;
+    for (int r = 0; r < 4; ++r) {
+      const int d0 = n * 128 + (g * 4 + r) * kE;
+      if (d0 >= D) continue;
 #pragma unroll
-        for (int d = 0; d < kE; d += 4) {
-          const float o[4] = {O[n][d][r] * f, O[n][d + 1][r] * f, O[n][d + 2][r] * f, O[n][d + 3][r] * f};
-          if (all)
-            store4(const_cast<void*>(A.out.p), A.out_kind, to + d0 + d, o);
-          else
-            *reinterpret_cast<cq_v4f*>(part + d0 + d) = cq_v4f{o[0], o[1], o[2], o[3]};
-        }
+      for (int d = 0; d < kE; d += 4) {
+        const float o[4] = {state.O[n][d][r] * f, state.O[n][d + 1][r] * f, state.O[n][d + 2][r] * f, state.O[n][d + 3][r] * f};
+        if (all)
+          store4(const_cast<void*>(A.out.p), A.out_kind, to + d0 + d, o);
+        else
+          *reinterpret_cast<cq_v4f*>(part + d0 + d) = cq_v4f{o[0], o[1], o[2], o[3]};
       }
+    }
+}
+
+// One share of the work per wavefront.
+template <int CK, int DPAD, bool HIGH>
+__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && DPAD == 64 ? 4 : 2) void cache_attention_kernel(attention_args A) {
+  const int lane = threadIdx.x & 63;
+  // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
+  const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
+  const int unit = __builtin_amdgcn_readfirstlane(block * kWaves + (threadIdx.x >> 6));
+  const int columns = A.C.heads * A.tiles, number = unit / columns, column = unit - number * columns;
+  if (number >= A.shares) return;
+  const int tile = column / A.C.heads, h = column - tile * A.C.heads;
+  const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16;
+  sequences near;
+  const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
+  const uint32_t from_step = number * share, to_step = min(total, from_step + share);
+  if (from_step >= to_step) return;
+  if (A.C.n_seqs > 64) near = look_at(A, lane, 0, 0u);
+  // the sequence in which the share begins
+  int s = 0;
+  for (;;) {
+    const uint64_t behind = __ballot(near.upto > from_step);
+    s = near.base + (behind ? __builtin_ctzll(behind) : 64);
+    if (behind) break;
+    near = look_at(A, lane, near.base + 64, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));   // (from_step < total: one follows)
   }
+  for (; s < A.C.n_seqs; ++s) {
+    if (s - near.base == 64) near = look_at(A, lane, s, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));
+    const int steps = __builtin_amdgcn_readlane(near.steps, s - near.base);
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, s - near.base) - steps;
+    if (before >= to_step) break;
+    if (steps == 0) continue;
+    const int first = from_step > before ? (int)(from_step - before) : 0, last = min((int)(to_step - before), steps);
+    const int start = __builtin_amdgcn_readlane(near.begin, s - near.base);
+    const int end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + last * kTile);
+    row_state<DPAD> state;
+    state.clear();
+    attend<CK, DPAD, HIGH, kTile>(A, s, h, first_head, rows, start + first * kTile, end, state);
+    put_rows<CK, DPAD>(A, s, h, first_head, rows, first == 0 && last == steps, (size_t)number + s, state);
   }
+}
+
+// Short sequences: the wavefronts of a workgroup share the positions of one sequence and key head and join their results in LDS, half of
+// them giving theirs to the other half, until one is left.  One launch, no workspace.
+constexpr int direct_waves(int dpad) { return dpad == 256 ? 4 : 8; }
+
+template <int CK, int DPAD, bool HIGH>
+__global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direct_kernel(attention_args A) {
+  constexpr int W = direct_waves(DPAD), kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
+  __shared__ cq_v4f sums[W / 2][kChunks * kE][64];
+  __shared__ float stats[W / 2][2][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
+  const int columns = A.C.heads * A.tiles, s = block / columns, column = block - s * columns;
+  if (s >= A.C.n_seqs) return;
+  const int tile = column / A.C.heads, h = column - tile * A.C.heads;
+  const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16;
+  int begin, end;
+  span_of(A.C, A.window, s, begin, end);
+  row_state<DPAD> state;
+  state.clear();
+  if (begin + wave * kTile < end) attend<CK, DPAD, HIGH, W * kTile>(A, s, h, first_head, rows, begin + wave * kTile, end, state);
+#pragma unroll
+  for (int half = W / 2; half > 0; half /= 2) {
+    if (begin + half * kTile < end) {   // (else they have nothing to give)
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+          for (int d = 0; d < kE; ++d) sums[wave - half][n * kE + d][lane] = state.O[n][d];
+        stats[wave - half][0][lane] = state.m;
+        stats[wave - half][1][lane] = state.l;
+      }
+      __syncthreads();
+      if (wave < half) {
+        const float pm = stats[wave][0][lane], top = fmaxf(state.m, pm), base = top == -INFINITY ? 0.f : top;
+        const float a = __builtin_amdgcn_exp2f(state.m - base), b = __builtin_amdgcn_exp2f(pm - base);
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+          for (int d = 0; d < kE; ++d) state.O[n][d] = state.O[n][d] * a + sums[wave][n * kE + d][lane] * b;
+        state.l = fmaf(state.l, a, stats[wave][1][lane] * b);
+        state.m = top;
+      }
+      __syncthreads();
+    }
+  }
+  if (wave == 0) put_rows<CK, DPAD>(A, s, h, first_head, rows, true, 0, state);
 }
 
 // Joins the parts of sequences that lie in several shares, in order: a group of threads takes every n-th part of a row (or of 32 of its
@@ -529,6 +606,15 @@ __global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A,
   if (d == 0 && A.lse) A.lse[row] = lse;
 }
 
+// Whether one launch of a workgroup per sequence and key head is taken: for lengths of four steps of its wavefronts (two of wide heads) and no
+// more workgroups than compute units.  From Python, 32 query and 8 key heads of 128 in bf16, both ways: 1 sequence of 512 positions 12 us
+// (shares 16), of 1024 15 (16), of 2048 25 (16); 32 of up to 1024 23 (26), of up to 2048 39 (37); 128 of up to 256 33 (28).
+inline bool direct(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
+  const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
+  const int span = window > 0 && window < max_length ? window : max_length;
+  return n_seqs * columns <= 256 && span <= (padded(C->D) == 256 ? 256 : 1024);
+}
+
 // Shares of a head's work: about as many wavefronts as the chip holds at once, at least one for every sequence, and no more than there
 // are steps where the lengths are as expected.
 inline long shares_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
@@ -543,6 +629,15 @@ inline long shares_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int
   return shares < steps ? shares : steps;
 }
 
+inline attention_args from_sequence(attention_args a, long s) {
+  a.C.table += s * a.C.table_stride;
+  a.C.lengths += s;
+  a.q = rows_from(a.q, a.q_kind, s);
+  a.out = rows_from(a.out, a.out_kind, s);
+  if (a.lse) a.lse += s * a.G * a.C.heads;
+  return a;
+}
+
 inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_length) {
   const cq_status st = check_cache(C);
   if (st != CQ_OK) return st;
@@ -554,7 +649,7 @@ inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_
 
 extern "C" size_t cq_cache_attention_workspace_bytes(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
   if (check_attention(C, n_seqs, Hq, max_length) != CQ_OK) return 0;
-  if (n_seqs == 0) return 0;
+  if (n_seqs == 0 || direct(C, n_seqs, Hq, max_length, window)) return 0;
   return ((size_t)shares_of(C, n_seqs, Hq, max_length, window) + n_seqs) * Hq * (C->D + 2) * 4;
 }
 
@@ -574,7 +669,8 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if ((long)S->n * q->n > 1l << 30 || (double)S->n * S->width * C->page_size > 64e9) return CQ_ERR_SHAPE;
   if (S->n == 0) return CQ_OK;
   const size_t need = cq_cache_attention_workspace_bytes(C, S->n, q->n, P->max_length, P->window);
-  if (!workspace || workspace_bytes < need) return CQ_ERR_WORKSPACE;
+  if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
+  const bool at_once = need == 0;
   const long shares = shares_of(C, S->n, q->n, P->max_length, P->window);
   attention_args a;
   a.C = make_cache_args(C, S);
@@ -600,9 +696,24 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.stat = a.part + ((size_t)shares + S->n) * q->n * C->D;
   const bool high = q->kind == CQ_A_F32 || out->kind == CQ_A_F32 || (C->kind == CQ_A_BF16 && q->kind == CQ_A_F16);
   const int dpad = padded(C->D);
-  a.blocks = (int)cq_align_up((size_t)((shares * C->heads * a.tiles + kWaves - 1) / kWaves), 8);
-#define LAUNCH(CK, DPAD, HIGH) \
-  hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(kWaves * 64), 0, (hipStream_t)stream, a)
+  hipStream_t str = (hipStream_t)stream;
+  const long columns = (long)C->heads * a.tiles;
+  // (sequences of a launch: its threads are counted in 32 bits)
+  const long most = at_once ? kMostThreads / 1024 / columns : S->n;
+  for (long from = 0; from < S->n; from += most) {
+    attention_args b = a;
+    if (at_once) {
+      b = from_sequence(a, from);
+      b.C.n_seqs = (int)(S->n - from < most ? S->n - from : most);
+    }
+    b.blocks = (int)cq_align_up((size_t)(at_once ? b.C.n_seqs * columns : (shares * columns + kWaves - 1) / kWaves), 8);
+#define LAUNCH(CK, DPAD, HIGH)                                                                                                          \
+  do {                                                                                                                                  \
+    if (at_once)                                                                                                                        \
+      hipLaunchKernelGGL((cache_attention_direct_kernel<CK, DPAD, HIGH>), dim3(b.blocks), dim3(direct_waves(DPAD) * 64), 0, str, b);    \
+    else                                                                                                                                \
+      hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(b.blocks), dim3(kWaves * 64), 0, str, b);                       \
+  } while (0)
 #define WIDTHS(CK, HIGH)                      \
   do {                                        \
     if (dpad == 64) LAUNCH(CK, 64, HIGH);     \
@@ -614,20 +725,22 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
     if (high) WIDTHS(CK, true);  \
     else WIDTHS(CK, false);      \
   } while (0)
-  if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
-  else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
-  else KINDS(CQ_C_E4M3);
+    if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
+    else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
+    else KINDS(CQ_C_E4M3);
 #undef KINDS
 #undef WIDTHS
 #undef LAUNCH
+  }
+  if (at_once) return cq_check_launch();
   // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
   const bool many = shares >= 16l * S->n;
   const int quads = many && C->D > 32 ? 8 : C->D / 4, threads = many ? 256 : 64;
-  const long all = (long)S->n * q->n, at_once = kMostThreads / threads;
-  for (long from = 0; from < all; from += at_once) {
-    const dim3 grid((unsigned)(all - from < at_once ? all - from : at_once), (C->D / 4 + quads - 1) / quads);
-    if (many) hipLaunchKernelGGL((attention_join_kernel<256>), grid, dim3(256), 0, (hipStream_t)stream, a, (int)from, quads);
-    else hipLaunchKernelGGL((attention_join_kernel<64>), grid, dim3(64), 0, (hipStream_t)stream, a, (int)from, quads);
+  const long all = (long)S->n * q->n, per_launch = kMostThreads / threads;
+  for (long from = 0; from < all; from += per_launch) {
+    const dim3 grid((unsigned)(all - from < per_launch ? all - from : per_launch), (C->D / 4 + quads - 1) / quads);
+    if (many) hipLaunchKernelGGL((attention_join_kernel<256>), grid, dim3(256), 0, str, a, (int)from, quads);
+    else hipLaunchKernelGGL((attention_join_kernel<64>), grid, dim3(64), 0, str, a, (int)from, quads);
   }
   return cq_check_launch();
 }
