@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
       int h0;
       const int which = what(first + i, h0);
       const head_rows& R = which == 0 ? A.q : which == 1 ? A.k : A.v;
-      raw[i] = head_fetch<XK, WHOLE>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
+      raw[i] = head_fetch<XK, WHOLE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
   fetch(group);
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
   if (to.seq < 0) return;   // (nothing is written, the queries neither)
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.positions ? A.positions[t] : to.position);
   float w_q[8], w_k[8];
-  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
+  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
   const long at = to.page * A.C.page + to.slot * A.C.slot;
   for (; group < end; group += kGroups) {
     float v[kGroups][8];
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
       if (which < 2) turn_values<INTER, false>(s, turn, v[i]);
       if (group + i >= end) break;
       if (which == 0) {
-        if (h < A.q.n) head_store<XK, WHOLE>(const_cast<void*>(A.q_out.p), t * A.q_out.token + h * A.q_out.head, s, v[i]);
+        if (h < A.q.n) head_store<XK, WHOLE, INTER>(const_cast<void*>(A.q_out.p), t * A.q_out.token + h * A.q_out.head, s, v[i]);
       } else if (to.page >= 0 && h < A.C.heads) {
         if constexpr (CK == CQ_C_E4M3) {
           const float* scale = which == 2 ? A.C.v_scale : A.C.k_scale;
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
             for (int e = 0; e < 8; ++e) v[i][e] /= sc;
           }
         }
-        head_store<CK, WHOLE>(which == 2 ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
+        head_store<CK, WHOLE, INTER>(which == 2 ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
       }
     }
   }

@@ -33,14 +33,14 @@ __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
       const bool key = first + i >= A.groups_q;
       const head_rows& R = key ? A.k : A.q;
       const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
-      raw[i] = head_fetch<XK, WHOLE>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
+      raw[i] = head_fetch<XK, WHOLE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
   fetch(group);
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.L.rot ? A.positions[t] : 0);
   float w_q[8], w_k[8];
-  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
+  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
   for (; group < end; group += kGroups) {
     float v[kGroups][8];
 #pragma unroll
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
       }
       turn_values<INTER, false>(s, turn, v[i]);
       if (group + i < end && h0 + sub < R.n)
-        head_store<OK, WHOLE>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, v[i]);
+        head_store<OK, WHOLE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, v[i]);
     }
   }
 }

@@ -50,8 +50,8 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const head_slot s(A.L, lane % LANES);
   float w_q[8], w_k[8], acc_q[8], acc_k[8];
-  head_weights<WHOLE>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE>(A.w_k, A.wkind, s, w_k);
+  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc_q[e] = acc_k[e] = 0.f;
   const int sub = lane / LANES;
@@ -70,8 +70,8 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
         const head_rows &X = key ? A.k : A.q, &G = key ? A.dk_out : A.dq_out;
         const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
         const bool on = first + i < end && h0 + sub < G.n;
-        raw_d[i] = head_fetch<OK, WHOLE>(G.p, t * G.token + h0 * G.head + sub * G.head, s, on);
-        raw_x[i] = head_fetch<XK, WHOLE>(X.p, t * X.token + h0 * X.head + sub * X.head, s, on && (key ? A.w_k : A.w_q));
+        raw_d[i] = head_fetch<OK, WHOLE, INTER>(G.p, t * G.token + h0 * G.head + sub * G.head, s, on);
+        raw_x[i] = head_fetch<XK, WHOLE, INTER>(X.p, t * X.token + h0 * X.head + sub * X.head, s, on && (key ? A.w_k : A.w_q));
       }
     };
     fetch(group);
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
           if (A.w_q) head_back<LANES>(x[i], g[i], w_q, acc_q, A.inv_D, A.eps);
         }
         if (group + i < end && h0 + sub < R.n)
-          head_store<XK, WHOLE>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, g[i]);
+          head_store<XK, WHOLE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, g[i]);
       }
     }
   }

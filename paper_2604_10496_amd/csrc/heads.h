@@ -34,7 +34,7 @@ inline head_layout make_head_layout(int D, int rot, int inter) {
   head_layout L;
   L.D = D;
   L.rot = rot;
-  L.inter = inter && rot > 0;
+  L.inter = inter || rot == 0;
   L.turned = inter ? (rot + 7) / 8 : (rot / 2 + 3) / 4;
   L.used = L.turned + (D - rot + 7) / 8;
   L.lanes = L.used <= 8 ? 8 : L.used <= 16 ? 16 : L.used <= 32 ? 32 : 64;
@@ -221,12 +221,19 @@ struct head_raw {
 };
 
 // WHOLE: the layout's lanes hold eight values or none, and the code for fewer, ten times as long, is left out (what single tokens wait
-// for is instructions: 1 token of 40 heads 6.6 us with it)
-template <int KIND, bool WHOLE>
+// for is instructions: 1 token of 40 heads 6.6 us with it).  SIDE: a lane's quads lie side by side (all but pairs apart).
+template <int KIND, bool WHOLE, bool SIDE>
 __device__ __forceinline__ head_raw<KIND> head_fetch(const void* p, long at, const head_slot& s, bool on) {
   head_raw<KIND> r;
   if constexpr (WHOLE) {
     const bool there = on && s.na;
+    if constexpr (SIDE && KIND != CQ_A_F32) {
+      cq_v4u w = {0u, 0u, 0u, 0u};
+      if (there) w = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(p) + (at + s.a) * 2);
+      r.a.w = cq_v2u{w[0], w[1]};
+      r.b.w = cq_v2u{w[2], w[3]};
+      return r;
+    }
     r.a = quad_fetch<KIND, WHOLE>(p, at + s.a, there ? 4 : 0);
     r.b = quad_fetch<KIND, WHOLE>(p, at + s.b, there ? 4 : 0);
   } else {
@@ -245,13 +252,17 @@ __device__ __forceinline__ void head_values(const head_raw<KIND>& r, float (&v)[
   }
 }
 
-template <int KIND, bool WHOLE>
+template <int KIND, bool WHOLE, bool SIDE>
 __device__ __forceinline__ void head_store(void* p, long at, const head_slot& s, const float (&v)[8]) {
   const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
   if constexpr (WHOLE) {
     if (s.na) {
-      quad_store<KIND>(p, at + s.a, 4, a);
-      quad_store<KIND>(p, at + s.b, 4, b);
+      if constexpr (SIDE && (KIND == CQ_A_F16 || KIND == CQ_A_BF16)) {
+        row_store8<KIND>(p, (size_t)(at + s.a), 8, v);
+      } else {
+        quad_store<KIND>(p, at + s.a, 4, a);
+        quad_store<KIND>(p, at + s.b, 4, b);
+      }
     }
   } else {
     quad_store<KIND>(p, at + s.a, s.na, a);
@@ -260,17 +271,17 @@ __device__ __forceinline__ void head_store(void* p, long at, const head_slot& s,
 }
 
 // a lane's share of a norm's weights (ones without a norm)
-template <bool WHOLE>
+template <bool WHOLE, bool SIDE>
 __device__ __forceinline__ void head_weights(const void* w, int kind, const head_slot& s, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 1.f;
   if (!w) return;
   if (kind == CQ_A_F32)
-    head_values<CQ_A_F32>(head_fetch<CQ_A_F32, WHOLE>(w, 0, s, true), v);
+    head_values<CQ_A_F32>(head_fetch<CQ_A_F32, WHOLE, SIDE>(w, 0, s, true), v);
   else if (kind == CQ_A_F16)
-    head_values<CQ_A_F16>(head_fetch<CQ_A_F16, WHOLE>(w, 0, s, true), v);
+    head_values<CQ_A_F16>(head_fetch<CQ_A_F16, WHOLE, SIDE>(w, 0, s, true), v);
   else
-    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16, WHOLE>(w, 0, s, true), v);
+    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16, WHOLE, SIDE>(w, 0, s, true), v);
 }
 
 // cosines and sines of a lane's four pairs
@@ -359,7 +370,7 @@ __device__ __forceinline__ void head_normed(float (&v)[8], const float (&w)[8], 
 }  // namespace
 
 // Runs LAUNCH(..., LANES, WHOLE, INTER) for the lanes of a row (64 of them are never all whole: that would take 512 values).  Pairs of
-// neighbours and pairs apart are two kernels: in one the compiler reads a row's values by index, from scratch memory.
+// neighbours (or none) and pairs apart are two kernels: in one the compiler reads a row's values by index, from scratch memory.
 #define CQ_HEAD_WIDTHS(LAUNCH, L, INTER, ...)                                   \
   do {                                                                          \
     if ((L).whole && (L).lanes == 8) LAUNCH(__VA_ARGS__, 8, true, INTER);       \
