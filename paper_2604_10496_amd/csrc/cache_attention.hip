@@ -31,6 +31,7 @@ struct attention_args {
   int G, tiles;          // queries of a key head, groups of 16 of them
   int q_kind, out_kind, shift;   // shift: log2 of the page size, -1 where it is no power of two
   int window, shares;    // shares of the work of a head
+  int step_log;          // log2 of the positions of a step
   int blocks;            // workgroups, a multiple of eight
   uint32_t page16, slot16;   // strides in units of 16 bytes
   float scale, softcap;
@@ -53,7 +54,7 @@ struct sequences {
   uint32_t upto;
 };
 
-__device__ __forceinline__ int steps_of(int begin, int end) { return (end - begin + kTile - 1) / kTile; }
+__device__ __forceinline__ int steps_of(const attention_args& A, int begin, int end) { return (end - begin + (1 << A.step_log) - 1) >> A.step_log; }
 
 // (wave_sum's exchanges, as a running sum over the lanes)
 __device__ __forceinline__ uint32_t sum_up_to(uint32_t n) {
@@ -73,7 +74,7 @@ __device__ __forceinline__ sequences look_at(const attention_args& A, int lane, 
   q.base = base;
   q.begin = q.end = 0;
   if (base + lane < A.C.n_seqs) span_of(A.C, A.window, base + lane, q.begin, q.end);
-  q.steps = steps_of(q.begin, q.end);
+  q.steps = steps_of(A, q.begin, q.end);
   q.upto = before + sum_up_to((uint32_t)q.steps);
   return q;
 }
@@ -114,8 +115,15 @@ struct operand;
 template <>
 struct operand<CQ_A_BF16> {
   static constexpr int kQuery = 3;
-  static __device__ __forceinline__ uint16_t round(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-  static __device__ __forceinline__ float value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+  // a and b rounded to two operands, and what that leaves of them
+  static __device__ __forceinline__ uint32_t round(float& a, float& b, bool rest) {
+    const uint32_t w = pack2<CQ_A_BF16>(a, b);
+    if (rest) {
+      a -= __uint_as_float(w << 16);
+      b -= __uint_as_float(w & 0xffff0000u);
+    }
+    return w;
+  }
   static __device__ __forceinline__ cq_v4f mfma(cq_v4u a, cq_v4u b, cq_v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cq_v8bf16, a), __builtin_bit_cast(cq_v8bf16, b), c, 0, 0, 0);
   }
@@ -123,8 +131,16 @@ struct operand<CQ_A_BF16> {
 template <>
 struct operand<CQ_A_F16> {
   static constexpr int kQuery = 2;
-  static __device__ __forceinline__ uint16_t round(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
-  static __device__ __forceinline__ float value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+  static __device__ __forceinline__ uint32_t round(float& a, float& b, bool rest) {
+    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float two_f32;
+    typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 two_f16;
+    const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((two_f32{a, b}), two_f16));
+    if (rest) {   // one instruction each, which takes a half of w as it is
+      asm("v_fma_mix_f32 %0, %1, -1.0, %0 op_sel:[0,0,0] op_sel_hi:[1,0,0]" : "+v"(a) : "v"(w));
+      asm("v_fma_mix_f32 %0, %1, -1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(b) : "v"(w));
+    }
+    return w;
+  }
   static __device__ __forceinline__ cq_v4f mfma(cq_v4u a, cq_v4u b, cq_v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(cq_v8f16, a), __builtin_bit_cast(cq_v8f16, b), c, 0, 0, 0);
   }
@@ -139,15 +155,9 @@ __device__ __forceinline__ void split8(const float (&v)[8], cq_v4u (&w)[PARTS]) 
 #pragma unroll
   for (int i = 0; i < 8; ++i) rest[i] = v[i];
 #pragma unroll
-  for (int n = 0; n < PARTS; ++n) {
+  for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint16_t a = operand<CK>::round(rest[2 * i]), b = operand<CK>::round(rest[2 * i + 1]);
-      rest[2 * i] -= operand<CK>::value(a);
-      rest[2 * i + 1] -= operand<CK>::value(b);
-      w[n][i] = (uint32_t)a | ((uint32_t)b << 16);
-    }
-  }
+    for (int i = 0; i < 4; ++i) w[n][i] = operand<CK>::round(rest[2 * i], rest[2 * i + 1], n + 1 < PARTS);
 }
 
 // two e4m3 codes (half HI of a word) as two f16
@@ -159,7 +169,7 @@ __device__ __forceinline__ uint32_t two_f16(uint32_t codes) {
 // Wavefronts of a SIMD that share the work: as many as ask for 16 KB at a time, which is a step of 128 dims of 16 bits.  With one of those
 // 48 sequences of up to 4096 positions take 78 us and their join 5.6, with two 80 and 6.5, with four 84 and 6.8; 64 dims of 8 bits
 // 33 with two, 30 with four, 35 with eight.
-constexpr int resident(int kind, int dpad) { return dpad >= 256 ? 1 : (kind == CQ_C_E4M3 ? 2 : 1) * 128 / dpad; }
+constexpr int resident(int kind, int dpad) { return dpad == 64 || (dpad == 128 && kind == CQ_C_E4M3) ? 2 : 1; }
 inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 // What a kernel's lanes hold of a row's results: query c's at dims 128 n + kE (4 g + r) + d, unscaled, the maximum (base 2) of its scores
@@ -180,6 +190,9 @@ struct row_state {
   }
 };
 
+// Tiles of a step, worked on together: 16 KB of keys and values at a time, but for wide heads, as far as the registers go.
+constexpr int together(int kind, int dpad) { return dpad == 64 || (kind == CQ_C_E4M3 && dpad == 128) ? 2 : 1; }
+
 // One wavefront's attention of the queries first_head .. first_head + rows - 1 of sequence s over the positions begin .. end-1 (there is
 // one), 32 at a time, of which it takes every NEXT / 32nd 32.
 template <int CK, int DPAD, bool HIGH, int NEXT>
@@ -193,6 +206,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   constexpr int kP = HIGH ? operand<CK>::kQuery : 2;
   constexpr int kKWords = k8 ? DPAD / 64 : DPAD / 32;            // 16-byte pieces of a row of K per lane
   constexpr int kVWords = kE * kSize / 4;                        // words of a row of V per lane and chunk
+  constexpr int kTogether = together(CK, DPAD), kRows = kTogether * kTile;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int D = A.C.D;
   const bool whole = D == DPAD;
@@ -201,24 +215,25 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   const char* const K = reinterpret_cast<const char*>(A.C.k) + (long)h * A.C.head * kSize + g * 16;
   const char* const V = reinterpret_cast<const char*>(A.C.v) + (long)h * A.C.head * kSize + (c * kE < D ? c * kE : 0) * kSize;
   const int32_t* table = A.C.table + (long)s * A.C.table_stride;
-  // the page of position from + lane % 32 (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
+  // the page of position from + lane (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
   // are not there are read from page 0 and left out afterwards, so that no load stands behind a branch.
   auto page_of = [&](int from) {
-    const int p = min(from + (lane & 31), end - 1);
+    const int p = min(from + (lane & (kRows - 1)), end - 1);
     return table[A.shift >= 0 ? p >> A.shift : p / A.C.page_size];
   };
-  auto row_of = [&](int from, int page, uint32_t& there) {
-    const int p = from + (lane & 31);
+  auto row_of = [&](int from, int page, uint64_t& there) {
+    const int p = from + (lane & (kRows - 1));
     const int slot = A.shift >= 0 ? p & (A.C.page_size - 1) : p % A.C.page_size;
     const bool on = p < end && (uint32_t)page < (uint32_t)A.C.pages;
-    there = (uint32_t)__ballot(on);
+    there = __ballot(on);
     return on ? (uint32_t)page * A.page16 + (uint32_t)slot * A.slot16 : 0u;
   };
-  cq_v4u k[2][kKWords];                     // K: rows c and 16 + c
-  uint32_t v[kChunks][8][kVWords];          // V: dims kE c .. of rows 4g .. 4g+3 and 16 + 4g ..
+  cq_v4u k[2 * kTogether][kKWords];               // K: rows c and 16 + c of a tile
+  uint32_t v[kChunks][8 * kTogether][kVWords];    // V: dims kE c .. of rows 4g .. 4g+3 and 16 + 4g .. of a tile
+  uint64_t there;                                 // which of the rows are
   auto load_k = [&](uint32_t at) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < 2 * kTogether; ++n) {
       const char* p = K + ((size_t)(uint32_t)__shfl((int)at, n * 16 + c) << 4);
 #pragma unroll
       for (int i = 0; i < kKWords; ++i) {
@@ -230,7 +245,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   };
   auto load_v = [&](uint32_t at) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 8 * kTogether; ++j) {
       const char* p = V + ((size_t)(uint32_t)__shfl((int)at, (j >> 2) * 16 + g * 4 + (j & 3)) << 4);
 #pragma unroll
       for (int n = 0; n < kChunks; ++n) {
@@ -251,11 +266,9 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     }
   };
 
-  const float cap2 = A.softcap > 0.f ? 2.f * kLog2e / A.softcap : 0.f;
 
   // what does not wait for anything first: pages, queries, then K and V; the queries become operands while those are under way
-  uint32_t there;
-  const int page0 = page_of(begin);
+  const int first_page = page_of(begin);
   int page = page_of(begin + kNext);
   cq_v4u raw[kSteps][2];
   {
@@ -273,7 +286,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     }
   }
   {
-    const uint32_t at = row_of(begin, page0, there);
+    const uint32_t at = row_of(begin, first_page, there);
     load_k(at);
     load_v(at);
   }
@@ -306,26 +319,28 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) split8<CK, kQ>(v[i], Q[i]);
   }
-  const float factor = A.scale * back * (k8 && A.C.k_scale ? A.C.k_scale[h] : 1.f);
+  // what a product is multiplied by: for its score in units of ln 2, or with a cap twice its quotient by that
+  const float factor = A.scale * back * (k8 && A.C.k_scale ? A.C.k_scale[h] : 1.f), cap = A.softcap * kLog2e;
+  const float into = (A.softcap > 0.f ? 2.f * factor / A.softcap : factor) * kLog2e;
 
 
   // K of the next positions is asked for when this step's scores are there, V when its products are: a step's rows are under way
   // during the half of a step behind it, in the registers that have just been read.  Its pages are asked for a step earlier.
   for (int from = begin; from < end; from += kNext) {
-    const uint32_t mine = there;
+    const uint64_t mine = there;
     const uint32_t at = row_of(from + kNext, page, there);
     page = page_of(from + 2 * kNext);
     if (!whole) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < 2 * kTogether; ++n)
 #pragma unroll
         for (int i = 0; i < kKWords; ++i)
           if (i * 64 + g * 16 >= D * kSize) k[n][i] = cq_v4u{0u, 0u, 0u, 0u};
     }
     // scores of query c at positions 4g + r and 16 + 4g + r
-    float z[8];
+    float z[8 * kTogether];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < 2 * kTogether; ++n) {
       cq_v4f acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
@@ -341,20 +356,22 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
         for (int q = kQ - 1; q >= 0; --q) acc = operand<CK>::mfma(a, Q[i][q], acc);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r] * factor;
+      for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r];
     }
     if (from + kNext < end) load_k(at);
+    // in units of ln 2
     if (A.softcap > 0.f) {
       // tanh x = 1 - 2 / (1 + e^(2x)), off by some units of the last place of 1
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = A.softcap * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z[j] * cap2)), 1.f);
+      for (int j = 0; j < 8 * kTogether; ++j) z[j] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z[j] * into)), cap);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8 * kTogether; ++j) z[j] *= into;
     }
+    if (mine != ~0ull) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] *= kLog2e;
-    if (mine != 0xffffffffu) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool on = mine >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1u;
+      for (int j = 0; j < 8 * kTogether; ++j) {
+        const bool on = mine >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1ull;
         z[j] = on ? z[j] : -INFINITY;
 #pragma unroll
         for (int n = 0; n < kChunks; ++n)
@@ -364,7 +381,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     }
     float top = m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, z[j]);
+    for (int j = 0; j < 8 * kTogether; ++j) top = fmaxf(top, z[j]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const float base = top == -INFINITY ? 0.f : top;
@@ -377,36 +394,39 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
         for (int d = 0; d < kE; ++d) O[n][d] *= shrink;
       m = top;
     }
-    float p[8];
+    float p[kTogether][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p[j] = __builtin_amdgcn_exp2f(z[j] - base);
-      l += p[j];
+    for (int j = 0; j < 8 * kTogether; ++j) {
+      p[j >> 3][j & 7] = __builtin_amdgcn_exp2f(z[j] - base);
+      l += p[j >> 3][j & 7];
     }
-    cq_v4u P[kP];
-    split8<CK, kP>(p, P);
 #pragma unroll
-    for (int n = 0; n < kChunks; ++n) {
+    for (int t = 0; t < kTogether; ++t) {
+      cq_v4u P[kP];
+      split8<CK, kP>(p[t], P);
 #pragma unroll
-      for (int d = 0; d < kE; d += 2) {
-        uint32_t two[8];   // dims d, d+1 of the eight rows
+      for (int n = 0; n < kChunks; ++n) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if constexpr (k8)
-            two[j] = d & 2 ? two_f16<true>(v[n][j][d >> 2]) : two_f16<false>(v[n][j][d >> 2]);
-          else
-            two[j] = v[n][j][d >> 1];
-        }
-        cq_v4u lo, hi;
+        for (int d = 0; d < kE; d += 2) {
+          uint32_t two[8];   // dims d, d+1 of the eight rows
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          lo[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x05040100u);
-          hi[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x07060302u);
-        }
+          for (int j = 0; j < 8; ++j) {
+            if constexpr (k8)
+              two[j] = d & 2 ? two_f16<true>(v[n][t * 8 + j][d >> 2]) : two_f16<false>(v[n][t * 8 + j][d >> 2]);
+            else
+              two[j] = v[n][t * 8 + j][d >> 1];
+          }
+          cq_v4u lo, hi;
 #pragma unroll
-        for (int q = kP - 1; q >= 0; --q) {
-          O[n][d] = operand<CK>::mfma(lo, P[q], O[n][d]);
-          O[n][d + 1] = operand<CK>::mfma(hi, P[q], O[n][d + 1]);
+          for (int w = 0; w < 4; ++w) {
+            lo[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x05040100u);
+            hi[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x07060302u);
+          }
+#pragma unroll
+          for (int q = kP - 1; q >= 0; --q) {
+            O[n][d] = operand<CK>::mfma(lo, P[q], O[n][d]);
+            O[n][d + 1] = operand<CK>::mfma(hi, P[q], O[n][d + 1]);
+          }
         }
       }
     }
@@ -454,7 +474,7 @@ __device__ __forceinline__ void put_rows(const attention_args& A, int s, int h, 
 
 // One share of the work per wavefront.
 template <int CK, int DPAD, bool HIGH>
-__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && DPAD == 64 ? 4 : 2) void cache_attention_kernel(attention_args A) {
+__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attention_kernel(attention_args A) {
   const int lane = threadIdx.x & 63;
   // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
   const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
@@ -484,10 +504,10 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : CK == CQ_C_E4M3 && D
     if (steps == 0) continue;
     const int first = from_step > before ? (int)(from_step - before) : 0, last = min((int)(to_step - before), steps);
     const int start = __builtin_amdgcn_readlane(near.begin, s - near.base);
-    const int end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + last * kTile);
+    const int end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + (last << A.step_log));
     row_state<DPAD> state;
     state.clear();
-    attend<CK, DPAD, HIGH, kTile>(A, s, h, first_head, rows, start + first * kTile, end, state);
+    attend<CK, DPAD, HIGH, together(CK, DPAD) * kTile>(A, s, h, first_head, rows, start + (first << A.step_log), end, state);
     put_rows<CK, DPAD>(A, s, h, first_head, rows, first == 0 && last == steps, (size_t)number + s, state);
   }
 }
@@ -511,10 +531,11 @@ __global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direc
   span_of(A.C, A.window, s, begin, end);
   row_state<DPAD> state;
   state.clear();
-  if (begin + wave * kTile < end) attend<CK, DPAD, HIGH, W * kTile>(A, s, h, first_head, rows, begin + wave * kTile, end, state);
+  constexpr int kStep = together(CK, DPAD) * kTile;
+  if (begin + wave * kStep < end) attend<CK, DPAD, HIGH, W * kStep>(A, s, h, first_head, rows, begin + wave * kStep, end, state);
 #pragma unroll
   for (int half = W / 2; half > 0; half /= 2) {
-    if (begin + half * kTile < end) {   // (else they have nothing to give)
+    if (begin + half * kStep < end) {   // (else they have nothing to give)
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
         for (int n = 0; n < kChunks; ++n)
@@ -620,22 +641,14 @@ inline bool direct(const cq_cache* C, int n_seqs, int Hq, int max_length, int wi
 inline long shares_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
   const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
   const long span = window > 0 && window < max_length ? window : max_length;
-  const long steps = ((span + kTile - 1) / kTile > 0 ? (span + kTile - 1) / kTile : 1) * n_seqs;
+  const int step = kTile * together(C->kind, padded(C->D));
+  const long steps = ((span + step - 1) / step > 0 ? (span + step - 1) / step : 1) * n_seqs;
   const long held = 1024l * resident(C->kind, padded(C->D));
   long shares = (held + columns - 1) / columns;
   if (shares < n_seqs) shares = n_seqs;
   const long most = (kMostThreads / 64 / columns) & ~7l;   // (a launch's threads are counted in 32 bits)
   if (shares > most) shares = most;
   return shares < steps ? shares : steps;
-}
-
-inline attention_args from_sequence(attention_args a, long s) {
-  a.C.table += s * a.C.table_stride;
-  a.C.lengths += s;
-  a.q = rows_from(a.q, a.q_kind, s);
-  a.out = rows_from(a.out, a.out_kind, s);
-  if (a.lse) a.lse += s * a.G * a.C.heads;
-  return a;
 }
 
 inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_length) {
@@ -682,6 +695,7 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   for (int i = 0; i < 31; ++i)
     if (C->page_size == 1 << i) a.shift = i;
   a.shares = (int)shares;
+  a.step_log = together(C->kind, padded(C->D)) == 2 ? 6 : 5;
   a.window = P->window;
   const long unit = 16 / cache_elem(C->kind);
   a.page16 = (uint32_t)(C->page_stride / unit);
@@ -698,21 +712,13 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   const int dpad = padded(C->D);
   hipStream_t str = (hipStream_t)stream;
   const long columns = (long)C->heads * a.tiles;
-  // (sequences of a launch: its threads are counted in 32 bits)
-  const long most = at_once ? kMostThreads / 1024 / columns : S->n;
-  for (long from = 0; from < S->n; from += most) {
-    attention_args b = a;
-    if (at_once) {
-      b = from_sequence(a, from);
-      b.C.n_seqs = (int)(S->n - from < most ? S->n - from : most);
-    }
-    b.blocks = (int)cq_align_up((size_t)(at_once ? b.C.n_seqs * columns : (shares * columns + kWaves - 1) / kWaves), 8);
+  a.blocks = (int)cq_align_up((size_t)(at_once ? S->n * columns : (shares * columns + kWaves - 1) / kWaves), 8);
 #define LAUNCH(CK, DPAD, HIGH)                                                                                                          \
   do {                                                                                                                                  \
     if (at_once)                                                                                                                        \
-      hipLaunchKernelGGL((cache_attention_direct_kernel<CK, DPAD, HIGH>), dim3(b.blocks), dim3(direct_waves(DPAD) * 64), 0, str, b);    \
+      hipLaunchKernelGGL((cache_attention_direct_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(direct_waves(DPAD) * 64), 0, str, a);    \
     else                                                                                                                                \
-      hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(b.blocks), dim3(kWaves * 64), 0, str, b);                       \
+      hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(kWaves * 64), 0, str, a);                       \
   } while (0)
 #define WIDTHS(CK, HIGH)                      \
   do {                                        \
@@ -725,13 +731,12 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
     if (high) WIDTHS(CK, true);  \
     else WIDTHS(CK, false);      \
   } while (0)
-    if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
-    else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
-    else KINDS(CQ_C_E4M3);
+  if (C->kind == CQ_A_F16) KINDS(CQ_A_F16);
+  else if (C->kind == CQ_A_BF16) KINDS(CQ_A_BF16);
+  else KINDS(CQ_C_E4M3);
 #undef KINDS
 #undef WIDTHS
 #undef LAUNCH
-  }
   if (at_once) return cq_check_launch();
   // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
   const bool many = shares >= 16l * S->n;
