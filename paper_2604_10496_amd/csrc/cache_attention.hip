@@ -13,9 +13,12 @@
 // that add up to 16 bits at least, 22 where queries or results are fp32: rounded once to 8 bits, P alone would cost the result
 // as much as its own rounding.
 // The work is cut into equal shares: the steps of all sequences, one sequence behind the other, are divided among as many wavefronts as
-// the chip holds, whatever the lengths; a share may begin and end inside a sequence and hold several.  A sequence inside one share is
+// the memory needs, whatever the lengths; a share may begin and end inside a sequence and hold several.  A sequence inside one share is
 // finished there; the others' parts are joined, in order, by a second launch.  The four wavefronts of a workgroup take neighbouring
-// heads, whose rows lie side by side.
+// heads, whose rows lie side by side.  Few short sequences and many of them have ways of their own (plan_of).
+// 32 query and 8 key heads of 128 in bf16, 48 sequences of 1 to 4096 positions (404 MB): 74 to 78 us = 5.4 TB/s (a plain read 5.95), and 5.1 for
+// the join.  One sequence of 131071 positions in f16, 4 key heads, results in fp32 (268 MB): 49 us = 5.5 TB/s, and 5.7.  64 dims in e4m3
+// (61 sequences, the last 2000 positions, 98 MB): 25 to 30 us and 5: products of 64 dims for 5 of 16 columns take as long as the reads.
 #include <type_traits>
 
 #include "cache.h"
@@ -472,7 +475,7 @@ __device__ __forceinline__ void put_rows(const attention_args& A, int s, int h, 
     }
 }
 
-// One share of the work per wavefront.
+// One share of the work per wavefront, or one sequence where there are many.
 template <int CK, int DPAD, bool HIGH>
 __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attention_kernel(attention_args A) {
   const int lane = threadIdx.x & 63;
@@ -480,23 +483,41 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attent
   const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
   const int unit = __builtin_amdgcn_readfirstlane(block * kWaves + (threadIdx.x >> 6));
   const int columns = A.C.heads * A.tiles, number = unit / columns, column = unit - number * columns;
-  if (number >= A.shares) return;
+  if (number >= (A.shares ? A.shares : A.C.n_seqs)) return;
   const int tile = column / A.C.heads, h = column - tile * A.C.heads;
   const int rows = min(16, A.G - tile * 16), first_head = h * A.G + tile * 16;
+  row_state<DPAD> state;
+  state.clear();
   sequences near;
-  const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
-  const uint32_t from_step = number * share, to_step = min(total, from_step + share);
-  if (from_step >= to_step) return;
-  if (A.C.n_seqs > 64) near = look_at(A, lane, 0, 0u);
-  // the sequence in which the share begins
-  int s = 0;
-  for (;;) {
-    const uint64_t behind = __ballot(near.upto > from_step);
-    s = near.base + (behind ? __builtin_ctzll(behind) : 64);
-    if (behind) break;
-    near = look_at(A, lane, near.base + 64, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));   // (from_step < total: one follows)
+  uint32_t from_step = 0, to_step;
+  int s, behind_last;
+  if (A.shares) {
+    const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
+    from_step = number * share;
+    to_step = min(total, from_step + share);
+    if (from_step >= to_step) return;
+    if (A.C.n_seqs > 64) near = look_at(A, lane, 0, 0u);
+    // the sequence in which the share begins
+    for (;;) {
+      const uint64_t behind = __ballot(near.upto > from_step);
+      s = near.base + (behind ? __builtin_ctzll(behind) : 64);
+      if (behind) break;
+      near = look_at(A, lane, near.base + 64, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));   // (from_step < total: one follows)
+    }
+    behind_last = A.C.n_seqs;
+  } else {
+    // a sequence for each wavefront
+    s = near.base = number;
+    behind_last = number + 1;
+    span_of(A.C, A.window, s, near.begin, near.end);
+    near.steps = steps_of(A, near.begin, near.end);
+    near.upto = to_step = (uint32_t)near.steps;
+    if (near.steps == 0) {
+      put_rows<CK, DPAD>(A, s, h, first_head, rows, true, 0, state);
+      return;
+    }
   }
-  for (; s < A.C.n_seqs; ++s) {
+  for (; s < behind_last; ++s) {
     if (s - near.base == 64) near = look_at(A, lane, s, (uint32_t)__builtin_amdgcn_readlane((int)near.upto, 63));
     const int steps = __builtin_amdgcn_readlane(near.steps, s - near.base);
     const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)near.upto, s - near.base) - steps;
@@ -505,7 +526,6 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attent
     const int first = from_step > before ? (int)(from_step - before) : 0, last = min((int)(to_step - before), steps);
     const int start = __builtin_amdgcn_readlane(near.begin, s - near.base);
     const int end = min(__builtin_amdgcn_readlane(near.end, s - near.base), start + (last << A.step_log));
-    row_state<DPAD> state;
     state.clear();
     attend<CK, DPAD, HIGH, together(CK, DPAD) * kTile>(A, s, h, first_head, rows, start + (first << A.step_log), end, state);
     put_rows<CK, DPAD>(A, s, h, first_head, rows, first == 0 && last == steps, (size_t)number + s, state);
@@ -627,28 +647,30 @@ __global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A,
   if (d == 0 && A.lse) A.lse[row] = lse;
 }
 
-// Whether one launch of a workgroup per sequence and key head is taken: for lengths of four steps of its wavefronts (two of wide heads) and no
-// more workgroups than compute units.  From Python, 32 query and 8 key heads of 128 in bf16, both ways: 1 sequence of 512 positions 12 us
-// (shares 16), of 1024 15 (16), of 2048 25 (16); 32 of up to 1024 23 (26), of up to 2048 39 (37); 128 of up to 256 33 (28).
-inline bool direct(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
-  const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
-  const int span = window > 0 && window < max_length ? window : max_length;
-  return n_seqs * columns <= 256 && span <= (padded(C->D) == 256 ? 256 : 1024);
-}
+// How a call's work is divided.
+//   by_group: one launch of a workgroup per sequence and key head, for lengths of four steps of its wavefronts (two of wide heads) and no more
+//   workgroups than compute units.  From Python, 32 query and 8 key heads of 128 in bf16, both ways: 1 sequence of 512 positions 12 us (shares
+//   16), of 1024 15 (16), of 2048 25 (16); 32 of up to 1024 23 (26), of up to 2048 39 (37); 128 of up to 256 33 (28).
+//   by_sequence: one launch of a wavefront per sequence and key head, where twice the longest sequence's positions are no more than there are
+//   of those: the longest does not outlast the rest.  The same heads, both ways: 128 sequences of up to 100 positions 13 us (shares 21), of up
+//   to 1000 76 (67); 1000 of up to 300 138 (217); 512 of up to 1000 224 (230), of up to 4000 840 (717).
+//   by_share: as many shares as there are wavefronts of `resident`, no more than there are steps where the lengths are as expected.  512
+//   sequences of up to 4000 positions: 5.97 TB/s, the rate of a plain read of that size.
+enum way { by_group, by_sequence, by_share };
+struct plan {
+  way how;
+  long shares;
+};
 
-// Shares of a head's work: about as many wavefronts as the chip holds at once, at least one for every sequence, and no more than there
-// are steps where the lengths are as expected.
-inline long shares_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
+inline plan plan_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
   const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
   const long span = window > 0 && window < max_length ? window : max_length;
-  const int step = kTile * together(C->kind, padded(C->D));
-  const long steps = ((span + step - 1) / step > 0 ? (span + step - 1) / step : 1) * n_seqs;
-  const long held = 1024l * resident(C->kind, padded(C->D));
-  long shares = (held + columns - 1) / columns;
-  if (shares < n_seqs) shares = n_seqs;
-  const long most = (kMostThreads / 64 / columns) & ~7l;   // (a launch's threads are counted in 32 bits)
-  if (shares > most) shares = most;
-  return shares < steps ? shares : steps;
+  const int dpad = padded(C->D), step = kTile * together(C->kind, dpad);
+  if (n_seqs * columns <= 256 && span <= (dpad == 256 ? 256 : 1024)) return {by_group, 0};
+  // (a launch's threads are counted in 32 bits)
+  if (2 * span <= n_seqs * columns && n_seqs * columns <= kMostThreads / 64 - 64) return {by_sequence, 0};
+  const long steps = (span > step ? (span + step - 1) / step : 1) * n_seqs, shares = (1024l * resident(C->kind, dpad) + columns - 1) / columns;
+  return {by_share, shares < steps ? shares : steps};
 }
 
 inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_length) {
@@ -662,8 +684,8 @@ inline cq_status check_attention(const cq_cache* C, int n_seqs, int Hq, int max_
 
 extern "C" size_t cq_cache_attention_workspace_bytes(const cq_cache* C, int n_seqs, int Hq, int max_length, int window) {
   if (check_attention(C, n_seqs, Hq, max_length) != CQ_OK) return 0;
-  if (n_seqs == 0 || direct(C, n_seqs, Hq, max_length, window)) return 0;
-  return ((size_t)shares_of(C, n_seqs, Hq, max_length, window) + n_seqs) * Hq * (C->D + 2) * 4;
+  const plan p = plan_of(C, n_seqs, Hq, max_length, window);
+  return n_seqs == 0 || p.how != by_share ? 0 : ((size_t)p.shares + n_seqs) * Hq * (C->D + 2) * 4;
 }
 
 extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S, const cq_attention_spec* P, const cq_heads* q,
@@ -683,8 +705,7 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if (S->n == 0) return CQ_OK;
   const size_t need = cq_cache_attention_workspace_bytes(C, S->n, q->n, P->max_length, P->window);
   if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
-  const bool at_once = need == 0;
-  const long shares = shares_of(C, S->n, q->n, P->max_length, P->window);
+  const plan p = plan_of(C, S->n, q->n, P->max_length, P->window);
   attention_args a;
   a.C = make_cache_args(C, S);
   a.G = q->n / C->heads;
@@ -694,7 +715,7 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.shift = -1;
   for (int i = 0; i < 31; ++i)
     if (C->page_size == 1 << i) a.shift = i;
-  a.shares = (int)shares;
+  a.shares = (int)p.shares;
   a.step_log = together(C->kind, padded(C->D)) == 2 ? 6 : 5;
   a.window = P->window;
   const long unit = 16 / cache_elem(C->kind);
@@ -707,15 +728,15 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.out = make_head_rows(out);
   a.lse = lse;
   a.part = (float*)workspace;
-  a.stat = a.part + ((size_t)shares + S->n) * q->n * C->D;
+  a.stat = a.part + ((size_t)p.shares + S->n) * q->n * C->D;
   const bool high = q->kind == CQ_A_F32 || out->kind == CQ_A_F32 || (C->kind == CQ_A_BF16 && q->kind == CQ_A_F16);
   const int dpad = padded(C->D);
   hipStream_t str = (hipStream_t)stream;
-  const long columns = (long)C->heads * a.tiles;
-  a.blocks = (int)cq_align_up((size_t)(at_once ? S->n * columns : (shares * columns + kWaves - 1) / kWaves), 8);
+  const long columns = (long)C->heads * a.tiles, units = (p.how == by_share ? p.shares : S->n) * columns;
+  a.blocks = (int)cq_align_up((size_t)(p.how == by_group ? units : (units + kWaves - 1) / kWaves), 8);
 #define LAUNCH(CK, DPAD, HIGH)                                                                                                          \
   do {                                                                                                                                  \
-    if (at_once)                                                                                                                        \
+    if (p.how == by_group)                                                                                                              \
       hipLaunchKernelGGL((cache_attention_direct_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(direct_waves(DPAD) * 64), 0, str, a);    \
     else                                                                                                                                \
       hipLaunchKernelGGL((cache_attention_kernel<CK, DPAD, HIGH>), dim3(a.blocks), dim3(kWaves * 64), 0, str, a);                       \
@@ -737,9 +758,9 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
 #undef KINDS
 #undef WIDTHS
 #undef LAUNCH
-  if (at_once) return cq_check_launch();
+  if (p.how != by_share) return cq_check_launch();
   // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
-  const bool many = shares >= 16l * S->n;
+  const bool many = p.shares >= 16l * S->n;
   const int quads = many && C->D > 32 ? 8 : C->D / 4, threads = many ? 256 : 64;
   const long all = (long)S->n * q->n, per_launch = kMostThreads / threads;
   for (long from = 0; from < all; from += per_launch) {
