@@ -417,6 +417,7 @@ typedef struct {
  *     pairs (a, b) of the first `rot` of D values:  a' = a c - b s,  b' = b c + a s,   (c, s) = rot_scale (cos, sin)(t freq[i])
  *   pair i is (i, i + rot/2), or with `interleaved` (2i, 2i + 1); the other values are not rotated.  freq [rot/2] f64: radians per
  *   position; t freq is taken modulo a revolution in 64 bits, so that any 32-bit position keeps the accuracy of fp32.
+ *   A row whose sum of squares leaves fp32's range has a norm of zeros (NaN where the row is infinite).
  *   w_q, w_k [D] of weight_kind: CQ_A_F32, CQ_A_F16 or CQ_A_BF16.  1 <= D <= 256, rot even, 0 <= rot <= D; 0 < eps < inf.
  */
 typedef struct {
@@ -495,8 +496,10 @@ cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, const cq_hea
  *   Positions whose page is not there do not take part; a row without any that does, or all of whose scores are -inf, gives zeros and the
  *   lse of its sink (-inf without).  What lies behind a sequence's length is not read.  out [S->n, q->n] of any kind; lse [S->n, q->n] f32 or
  *   NULL.  Scores, softmax and sums in fp32; the products' operands carry 16 bits at least, 22 where q or out is fp32.
- *   max_length: what the lengths are expected to reach.  The cache is cut into parts for it; longer sequences take longer, no more.
- *   workspace: cq_cache_attention_workspace_bytes() bytes (0: none needed).
+ *   max_length: what the lengths are expected to reach, <= 2^30.  The work is divided for it; longer sequences take longer, no more.
+ *   Up to 2^32 pieces of 16 bytes between the first and the last row of k, and of v; n * width * page_size <= 64e9, n * q->n <= 2^30.
+ *   The order of the sums depends on the sizes and on the lengths of the whole batch.
+ *   workspace: cq_cache_attention_workspace_bytes() bytes (0: none needed, NULL allowed).
  */
 typedef struct {
   float scale, softcap;

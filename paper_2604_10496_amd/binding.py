@@ -925,8 +925,8 @@ def _heads(t, what: str, T, n, D, dtype, index: int) -> Heads:
     if t.get_device() != index or len(shape) != 3 or shape[0] != T or n is not None and shape[1] != n or shape[2] != D or (
             dtype is not None and t.dtype is not dtype):
         _wrong(t, what, (T, n, D), dtype, index)
-    if stride[2] != 1 and D > 1:
-        raise ValueError(f"{what}: a head's values are {stride[2]} apart")
+    if stride[2] != 1 and D > 1 or T > 1 << 30:
+        raise ValueError(f"{what}: a head's values are {stride[2]} apart" if T <= 1 << 30 else f"{what}: {T} tokens are too many")
     return Heads(t.data_ptr(), _KINDS.get(t.dtype) or _kind(t.dtype, what), shape[1], stride[0], stride[1])
 
 
@@ -1134,7 +1134,9 @@ def cq_cache_attention(cache: PagedCache, q, page_table, lengths, scale: Optiona
     hq = _heads(q, "q", S, None, D, None, index)
     Hq = hq.n
     if max_length is None:
-        max_length = s.width * c.page_size
+        max_length = min(s.width * c.page_size, 1 << 30)
+    if not (0 <= max_length <= 1 << 30 and 0 <= window < 1 << 31):
+        raise ValueError(f"max_length {max_length}, window {window}: out of range")
     spec = AttentionSpec(D ** -0.5 if scale is None else scale, softcap, window, max_length, _at(sinks, "sinks", (Hq,), f32, index))
     out, ho = _out_heads(out, "out", q, hq, out_dtype or (q.dtype if out is None else out.dtype), index)
     empty, lse, ws = _DTYPES["empty"], None, None

@@ -55,11 +55,11 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc_q[e] = acc_k[e] = 0.f;
   const int sub = lane / LANES;
-  const long units = (long)A.T * A.split;
+  const int units = A.T * A.split;   // (a token has several where there are few: at most 2^30)
   // the workgroups take units in turn, so that few tokens spread out
-  for (long unit = (long)wave * gridDim.x + blockIdx.x; unit < units; unit += (long)kWaves * gridDim.x) {
-    const int t = (int)(unit / A.split);
-    int group = (int)(unit - (long)t * A.split) * A.per_unit;
+  for (int unit = wave * gridDim.x + blockIdx.x; unit < units; unit += kWaves * gridDim.x) {
+    const int t = unit / A.split;
+    int group = (unit - t * A.split) * A.per_unit;
     const int end = min(A.groups, group + A.per_unit);
     head_raw<XK> raw_x[kGroups];
     head_raw<OK> raw_d[kGroups];

@@ -68,6 +68,10 @@ inline cq_status check_heads_out(const cq_heads* in, const cq_heads* out, int T,
   const cq_status st = check_heads(out, T);
   if (st != CQ_OK) return st;
   if (out->n != in->n || (out->n > 1 && out->head_stride < D) || (T > 1 && out->token_stride < D)) return CQ_ERR_SHAPE;
+  // (one of the steps over all rows of the other)
+  if (out->n > 1 && T > 1 && out->head_stride < (T - 1) * (double)out->token_stride + D &&
+      out->token_stride < (out->n - 1) * (double)out->head_stride + D)
+    return CQ_ERR_SHAPE;
   return CQ_OK;
 }
 

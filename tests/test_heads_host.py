@@ -115,6 +115,7 @@ def test_head_norm_refusals():
     assert call(eps=0.0) == 2 and call(eps=float("nan")) == 2 and call(eps=float("inf")) == 2 and call(rot_scale=float("inf")) == 2
     assert call(q=_heads(n=0)) == 2 and call(q=_heads(n=20000)) == 2 and call(q=_heads(n=3)) == 2
     assert call(qo=_heads(head=63)) == 2 and call(ko=_heads(token=63)) == 2        # rows on another's place
+    assert call(qo=_heads(token=64, head=64)) == 2 and call(qo=_heads(token=64, head=192)) == 2
     assert call(q=_heads(kind=7)) == 3 and call(weight_kind=9) == 3 and call(k=_heads(kind=F16)) == 3
     assert call(qo=_heads(kind=F32), ko=_heads(kind=F32)) == 3                     # 16-bit rows stay what they are
     assert call(qo=_heads(kind=F16)) == 3 and call(q=_heads(kind=E4M3)) == 3
