@@ -32,7 +32,8 @@ constexpr int kWaves = 4;         // of a workgroup, each by itself
 struct attention_args {
   cache_args C;
   int G, tiles;          // queries of a key head, groups of 16 of them
-  int q_kind, out_kind, shift;   // shift: log2 of the page size, -1 where it is no power of two
+  int q_kind, out_kind;
+  uint32_t per_page, per_page_shift;   // p / page_size = p per_page / 2^(32 + shift) (per_page 0: pages of one)
   int window, shares;    // shares of the work of a head
   int step_log;          // log2 of the positions of a step
   int blocks;            // workgroups, a multiple of eight
@@ -111,6 +112,14 @@ __device__ __forceinline__ void store4(void* p, int kind, long at, const float (
   if (kind == CQ_A_F32) quad_store<CQ_A_F32>(p, at, 4, v);
   else if (kind == CQ_A_F16) quad_store<CQ_A_F16>(p, at, 4, v);
   else quad_store<CQ_A_BF16>(p, at, 4, v);
+}
+
+// the largest of a value in the four lanes l % 16, in each of them
+__device__ __forceinline__ float rows_of_lanes_max(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 template <int CK>
@@ -220,13 +229,11 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   const int32_t* table = A.C.table + (long)s * A.C.table_stride;
   // the page of position from + lane (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
   // are not there are read from page 0 and left out afterwards, so that no load stands behind a branch.
-  auto page_of = [&](int from) {
-    const int p = min(from + (lane & (kRows - 1)), end - 1);
-    return table[A.shift >= 0 ? p >> A.shift : p / A.C.page_size];
-  };
+  auto column_of = [&](int p) { return A.per_page ? (int)(__umulhi((uint32_t)p, A.per_page) >> A.per_page_shift) : p; };
+  auto page_of = [&](int from) { return table[column_of(min(from + (lane & (kRows - 1)), end - 1))]; };
   auto row_of = [&](int from, int page, uint64_t& there) {
     const int p = from + (lane & (kRows - 1));
-    const int slot = A.shift >= 0 ? p & (A.C.page_size - 1) : p % A.C.page_size;
+    const int slot = p - column_of(p) * A.C.page_size;
     const bool on = p < end && (uint32_t)page < (uint32_t)A.C.pages;
     there = __ballot(on);
     return on ? (uint32_t)page * A.page16 + (uint32_t)slot * A.slot16 : 0u;
@@ -273,6 +280,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   // what does not wait for anything first: pages, queries, then K and V; the queries become operands while those are under way
   const int first_page = page_of(begin);
   int page = page_of(begin + kNext);
+  const float k_scale = k8 && A.C.k_scale ? A.C.k_scale[h] : 1.f, factor = A.scale * k_scale;
   cq_v4u raw[kSteps][2];
   {
     const size_t size = A.q_kind == CQ_A_F32 ? 4 : 2;
@@ -306,6 +314,11 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
     }
+    // scores of a negative factor are those of the negative queries, of none those of zeros
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = factor == 0.f ? 0.f : factor < 0.f ? -v[i][e] : v[i][e];
     if constexpr (CK != CQ_A_BF16) {
       // f16 has less of a range than the other types: the row's largest value to 2^9 .. 2^10
       most = fmaxf(most, __shfl_xor(most, 16));
@@ -322,10 +335,12 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) split8<CK, kQ>(v[i], Q[i]);
   }
-  // what a product is multiplied by: for its score in units of ln 2, or with a cap twice its quotient by that
-  const float factor = A.scale * back * (k8 && A.C.k_scale ? A.C.k_scale[h] : 1.f), cap = A.softcap * kLog2e;
-  const float into = (A.softcap > 0.f ? 2.f * factor / A.softcap : factor) * kLog2e;
-
+  // Products q.k to scores in units of ln 2: times `into`, which is not negative (see above), in the exponent's own instruction; the
+  // maximum is kept in the products' units.  With a cap the scores themselves are, and `into` is what the cap's exponential takes.
+  const bool capped = A.softcap > 0.f;
+  const float cap = A.softcap * kLog2e, times = fabsf(factor) * back * kLog2e * (capped ? 2.f / A.softcap : 1.f);
+  const float into = times < 1e-37f ? 1e-37f : times;   // (none times infinity would be no number)
+  const float unit = capped ? 1.f : into;
 
   // K of the next positions is asked for when this step's scores are there, V when its products are: a step's rows are under way
   // during the half of a step behind it, in the registers that have just been read.  Its pages are asked for a step earlier.
@@ -362,14 +377,10 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
       for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r];
     }
     if (from + kNext < end) load_k(at);
-    // in units of ln 2
-    if (A.softcap > 0.f) {
+    if (capped) {
       // tanh x = 1 - 2 / (1 + e^(2x)), off by some units of the last place of 1
 #pragma unroll
       for (int j = 0; j < 8 * kTogether; ++j) z[j] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z[j] * into)), cap);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8 * kTogether; ++j) z[j] *= into;
     }
     if (mine != ~0ull) {
 #pragma unroll
@@ -385,11 +396,10 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     float top = m;
 #pragma unroll
     for (int j = 0; j < 8 * kTogether; ++j) top = fmaxf(top, z[j]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float base = top == -INFINITY ? 0.f : top;
+    top = rows_of_lanes_max(top);
+    const float base = top == -INFINITY ? 0.f : top * unit;
     if (__ballot(top > m)) {
-      const float shrink = __builtin_amdgcn_exp2f(m - base);
+      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, unit, -base));
       l *= shrink;
 #pragma unroll
       for (int n = 0; n < kChunks; ++n)
@@ -400,7 +410,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     float p[kTogether][8];
 #pragma unroll
     for (int j = 0; j < 8 * kTogether; ++j) {
-      p[j >> 3][j & 7] = __builtin_amdgcn_exp2f(z[j] - base);
+      p[j >> 3][j & 7] = __builtin_amdgcn_exp2f(fmaf(z[j], unit, -base));
       l += p[j >> 3][j & 7];
     }
 #pragma unroll
@@ -435,6 +445,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     }
     if (from + kNext < end) load_v(at);
   }
+  m *= unit;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 }
@@ -712,9 +723,14 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   a.tiles = (a.G + 15) / 16;
   a.q_kind = q->kind;
   a.out_kind = out->kind;
-  a.shift = -1;
-  for (int i = 0; i < 31; ++i)
-    if (C->page_size == 1 << i) a.shift = i;
+  // division by the page size d, 2^s < d <= 2^(s+1), as a product with ceil(2^(32+s) / d), which is less than 2^32: it is off by less than d <=
+  // 2^(s+1) of 2^(32+s), so that the quotient of a position below 2^31 is off by less than 1 / d
+  a.per_page = a.per_page_shift = 0;
+  if (C->page_size > 1) {
+    while ((2 << a.per_page_shift) < C->page_size) ++a.per_page_shift;
+    const uint64_t d = (uint64_t)C->page_size;
+    a.per_page = (uint32_t)(((1ull << (32 + a.per_page_shift)) + d - 1) / d);
+  }
   a.shares = (int)p.shares;
   a.step_log = together(C->kind, padded(C->D)) == 2 ? 6 : 5;
   a.window = P->window;

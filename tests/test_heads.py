@@ -334,7 +334,7 @@ def _check_attention(cq, cache, q, table, lens, out_kind=None, sample=None, **kw
     out_kind = out_kind or kind
     S, Hq, D = q.shape
     k, v = (_np(x) if s is None else _np(x) * _np(s)[:, None] for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
-    scale = kw.get("scale") or D ** -0.5
+    scale = D ** -0.5 if kw.get("scale") is None else kw["scale"]
     # expected lengths decide whether a workgroup takes a sequence or wavefronts take shares of all: both ways
     ways = [cq.cq_cache_attention(cache, q, table, lens, out_dtype=_t(out_kind), **{**kw, "max_length": n})
             for n in (kw.get("max_length"), 1 << 20)]
@@ -397,6 +397,21 @@ def test_attention_window_softcap_sinks(cq, window, softcap, sinks):
     assert not got["out"][1].any()
     if sinks:
         assert (got["lse"][1] - kw["sinks"]).abs().max() <= 4 * U * kw["sinks"].abs().max()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-44, 3.0])
+@pytest.mark.parametrize("softcap", [0.0, 5.0])
+@pytest.mark.parametrize("cache_kind", ["bf16", "f16", "e4m3"])
+def test_attention_scales(cq, scale, softcap, cache_kind):
+    import torch
+    g = torch.Generator().manual_seed(25)
+    cache, table, lens = _paged(cq, g, [70, 0, 1, 40], 16, 2, 64, cache_kind, 0.5 if cache_kind == "e4m3" else None)
+    if cache.k_scale is not None:
+        cache.k_scale[1] *= -1
+    sinks = torch.randn(4, generator=g).cuda()
+    for kw in ({}, {"sinks": sinks}):
+        got = _check_attention(cq, cache, _rows(g, 4, 4, 64, "bf16"), table, lens, scale=scale, softcap=softcap, **kw)
+        assert not got["out"][1].any()
 
 
 @pytest.mark.parametrize("max_length", [1, 100, 5000, 1 << 20, None])
@@ -645,3 +660,38 @@ def test_results_do_not_depend_on_timing(cq):
         a, b = cq.cq_cache_attention(cache, q, table, lens), cq.cq_head_norm_grad(norm, x, None, pos, dy)
         assert torch.equal(a["out"], first[0]["out"]) and torch.equal(a["lse"], first[0]["lse"])
         assert torch.equal(b["dq"], first[1]["dq"]) and torch.equal(b["dw_q"], first[1]["dw_q"])
+
+
+def test_handles_look_at_their_tensors_at_every_call(cq):
+    import torch
+    g = torch.Generator().manual_seed(26)
+    norm = _norm(cq, g, 64, 64, False, "f32")
+    q = _rows(g, 3, 2, 64, "bf16")
+    pos = torch.arange(3, dtype=torch.int32).cuda()
+    want = cq.cq_head_norm(norm, q, None, pos)["q"]
+    kept = norm.w_q
+    for bad in (kept.bfloat16(), kept[:32], kept.cpu(), torch.stack([kept, kept], 1)[:, 0]):
+        norm.w_q = bad
+        with pytest.raises(ValueError, match="w_q|w_k"):
+            cq.cq_head_norm(norm, q, q, pos)
+    norm.w_q = kept * 2                                     # another weight is taken as it is
+    assert torch.equal(cq.cq_head_norm(norm, q, None, pos)["q"], want * 2)
+    norm.w_q, norm.freq = kept, norm.freq.float()
+    with pytest.raises(ValueError, match="freq"):
+        cq.cq_head_norm(norm, q, None, pos)
+    cache, table, lens = _paged(cq, g, [20, 3], 16, 2, 64, "bf16")
+    q = _rows(g, 2, 4, 64, "bf16")
+    want = cq.cq_cache_attention(cache, q, table, lens)["out"]
+    k, v = cache.k, cache.v
+    for bad_k, bad_v in ((k.half(), v), (k, v[:1]), (k.permute(0, 2, 1, 3), v), (k[..., ::2], v[..., ::2])):
+        cache.k, cache.v = bad_k, bad_v
+        with pytest.raises(ValueError, match="pages of one layout"):
+            cq.cq_cache_attention(cache, q, table, lens)
+    cache.k, cache.v = k.clone(), v.clone()
+    k.zero_()
+    assert torch.equal(cq.cq_cache_attention(cache, q, table, lens)["out"], want)
+    for bad in (dict(q=q[:1]), dict(q=q[..., :32]), dict(lengths=lens[:1]), dict(lengths=lens.long()), dict(page_table=table.long()),
+                dict(page_table=table[0]), dict(sinks=torch.zeros(3, device="cuda")), dict(window=1 << 31), dict(window=-1),
+                dict(max_length=1 << 31), dict(q=q.cpu())):
+        with pytest.raises((ValueError, cq.CqError)):
+            cq.cq_cache_attention(cache, **{"q": q, "page_table": table, "lengths": lens, **bad})
