@@ -883,7 +883,7 @@ _DTYPES: Dict[str, object] = {}      # filled once torch is known
 def _dtypes() -> Dict[str, object]:
     if not _DTYPES:
         import torch
-        _DTYPES.update(i32=torch.int32, f32=torch.float32, f64=torch.float64, empty=torch.empty, empty_like=torch.empty_like)
+        _DTYPES.update(i32=torch.int32, f32=torch.float32, f64=torch.float64, empty=torch.empty, empty_like=torch.empty_like, contiguous=torch.contiguous_format)
         _DTYPES.update(current=torch._C._cuda_getDevice, stream=torch._C._cuda_getCurrentRawStream)
         _DTYPES["cache"] = {torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16, torch.float8_e4m3fn: CQ_C_E4M3}
         _kind(torch.float32, "")
@@ -932,11 +932,11 @@ def _heads(t, what: str, T, n, D, dtype, index: int) -> Heads:
 
 def _new_heads(like, h: Heads, dtype):
     """New rows for these: the tensor, and what a call hands on."""
-    T, n, D = like.shape
+    _, n, D = like.shape
     if dtype is like.dtype and like.is_contiguous():
         t = _DTYPES["empty_like"](like)
     else:
-        t = _DTYPES["empty"]((T, n, D), dtype=dtype, device=like.device)
+        t = _DTYPES["empty_like"](like, dtype=dtype, memory_format=_DTYPES["contiguous"])
     return t, Heads(t.data_ptr(), _KINDS.get(dtype) or _kind(dtype, "out_dtype"), n, n * D, D)
 
 
@@ -1144,6 +1144,6 @@ def cq_cache_attention(cache: PagedCache, q, page_table, lengths, scale: Optiona
         lse = empty((S, Hq), dtype=f32, device=q.device)
     nbytes = lib.cq_cache_attention_workspace_bytes(c, S, Hq, max_length, window)
     if nbytes:
-        ws = empty(nbytes >> 2, dtype=f32, device=q.device)
+        ws = lengths.new_empty(nbytes >> 2)
     _on_device(lib.cq_cache_attention, index, c, s, spec, hq, ho, _ptr(lse), _ptr(ws), nbytes)
     return {"out": out, "lse": lse}
