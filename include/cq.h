@@ -439,9 +439,10 @@ cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, const cq_heads*
  * Its gradients, from q and k as the forward pass took them (not read where there is no norm: NULL allowed) and the gradients of its
  * results (either may be NULL: then that side is left out).  d_q, d_k of the rows' kind; d_w_q, d_w_k [D] of weight_kind (NULL: not
  * wanted).  Sums in fp32 in an order that depends on the sizes alone.  d_q may be d_q_out, and d_k d_k_out, of one kind.
- *   workspace: cq_head_norm_grad_workspace_bytes(P, T) bytes, which never falls as T grows; not needed without d_w_q and d_w_k.
+ *   workspace: cq_head_norm_grad_workspace_bytes(P, n_heads, T) bytes, n_heads those of d_q_out and d_k_out together; it never falls as T
+ *   grows (0 for few rows: NULL allowed); not needed without d_w_q and d_w_k.
  */
-size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int T);
+size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int n_heads, int T);
 cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q, const cq_heads* k, const int32_t* positions, int T,
                             const cq_heads* d_q_out, const cq_heads* d_k_out, const cq_heads* d_q, const cq_heads* d_k, void* d_w_q,
                             void* d_w_k, void* workspace, size_t workspace_bytes, cq_stream stream);

@@ -186,7 +186,7 @@ def load_library() -> ctypes.CDLL:
     lib.cq_head_norm.restype = ci
     lib.cq_head_norm.argtypes = [spec, heads, heads, vp, ci, heads, heads, vp]
     lib.cq_head_norm_grad_workspace_bytes.restype = sz
-    lib.cq_head_norm_grad_workspace_bytes.argtypes = [spec, ci]
+    lib.cq_head_norm_grad_workspace_bytes.argtypes = [spec, ci, ci]
     lib.cq_head_norm_grad.restype = ci
     lib.cq_head_norm_grad.argtypes = [spec, heads, heads, vp, ci, heads, heads, heads, heads, vp, vp, vp, sz, vp]
     lib.cq_cache_append.restype = ci
@@ -1027,26 +1027,35 @@ def cq_head_norm_grad(norm: HeadNorm, q=None, k=None, positions=None, dq=None, d
         raise ValueError("dq, dk: there are no gradients")
     index, T, D, d_dtype = _gpu_of(some, "dq" if dq is not None else "dk"), some.shape[0], norm.D, some.dtype
     spec = norm.struct(index)
-    like = _DTYPES["empty_like"]
-    x_of, d_of, o_of, out_of, w_of, dtype = [None] * 2, [None] * 2, [None] * 2, [None] * 2, [None] * 2, None
-    for i, (name, x, d, w) in enumerate((("q", q, dq, norm.w_q), ("k", k, dk, norm.w_k))):
-        if d is None:
-            continue
-        if x is None:
-            raise ValueError(f"{name}: its gradient needs it")
-        dtype = dtype or x.dtype
-        x_of[i] = h = _heads(x, name, T, None, D, dtype, index)
-        d_of[i] = _heads(d, "d" + name, T, h.n, D, d_dtype, index)
-        out_of[i], o_of[i] = _new_heads(x, h, dtype)
-        if want_weights and w is not None:
-            w_of[i] = like(w)
-    ws, nbytes = None, 0
-    if w_of[0] is not None or w_of[1] is not None:
-        nbytes = lib.cq_head_norm_grad_workspace_bytes(spec, T)
-        ws = _DTYPES["empty"](nbytes >> 2, dtype=_DTYPES["f32"], device=some.device)
-    _on_device(lib.cq_head_norm_grad, index, spec, x_of[0], x_of[1], _at(positions, "positions", (T,), _DTYPES["i32"], index), T, d_of[0],
-               d_of[1], o_of[0], o_of[1], _ptr(w_of[0]), _ptr(w_of[1]), _ptr(ws), nbytes)
-    return {"dq": out_of[0], "dk": out_of[1], "dw_q": w_of[0], "dw_k": w_of[1]}
+    x = q if dq is not None else k
+    dtype = None if x is None else x.dtype
+    hq = gq = oq = o_dq = dw_q = hk = gk = ok = o_dk = dw_k = ws = None
+    n = nbytes = 0
+    if dq is not None:
+        if q is None:
+            raise ValueError("q: its gradient needs it")
+        hq = _heads(q, "q", T, None, D, dtype, index)
+        n = hq.n
+        gq = _heads(dq, "dq", T, n, D, d_dtype, index)
+        o_dq, oq = _new_heads(q, hq, dtype)
+        if want_weights and norm.w_q is not None:
+            dw_q = _DTYPES["empty_like"](norm.w_q)
+    if dk is not None:
+        if k is None:
+            raise ValueError("k: its gradient needs it")
+        hk = _heads(k, "k", T, None, D, dtype, index)
+        gk = _heads(dk, "dk", T, hk.n, D, d_dtype, index)
+        n += hk.n
+        o_dk, ok = _new_heads(k, hk, dtype)
+        if want_weights and norm.w_k is not None:
+            dw_k = _DTYPES["empty_like"](norm.w_k)
+    if dw_q is not None or dw_k is not None:
+        nbytes = lib.cq_head_norm_grad_workspace_bytes(spec, n, T)
+        if nbytes:
+            ws = _DTYPES["empty"](nbytes >> 2, dtype=_DTYPES["f32"], device=some.device)
+    _on_device(lib.cq_head_norm_grad, index, spec, hq, hk, _at(positions, "positions", (T,), _DTYPES["i32"], index), T, gq, gk, oq, ok,
+               _ptr(dw_q), _ptr(dw_k), _ptr(ws), nbytes)
+    return {"dq": o_dq, "dk": o_dk, "dw_q": dw_q, "dw_k": dw_k}
 
 
 class PagedCache:

@@ -12,6 +12,9 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMostParts = 256;   // one workgroup per compute unit
 
 inline int weight_parts(int T) { return T < kMostParts ? T : kMostParts; }
+
+// Few rows (up to four groups of them for each of its wavefronts): one workgroup, which has the whole of the weights' gradients.
+inline bool one_workgroup(const head_layout& L, long rows) { return rows * L.lanes <= 4 * kThreads; }
 inline size_t weight_row(int D) { return cq_align_up((size_t)D, 8); }
 
 struct head_grad_args {
@@ -22,7 +25,8 @@ struct head_grad_args {
   const void *w_q, *w_k;
   const int32_t* positions;
   head_rows q, k, dq_out, dk_out, dq, dk;
-  float* part;   // [workgroups][2][D], NULL: not wanted
+  float* part;   // [workgroups][2][D], NULL: not wanted, or
+  void *dw_q, *dw_k;   // the weights' gradients themselves, from one workgroup
 };
 
 // g: the gradient behind a row's norm -> in front of it; its share of the weight's gradient
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
       }
     }
   }
-  if (!A.part) return;
+  if (!A.part && !A.dw_q && !A.dw_k) return;
   __shared__ float lds[kWaves][2 * kMaxHeadWidth];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -127,8 +131,14 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
     float v = 0.f;
 #pragma unroll
     for (int n = 0; n < kWaves; ++n) v += lds[n][c];
-    const int key = c >= A.L.D;
-    A.part[(size_t)blockIdx.x * 2 * Dp + key * Dp + c - key * A.L.D] = v;
+    const int key = c >= A.L.D, at = c - key * A.L.D;
+    if (A.part) {
+      A.part[(size_t)blockIdx.x * 2 * Dp + key * Dp + at] = v;
+    } else if (void* dw = key ? A.dw_k : A.dw_q) {
+      if (A.wkind == CQ_A_F32) elem_store<CQ_A_F32>(dw, at, v);
+      else if (A.wkind == CQ_A_F16) elem_store<CQ_A_F16>(dw, at, v);
+      else elem_store<CQ_A_BF16>(dw, at, v);
+    }
   }
 }
 
@@ -158,8 +168,9 @@ __global__ __launch_bounds__(256) void head_weight_sum_kernel(const float* part,
 
 }  // namespace
 
-extern "C" size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int T) {
-  if (check_head_spec(P) != CQ_OK || T < 0) return 0;
+extern "C" size_t cq_head_norm_grad_workspace_bytes(const cq_head_spec* P, int n_heads, int T) {
+  if (check_head_spec(P) != CQ_OK || T < 0 || n_heads <= 0) return 0;
+  if (one_workgroup(make_head_layout(P->D, P->rot, P->interleaved != 0), (long)n_heads * T)) return 0;
   return cq_align_up((size_t)(weight_parts(T)) * 2 * weight_row(P->D) * 4, 256);
 }
 
@@ -180,7 +191,9 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
   if ((d_q_out && d_k_out && (d_k->kind != kind || d_k_out->kind != out)) || (out != kind && kind != CQ_A_F32)) return CQ_ERR_UNSUPPORTED;
   if ((norm_q && q->kind != kind) || (norm_k && k->kind != kind)) return CQ_ERR_UNSUPPORTED;
   const bool weights = d_w_q || d_w_k;
-  if (weights && T > 0 && (!workspace || workspace_bytes < cq_head_norm_grad_workspace_bytes(P, T))) return CQ_ERR_WORKSPACE;
+  const int n_heads = (d_q_out ? d_q_out->n : 0) + (d_k_out ? d_k_out->n : 0);
+  const size_t need = weights ? cq_head_norm_grad_workspace_bytes(P, n_heads, T) : 0;
+  if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
   if (T > 0 && P->rot > 0 && !positions) return CQ_ERR_NULL;
   if (T == 0 && !weights) return CQ_OK;
   hipStream_t str = (hipStream_t)stream;
@@ -201,12 +214,15 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
   a.dk_out = make_head_rows(d_k_out);
   a.dq = make_head_rows(d_q_out ? d_q : nullptr);
   a.dk = make_head_rows(d_k_out ? d_k : nullptr);
-  a.part = weights ? (float*)workspace : nullptr;
-  const int parts = weight_parts(T);
+  const bool one = weights && T > 0 && need == 0;
+  a.part = weights && !one ? (float*)workspace : nullptr;
+  a.dw_q = one ? d_w_q : nullptr;
+  a.dw_k = one ? d_w_k : nullptr;
+  const int parts = one ? 1 : weight_parts(T);
   if (T > 0) {
     a.groups_q = head_groups(a.dq.n, a.L);
     a.groups = a.groups_q + head_groups(a.dk.n, a.L);
-    share_groups(a.groups, T, 2 * kMostParts * kWaves, a.per_unit, a.split);
+    share_groups(a.groups, T, one ? kWaves : 2 * kMostParts * kWaves, a.per_unit, a.split);
 #define LAUNCH(XK, OK, LANES, WHOLE, INTER) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES, WHOLE, INTER>), dim3(parts), dim3(kThreads), 0, str, a)
     if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
     else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
@@ -215,7 +231,7 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
     else CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_BF16);
 #undef LAUNCH
   }
-  if (weights) {
+  if (weights && !one) {
     const dim3 grid((P->D + 31) / 32, 2);
 #define SUM(WK) hipLaunchKernelGGL((head_weight_sum_kernel<WK>), grid, dim3(256), 0, str, a.part, T > 0 ? parts : 0, P->D, d_w_q, d_w_k)
     if (P->weight_kind == CQ_A_F32) SUM(CQ_A_F32);

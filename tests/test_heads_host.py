@@ -133,10 +133,11 @@ def test_head_norm_grad_refusals():
     assert call(w_q=None) == 1 and call(dko=None) == 1                             # a weight's gradient without what it comes from
     assert call(T=-1) == 2 and call(D=300) == 2 and call(dq=_heads(n=3)) == 2 and call(q=_heads(n=3)) == 2 and call(dq=_heads(head=8)) == 2
     assert call(dqo=_heads(kind=F32)) == 3 and call(q=_heads(kind=F16)) == 3 and call(dk=_heads(kind=F32)) == 3
-    need = lib.cq_head_norm_grad_workspace_bytes(_spec(), 4)
-    assert need > 0 and call(n=need - 1) == 4 and call(ws=None) == 4
-    assert lib.cq_head_norm_grad_workspace_bytes(_spec(D=0), 4) == 0
-    sizes = [lib.cq_head_norm_grad_workspace_bytes(_spec(), T) for T in (0, 1, 2, 100, 255, 256, 300, 1 << 20)]
+    need = lib.cq_head_norm_grad_workspace_bytes(_spec(), 4, 4000)
+    assert need > 0 and call(T=4000, n=need - 1) == 4 and call(T=4000, ws=None) == 4
+    assert lib.cq_head_norm_grad_workspace_bytes(_spec(D=0), 4, 4000) == 0
+    assert lib.cq_head_norm_grad_workspace_bytes(_spec(), 40, 1) == 0              # few rows need none
+    sizes = [lib.cq_head_norm_grad_workspace_bytes(_spec(), 40, T) for T in (0, 1, 2, 20, 100, 255, 256, 300, 1 << 20)]
     assert sizes == sorted(sizes)
     assert call(T=0, wq=None, wk=None, ws=None, n=0) == 0
 
