@@ -57,7 +57,7 @@ __device__ __forceinline__ place place_of(const append_args& A, int t, int lane)
   return p;
 }
 
-template <int XK, int CK, int LANES, bool WHOLE, bool INTER>
+template <int XK, int CK, int LANES, int MODE, bool INTER>
 __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
   constexpr int kAtOnce = 64 / LANES;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
   int group = (unit - in_launch * A.parts) * A.per_part;
   const int end = min(A.groups, group + A.per_part);
   const int lane = threadIdx.x & 63, sub = lane / LANES;
-  const head_slot s(A.L, lane % LANES);
+  const head_slot s = make_slot<MODE>(A.L, lane % LANES);
   // which rows a group holds: 0 queries, 1 keys, 2 values, from head h0 on
   auto what = [&](int g, int& h0) {
     const int which = g < A.groups_q ? 0 : g < A.groups_k ? 1 : 2;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
       int h0;
       const int which = what(first + i, h0);
       const head_rows& R = which == 0 ? A.q : which == 1 ? A.k : A.v;
-      raw[i] = head_fetch<XK, WHOLE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
+      raw[i] = head_fetch<XK, MODE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
   fetch(group);
@@ -89,13 +89,16 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
   if (to.seq < 0) return;   // (nothing is written, the queries neither)
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.positions ? A.positions[t] : to.position);
   float w_q[8], w_k[8];
-  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
+  head_weights<MODE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<MODE, INTER>(A.w_k, A.wkind, s, w_k);
   const long at = to.page * A.C.page + to.slot * A.C.slot;
   for (; group < end; group += kGroups) {
     float v[kGroups][8];
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) head_values<XK>(raw[i], v[i]);
+    for (int i = 0; i < kGroups; ++i) {
+      head_values<XK>(raw[i], v[i]);
+      own_values<MODE>(s, v[i]);
+    }
     if (group + kGroups < end) fetch(group + kGroups);
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
       if (which < 2) turn_values<INTER, false>(s, turn, v[i]);
       if (group + i >= end) break;
       if (which == 0) {
-        if (h < A.q.n) head_store<XK, WHOLE, INTER>(const_cast<void*>(A.q_out.p), t * A.q_out.token + h * A.q_out.head, s, v[i]);
+        if (h < A.q.n) head_store<XK, MODE, INTER>(const_cast<void*>(A.q_out.p), t * A.q_out.token + h * A.q_out.head, s, v[i]);
       } else if (to.page >= 0 && h < A.C.heads) {
         if constexpr (CK == CQ_C_E4M3) {
           const float* scale = which == 2 ? A.C.v_scale : A.C.k_scale;
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(append_args A) {
             for (int e = 0; e < 8; ++e) v[i][e] /= sc;
           }
         }
-        head_store<CK, WHOLE, INTER>(which == 2 ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
+        head_store<CK, MODE, INTER>(which == 2 ? A.C.v : A.C.k, at + h * A.C.head, s, v[i]);
       }
     }
   }
@@ -171,7 +174,7 @@ extern "C" cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, c
     b.first = (int)from;
     b.T = (int)(T - from < most ? T - from : most);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, CK, LANES, WHOLE, INTER) hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES, WHOLE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
+#define LAUNCH(XK, CK, LANES, MODE, INTER) hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
 #define KINDS(XK)                                                              \
   do {                                                                         \
     if (C->kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, XK, CQ_A_F16);   \

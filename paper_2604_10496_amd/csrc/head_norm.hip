@@ -16,7 +16,7 @@ struct head_norm_args {
   head_rows q, k, q_out, k_out;
 };
 
-template <int XK, int OK, int LANES, bool WHOLE, bool INTER>
+template <int XK, int OK, int LANES, int MODE, bool INTER>
 __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
   constexpr int kAtOnce = 64 / LANES;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
   int group = (unit - t * A.parts) * A.per_part;
   const int end = min(A.groups, group + A.per_part);
   const int lane = threadIdx.x & 63, sub = lane / LANES;
-  const head_slot s(A.L, lane % LANES);
+  const head_slot s = make_slot<MODE>(A.L, lane % LANES);
   head_raw<XK> raw[kGroups];
   auto fetch = [&](int first) {
 #pragma unroll
@@ -33,18 +33,21 @@ __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
       const bool key = first + i >= A.groups_q;
       const head_rows& R = key ? A.k : A.q;
       const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
-      raw[i] = head_fetch<XK, WHOLE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
+      raw[i] = head_fetch<XK, MODE, INTER>(R.p, t * R.token + h0 * R.head + sub * R.head, s, first + i < end && h0 + sub < R.n);
     }
   };
   fetch(group);
   const head_turn turn = turn_of(A.L, s, A.freq, A.rot_scale, A.L.rot ? A.positions[t] : 0);
   float w_q[8], w_k[8];
-  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
+  head_weights<MODE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<MODE, INTER>(A.w_k, A.wkind, s, w_k);
   for (; group < end; group += kGroups) {
     float v[kGroups][8];
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) head_values<XK>(raw[i], v[i]);
+    for (int i = 0; i < kGroups; ++i) {
+      head_values<XK>(raw[i], v[i]);
+      own_values<MODE>(s, v[i]);
+    }
     if (group + kGroups < end) fetch(group + kGroups);
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
@@ -57,7 +60,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(head_norm_args A) {
       }
       turn_values<INTER, false>(s, turn, v[i]);
       if (group + i < end && h0 + sub < R.n)
-        head_store<OK, WHOLE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, v[i]);
+        head_store<OK, MODE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, v[i]);
     }
   }
 }
@@ -102,7 +105,7 @@ extern "C" cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, cons
     b.q_out = rows_from(a.q_out, out, from);
     b.k_out = rows_from(a.k_out, out, from);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, OK, LANES, WHOLE, INTER) hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES, WHOLE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
+#define LAUNCH(XK, OK, LANES, MODE, INTER) hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
     if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
     else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
     else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F32);

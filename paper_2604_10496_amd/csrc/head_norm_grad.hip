@@ -47,15 +47,15 @@ __device__ __forceinline__ void head_back(const float (&x)[8], float (&g)[8], co
   }
 }
 
-template <int XK, int OK, int LANES, bool WHOLE, bool INTER>
+template <int XK, int OK, int LANES, int MODE, bool INTER>
 __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
   constexpr int kAtOnce = 64 / LANES;
   constexpr int kGroups = XK == CQ_A_F32 ? 1 : 2;   // groups of rows in flight (two of fp32 take more registers than there are)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const head_slot s(A.L, lane % LANES);
+  const head_slot s = make_slot<MODE>(A.L, lane % LANES);
   float w_q[8], w_k[8], acc_q[8], acc_k[8];
-  head_weights<WHOLE, INTER>(A.w_q, A.wkind, s, w_q);
-  head_weights<WHOLE, INTER>(A.w_k, A.wkind, s, w_k);
+  head_weights<MODE, INTER>(A.w_q, A.wkind, s, w_q);
+  head_weights<MODE, INTER>(A.w_k, A.wkind, s, w_k);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc_q[e] = acc_k[e] = 0.f;
   const int sub = lane / LANES;
@@ -74,8 +74,8 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
         const head_rows &X = key ? A.k : A.q, &G = key ? A.dk_out : A.dq_out;
         const int h0 = (first + i - (key ? A.groups_q : 0)) * kAtOnce;
         const bool on = first + i < end && h0 + sub < G.n;
-        raw_d[i] = head_fetch<OK, WHOLE, INTER>(G.p, t * G.token + h0 * G.head + sub * G.head, s, on);
-        raw_x[i] = head_fetch<XK, WHOLE, INTER>(X.p, t * X.token + h0 * X.head + sub * X.head, s, on && (key ? A.w_k : A.w_q));
+        raw_d[i] = head_fetch<OK, MODE, INTER>(G.p, t * G.token + h0 * G.head + sub * G.head, s, on);
+        raw_x[i] = head_fetch<XK, MODE, INTER>(X.p, t * X.token + h0 * X.head + sub * X.head, s, on && (key ? A.w_k : A.w_q));
       }
     };
     fetch(group);
@@ -85,6 +85,7 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
         head_values<XK>(raw_x[i], x[i]);
+        own_values<MODE>(s, x[i]);
         head_values<OK>(raw_d[i], g[i]);
       }
       if (group + kGroups < end) fetch(group + kGroups);
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
           if (A.w_q) head_back<LANES>(x[i], g[i], w_q, acc_q, A.inv_D, A.eps);
         }
         if (group + i < end && h0 + sub < R.n)
-          head_store<XK, WHOLE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, g[i]);
+          head_store<XK, MODE, INTER>(const_cast<void*>(R.p), t * R.token + h0 * R.head + sub * R.head, s, g[i]);
       }
     }
   }
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void head_grad_kernel(head_grad_args A) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int c = (e < 4 ? s.a : s.b) + (e & 3);
-      if ((e & 3) < (e < 4 ? s.na : s.nb)) {
+      if ((e & 3) < (e < 4 ? s.na : s.nb) && (e & 3) >= (e < 4 ? s.sa : s.sb)) {
         lds[wave][c] = acc_q[e];
         lds[wave][A.L.D + c] = acc_k[e];
       }
@@ -223,7 +224,7 @@ extern "C" cq_status cq_head_norm_grad(const cq_head_spec* P, const cq_heads* q,
     a.groups_q = head_groups(a.dq.n, a.L);
     a.groups = a.groups_q + head_groups(a.dk.n, a.L);
     share_groups(a.groups, T, one ? kWaves : 2 * kMostParts * kWaves, a.per_unit, a.split);
-#define LAUNCH(XK, OK, LANES, WHOLE, INTER) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES, WHOLE, INTER>), dim3(parts), dim3(kThreads), 0, str, a)
+#define LAUNCH(XK, OK, LANES, MODE, INTER) hipLaunchKernelGGL((head_grad_kernel<XK, OK, LANES, MODE, INTER>), dim3(parts), dim3(kThreads), 0, str, a)
     if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
     else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
     else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F32);

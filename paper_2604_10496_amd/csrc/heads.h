@@ -27,8 +27,14 @@ struct head_layout {
   int turned;   // lanes that hold rotated values
   int used;     // lanes that hold any
   int lanes;    // 8, 16, 32 or 64
-  bool whole;   // each of them holds eight
+  int mode;
 };
+
+// whole: the used lanes hold eight values each.  shifted: the last of the rotated ones and the last of all are moved back to the last values
+// there are, of which their neighbours own the first (few rotated values are followed by others), so that no load or sum needs a loop
+// over single values: 4096 tokens of 40 heads of 80, 20 rotated, 29 us with such loops, 21 without.  general: rows of fewer than eight.  Each is a kernel of its own: the code for single values is ten times as long, and what single tokens wait for is
+// instructions (1 token of 40 heads in 4.2 us; 6.6 with it).
+constexpr int kGeneral = 0, kShifted = 1, kWhole = 2;
 
 inline head_layout make_head_layout(int D, int rot, int inter) {
   head_layout L;
@@ -37,8 +43,8 @@ inline head_layout make_head_layout(int D, int rot, int inter) {
   L.inter = inter || rot == 0;
   L.turned = inter ? (rot + 7) / 8 : (rot / 2 + 3) / 4;
   L.used = L.turned + (D - rot + 7) / 8;
+  L.mode = L.used * 8 == D ? kWhole : D >= 8 ? kShifted : kGeneral;
   L.lanes = L.used <= 8 ? 8 : L.used <= 16 ? 16 : L.used <= 32 ? 32 : 64;
-  L.whole = L.used * 8 == D;
   return L;
 }
 
@@ -120,7 +126,7 @@ struct quad<CQ_A_F32> {
   cq_v4u w;
 };
 
-template <int KIND, bool WHOLE>
+template <int KIND, int MODE>
 __device__ __forceinline__ quad<KIND> quad_fetch(const void* p, long at, int n) {
   quad<KIND> q;
   q.w = decltype(q.w){};
@@ -130,7 +136,7 @@ __device__ __forceinline__ quad<KIND> quad_fetch(const void* p, long at, int n) 
       q.w = *reinterpret_cast<const cq_v4u_any*>(b);
     else
       q.w = *reinterpret_cast<const cq_v2u_any*>(b);
-  } else if constexpr (!WHOLE) {
+  } else if constexpr (MODE == kGeneral) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       if (i < n) {
@@ -200,37 +206,49 @@ __device__ __forceinline__ void quad_store(void* p, long at, int n, const float 
   }
 }
 
-// which values a lane holds: na from column a, nb from column b; turned: they are rotated, as pairs first .. first+3
+// Which values a lane holds: the sa-th to na-th of four from column a, the sb-th to nb-th from column b; turned: they are rotated, as pairs
+// first .. first+3.
 struct head_slot {
-  int a, b, na, nb, first;
+  int a, b, na, nb, sa, sb, first;
   bool turned;
-  __device__ __forceinline__ head_slot(const head_layout& L, int j) {
-    const int half = L.rot >> 1;
-    const bool apart = j < L.turned && !L.inter;
-    turned = j < L.turned;
-    first = 4 * j;
-    const int from = apart ? 4 * j : turned ? 8 * j : L.rot + 8 * (j - L.turned);
-    const int left = (apart ? half : turned ? L.rot : L.D) - from;   // of which there are
-    const int more = apart ? left : left - 4;
-    a = from;
-    b = apart ? half + from : from + 4;
-    na = left < 0 ? 0 : left < 4 ? left : 4;
-    nb = more < 0 ? 0 : more < 4 ? more : 4;
-  }
 };
+
+template <int MODE>
+__device__ __forceinline__ head_slot make_slot(const head_layout& L, int j) {
+  head_slot s;
+  const int half = L.rot >> 1;
+  s.turned = j < L.turned;
+  const bool apart = s.turned && !L.inter;
+  int from = apart ? 4 * j : s.turned ? 8 * j : L.rot + 8 * (j - L.turned);
+  const int left = (apart ? half : s.turned ? L.rot : L.D) - from;   // of which there are
+  const int more = apart ? left : left - 4;
+  s.na = left < 0 ? 0 : left < 4 ? left : 4;
+  s.nb = more < 0 ? 0 : more < 4 ? more : 4;
+  s.sa = s.sb = 0;
+  if constexpr (MODE == kShifted) {
+    const int width = apart ? 4 : 8, back = left > 0 && left < width && from >= width - left ? width - left : 0;
+    from -= back;
+    if (back) s.na = s.nb = 4;
+    s.sa = back < 4 ? back : 4;
+    s.sb = apart ? back : back - s.sa;
+  }
+  s.first = apart ? from : from >> 1;
+  s.a = from;
+  s.b = apart ? half + from : from + 4;
+  return s;
+}
 
 template <int KIND>
 struct head_raw {
   quad<KIND> a, b;
 };
 
-// WHOLE: the layout's lanes hold eight values or none, and the code for fewer, ten times as long, is left out (what single tokens wait
-// for is instructions: 1 token of 40 heads 6.6 us with it).  SIDE: a lane's quads lie side by side (all but pairs apart).
-template <int KIND, bool WHOLE, bool SIDE>
+// SIDE: a lane's quads lie side by side (all but pairs apart).
+template <int KIND, int MODE, bool SIDE>
 __device__ __forceinline__ head_raw<KIND> head_fetch(const void* p, long at, const head_slot& s, bool on) {
   head_raw<KIND> r;
-  if constexpr (WHOLE) {
-    const bool there = on && s.na;
+  if constexpr (MODE != kGeneral) {
+    const bool there = on && s.na;   // (all eight values are)
     if constexpr (SIDE && KIND != CQ_A_F32) {
       cq_v4u w = {0u, 0u, 0u, 0u};
       if (there) w = *reinterpret_cast<const cq_v4u_any*>(reinterpret_cast<const char*>(p) + (at + s.a) * 2);
@@ -238,11 +256,11 @@ __device__ __forceinline__ head_raw<KIND> head_fetch(const void* p, long at, con
       r.b.w = cq_v2u{w[2], w[3]};
       return r;
     }
-    r.a = quad_fetch<KIND, WHOLE>(p, at + s.a, there ? 4 : 0);
-    r.b = quad_fetch<KIND, WHOLE>(p, at + s.b, there ? 4 : 0);
+    r.a = quad_fetch<KIND, MODE>(p, at + s.a, there ? 4 : 0);
+    r.b = quad_fetch<KIND, MODE>(p, at + s.b, there ? 4 : 0);
   } else {
-    r.a = quad_fetch<KIND, WHOLE>(p, at + s.a, on ? s.na : 0);
-    r.b = quad_fetch<KIND, WHOLE>(p, at + s.b, on ? s.nb : 0);
+    r.a = quad_fetch<KIND, MODE>(p, at + s.a, on ? s.na : 0);
+    r.b = quad_fetch<KIND, MODE>(p, at + s.b, on ? s.nb : 0);
   }
   return r;
 }
@@ -256,36 +274,60 @@ __device__ __forceinline__ void head_values(const head_raw<KIND>& r, float (&v)[
   }
 }
 
-template <int KIND, bool WHOLE, bool SIDE>
+// the values for the row's sums: a neighbour's as zeros
+template <int MODE>
+__device__ __forceinline__ void own_values(const head_slot& s, float (&v)[8]) {
+  if constexpr (MODE == kShifted) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (i & 3) < (i < 4 ? s.sa : s.sb) || (i & 3) >= (i < 4 ? s.na : s.nb) ? 0.f : v[i];
+  }
+}
+
+// the values from the from-th to the end-th
+template <int KIND>
+__device__ __forceinline__ void quad_store_some(void* p, long at, int from, int end, const float (&v)[4]) {
+  if (from == 0 && end == 4) {
+    quad_store<KIND>(p, at, 4, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float one[4] = {v[i], 0.f, 0.f, 0.f};
+      if (i >= from && i < end) quad_store<KIND>(p, at + i, 1, one);
+    }
+  }
+}
+
+template <int KIND, int MODE, bool SIDE>
 __device__ __forceinline__ void head_store(void* p, long at, const head_slot& s, const float (&v)[8]) {
   const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-  if constexpr (WHOLE) {
-    if (s.na) {
-      if constexpr (SIDE && (KIND == CQ_A_F16 || KIND == CQ_A_BF16)) {
-        row_store8<KIND>(p, (size_t)(at + s.a), 8, v);
-      } else {
-        quad_store<KIND>(p, at + s.a, 4, a);
-        quad_store<KIND>(p, at + s.b, 4, b);
-      }
-    }
-  } else {
+  if constexpr (MODE == kGeneral) {
     quad_store<KIND>(p, at + s.a, s.na, a);
     quad_store<KIND>(p, at + s.b, s.nb, b);
+  } else if (s.na) {
+    if constexpr (SIDE && MODE == kWhole && (KIND == CQ_A_F16 || KIND == CQ_A_BF16)) {
+      row_store8<KIND>(p, (size_t)(at + s.a), 8, v);
+    } else if constexpr (MODE == kWhole) {
+      quad_store<KIND>(p, at + s.a, 4, a);
+      quad_store<KIND>(p, at + s.b, 4, b);
+    } else {
+      quad_store_some<KIND>(p, at + s.a, s.sa, s.na, a);
+      quad_store_some<KIND>(p, at + s.b, s.sb, s.nb, b);
+    }
   }
 }
 
 // a lane's share of a norm's weights (ones without a norm)
-template <bool WHOLE, bool SIDE>
+template <int MODE, bool SIDE>
 __device__ __forceinline__ void head_weights(const void* w, int kind, const head_slot& s, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 1.f;
   if (!w) return;
   if (kind == CQ_A_F32)
-    head_values<CQ_A_F32>(head_fetch<CQ_A_F32, WHOLE, SIDE>(w, 0, s, true), v);
+    head_values<CQ_A_F32>(head_fetch<CQ_A_F32, MODE, SIDE>(w, 0, s, true), v);
   else if (kind == CQ_A_F16)
-    head_values<CQ_A_F16>(head_fetch<CQ_A_F16, WHOLE, SIDE>(w, 0, s, true), v);
+    head_values<CQ_A_F16>(head_fetch<CQ_A_F16, MODE, SIDE>(w, 0, s, true), v);
   else
-    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16, WHOLE, SIDE>(w, 0, s, true), v);
+    head_values<CQ_A_BF16>(head_fetch<CQ_A_BF16, MODE, SIDE>(w, 0, s, true), v);
 }
 
 // cosines and sines of a lane's four pairs
@@ -373,17 +415,18 @@ __device__ __forceinline__ void head_normed(float (&v)[8], const float (&w)[8], 
 
 }  // namespace
 
-// Runs LAUNCH(..., LANES, WHOLE, INTER) for the lanes of a row (64 of them are never all whole: that would take 512 values).  Pairs of
-// neighbours (or none) and pairs apart are two kernels: in one the compiler reads a row's values by index, from scratch memory.
-#define CQ_HEAD_WIDTHS(LAUNCH, L, INTER, ...)                                   \
-  do {                                                                          \
-    if ((L).whole && (L).lanes == 8) LAUNCH(__VA_ARGS__, 8, true, INTER);       \
-    else if ((L).whole && (L).lanes == 16) LAUNCH(__VA_ARGS__, 16, true, INTER); \
-    else if ((L).whole) LAUNCH(__VA_ARGS__, 32, true, INTER);                   \
-    else if ((L).lanes == 8) LAUNCH(__VA_ARGS__, 8, false, INTER);              \
-    else if ((L).lanes == 16) LAUNCH(__VA_ARGS__, 16, false, INTER);            \
-    else if ((L).lanes == 32) LAUNCH(__VA_ARGS__, 32, false, INTER);            \
-    else LAUNCH(__VA_ARGS__, 64, false, INTER);                                 \
+// Runs LAUNCH(..., LANES, MODE, INTER) for a layout (64 lanes are never all whole: that would take 512 values).  Pairs of neighbours (or
+// none) and pairs apart are two kernels: in one the compiler reads a row's values by index, from scratch memory.
+#define CQ_HEAD_WIDTHS(LAUNCH, L, INTER, ...)                                                        \
+  do {                                                                                               \
+    if ((L).mode == kWhole && (L).lanes == 8) LAUNCH(__VA_ARGS__, 8, kWhole, INTER);                 \
+    else if ((L).mode == kWhole && (L).lanes == 16) LAUNCH(__VA_ARGS__, 16, kWhole, INTER);          \
+    else if ((L).mode == kWhole) LAUNCH(__VA_ARGS__, 32, kWhole, INTER);                             \
+    else if ((L).mode == kShifted && (L).lanes == 8) LAUNCH(__VA_ARGS__, 8, kShifted, INTER);        \
+    else if ((L).mode == kShifted && (L).lanes == 16) LAUNCH(__VA_ARGS__, 16, kShifted, INTER);      \
+    else if ((L).mode == kShifted && (L).lanes == 32) LAUNCH(__VA_ARGS__, 32, kShifted, INTER);      \
+    else if ((L).mode == kShifted) LAUNCH(__VA_ARGS__, 64, kShifted, INTER);                         \
+    else LAUNCH(__VA_ARGS__, 8, kGeneral, INTER);                                                    \
   } while (0)
 #define CQ_HEAD_LANES(LAUNCH, L, ...)                              \
   do {                                                             \

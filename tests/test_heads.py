@@ -57,7 +57,8 @@ def _rows(g, T, n, D, kind, scale=1.5):
 
 SHAPES = [  # D, rot, interleaved
     (128, 128, False), (64, 32, True), (80, 20, True), (80, 20, False), (1, 0, False), (7, 2, False), (33, 10, True), (256, 256, False),
-    (256, 2, False), (250, 6, True), (96, 96, True), (2, 2, False), (13, 12, False), (128, 0, False)]
+    (256, 2, False), (250, 6, True), (96, 96, True), (2, 2, False), (13, 12, False), (128, 0, False), (8, 2, False),
+    (9, 6, False), (9, 6, True), (15, 8, False), (15, 10, True), (20, 18, False), (200, 198, False), (255, 30, True), (254, 12, False)]
 KINDS = [("bf16", "bf16", "bf16"), ("f16", "f16", "f32"), ("f32", "f32", "f32"), ("f32", "bf16", "bf16"), ("f32", "f16", "f16"),
          ("bf16", "bf16", "f32")]
 
