@@ -464,7 +464,8 @@ typedef struct {
   const float* v_scale;
 } cq_cache;
 /*
- * The sequences of a call: position p of sequence s lies in slot p % page_size of page page_table[s * stride + p / page_size].  Entries
+ * The sequences of a call: position p of sequence s lies in slot p % page_size of page page_table[s * stride + p / page_size] (stride 0: one row for
+ * all, as for several tokens of a sequence that are attended to at once, each with the length that ends with it).  Entries
  * outside [0, pages) are pages that are not there: nothing is written to or read from them.  lengths [n]: tokens of each sequence, the new ones of
  * this call among them (the same array serves the append and the attention behind it).  width * page_size <= 2^30.
  */
@@ -498,7 +499,7 @@ cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, const cq_hea
  *   lse of its sink (-inf without).  What lies behind a sequence's length is not read.  out [S->n, q->n] of any kind; lse [S->n, q->n] f32 or
  *   NULL.  Scores, softmax and sums in fp32; the products' operands carry 16 bits at least, 22 where q or out is fp32.
  *   max_length: what the lengths are expected to reach, <= 2^30.  The work is divided for it; longer sequences take longer, no more.
- *   Up to 2^32 pieces of 16 bytes between the first and the last row of k, and of v; n * width * page_size <= 64e9, n * q->n <= 2^30.
+ *   Up to 2^32 pieces of 16 bytes between the first and the last row of k, and of v; n * q->n < 2^25.
  *   The order of the sums depends on the sizes and on the lengths of the whole batch.
  *   workspace: cq_cache_attention_workspace_bytes() bytes (0: none needed, NULL allowed).
  */

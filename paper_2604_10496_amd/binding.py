@@ -1098,11 +1098,11 @@ class PagedCache:
 
 
 def _sequences(page_table, lengths, index: int) -> Sequences:
-    i32, shape = _DTYPES["i32"], page_table.shape
-    if len(shape) != 2 or page_table.dtype is not i32 or page_table.get_device() != index:
+    i32, shape, stride = _DTYPES["i32"], page_table.shape, page_table.stride()
+    if len(shape) != 2 or page_table.dtype is not i32 or page_table.get_device() != index or stride[1] != 1 and shape[1] > 1:
         _wrong(page_table, "page_table", (None, None), i32, index)
     S, width = shape
-    return Sequences(S, width, _rows(page_table, "page_table", shape), page_table.data_ptr(), _at(lengths, "lengths", (S,), i32, index))
+    return Sequences(S, width, stride[0], page_table.data_ptr(), _at(lengths, "lengths", (S,), i32, index))
 
 
 def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=None, positions=None, norm: Optional[HeadNorm] = None, q=None,
@@ -1110,7 +1110,7 @@ def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=No
     """Keys and values k, v [T, heads, D] of new tokens into the cache, keys with norm and rotation on the way; returns the queries q [T, Hq, D]
     with theirs (None without).
 
-    page_table [S, width] i32, lengths [S] i32 with the new tokens counted; seq_offsets [S + 1] i32: the new tokens of each sequence (None:
+    page_table [S, width] i32 (a row may be expanded), lengths [S] i32 with the new tokens counted; seq_offsets [S + 1] i32: the new tokens of each sequence (None:
     one each); positions [T] i32: rotate by these instead of by the positions in the cache.  Rows of tokens outside all sequences are
     not written (in a new q_out they hold anything)."""
     lib = _lib or load_library()

@@ -24,7 +24,7 @@ inline cq_status check_cache(const cq_cache* C) {
 
 inline cq_status check_sequences(const cq_sequences* S, const cq_cache* C) {
   if (!S) return CQ_ERR_NULL;
-  if (S->n < 0 || S->width < 0 || S->stride < 0 || (S->n > 1 && S->stride < S->width)) return CQ_ERR_SHAPE;
+  if (S->n < 0 || S->width < 0 || S->stride < 0) return CQ_ERR_SHAPE;
   if ((long)S->width * C->page_size > 1l << 30) return CQ_ERR_SHAPE;   // (positions are counted in 32 bits)
   if (S->n > 0 && (!S->lengths || (S->width > 0 && !S->page_table))) return CQ_ERR_NULL;
   return CQ_OK;

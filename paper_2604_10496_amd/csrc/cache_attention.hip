@@ -595,10 +595,10 @@ __global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direc
 // Joins the parts of sequences that lie in several shares, in order: a group of threads takes every n-th part of a row (or of 32 of its
 // dims: `quads` of four each) with a running maximum, then the groups in order.  Rows of sequences without positions are written here too.
 template <int kJoin>
-__global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A, int first_row, int quads) {
+__global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A, int quads) {
   __shared__ cq_v4f sums[kJoin];
   __shared__ float stats[kJoin][2];
-  const int heads = A.G * A.C.heads, row = first_row + blockIdx.x, s = row / heads, head = row - s * heads, tid = threadIdx.x, lane = tid & 63;
+  const int heads = A.G * A.C.heads, row = blockIdx.x, s = row / heads, head = row - s * heads, tid = threadIdx.x, lane = tid & 63;
   sequences near;
   const uint32_t total = all_steps(A, lane, near), share = (total + A.shares - 1) / (uint32_t)A.shares;
   if (near.base > s || s >= near.base + 64) {
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A,
 //   workgroups than compute units.  From Python, 32 query and 8 key heads of 128 in bf16, both ways: 1 sequence of 512 positions 12 us (shares
 //   16), of 1024 15 (16), of 2048 25 (16); 32 of up to 1024 23 (26), of up to 2048 39 (37); 128 of up to 256 33 (28).
 //   by_sequence: one launch of a wavefront per sequence and key head, where twice the longest sequence's positions are no more than there are
-//   of those: the longest does not outlast the rest.  The same heads, both ways: 128 sequences of up to 100 positions 13 us (shares 21), of up
+//   of those: the longest does not outlast the rest; and beyond 2048 sequences, whose lengths every wavefront would have to add up.  The same heads, both ways: 128 sequences of up to 100 positions 13 us (shares 21), of up
 //   to 1000 76 (67); 1000 of up to 300 138 (217); 512 of up to 1000 224 (230), of up to 4000 840 (717).
 //   by_share: as many shares as there are wavefronts of `resident`, no more than there are steps where the lengths are as expected.  512
 //   sequences of up to 4000 positions: 5.97 TB/s, the rate of a plain read of that size.
@@ -678,8 +678,7 @@ inline plan plan_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int w
   const long span = window > 0 && window < max_length ? window : max_length;
   const int dpad = padded(C->D), step = kTile * together(C->kind, dpad);
   if (n_seqs * columns <= 256 && span <= (dpad == 256 ? 256 : 1024)) return {by_group, 0};
-  // (a launch's threads are counted in 32 bits)
-  if (2 * span <= n_seqs * columns && n_seqs * columns <= kMostThreads / 64 - 64) return {by_sequence, 0};
+  if (2 * span <= n_seqs * columns || n_seqs > 2048) return {by_sequence, 0};
   const long steps = (span > step ? (span + step - 1) / step : 1) * n_seqs, shares = (1024l * resident(C->kind, dpad) + columns - 1) / columns;
   return {by_share, shares < steps ? shares : steps};
 }
@@ -711,8 +710,8 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if (C->pages > 0 &&
       ((C->pages - 1) * (double)C->page_stride + (C->page_size - 1) * (double)C->slot_stride) * cache_elem(C->kind) / 16 >= 4294967295.)
     return CQ_ERR_SHAPE;
-  // (rows and steps are counted in 32 bits)
-  if ((long)S->n * q->n > 1l << 30 || (double)S->n * S->width * C->page_size > 64e9) return CQ_ERR_SHAPE;
+  // (a launch's threads are counted in 32 bits)
+  if ((long)S->n * q->n > kMostThreads / 64 - 64) return CQ_ERR_SHAPE;
   if (S->n == 0) return CQ_OK;
   const size_t need = cq_cache_attention_workspace_bytes(C, S->n, q->n, P->max_length, P->window);
   if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
@@ -777,12 +776,9 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if (p.how != by_share) return cq_check_launch();
   // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
   const bool many = p.shares >= 16l * S->n;
-  const int quads = many && C->D > 32 ? 8 : C->D / 4, threads = many ? 256 : 64;
-  const long all = (long)S->n * q->n, per_launch = kMostThreads / threads;
-  for (long from = 0; from < all; from += per_launch) {
-    const dim3 grid((unsigned)(all - from < per_launch ? all - from : per_launch), (C->D / 4 + quads - 1) / quads);
-    if (many) hipLaunchKernelGGL((attention_join_kernel<256>), grid, dim3(256), 0, str, a, (int)from, quads);
-    else hipLaunchKernelGGL((attention_join_kernel<64>), grid, dim3(64), 0, str, a, (int)from, quads);
-  }
+  const int quads = many && C->D > 32 ? 8 : C->D / 4;
+  const dim3 grid(S->n * q->n, (C->D / 4 + quads - 1) / quads);
+  if (many) hipLaunchKernelGGL((attention_join_kernel<256>), grid, dim3(256), 0, str, a, quads);
+  else hipLaunchKernelGGL((attention_join_kernel<64>), grid, dim3(64), 0, str, a, quads);
   return cq_check_launch();
 }

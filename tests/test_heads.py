@@ -211,6 +211,27 @@ def test_rows_beyond_32_bit_offsets(cq):
     assert torch.equal(q, want)
 
 
+def test_batches_beyond_one_launch(cq):
+    """2^25 + 5 tokens: a launch has 2^31 threads, 64 for each.  Against the same rows in two calls."""
+    import torch
+    T, D = (1 << 25) + 5, 8
+    x = torch.randn((T, 1, D), device="cuda", dtype=torch.bfloat16)
+    norm = _norm(cq, torch.Generator().manual_seed(4), D, D, False, "f32")
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    got = cq.cq_head_norm(norm, x, None, pos)["q"]
+    half = T // 2
+    for a, b in ((0, half), (half, T)):
+        assert torch.equal(got[a:b], cq.cq_head_norm(norm, x[a:b], None, pos[a:b])["q"])
+    page = 1 << 14
+    pages = -(-T // page)
+    cache = cq.PagedCache(*(torch.zeros((pages, page, 1, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1)
+    off = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    cq.cq_cache_append(cache, x, x, table, off[1:].clone(), off, norm=norm)
+    k, v = (c.view(-1, 1, D)[:T] for c in (cache.k, cache.v))
+    assert torch.equal(v, x) and torch.equal(k, cq.cq_head_norm(norm, None, x, pos)["k"])
+
+
 # ------------------------------------------------------------------------------------------------
 # the cache
 # ------------------------------------------------------------------------------------------------
@@ -435,6 +456,19 @@ def test_attention_many_sequences(cq, S, longest, Hk):
     for window in (0, 50):
         got = _check_attention(cq, cache, _rows(g, S, 2 * Hk, 64, "bf16"), table, lens, window=window, max_length=longest)
         assert not got["out"][lens == 0].any()
+
+
+def test_attention_of_thousands_and_of_several_tokens_of_one(cq):
+    """3000 sequences; then the last tokens of a sequence at once, by one row of the table for all of them."""
+    import torch
+    g = torch.Generator().manual_seed(27)
+    lengths = torch.randint(0, 40, (3000,), generator=g)
+    cache, table, lens = _paged(cq, g, lengths.tolist(), 16, 1, 16, "bf16")
+    _check_attention(cq, cache, _rows(g, 3000, 2, 16, "bf16"), table, lens)
+    cache, table, lens = _paged(cq, g, [90], 16, 2, 64, "bf16")
+    q = _rows(g, 5, 4, 64, "bf16")
+    lens = torch.arange(86, 91, dtype=torch.int32).cuda()
+    _check_attention(cq, cache, q, table.expand(5, -1), lens)
 
 
 def test_attention_all_empty(cq):

@@ -156,7 +156,7 @@ def test_cache_append_refusals():
     for bad in (dict(D=60), dict(D=264), dict(D=0), dict(heads=0), dict(page_size=0), dict(pages=-1), dict(page_stride=2044),
                 dict(slot_stride=56), dict(slot_stride=132), dict(head_stride=32), dict(k=264), dict(kind=E4M3, D=72)):
         assert call(c=bad) == 2, bad
-    for bad in (dict(n=-1), dict(width=-1), dict(stride=3), dict(width=1 << 27, stride=1 << 27)):
+    for bad in (dict(n=-1), dict(width=-1), dict(stride=-1), dict(width=1 << 27, stride=1 << 27)):
         assert call(s=bad, off=ONE) == 2, bad
     assert call(c=dict(kind=F32)) == 3 and call(c=dict(k_scale=256)) == 3 and call(v=_heads(kind=F16)) == 3 and call(q=_heads(kind=F16)) == 3
     assert call(qo=_heads(kind=F16)) == 3
