@@ -499,7 +499,8 @@ cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, const cq_hea
  *   lse of its sink (-inf without).  What lies behind a sequence's length is not read.  out [S->n, q->n] of any kind; lse [S->n, q->n] f32 or
  *   NULL.  Scores, softmax and sums in fp32; the products' operands carry 16 bits at least, 22 where q or out is fp32.
  *   max_length: what the lengths are expected to reach, <= 2^30.  The work is divided for it; longer sequences take longer, no more.
- *   Up to 2^32 pieces of 16 bytes between the first and the last row of k, and of v; n * q->n < 2^25.
+ *   Up to 2^32 pieces of 16 bytes between the first and the last row of k, and of v; n * q->n < 2^25, n * width * page_size
+ *   <= 64e9.
  *   The order of the sums depends on the sizes and on the lengths of the whole batch.
  *   workspace: cq_cache_attention_workspace_bytes() bytes (0: none needed, NULL allowed).
  */

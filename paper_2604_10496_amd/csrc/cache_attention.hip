@@ -178,9 +178,9 @@ __device__ __forceinline__ uint32_t two_f16(uint32_t codes) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)codes, 1.f, HI));
 }
 
-// Wavefronts of a SIMD that share the work: as many as ask for 16 KB at a time, which is a step of 128 dims of 16 bits.  With one of those
-// 48 sequences of up to 4096 positions take 78 us and their join 5.6, with two 80 and 6.5, with four 84 and 6.8; 64 dims of 8 bits
-// 33 with two, 30 with four, 35 with eight.
+// Wavefronts of a SIMD that share the work: one whose steps read 16 KB keeps up with the memory, two where more operations come on each byte.  48
+// sequences of up to 4096 positions, 8 key heads: 128 dims in bf16 with one 78 us and the join 5.6, with two 80 and 6.5, with four 84 and 6.8; from
+// Python 64 dims in bf16 49 with one, 46 with two; 128 dims in e4m3 54 and 50; 64 dims in e4m3 (up to 8000 positions) 51 with two, 54 with three.
 constexpr int resident(int kind, int dpad) { return dpad == 64 || (dpad == 128 && kind == CQ_C_E4M3) ? 2 : 1; }
 inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
@@ -275,7 +275,6 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
       }
     }
   };
-
 
   // what does not wait for anything first: pages, queries, then K and V; the queries become operands while those are under way
   const int first_page = page_of(begin);
@@ -710,8 +709,8 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
   if (C->pages > 0 &&
       ((C->pages - 1) * (double)C->page_stride + (C->page_size - 1) * (double)C->slot_stride) * cache_elem(C->kind) / 16 >= 4294967295.)
     return CQ_ERR_SHAPE;
-  // (a launch's threads are counted in 32 bits)
-  if ((long)S->n * q->n > kMostThreads / 64 - 64) return CQ_ERR_SHAPE;
+  // (a launch's threads and the steps of all sequences are counted in 32 bits)
+  if ((long)S->n * q->n > kMostThreads / 64 - 64 || (double)S->n * S->width * C->page_size > 64e9) return CQ_ERR_SHAPE;
   if (S->n == 0) return CQ_OK;
   const size_t need = cq_cache_attention_workspace_bytes(C, S->n, q->n, P->max_length, P->window);
   if (need && (!workspace || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
