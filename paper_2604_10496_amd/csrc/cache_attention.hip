@@ -181,29 +181,82 @@ __device__ __forceinline__ uint32_t two_f16(uint32_t codes) {
 // Wavefronts of a SIMD that share the work: one whose steps read 16 KB keeps up with the memory, two where more operations come on each byte.  48
 // sequences of up to 4096 positions, 8 key heads: 128 dims in bf16 with one 78 us and the join 5.6, with two 80 and 6.5, with four 84 and 6.8; from
 // Python 64 dims in bf16 49 with one, 46 with two; 128 dims in e4m3 54 and 50; 64 dims in e4m3 (up to 8000 positions) 51 with two, 54 with three.
-constexpr int resident(int kind, int dpad) { return dpad == 64 || (dpad == 128 && kind == CQ_C_E4M3) ? 2 : 1; }
-inline int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+constexpr int resident(int kind, int dpad) { return dpad < 128 || (dpad == 128 && kind == CQ_C_E4M3) ? 2 : 1; }
+// Widths that there are kernels for: heads of others are computed as the next.  48 sequences of up to 4096 positions, 8 key heads of 80 in
+// bf16, as 128 72 us, as 96 61; of 96 74 and 67; of 192, as 256 120, 117; in e4m3 90 and 79.
+inline int padded(int D) { return D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
 
-// What a kernel's lanes hold of a row's results: query c's at dims 128 n + kE (4 g + r) + d, unscaled, the maximum (base 2) of its scores
-// and the sum of the exponentials behind it (this lane's positions).
+// The dims of V that a lane takes: E0 neighbours of the first 16 E0, and E1 of the 16 E1 behind them.
+template <int DPAD>
+struct dims {
+  static constexpr int E0 = DPAD >= 128 ? 8 : 4, N = DPAD / 16, E1 = N - E0;
+};
+
+// What a kernel's lanes hold of a row's results: query c's at dims E0 (4 g + r) + d, then 16 E0 + E1 (4 g + r) + d, unscaled, the maximum
+// (base 2) of its scores and the sum of the exponentials behind it (this lane's positions).
 template <int DPAD>
 struct row_state {
-  static constexpr int kE = DPAD >= 128 ? 8 : DPAD / 16;    // neighbouring dims of a lane in V
-  static constexpr int kChunks = DPAD / (16 * kE);
-  cq_v4f O[kChunks][kE];
+  cq_v4f O[dims<DPAD>::N];
   float m, l;
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-      for (int d = 0; d < kE; ++d) O[n][d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < dims<DPAD>::N; ++d) O[d] = cq_v4f{0.f, 0.f, 0.f, 0.f};
     m = -INFINITY;
     l = 0.f;
   }
 };
 
+// A row's neighbouring values of `BYTES` bytes, as words.
+template <int BYTES>
+struct piece {
+  static constexpr int N = BYTES < 4 ? 1 : BYTES / 4;
+  uint32_t w[N];
+  __device__ __forceinline__ void load(const char* p) {
+    if constexpr (BYTES == 16) {
+      const cq_v4u x = *reinterpret_cast<const cq_v4u*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = x[i];
+    } else if constexpr (BYTES == 8) {
+      const cq_v2u x = *reinterpret_cast<const cq_v2u*>(p);
+      w[0] = x[0];
+      w[1] = x[1];
+    } else if constexpr (BYTES == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (BYTES == 2) {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+  }
+};
+
+// O += V^T P^T for E neighbouring dims of a tile's eight rows: the 8 x E block turned in registers, two dims at a time
+template <int CK, int E, int PARTS>
+__device__ __forceinline__ void add_products(const piece<E * (CK == CQ_C_E4M3 ? 1 : 2)>* rows, const cq_v4u (&P)[PARTS], cq_v4f* O) {
+#pragma unroll
+  for (int d = 0; d < E; d += 2) {
+    uint32_t two[8];   // dims d, d+1 of the eight rows
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (CK == CQ_C_E4M3)
+        two[j] = d & 2 ? two_f16<true>(rows[j].w[d >> 2]) : two_f16<false>(rows[j].w[d >> 2]);
+      else
+        two[j] = rows[j].w[d >> 1];
+    }
+    cq_v4u lo, hi;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      lo[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x05040100u);
+      hi[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x07060302u);
+    }
+#pragma unroll
+    for (int q = PARTS - 1; q >= 0; --q) {
+      O[d] = operand<CK>::mfma(lo, P[q], O[d]);
+      O[d + 1] = operand<CK>::mfma(hi, P[q], O[d + 1]);
+    }
+  }
+}
+
 // Tiles of a step, worked on together: 16 KB of keys and values at a time, but for wide heads, as far as the registers go.
-constexpr int together(int kind, int dpad) { return dpad == 64 || (kind == CQ_C_E4M3 && dpad == 128) ? 2 : 1; }
+constexpr int together(int kind, int dpad) { return dpad == 64 || (kind == CQ_C_E4M3 && dpad <= 128) ? 2 : 1; }
 
 // One wavefront's attention of the queries first_head .. first_head + rows - 1 of sequence s over the positions begin .. end-1 (there is
 // one), 32 at a time, of which it takes every NEXT / 32nd 32.
@@ -212,20 +265,21 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
                                        row_state<DPAD>& state) {
   constexpr bool k8 = CK == CQ_C_E4M3;
   constexpr int kSize = k8 ? 1 : 2, kNext = NEXT;
-  constexpr int kSteps = DPAD / 32;                  // products over a row's dims
-  constexpr int kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
+  constexpr int E0 = dims<DPAD>::E0, E1 = dims<DPAD>::E1, kSecond = 16 * E0;
+  constexpr int kKWords = k8 ? (DPAD + 63) / 64 : DPAD / 32;     // 16-byte pieces of a row of K per lane
+  constexpr int kSteps = k8 ? 2 * kKWords : kKWords;             // products over a row's dims
   constexpr int kQ = HIGH ? operand<CK>::kQuery : 1;
   constexpr int kP = HIGH ? operand<CK>::kQuery : 2;
-  constexpr int kKWords = k8 ? DPAD / 64 : DPAD / 32;            // 16-byte pieces of a row of K per lane
-  constexpr int kVWords = kE * kSize / 4;                        // words of a row of V per lane and chunk
   constexpr int kTogether = together(CK, DPAD), kRows = kTogether * kTile;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int D = A.C.D;
-  const bool whole = D == DPAD;
+  const bool whole = D == DPAD && (!k8 || DPAD % 64 == 0);
   auto& O = state.O;
   float &m = state.m, &l = state.l;
   const char* const K = reinterpret_cast<const char*>(A.C.k) + (long)h * A.C.head * kSize + g * 16;
-  const char* const V = reinterpret_cast<const char*>(A.C.v) + (long)h * A.C.head * kSize + (c * kE < D ? c * kE : 0) * kSize;
+  // (lanes without dims read others, for results that are not stored)
+  const int first_at = c * E0 < D ? c * E0 : 0, second_at = kSecond + c * E1 < D ? kSecond + c * E1 : 0;
+  const char* const V = reinterpret_cast<const char*>(A.C.v) + ((long)h * A.C.head + first_at) * kSize;
   const int32_t* table = A.C.table + (long)s * A.C.table_stride;
   // the page of position from + lane (of the last one behind the end), and where its row lies, in units of 16 bytes.  Rows that
   // are not there are read from page 0 and left out afterwards, so that no load stands behind a branch.
@@ -239,7 +293,8 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     return on ? (uint32_t)page * A.page16 + (uint32_t)slot * A.slot16 : 0u;
   };
   cq_v4u k[2 * kTogether][kKWords];               // K: rows c and 16 + c of a tile
-  uint32_t v[kChunks][8 * kTogether][kVWords];    // V: dims kE c .. of rows 4g .. 4g+3 and 16 + 4g .. of a tile
+  piece<E0 * kSize> v0[8 * kTogether];            // V: of rows 4g .. 4g+3 and 16 + 4g .. of a tile
+  piece<E1 * kSize> v1[8 * kTogether];
   uint64_t there;                                 // which of the rows are
   auto load_k = [&](uint32_t at) {
 #pragma unroll
@@ -257,22 +312,8 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
 #pragma unroll
     for (int j = 0; j < 8 * kTogether; ++j) {
       const char* p = V + ((size_t)(uint32_t)__shfl((int)at, (j >> 2) * 16 + g * 4 + (j & 3)) << 4);
-#pragma unroll
-      for (int n = 0; n < kChunks; ++n) {
-        // (lanes without dims read others, for results that are not stored)
-        const char* x = p + (n == 0 || whole || c * kE + 128 < D ? n * 128 * kSize : 0);
-        if constexpr (kVWords == 4) {
-          const cq_v4u w = *reinterpret_cast<const cq_v4u*>(x);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[n][j][i] = w[i];
-        } else if constexpr (kVWords == 2) {
-          const cq_v2u w = *reinterpret_cast<const cq_v2u*>(x);
-          v[n][j][0] = w[0];
-          v[n][j][1] = w[1];
-        } else {
-          v[n][j][0] = *reinterpret_cast<const uint32_t*>(x);
-        }
-      }
+      v0[j].load(p);
+      if constexpr (E1 > 0) v1[j].load(p + (second_at - first_at) * kSize);
     }
   };
 
@@ -304,35 +345,34 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   cq_v4u Q[kSteps][kQ];
   float back = 1.f;   // what the queries were divided by
   {
-    float v[kSteps][8], most = 0.f;
+    float x[kSteps][8], most = 0.f;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if (A.q_kind == CQ_A_F32) row_values<CQ_A_F32>(row8<CQ_A_F32>{{raw[i][0], raw[i][1]}}, v[i]);
-      else if (A.q_kind == CQ_A_F16) row_values<CQ_A_F16>(row8<CQ_A_F16>{{raw[i][0]}}, v[i]);
-      else row_values<CQ_A_BF16>(row8<CQ_A_BF16>{{raw[i][0]}}, v[i]);
+      if (A.q_kind == CQ_A_F32) row_values<CQ_A_F32>(row8<CQ_A_F32>{{raw[i][0], raw[i][1]}}, x[i]);
+      else if (A.q_kind == CQ_A_F16) row_values<CQ_A_F16>(row8<CQ_A_F16>{{raw[i][0]}}, x[i]);
+      else row_values<CQ_A_BF16>(row8<CQ_A_BF16>{{raw[i][0]}}, x[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][e]));
     }
     // scores of a negative factor are those of the negative queries, of none those of zeros
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = factor == 0.f ? 0.f : factor < 0.f ? -v[i][e] : v[i][e];
+      for (int e = 0; e < 8; ++e) x[i][e] = factor == 0.f ? 0.f : factor < 0.f ? -x[i][e] : x[i][e];
     if constexpr (CK != CQ_A_BF16) {
       // f16 has less of a range than the other types: the row's largest value to 2^9 .. 2^10
-      most = fmaxf(most, __shfl_xor(most, 16));
-      most = fmaxf(most, __shfl_xor(most, 32));
+      most = rows_of_lanes_max(most);
       if (most > 0.f && most < INFINITY) {
         const int e = 10 - __builtin_amdgcn_frexp_expf(most);
         back = ldexpf(1.f, -e);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = ldexpf(v[i][j], e);
+          for (int j = 0; j < 8; ++j) x[i][j] = ldexpf(x[i][j], e);
       }
     }
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) split8<CK, kQ>(v[i], Q[i]);
+    for (int i = 0; i < kSteps; ++i) split8<CK, kQ>(x[i], Q[i]);
   }
   // Products q.k to scores in units of ln 2: times `into`, which is not negative (see above), in the exponent's own instruction; the
   // maximum is kept in the products' units.  With a cap the scores themselves are, and `into` is what the cap's exponential takes.
@@ -387,9 +427,11 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
         const bool on = mine >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1ull;
         z[j] = on ? z[j] : -INFINITY;
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n)
+        for (int w = 0; w < v0[j].N; ++w) v0[j].w[w] = on ? v0[j].w[w] : 0u;
+        if constexpr (E1 > 0) {
 #pragma unroll
-          for (int w = 0; w < kVWords; ++w) v[n][j][w] = on ? v[n][j][w] : 0u;
+          for (int w = 0; w < v1[j].N; ++w) v1[j].w[w] = on ? v1[j].w[w] : 0u;
+        }
       }
     }
     float top = m;
@@ -401,9 +443,7 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
       const float shrink = __builtin_amdgcn_exp2f(fmaf(m, unit, -base));
       l *= shrink;
 #pragma unroll
-      for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-        for (int d = 0; d < kE; ++d) O[n][d] *= shrink;
+      for (int d = 0; d < dims<DPAD>::N; ++d) O[d] *= shrink;
       m = top;
     }
     float p[kTogether][8];
@@ -416,31 +456,8 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
     for (int t = 0; t < kTogether; ++t) {
       cq_v4u P[kP];
       split8<CK, kP>(p[t], P);
-#pragma unroll
-      for (int n = 0; n < kChunks; ++n) {
-#pragma unroll
-        for (int d = 0; d < kE; d += 2) {
-          uint32_t two[8];   // dims d, d+1 of the eight rows
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if constexpr (k8)
-              two[j] = d & 2 ? two_f16<true>(v[n][t * 8 + j][d >> 2]) : two_f16<false>(v[n][t * 8 + j][d >> 2]);
-            else
-              two[j] = v[n][t * 8 + j][d >> 1];
-          }
-          cq_v4u lo, hi;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            lo[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x05040100u);
-            hi[w] = __builtin_amdgcn_perm(two[2 * w + 1], two[2 * w], 0x07060302u);
-          }
-#pragma unroll
-          for (int q = kP - 1; q >= 0; --q) {
-            O[n][d] = operand<CK>::mfma(lo, P[q], O[n][d]);
-            O[n][d + 1] = operand<CK>::mfma(hi, P[q], O[n][d + 1]);
-          }
-        }
-      }
+      add_products<CK, E0, kP>(&v0[8 * t], P, &O[0]);
+      if constexpr (E1 > 0) add_products<CK, E1, kP>(&v1[8 * t], P, &O[E0]);
     }
     if (from + kNext < end) load_v(at);
   }
@@ -449,45 +466,63 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   l += __shfl_xor(l, 32);
 }
 
+// E neighbouring dims of each of a lane's four places behind dim `base`, times f: finished at `to` of the output, or (not all) into part
+template <int E>
+__device__ __forceinline__ void put_dims(const attention_args& A, bool all, long to, float* part, int base, const cq_v4f* O, float f) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int at = base + (g * 4 + r) * E;
+    if (at >= A.C.D) continue;
+    if constexpr (E == 2) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const float o = O[d][r] * f;
+        if (!all) part[at + d] = o;
+        else if (A.out_kind == CQ_A_F32) elem_store<CQ_A_F32>(const_cast<void*>(A.out.p), to + at + d, o);
+        else if (A.out_kind == CQ_A_F16) elem_store<CQ_A_F16>(const_cast<void*>(A.out.p), to + at + d, o);
+        else elem_store<CQ_A_BF16>(const_cast<void*>(A.out.p), to + at + d, o);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < E; d += 4) {
+        const float o[4] = {O[d][r] * f, O[d + 1][r] * f, O[d + 2][r] * f, O[d + 3][r] * f};
+        if (all)
+          store4(const_cast<void*>(A.out.p), A.out_kind, to + at + d, o);
+        else
+          *reinterpret_cast<cq_v4f*>(part + at + d) = cq_v4f{o[0], o[1], o[2], o[3]};
+      }
+    }
+  }
+}
+
 // A row's results: finished, or as part `line` of those that the second launch joins.
 template <int CK, int DPAD>
 __device__ __forceinline__ void put_rows(const attention_args& A, int s, int h, int first_head, int rows, bool all, size_t number,
                                          const row_state<DPAD>& state) {
-  constexpr int kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, D = A.C.D, head = first_head + c, heads = A.G * A.C.heads;
+  constexpr int E0 = dims<DPAD>::E0, E1 = dims<DPAD>::E1;
+  const int lane = threadIdx.x & 63, c = lane & 15, head = first_head + c, heads = A.G * A.C.heads;
   if (c >= rows) return;
   const size_t line = number * heads + head;
   float f = 1.f, lse;
   if (all) {
     close_row(state.m, state.l, A.sinks, head, f, lse);
     if (CK == CQ_C_E4M3 && A.C.v_scale) f *= A.C.v_scale[h];
-    if (g == 0 && A.lse) A.lse[(size_t)s * heads + head] = lse;
-  } else if (g == 0) {
+    if (lane < 16 && A.lse) A.lse[(size_t)s * heads + head] = lse;
+  } else if (lane < 16) {
     A.stat[line * 2] = state.m;
     A.stat[line * 2 + 1] = state.l;
   }
   const long to = (long)s * A.out.token + (long)head * A.out.head;
-  float* part = A.part + line * D;
-#pragma unroll
-  for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int d0 = n * 128 + (g * 4 + r) * kE;
-      if (d0 >= D) continue;
-#pragma unroll
-      for (int d = 0; d < kE; d += 4) {
-        const float o[4] = {state.O[n][d][r] * f, state.O[n][d + 1][r] * f, state.O[n][d + 2][r] * f, state.O[n][d + 3][r] * f};
-        if (all)
-          store4(const_cast<void*>(A.out.p), A.out_kind, to + d0 + d, o);
-        else
-          *reinterpret_cast<cq_v4f*>(part + d0 + d) = cq_v4f{o[0], o[1], o[2], o[3]};
-      }
-    }
+  float* part = A.part + line * A.C.D;
+  put_dims<E0>(A, all, to, part, 0, &state.O[0], f);
+  if constexpr (E1 > 0) put_dims<E1>(A, all, to, part, 16 * E0, &state.O[E0], f);
 }
 
 // One share of the work per wavefront, or one sequence where there are many.
+// (Registers: two wavefronts per SIMD, but for wide heads, and for 128 dims in bf16 with three parts of queries and P, which spill then.)
 template <int CK, int DPAD, bool HIGH>
-__global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attention_kernel(attention_args A) {
+__global__ __launch_bounds__(kWaves * 64, DPAD > 128 || (DPAD == 128 && CK == CQ_A_BF16 && HIGH) ? 1 : 2) void cache_attention_kernel(attention_args A) {
   const int lane = threadIdx.x & 63;
   // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
   const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
@@ -544,12 +579,12 @@ __global__ __launch_bounds__(kWaves * 64, DPAD == 256 ? 1 : 2) void cache_attent
 
 // Short sequences: the wavefronts of a workgroup share the positions of one sequence and key head and join their results in LDS, half of
 // them giving theirs to the other half, until one is left.  One launch, no workspace.
-constexpr int direct_waves(int dpad) { return dpad == 256 ? 4 : 8; }
+constexpr int direct_waves(int dpad) { return dpad > 128 ? 4 : 8; }
 
 template <int CK, int DPAD, bool HIGH>
 __global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direct_kernel(attention_args A) {
-  constexpr int W = direct_waves(DPAD), kE = row_state<DPAD>::kE, kChunks = row_state<DPAD>::kChunks;
-  __shared__ cq_v4f sums[W / 2][kChunks * kE][64];
+  constexpr int W = direct_waves(DPAD), N = dims<DPAD>::N;
+  __shared__ cq_v4f sums[W / 2][N][64];
   __shared__ float stats[W / 2][2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
@@ -568,9 +603,7 @@ __global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direc
     if (begin + half * kStep < end) {   // (else they have nothing to give)
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-          for (int d = 0; d < kE; ++d) sums[wave - half][n * kE + d][lane] = state.O[n][d];
+        for (int d = 0; d < N; ++d) sums[wave - half][d][lane] = state.O[d];
         stats[wave - half][0][lane] = state.m;
         stats[wave - half][1][lane] = state.l;
       }
@@ -579,9 +612,7 @@ __global__ __launch_bounds__(direct_waves(DPAD) * 64) void cache_attention_direc
         const float pm = stats[wave][0][lane], top = fmaxf(state.m, pm), base = top == -INFINITY ? 0.f : top;
         const float a = __builtin_amdgcn_exp2f(state.m - base), b = __builtin_amdgcn_exp2f(pm - base);
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-          for (int d = 0; d < kE; ++d) state.O[n][d] = state.O[n][d] * a + sums[wave][n * kE + d][lane] * b;
+        for (int d = 0; d < N; ++d) state.O[d] = state.O[d] * a + sums[wave][d][lane] * b;
         state.l = fmaf(state.l, a, stats[wave][1][lane] * b);
         state.m = top;
       }
@@ -676,7 +707,7 @@ inline plan plan_of(const cq_cache* C, int n_seqs, int Hq, int max_length, int w
   const long columns = (long)C->heads * ((Hq / C->heads + 15) / 16);
   const long span = window > 0 && window < max_length ? window : max_length;
   const int dpad = padded(C->D), step = kTile * together(C->kind, dpad);
-  if (n_seqs * columns <= 256 && span <= (dpad == 256 ? 256 : 1024)) return {by_group, 0};
+  if (n_seqs * columns <= 256 && span <= (dpad > 128 ? 256 : 1024)) return {by_group, 0};
   if (2 * span <= n_seqs * columns || n_seqs > 2048) return {by_sequence, 0};
   const long steps = (span > step ? (span + step - 1) / step : 1) * n_seqs, shares = (1024l * resident(C->kind, dpad) + columns - 1) / columns;
   return {by_share, shares < steps ? shares : steps};
@@ -758,7 +789,9 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
 #define WIDTHS(CK, HIGH)                      \
   do {                                        \
     if (dpad == 64) LAUNCH(CK, 64, HIGH);     \
+    else if (dpad == 96) LAUNCH(CK, 96, HIGH);   \
     else if (dpad == 128) LAUNCH(CK, 128, HIGH); \
+    else if (dpad == 192) LAUNCH(CK, 192, HIGH); \
     else LAUNCH(CK, 256, HIGH);               \
   } while (0)
 #define KINDS(CK)                \
