@@ -484,7 +484,8 @@ typedef struct {
  *   were.  NULL with T = S->n: one new token of every sequence.  Tokens before position 0 or beyond the table's row are left out too;
  *   those whose page is not there write no key or value.
  *   positions [T] i32 or NULL: rotate by these instead of by the positions in the cache.
- *   Two tokens of a call must not share a slot (a page that stands twice among the entries that it writes to): one of the two, or a mixture, would remain.
+ *   Two tokens of a call must not share a slot (a page that stands twice among the entries that it writes to): one of the two, or a
+ *   mixture, would remain.
  */
 cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, const cq_head_spec* P, const cq_heads* q, const cq_heads* k,
                           const cq_heads* v, const int32_t* seq_offsets, const int32_t* positions, int T, const cq_heads* q_out,

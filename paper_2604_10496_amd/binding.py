@@ -883,7 +883,8 @@ _DTYPES: Dict[str, object] = {}      # filled once torch is known
 def _dtypes() -> Dict[str, object]:
     if not _DTYPES:
         import torch
-        _DTYPES.update(i32=torch.int32, f32=torch.float32, f64=torch.float64, empty=torch.empty, empty_like=torch.empty_like, contiguous=torch.contiguous_format)
+        _DTYPES.update(i32=torch.int32, f32=torch.float32, f64=torch.float64, empty=torch.empty, empty_like=torch.empty_like,
+                       contiguous=torch.contiguous_format)
         _DTYPES.update(current=torch._C._cuda_getDevice, stream=torch._C._cuda_getCurrentRawStream)
         _DTYPES["cache"] = {torch.float16: CQ_A_F16, torch.bfloat16: CQ_A_BF16, torch.float8_e4m3fn: CQ_C_E4M3}
         _kind(torch.float32, "")
@@ -1110,8 +1111,8 @@ def cq_cache_append(cache: PagedCache, k, v, page_table, lengths, seq_offsets=No
     """Keys and values k, v [T, heads, D] of new tokens into the cache, keys with norm and rotation on the way; returns the queries q [T, Hq, D]
     with theirs (None without).
 
-    page_table [S, width] i32 (a row may be expanded), lengths [S] i32 with the new tokens counted; seq_offsets [S + 1] i32: the new tokens of each sequence (None:
-    one each); positions [T] i32: rotate by these instead of by the positions in the cache.  Rows of tokens outside all sequences are
+    page_table [S, width] i32 (a row may be expanded), lengths [S] i32 with the new tokens counted; seq_offsets [S + 1] i32: the new tokens
+    of each sequence (None: one each); positions [T] i32: rotate by these instead of by the positions in the cache.  Rows of tokens outside all sequences are
     not written (in a new q_out they hold anything)."""
     lib = _lib or load_library()
     index, T, dtype = _gpu_of(k, "k"), k.shape[0], k.dtype

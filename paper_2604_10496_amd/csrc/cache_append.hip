@@ -176,7 +176,8 @@ extern "C" cq_status cq_cache_append(const cq_cache* C, const cq_sequences* S, c
     b.first = (int)from;
     b.T = (int)(T - from < most ? T - from : most);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, CK, LANES, MODE, INTER) hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
+#define LAUNCH(XK, CK, LANES, MODE, INTER) \
+  hipLaunchKernelGGL((cache_append_kernel<XK, CK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
 #define KINDS(XK)                                                              \
   do {                                                                         \
     if (C->kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, XK, CQ_A_F16);   \

@@ -520,9 +520,11 @@ __device__ __forceinline__ void put_rows(const attention_args& A, int s, int h, 
 }
 
 // One share of the work per wavefront, or one sequence where there are many.
-// (Registers: two wavefronts per SIMD, but for wide heads, and for 128 dims in bf16 with three parts of queries and P, which spill then.)
+// Registers are those of two wavefronts per SIMD, but for wide heads, and for 128 dims in bf16 with three parts of queries and P, which spill then.
+constexpr int least_waves(int kind, int dpad, bool high) { return dpad > 128 || (dpad == 128 && kind == CQ_A_BF16 && high) ? 1 : 2; }
+
 template <int CK, int DPAD, bool HIGH>
-__global__ __launch_bounds__(kWaves * 64, DPAD > 128 || (DPAD == 128 && CK == CQ_A_BF16 && HIGH) ? 1 : 2) void cache_attention_kernel(attention_args A) {
+__global__ __launch_bounds__(kWaves * 64, least_waves(CK, DPAD, HIGH)) void cache_attention_kernel(attention_args A) {
   const int lane = threadIdx.x & 63;
   // workgroups go to the eight XCDs in turn: each XCD takes shares one behind the other, and the heads of a share together
   const int block = (blockIdx.x & 7) * (A.blocks >> 3) + (blockIdx.x >> 3);
@@ -693,8 +695,9 @@ __global__ __launch_bounds__(kJoin) void attention_join_kernel(attention_args A,
 //   workgroups than compute units.  From Python, 32 query and 8 key heads of 128 in bf16, both ways: 1 sequence of 512 positions 12 us (shares
 //   16), of 1024 15 (16), of 2048 25 (16); 32 of up to 1024 23 (26), of up to 2048 39 (37); 128 of up to 256 33 (28).
 //   by_sequence: one launch of a wavefront per sequence and key head, where twice the longest sequence's positions are no more than there are
-//   of those: the longest does not outlast the rest; and beyond 2048 sequences, whose lengths every wavefront would have to add up.  The same heads, both ways: 128 sequences of up to 100 positions 13 us (shares 21), of up
-//   to 1000 76 (67); 1000 of up to 300 138 (217); 512 of up to 1000 224 (230), of up to 4000 840 (717).
+//   of those: the longest does not outlast the rest; and beyond 2048 sequences, whose lengths every wavefront would have to add up.  The
+//   same heads, both ways: 128 sequences of up to 100 positions 13 us (shares 21), of up to 1000 76 (67); 1000 of up to 300 138 (217); 512 of
+//   up to 1000 224 (230), of up to 4000 840 (717).
 //   by_share: as many shares as there are wavefronts of `resident`, no more than there are steps where the lengths are as expected.  512
 //   sequences of up to 4000 positions: 5.97 TB/s, the rate of a plain read of that size.
 enum way { by_group, by_sequence, by_share };

@@ -108,7 +108,8 @@ extern "C" cq_status cq_head_norm(const cq_head_spec* P, const cq_heads* q, cons
     b.q_out = rows_from(a.q_out, out, from);
     b.k_out = rows_from(a.k_out, out, from);
     const dim3 grid((unsigned)(((long)b.T * b.parts + 3) / 4));
-#define LAUNCH(XK, OK, LANES, MODE, INTER) hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
+#define LAUNCH(XK, OK, LANES, MODE, INTER) \
+  hipLaunchKernelGGL((head_norm_kernel<XK, OK, LANES, MODE, INTER>), grid, dim3(256), 0, (hipStream_t)stream, b)
     if (kind == CQ_A_F16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F16, CQ_A_F16);
     else if (kind == CQ_A_BF16) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_BF16, CQ_A_BF16);
     else if (out == CQ_A_F32) CQ_HEAD_LANES(LAUNCH, a.L, CQ_A_F32, CQ_A_F32);

@@ -32,8 +32,9 @@ struct head_layout {
 
 // whole: the used lanes hold eight values each.  shifted: the last of the rotated ones and the last of all are moved back to the last values
 // there are, of which their neighbours own the first (few rotated values are followed by others), so that no load or sum needs a loop
-// over single values: 4096 tokens of 40 heads of 80, 20 rotated, 29 us with such loops, 21 without.  general: rows of fewer than eight.  Each is a kernel of its own: the code for single values is ten times as long, and what single tokens wait for is
-// instructions (1 token of 40 heads in 4.2 us; 6.6 with it).
+// over single values: 4096 tokens of 40 heads of 80, 20 rotated, 29 us with such loops, 21 without.  general: rows of fewer than eight.  Each
+// is a kernel of its own: the code for single values is ten times as long, and what single tokens wait for is instructions (1 token of
+// 40 heads in 4.2 us; 6.6 with it).
 constexpr int kGeneral = 0, kShifted = 1, kWhole = 2;
 
 inline head_layout make_head_layout(int D, int rot, int inter) {

@@ -100,7 +100,8 @@ def test_head_norm_and_gradients(cq, D, rot, inter, kind, out, weight):
         _close(grads["dw_" + n], dw, mw, (64 + T * x.shape[1]) * U, weight, "dw_" + n)
 
 
-@pytest.mark.parametrize("T,Hq,Hk", [(1, 1, 1), (12, 32, 8), (13, 32, 8), (40, 3, 1), (1, 71, 1), (2, 32, 8), (300, 5, 0), (0, 3, 1), (4099, 2, 1), (700, 0, 16)])
+@pytest.mark.parametrize("T,Hq,Hk", [(1, 1, 1), (12, 32, 8), (13, 32, 8), (40, 3, 1), (1, 71, 1), (2, 32, 8), (300, 5, 0), (0, 3, 1), (4099, 2, 1),
+                                     (700, 0, 16)])
 @pytest.mark.parametrize("norms", [(True, True), (True, False), (False, True), (False, False)])
 def test_batches_heads_and_missing_norms(cq, T, Hq, Hk, norms):
     import torch
