@@ -255,7 +255,8 @@ __device__ __forceinline__ void add_products(const piece<E * (CK == CQ_C_E4M3 ? 
   }
 }
 
-// Tiles of a step, worked on together: 16 KB of keys and values at a time, but for wide heads, as far as the registers go.
+// Tiles of a step, worked on together, as far as the registers go: what a step costs beside its products comes once for both (48 sequences of up
+// to 4096 positions in e4m3, 8 key heads of 128: 59 us with one, 50 with two).
 constexpr int together(int kind, int dpad) { return dpad == 64 || (kind == CQ_C_E4M3 && dpad <= 128) ? 2 : 1; }
 
 // One wavefront's attention of the queries first_head .. first_head + rows - 1 of sequence s over the positions begin .. end-1 (there is
@@ -809,7 +810,8 @@ extern "C" cq_status cq_cache_attention(const cq_cache* C, const cq_sequences* S
 #undef WIDTHS
 #undef LAUNCH
   if (p.how != by_share) return cq_check_launch();
-  // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them.
+  // Many parts per sequence: 32 dims of a row per workgroup of four wavefronts, in which 32 groups of threads share them (512 parts of 32 rows
+  // 6.7 us, with whole rows 14.2; 5 parts of 1536 rows 12.2 and 6.5).
   const bool many = p.shares >= 16l * S->n;
   const int quads = many && C->D > 32 ? 8 : C->D / 4;
   const dim3 grid(S->n * q->n, (C->D / 4 + quads - 1) / quads);
