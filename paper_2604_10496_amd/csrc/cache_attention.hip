@@ -255,6 +255,26 @@ __device__ __forceinline__ void add_products(const piece<E * (CK == CQ_C_E4M3 ? 
   }
 }
 
+// cap * tanh x of y = 2x log2 e and z = cap * x.  QUICK: 1 - 2 / (1 + e^(2x)), off by up to 6 units (2^-24) of the cap.  Otherwise within 11
+// of the result: below |x| = 5/8 the odd polynomial that interpolates tanh at the Chebyshev points of y^2 (off by 0.3, 2 with its rounding).
+// Quick for 16-bit queries and results under caps up to 64: 2^-15 of a weight at most, where 2^-12 is half a step of the result.  61 sequences,
+// the last 2000 positions of 64 dims in e4m3, 16 columns of scores for 5 queries: 29.4 us quick, 32.1 otherwise.
+template <bool QUICK>
+__device__ __forceinline__ float capped_score(float y, float z, float cap) {
+  const float high = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y)), cap);
+  if constexpr (QUICK) {
+    return high;
+  } else {
+    const float t = y * y;
+    float p = -1.524229940e-07f;
+    p = fmaf(p, t, 4.370435082e-06f);
+    p = fmaf(p, t, -9.331808877e-05f);
+    p = fmaf(p, t, 1.923544510e-03f);
+    p = fmaf(p, t, -4.003774589e-02f);
+    return fabsf(y) < 1.8f ? fmaf(z * t, p, z) : high;
+  }
+}
+
 // Tiles of a step, worked on together, as far as the registers go: what a step costs beside its products comes once for both (48 sequences of up
 // to 4096 positions in e4m3, 8 key heads of 128: 59 us with one, 50 with two).
 constexpr int together(int kind, int dpad) { return dpad == 64 || (kind == CQ_C_E4M3 && dpad <= 128) ? 2 : 1; }
@@ -377,9 +397,10 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
   }
   // Products q.k to scores in units of ln 2: times `into`, which is not negative (see above), in the exponent's own instruction; the
   // maximum is kept in the products' units.  With a cap the scores themselves are, and `into` is what the cap's exponential takes.
-  const bool capped = A.softcap > 0.f;
-  const float cap = A.softcap * kLog2e, times = fabsf(factor) * back * kLog2e * (capped ? 2.f / A.softcap : 1.f);
-  const float into = times < 1e-37f ? 1e-37f : times;   // (none times infinity would be no number)
+  const bool capped = A.softcap > 0.f, quick = !HIGH && capped && A.softcap <= 64.f;
+  const float cap = A.softcap * kLog2e, plain = fabsf(factor) * back * kLog2e;
+  const float times = capped ? plain * fminf(2.f / A.softcap, 3e38f) : plain;
+  const float into = times < 1e-37f ? 1e-37f : capped && times > 1e37f ? 1e37f : times;   // (none times infinity would be no number)
   const float unit = capped ? 1.f : into;
 
   // K of the next positions is asked for when this step's scores are there, V when its products are: a step's rows are under way
@@ -417,10 +438,12 @@ __device__ __forceinline__ void attend(const attention_args& A, int s, int h, in
       for (int r = 0; r < 4; ++r) z[n * 4 + r] = acc[r];
     }
     if (from + kNext < end) load_k(at);
-    if (capped) {
-      // tanh x = 1 - 2 / (1 + e^(2x)), off by some units of the last place of 1
+    if (quick) {
 #pragma unroll
-      for (int j = 0; j < 8 * kTogether; ++j) z[j] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z[j] * into)), cap);
+      for (int j = 0; j < 8 * kTogether; ++j) z[j] = capped_score<true>(z[j] * into, 0.f, cap);
+    } else if (capped) {
+#pragma unroll
+      for (int j = 0; j < 8 * kTogether; ++j) z[j] = capped_score<false>(z[j] * into, z[j] * plain, cap);
     }
     if (mine != ~0ull) {
 #pragma unroll

@@ -437,6 +437,26 @@ def test_attention_scales(cq, scale, softcap, cache_kind):
         assert not got["out"][1].any()
 
 
+@pytest.mark.parametrize("softcap", [1e-42, 1e-3, 0.05, 1.0, 30.0, 64.0, 65.0, 1e4, 1e30])
+@pytest.mark.parametrize("kind,cache_kind", [("f32", "bf16"), ("bf16", "e4m3")])
+def test_attention_caps_keep_scores(cq, softcap, kind, cache_kind):
+    import torch
+    g = torch.Generator().manual_seed(26)
+    cache, table, lens = _paged(cq, g, [70, 3, 1, 16], 16, 2, 64, cache_kind, 0.5 if cache_kind == "e4m3" else None)
+    q = _rows(g, 4, 4, 64, kind)
+    k, v = (_np(x) if s is None else _np(x) * _np(s)[:, None] for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+    _, lse, _, dot, top = O.attention(_np(q), k, v, table.cpu().numpy(), lens.cpu().numpy(), 0.01, 0, softcap, None)
+    # tanh's argument is off by at most 8 U of itself (five products, the last rounded once more, a constant), which is no more of the
+    # tanh; the exponential's form by 11 U of it above 5/8 (e^(2x) 2.5 U, the sum 1, its reciprocal 2, of which 1.6 / 0.55 remain), the
+    # cap by 1.5; the exponent in units of ln 2 by 2 again.  16-bit results under caps up to 64: by 6 U of the cap instead
+    bar = ((64 + 16) * U + 2.0 ** -22) * dot + 24 * U * top + (70 / 8 + 64) * U + 2 * U * np.abs(lse)
+    if kind != "f32" and softcap <= 64:
+        bar += 6 * U * softcap
+    for n in (None, 1 << 20):
+        got = cq.cq_cache_attention(cache, q, table, lens, scale=0.01, softcap=softcap, max_length=n)
+        assert (np.abs(_np(got["lse"]) - lse) <= bar).all()
+
+
 @pytest.mark.parametrize("max_length", [1, 100, 5000, 1 << 20, None])
 def test_attention_lengths_beyond_what_was_expected(cq, max_length):
     import torch
